@@ -477,6 +477,160 @@ symtile_status symtile_gemm_all_scatter_noalloc(symtile_heap* h, const void* A,
                                                 int rank, int world_size,
                                                 const symtile_gas_config* cfg, symtile_stream s);
 
+/* ---- output head: 4-bit product, token log probabilities, distillation ------
+ *
+ * A vocabulary-parallel head is a column-parallel layer (Section 4): every
+ * rank's product with its shard of the vocabulary lands in its column block of
+ * the gathered logits in every slot.  The calls below are what runs around it:
+ * the product of a few tokens with 4-bit weights, and what is read off rows of
+ * logits (any device memory; a slot's gathered output has row stride
+ * world_size * N_local).  The paper has none of them. */
+
+/* Most entries of a row: top alternatives (symtile_token_logprobs) and a
+ * teacher's list (symtile_distill_topk). */
+#define SYMTILE_TOP_MAX 128
+
+/* Bytes of the workspace of a symtile_token_logprobs (top) or
+ * symtile_distill_topk (top = 0) call on `device` with these sizes: rows are
+ * split over workgroups where there are too few to fill the GPU, and the parts
+ * of a row meet there.  0 where no row is split.  The workspace is 16-byte
+ * aligned device memory that must be zero before the first call that uses it;
+ * every call leaves its counters zero again, so calls of other sizes may
+ * follow.  Calls that share a workspace must not overlap in time.  EINVAL for
+ * what the calls refuse. */
+symtile_status symtile_logits_workspace_bytes(int device, int rows, int vocab, int dtype, int top,
+                                              size_t* bytes);
+
+/* With z = scale * logits[r, :], lse = log sum_v exp z_v, logp_v = z_v - lse and
+ * p_v = exp logp_v, for every row r:
+ *   logprob[r]  = logp_target (0 where targets[r] < 0: no token asked for; NaN
+ *                 where targets[r] >= vocab);
+ *   entropy[r]  = -sum_v p_v logp_v;
+ *   stats[r]    = (max_v logits_v, lse - scale * max_v logits_v), apart, since
+ *                 their sum cannot hold both where all logits are at the type's
+ *                 lowest value;
+ *   top_ids[r], top_logprobs[r]: the `top` largest logits in descending order,
+ *                 equal ones (+0 and -0 are equal) by ascending id, and their logp.
+ * and with dlogits the gradient of a loss whose derivatives with respect to
+ * logprob, entropy and lse are grad_logprob, grad_entropy and grad_lse (each
+ * NULL for zero):
+ *   dlogits_v = scale * (p_v * (grad_lse - grad_logprob)
+ *                        - p_v * (logp_v + entropy) * grad_entropy
+ *                        + (v = target ? grad_logprob : 0)).
+ * A logit of -inf is a masked token: p = 0, gradient 0.  In a row with nothing
+ * else logprob is -inf, entropy 0, stats (-inf, 0), the top entries are ids
+ * 0, 1, ... at -inf, and the gradient is 0.  A row with a NaN or +inf gives NaN
+ * (a NaN counts as the largest logit).  Sums are held in fp32; the gradient is
+ * rounded once to dtype.
+ *
+ *  logits        device [rows, vocab], row stride ld (0 = vocab) elements of
+ *                dtype (SYMTILE_F16, SYMTILE_BF16, SYMTILE_F32); rows may start
+ *                at any multiple of the element size.
+ *  scale         positive and finite (1 / temperature).
+ *  targets       device int64 [rows]; NULL where logprob is.
+ *  logprob, entropy, stats (fp32 [rows], [rows], [rows, 2]), top_ids,
+ *                top_logprobs (int64, fp32 [rows, top]): outputs; NULL = not
+ *                wanted.  dlogits needs entropy and stats.
+ *  top           0 .. min(vocab, SYMTILE_TOP_MAX).
+ *  dlogits       device [rows, vocab] of dtype, row stride ld_grad (0 = vocab);
+ *                NULL = no gradient.  May be logits itself (same address and
+ *                stride), otherwise must not overlap it.
+ *  workspace     see symtile_logits_workspace_bytes; may be NULL where that is 0.
+ * EINVAL for anything else; rows = 0 launches nothing. */
+symtile_status symtile_token_logprobs(int device, const void* logits, int rows, int vocab,
+                                      size_t ld, int dtype, float scale, const int64_t* targets,
+                                      float* logprob, float* entropy, float* stats, int top,
+                                      int64_t* top_ids, float* top_logprobs,
+                                      const float* grad_logprob, const float* grad_entropy,
+                                      const float* grad_lse, void* dlogits, size_t ld_grad,
+                                      void* workspace, size_t workspace_bytes, symtile_stream s);
+
+/* The gradient alone, for weights that follow from the values: entropy and
+ * stats are what symtile_token_logprobs wrote for these logits and scale. */
+symtile_status symtile_token_logprobs_backward(int device, const void* logits, int rows,
+                                               int vocab, size_t ld, int dtype, float scale,
+                                               const int64_t* targets, const float* entropy,
+                                               const float* stats, const float* grad_logprob,
+                                               const float* grad_entropy, const float* grad_lse,
+                                               void* dlogits, size_t ld_grad, symtile_stream s);
+
+/* What a teacher's list says (symtile_distill_topk). */
+typedef enum {
+    SYMTILE_DISTILL_RENORM = 0, /* values are logits or log probabilities of the listed tokens:
+                                   q = softmax(scale * values) over the list */
+    SYMTILE_DISTILL_REST = 1    /* values are log probabilities (at the temperature that the
+                                   student's scale stands for): q_j = exp values_j, and all
+                                   other tokens together are one more class with
+                                   q_R = max(0, 1 - sum_j q_j) */
+} symtile_distill_mode;
+
+/* Distillation from a teacher's top entries.  With p as above, list entries
+ * (ids[r, j], values[r, j]), p_R = the sum of p_v over v not in the list:
+ *   loss[r] = sum_j q_j (log q_j - log p_{ids_j})  [+ q_R (log q_R - log p_R)],
+ * and with dlogits the gradient for d(sum)/d(loss[r]) = row_grad[r], Q the sum
+ * of all q and q_R:
+ *   dlogits_v = scale * row_grad * (Q p_v - q_v),
+ * q_v the sum of q over the entries that name v, or q_R p_v / p_R for v not in
+ * the list.  An entry with a negative id is absent (lists of any length up to
+ * k; q = 0, NaN values included); a row without entries has loss 0 and gradient
+ * 0.  Entries of q = 0 contribute nothing.  Where no token outside the list has
+ * p_v > 0 there is no rest class.  A listed token whose logit is -inf gives loss
+ * +inf where q > 0 (its gradient is -q's); a row of -inf alone has gradient 0.
+ * An id >= vocab gives loss and gradient NaN.
+ *
+ *  ids           device int64 [rows, k]
+ *  values        device [rows, k] of values_dtype (F16, BF16, F32)
+ *  k             1 .. SYMTILE_TOP_MAX
+ *  loss          fp32 [rows]
+ *  stats         fp32 [rows, 4]: max logit, lse - scale * max, the same two over
+ *                the tokens outside the list; NULL = not wanted (dlogits needs it)
+ *  row_grad      fp32 [rows]; with dlogits only
+ * logits, scale, dlogits and workspace as in symtile_token_logprobs. */
+symtile_status symtile_distill_topk(int device, const void* logits, int rows, int vocab, size_t ld,
+                                    int dtype, float scale, const int64_t* ids, const void* values,
+                                    int values_dtype, int k, int mode, float* loss, float* stats,
+                                    const float* row_grad, void* dlogits, size_t ld_grad,
+                                    void* workspace, size_t workspace_bytes, symtile_stream s);
+
+/* The gradient alone; stats as symtile_distill_topk wrote them for the same
+ * logits, scale, list and mode. */
+symtile_status symtile_distill_topk_backward(int device, const void* logits, int rows, int vocab,
+                                             size_t ld, int dtype, float scale, const int64_t* ids,
+                                             const void* values, int values_dtype, int k, int mode,
+                                             const float* stats, const float* row_grad,
+                                             void* dlogits, size_t ld_grad, symtile_stream s);
+
+/* Output tile of symtile_w4_all_scatter: all rows (at most 64) by 16 columns. */
+#define SYMTILE_W4_TILE_M 64
+#define SYMTILE_W4_TILE_N 16
+
+/* Rank `rank`'s share of a column-parallel layer for a few tokens, with 4-bit
+ * weights: C_r[m, n] = sum_k X[m, k] (q[n, k] - zero[n, g]) scale[n, g], g = k /
+ * group, with fp32 accumulators, rounded once to dtype and stored into column
+ * block `rank` of the gathered output in every slot; after a tile's data the
+ * arrival counter of (rank, 0, tile) in that slot is incremented with release
+ * semantics at agent scope, as symtile_gemm_all_scatter does.
+ *
+ *  X        device [M, K] of dtype (SYMTILE_F16, SYMTILE_BF16), row stride ldx
+ *           (0 = K; a multiple of 8); M at most SYMTILE_W4_TILE_M
+ *           (EUNSUPPORTED above: the weights are read once per 64 tokens at most)
+ *  q        device uint8 [N_local, K/2]: row n holds the weights of output
+ *           column n, two consecutive k to a byte, the even one in the low bits
+ *  scales   device [N_local, ceil(K / group)] of dtype
+ *  zeros    device uint8 [N_local, ceil(K / group)], values 0..15 (the upper
+ *           bits are ignored); NULL = 8 everywhere
+ *  group    32, 64 or 128
+ *  C_gathered_local, arrived_local: as in symtile_gemm_all_scatter, with tiles of
+ *           SYMTILE_W4_TILE_M x SYMTILE_W4_TILE_N: uint32 [world_size][1][ceil(N_local / 16)]
+ *
+ * Requirements: K a multiple of 32, N_local of 8; X, q and C 16-byte aligned;
+ * M = 0 or N_local = 0 launches nothing, K = 0 stores zeros.  EINVAL otherwise. */
+symtile_status symtile_w4_all_scatter(symtile_heap* h, const void* X, const uint8_t* q,
+                                      const void* scales, const uint8_t* zeros,
+                                      void* C_gathered_local, uint32_t* arrived_local, int M,
+                                      int N_local, int K, int ldx, int group, int dtype, int rank,
+                                      int world_size, symtile_stream s);
+
 /* Rate of the realtime counter behind trace timestamps (the per-tile
  * timeline of Section 3.4, instrumentation), in kHz.  EINVAL for a bad device
  * or NULL khz. */

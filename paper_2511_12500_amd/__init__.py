@@ -19,10 +19,14 @@ _BINDING = (
     "symtile_heap_destroy", "symtile_heap_fill", "symtile_heap_info", "symtile_heap_ptr",
     "symtile_last_error", "symtile_tile_copy", "symtile_tile_copy_timed", "symtile_translate", "symtile_translate_device",
     "symtile_value_exercise", "symtile_version",
+    "DISTILL_RENORM", "DISTILL_REST", "TOP_MAX", "W4_TILE_M", "W4_TILE_N",
+    "symtile_distill_topk", "symtile_distill_topk_backward", "symtile_logits_workspace_bytes",
+    "symtile_token_logprobs", "symtile_token_logprobs_backward", "symtile_w4_all_scatter",
 )
 _HEAP = ("GatheredOutput", "Heap", "current_stream")
+_HEAD = ("TokenLogprobs", "TopDistillation", "W4Weight")
 
-__all__ = list(_BINDING + _HEAP)
+__all__ = list(_BINDING + _HEAP + _HEAD)
 
 
 def __getattr__(name):
@@ -32,6 +36,9 @@ def __getattr__(name):
     if name in _HEAP:
         from . import heap
         return getattr(heap, name)
+    if name in _HEAD:
+        from . import head
+        return getattr(head, name)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 

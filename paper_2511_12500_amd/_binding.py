@@ -11,6 +11,9 @@ F16, BF16, F32 = 1, 2, 3
 BULK_SYNC, FUSED_SEQ, WG_SPEC, UNFUSED_PC, WAVE_SPEC = 0, 1, 2, 3, 4
 SPLIT_REDUCE_AUTO, SPLIT_REDUCE_LAST, SPLIT_REDUCE_BANDED, SPLIT_REDUCE_KERNEL = 0, 1, 2, 3
 PUT, GET = 0, 1
+DISTILL_RENORM, DISTILL_REST = 0, 1
+TOP_MAX = 128                             # SYMTILE_TOP_MAX
+W4_TILE_M, W4_TILE_N = 64, 16             # SYMTILE_W4_TILE_M, SYMTILE_W4_TILE_N
 LOAD, STORE = 0, 1
 ATOMIC_OPS = {"add": 0, "xchg": 1, "cas": 2, "and": 3, "or": 4, "xor": 5, "min": 6, "max": 7}
 SEMS = {"relaxed": 0, "acquire": 1, "release": 2, "acq_rel": 3}
@@ -64,6 +67,7 @@ def _load():
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2511_12500_amd.build`")
     L = ctypes.CDLL(LIB_PATH)
     vp, sz, i32, u32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_uint32
+    f32 = ctypes.c_float
     pvp = ctypes.POINTER(ctypes.c_void_p)
     decl = {
         "symtile_heap_create": [i32, i32, sz, pvp],
@@ -92,6 +96,17 @@ def _load():
         "symtile_clock_rate_khz": [i32, ctypes.POINTER(i32)],
         "symtile_litmus_mp": [vp, sz, sz, i32, i32, i32, i32, i32, u32, vp, vp],
         "symtile_litmus_sb": [vp, sz, i32, i32, i32, i32, u32, vp, vp],
+        "symtile_logits_workspace_bytes": [i32, i32, i32, i32, i32, ctypes.POINTER(sz)],
+        "symtile_token_logprobs": [i32, vp, i32, i32, sz, i32, f32, vp, vp, vp, vp, i32, vp, vp,
+                                   vp, vp, vp, vp, sz, vp, sz, vp],
+        "symtile_token_logprobs_backward": [i32, vp, i32, i32, sz, i32, f32, vp, vp, vp, vp, vp,
+                                            vp, vp, sz, vp],
+        "symtile_distill_topk": [i32, vp, i32, i32, sz, i32, f32, vp, vp, i32, i32, i32, vp, vp,
+                                 vp, vp, sz, vp, sz, vp],
+        "symtile_distill_topk_backward": [i32, vp, i32, i32, sz, i32, f32, vp, vp, i32, i32, i32,
+                                          vp, vp, vp, sz, vp],
+        "symtile_w4_all_scatter": [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
+                                   i32, vp],
         "symtile_value_exercise": [vp, i32, sz, sz, sz, i32, i32, i32, vp],
     }
     for name, args in decl.items():
@@ -272,6 +287,73 @@ def symtile_gas_workspace_bytes(M: int, N_local: int, tile_m: int, tile_n: int,
     _check(lib.symtile_gas_workspace_bytes(M, N_local, tile_m, tile_n, split_k, ctypes.byref(out)),
            "symtile_gas_workspace_bytes")
     return out.value
+
+
+def symtile_logits_workspace_bytes(device: int, rows: int, vocab: int, dtype: int,
+                                   top: int = 0) -> int:
+    """Bytes of the workspace of symtile_token_logprobs (``top``) and
+    symtile_distill_topk (top = 0) calls."""
+    out = ctypes.c_size_t()
+    _check(lib.symtile_logits_workspace_bytes(device, rows, vocab, dtype, top, ctypes.byref(out)),
+           "symtile_logits_workspace_bytes")
+    return out.value
+
+
+def symtile_token_logprobs(device: int, logits: int, rows: int, vocab: int, ld: int, dtype: int,
+                           scale: float, targets: int, logprob: int, entropy: int, stats: int,
+                           top: int = 0, top_ids: int = 0, top_logprobs: int = 0,
+                           grad_logprob: int = 0, grad_entropy: int = 0, grad_lse: int = 0,
+                           dlogits: int = 0, ld_grad: int = 0, workspace: int = 0,
+                           workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib.symtile_token_logprobs(device, _vp(logits), rows, vocab, ld, dtype, scale,
+                                      _vp(targets), _vp(logprob), _vp(entropy), _vp(stats), top,
+                                      _vp(top_ids), _vp(top_logprobs), _vp(grad_logprob),
+                                      _vp(grad_entropy), _vp(grad_lse), _vp(dlogits), ld_grad,
+                                      _vp(workspace), workspace_bytes, _vp(stream)),
+           "symtile_token_logprobs")
+
+
+def symtile_token_logprobs_backward(device: int, logits: int, rows: int, vocab: int, ld: int,
+                                    dtype: int, scale: float, targets: int, entropy: int,
+                                    stats: int, grad_logprob: int, grad_entropy: int,
+                                    grad_lse: int, dlogits: int, ld_grad: int = 0,
+                                    stream: int = 0) -> None:
+    _check(lib.symtile_token_logprobs_backward(device, _vp(logits), rows, vocab, ld, dtype, scale,
+                                               _vp(targets), _vp(entropy), _vp(stats),
+                                               _vp(grad_logprob), _vp(grad_entropy),
+                                               _vp(grad_lse), _vp(dlogits), ld_grad, _vp(stream)),
+           "symtile_token_logprobs_backward")
+
+
+def symtile_distill_topk(device: int, logits: int, rows: int, vocab: int, ld: int, dtype: int,
+                         scale: float, ids: int, values: int, values_dtype: int, k: int, mode: int,
+                         loss: int, stats: int = 0, row_grad: int = 0, dlogits: int = 0,
+                         ld_grad: int = 0, workspace: int = 0, workspace_bytes: int = 0,
+                         stream: int = 0) -> None:
+    """mode: DISTILL_RENORM (0) or DISTILL_REST (1)."""
+    _check(lib.symtile_distill_topk(device, _vp(logits), rows, vocab, ld, dtype, scale, _vp(ids),
+                                    _vp(values), values_dtype, k, mode, _vp(loss), _vp(stats),
+                                    _vp(row_grad), _vp(dlogits), ld_grad, _vp(workspace),
+                                    workspace_bytes, _vp(stream)), "symtile_distill_topk")
+
+
+def symtile_distill_topk_backward(device: int, logits: int, rows: int, vocab: int, ld: int,
+                                  dtype: int, scale: float, ids: int, values: int,
+                                  values_dtype: int, k: int, mode: int, stats: int, row_grad: int,
+                                  dlogits: int, ld_grad: int = 0, stream: int = 0) -> None:
+    _check(lib.symtile_distill_topk_backward(device, _vp(logits), rows, vocab, ld, dtype, scale,
+                                             _vp(ids), _vp(values), values_dtype, k, mode,
+                                             _vp(stats), _vp(row_grad), _vp(dlogits), ld_grad,
+                                             _vp(stream)), "symtile_distill_topk_backward")
+
+
+def symtile_w4_all_scatter(h: int, X: int, q: int, scales: int, zeros: int, C_gathered_local: int,
+                           arrived_local: int, M: int, N_local: int, K: int, ldx: int, group: int,
+                           dtype: int, rank: int, world_size: int, stream: int = 0) -> None:
+    _check(lib.symtile_w4_all_scatter(_vp(h), _vp(X), _vp(q), _vp(scales), _vp(zeros),
+                                      _vp(C_gathered_local), _vp(arrived_local), M, N_local, K,
+                                      ldx, group, dtype, rank, world_size, _vp(stream)),
+           "symtile_w4_all_scatter")
 
 
 def symtile_litmus_mp(h: int, data_off: int, flag_off: int, pairs: int, rounds: int,

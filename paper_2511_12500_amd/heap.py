@@ -247,3 +247,29 @@ class GatheredOutput:
             self._cfg_ref, current_stream(self.heap.device) if stream is None else stream)
         if st:
             B._check(st, "symtile_gemm_all_scatter")
+
+    def run_w4(self, X: torch.Tensor, weight, rank: int, stream: int | None = None) -> None:
+        """The call of rank ``rank`` for a few tokens X [M, K] and its shard of
+        4-bit weights (``W4Weight`` of N_local columns): the product lands in
+        the same places and counts the same arrivals as ``run``'s, in tiles of
+        W4_TILE_M x W4_TILE_N, which this object must have been made with.
+        Enqueued on the stream, asynchronous; it can be captured in a graph."""
+        if X.dtype != self.dtype or weight.dtype != self.dtype:
+            raise TypeError("X and the weight's scales must have the output dtype")
+        if not X.is_cuda or X.dim() != 2 or X.stride(1) != 1:
+            raise ValueError("X must be a device matrix with contiguous rows")
+        M, K = X.shape
+        if M != self.M or weight.N != self.N_local or weight.K != K:
+            raise ValueError("shape mismatch")
+        if (self.tile_m, self.tile_n) != (B.W4_TILE_M, B.W4_TILE_N):
+            raise ValueError("the output must be made with W4_TILE_M x W4_TILE_N tiles")
+        ptrs = self._ptrs.get(rank)
+        if ptrs is None:
+            ptrs = self._ptrs[rank] = (self.heap.ptr(rank, self.c_off),
+                                       self.heap.ptr(rank, self.flag_off))
+        st = B.lib.symtile_w4_all_scatter(
+            self.heap.handle, X.data_ptr(), *weight.pointers, ptrs[0], ptrs[1], M, self.N_local, K,
+            X.stride(0) if M > 1 and K else 0, weight.group, self._dt, rank, self.heap.world,
+            current_stream(self.heap.device) if stream is None else stream)
+        if st:
+            B._check(st, "symtile_w4_all_scatter")
