@@ -489,6 +489,8 @@ symtile_status symtile_gemm_all_scatter_noalloc(symtile_heap* h, const void* A,
 /* Most entries of a row: top alternatives (symtile_token_logprobs) and a
  * teacher's list (symtile_distill_topk). */
 #define SYMTILE_TOP_MAX 128
+/* Most tokens of a vocabulary in the calls on rows of logits. */
+#define SYMTILE_VOCAB_MAX (1 << 21)
 
 /* Bytes of the workspace of a symtile_token_logprobs (top) or
  * symtile_distill_topk (top = 0) call on `device` with these sizes: rows are
@@ -536,6 +538,7 @@ symtile_status symtile_logits_workspace_bytes(int device, int rows, int vocab, i
  *                NULL = no gradient.  May be logits itself (same address and
  *                stride), otherwise must not overlap it.
  *  workspace     see symtile_logits_workspace_bytes; may be NULL where that is 0.
+ *  vocab         1 .. SYMTILE_VOCAB_MAX.
  * EINVAL for anything else; rows = 0 launches nothing. */
 symtile_status symtile_token_logprobs(int device, const void* logits, int rows, int vocab,
                                       size_t ld, int dtype, float scale, const int64_t* targets,

@@ -17,7 +17,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OBJDIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libsymtile.so")
-SOURCES = ["heap.hip", "tile_copy.hip", "gemm_all_scatter.hip", "logits.hip", "w4_scatter.hip"]
+SOURCES = ["heap.hip", "tile_copy.hip", "gemm_all_scatter.hip", "token_logprobs.hip", "distill.hip", "w4_scatter.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
@@ -48,7 +48,7 @@ def build_library(extra: list[str] | None = None, verbose: bool = False) -> str:
     """Compile every source and link ``libsymtile.so``; returns its path."""
     os.makedirs(OBJDIR, exist_ok=True)
     extra = list(extra or [])
-    with cf.ThreadPoolExecutor(max_workers=min(len(SOURCES), 4)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=min(len(SOURCES), 6)) as ex:
         objs = list(ex.map(lambda s: _compile(s, extra), SOURCES))
     tmp = LIB + ".tmp"
     cmd = [HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", *objs, "-o", tmp]

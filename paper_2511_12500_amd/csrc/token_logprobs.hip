@@ -1,0 +1,592 @@
+// Log probabilities of given tokens, entropies, the most likely tokens, and
+// their gradient, from rows of logits.
+//
+// With y_v = c (x_v - m) (base 2, logits_rows.h), e_v = 2^y_v, s = sum e_v and
+// t = sum e_v y_v over a row:
+//   logp_v = ln 2 (y_v - log2 s),   H = ln 2 (log2 s - t / s),
+//   d_v = scale (p_v (g_lse - g_lp) - p_v (logp_v + H) g_H) + [v = target] scale g_lp
+//       = e_v (A + B y_v) + [v = target] scale g_lp,
+// so the gradient of a logit is one more exponential of it and two constants of
+// its row.
+#include "logits_rows.h"
+#include "symtile_device.h"
+
+namespace {
+
+using namespace logits;
+
+constexpr int kCap = 1024;          // candidates for the top entries of a segment
+
+enum Phase { kValues, kStep, kGrad };   // the values, both (whole rows), the gradient
+
+struct LogprobParams {
+    const void* x;
+    void* dx;
+    size_t ld, ld_grad;
+    const int64_t* targets;
+    float *logprob, *entropy, *stats;
+    int64_t* top_ids;
+    float* top_logprobs;
+    const float *g_logprob, *g_entropy, *g_lse;
+    uint32_t* counters;
+    float* partials;
+    uint64_t* keys;
+    symtile_host::Div by_segs;
+    int row0, vocab, top, segs, seg_len;
+    float scale;
+};
+
+struct Shared {
+    float m[kMaxWaves], s[kMaxWaves], t[kMaxWaves], tau[kMaxWaves];
+    uint32_t count[2][kMaxWaves];
+    float x_target;
+    int n, last;
+    uint64_t bound;
+};
+
+// ---- the order of the top entries ------------------------------------------------
+// As whole numbers: the larger logit first (a NaN above all, -0 as +0), then the
+// smaller id.  0 is below every logit.
+__device__ __forceinline__ uint32_t order(float x) {
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    const uint32_t o = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+    return x != x ? 0xFFFFFFFFu : o;
+}
+__device__ __forceinline__ float ordered_value(uint32_t o) {
+    return __uint_as_float(o == 0xFFFFFFFFu ? 0x7FC00000u
+                           : o & 0x80000000u ? o ^ 0x80000000u
+                                             : ~o);
+}
+__device__ __forceinline__ uint64_t top_key(uint32_t o, int id) {
+    return (uint64_t)o << 32 | (0xFFFFFFFFu - (uint32_t)id);
+}
+__device__ __forceinline__ int key_id(uint64_t key) { return (int)(0xFFFFFFFFu - (uint32_t)key); }
+
+// Sum over the workgroup; `step` alternates between the two arrays, so that one
+// barrier a call is enough.
+__device__ __forceinline__ uint32_t block_count(uint32_t c, Shared& sh, int& step, int waves) {
+    c = wave_sum_u32(c);
+    uint32_t* a = sh.count[step & 1];
+    ++step;
+    if (threadIdx.x % 64 == 0) a[threadIdx.x / 64] = c;
+    __syncthreads();
+    uint32_t n = 0;
+    for (int w = 0; w < waves; ++w) n += a[w];
+    return n;
+}
+
+// n distinct keys in LDS; calls emit(place, key) for the `keep` largest.  The
+// place is the number of larger keys, counted by as many threads a key as there
+// are.
+template <class F>
+__device__ __forceinline__ void rank_keys(const uint64_t* keys, uint32_t* rank, int n, int keep,
+                                          F emit) {
+    const int threads = blockDim.x;
+    for (int i = threadIdx.x; i < n; i += threads) rank[i] = 0;
+    __syncthreads();
+    int parts = 1;
+    while (2 * parts * n <= threads) parts *= 2;
+    const int per = (n + parts - 1) / parts;
+    for (int at = threadIdx.x; at < n * parts; at += threads) {
+        const int i = at % n, first = at / n * per;
+        const uint64_t mine = keys[i];
+        uint32_t c = 0;
+        for (int j = first; j < min(first + per, n); ++j) c += keys[j] > mine;
+        if (c) atomicAdd(&rank[i], c);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += threads)
+        if ((int)rank[i] < keep) emit((int)rank[i], keys[i]);
+}
+
+// A bound for the wave's share of the top entries: the j-th largest of its
+// lanes' largest logits, to 16 bits of their order (rounded down); -inf where
+// there is none.
+__device__ __forceinline__ float wave_bound(float lane_max, int j) {
+    if (j > 64) return -kInf;
+    const uint32_t o = order(lane_max);
+    uint32_t p = 0;
+#pragma unroll
+    for (int b = 31; b >= 16; --b) {
+        const uint32_t trial = p | 1u << b;
+        const int n = __popcll(__ballot(o >= trial));
+        p = n >= j ? trial : p;
+    }
+    return p < 0x00800000u ? -kInf : ordered_value(p);
+}
+
+// The `keep` largest of a segment's elements (keep <= len), as keys with ids from
+// `id0` on, to emit(place, key).
+//
+// `tau` is at or below the keep-th largest where the bounds of the waves say so;
+// usually a few more than `keep` elements reach it, and those are ranked.  Where
+// too many do (ties, a row that is mostly masked, sorted rows, a NaN) the bound
+// is the keep-th largest of the threads' largest elements, and if that leaves too
+// many the keep-th largest element itself, found bit by bit; what is above the
+// bound is taken, and of the elements equal to it those of the lowest ids.
+template <int DT, int NV, class F>
+__device__ __forceinline__ void select_top(const Segment<DT, NV>& d, float lane_max, float tau,
+                                           bool sane, int keep, int id0, int len, Shared& sh,
+                                           uint64_t* keys, uint32_t* rank, F emit) {
+    constexpr int kVec = Elem<DT>::kVec;
+    const int threads = blockDim.x, waves = threads / 64, t = threadIdx.x;
+    auto at = [&](int i, int e) { return (i * threads + t) * kVec + e; };
+    if (t == 0) sh.n = 0;
+    __syncthreads();
+    if (sane && __ballot(lane_max >= tau)) {
+        d.each([&](int i, int e, float x) {
+            if (x >= tau) {
+                const int n = atomicAdd(&sh.n, 1);
+                if (n < kCap) keys[n] = top_key(order(x), id0 + at(i, e));
+            }
+        });
+    }
+    __syncthreads();
+    int n = sh.n;
+    if (!sane || n < keep || n > max(4 * keep, 128)) {
+        int step = 0;
+        __syncthreads();
+        uint32_t mine = 0;
+        d.each([&](int i, int e, float x) {
+            if (at(i, e) < len) mine = max(mine, order(x));
+        });
+        uint32_t T = 0;
+        for (int b = 31; b >= 0; --b) {
+            const uint32_t trial = T | 1u << b;
+            if ((int)block_count(mine >= trial, sh, step, waves) >= keep) T = trial;
+        }
+        auto above = [&](uint32_t bound) {
+            uint32_t c = 0;
+            d.each([&](int i, int e, float x) { c += at(i, e) < len && order(x) > bound; });
+            return (int)block_count(c, sh, step, waves);
+        };
+        int gt = above(T);
+        // ranking gt keys against a pass over the registers for each of 32 bits, in cycles
+        const float by_rank = 10.0f * (float)gt * (float)gt / (float)threads;
+        const float by_bits = 32.0f * (200.0f + 6.0f * NV * kVec * (float)waves);
+        if (gt > kCap || (gt > keep && by_rank > by_bits)) {
+            T = 0;
+            for (int b = 31; b >= 0; --b) {
+                const uint32_t trial = T | 1u << b;
+                if (above(trial - 1) >= keep) T = trial;
+            }
+            gt = above(T);
+        }
+        if (t == 0) sh.n = 0;
+        __syncthreads();
+        d.each([&](int i, int e, float x) {
+            const uint32_t o = order(x);
+            if (at(i, e) < len && o > T) keys[atomicAdd(&sh.n, 1)] = top_key(o, id0 + at(i, e));
+        });
+        // elements equal to T in the order of their ids: vector by vector of all threads
+        int taken = gt;
+        for (int i = 0; i < NV; ++i) {
+            if (taken >= keep) break;
+            uint32_t c = 0;
+            uint32_t tie = 0;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                if (k != i) continue;
+#pragma unroll
+                for (int e = 0; e < kVec; ++e)
+                    if (at(k, e) < len && order(element<DT>(d.v[k], e)) == T) tie |= 1u << e;
+            }
+            c = __popc(tie);
+            uint32_t before = c;     // inclusive over the wave's lanes
+#pragma unroll
+            for (int o = 1; o < 64; o *= 2) {
+                const uint32_t u = __shfl_up(before, o);
+                if (t % 64 >= o) before += u;
+            }
+            uint32_t* a = sh.count[step & 1];
+            ++step;
+            if (t % 64 == 63) a[t / 64] = before;
+            __syncthreads();
+            uint32_t base = 0, all = 0;
+            for (int w = 0; w < waves; ++w) {
+                base += w < t / 64 ? a[w] : 0;
+                all += a[w];
+            }
+            int place = taken + (int)(base + before - c);
+            for (int e = 0; e < kVec; ++e)
+                if (tie >> e & 1) {
+                    if (place < keep) keys[place] = top_key(T, id0 + at(i, e));
+                    ++place;
+                }
+            taken += (int)all;
+        }
+        n = max(gt, keep);
+        __syncthreads();
+    }
+    rank_keys(keys, rank, n, keep, emit);
+}
+
+// What the gradient of a row needs of it.
+struct RowGrad {
+    float a, b, own;
+};
+__device__ __forceinline__ RowGrad row_grad(const LogprobParams& p, int r, int64_t target, float m,
+                                            float log_s, float entropy, const Exponent& ex) {
+    RowGrad o;
+    float gl = p.g_logprob && target >= 0 ? p.g_logprob[r] : 0.0f;
+    if (target >= p.vocab) gl = __builtin_nanf("");
+    const float ge = p.g_entropy ? p.g_entropy[r] : 0.0f;
+    const float gs = p.g_lse ? p.g_lse[r] : 0.0f;
+    // p = 2^y / s', logp = ln2 (y - log2 s') with s' = s 2^shift, log s' = log s + ln2 shift
+    const float log_sy = log_s + kLn2 * ex.shift;
+    const float inv = expf(-log_sy) * p.scale;
+    o.a = inv * (gs - gl - ge * (entropy - log_sy));
+    o.b = -inv * ge * kLn2;
+    // a row of -inf alone has no gradient (all its e_v are 0)
+    o.own = m == -kInf && log_s == 0.0f ? 0.0f : gl * p.scale;
+    return o;
+}
+
+template <int DT, int NV, bool HUGE>
+__device__ __forceinline__ void write_grad(const Segment<DT, NV>& d,
+                                           typename Elem<DT>::type* __restrict__ dx, int len,
+                                           int64_t target, const RowGrad& g, const Exponent& ex) {
+    constexpr int kVec = Elem<DT>::kVec;
+    const int threads = blockDim.x;
+    const int at_target = target >= 0 && target < len ? (int)target : -kVec;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int at = (i * threads + (int)threadIdx.x) * kVec;
+        float f[kVec];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+            const float y = ex.template y<HUGE>(element<DT>(d.v[i], e));
+            f[e] = exp2_fast(y) * __builtin_fmaf(g.b, fmaxf(y, kFloorY), g.a);
+        }
+        if ((unsigned)(at_target - at) < (unsigned)kVec) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                if (at + e == at_target) f[e] += g.own;
+        }
+        Segment<DT, NV>::store(dx, len, at, pack<DT>(f));
+    }
+}
+
+template <int DT, int NV, bool HUGE>
+__device__ __forceinline__ void sums(const Segment<DT, NV>& d, const Exponent& ex, float* s,
+                                     float* t) {
+    float s0 = 0.0f, s1 = 0.0f, t0 = 0.0f, t1 = 0.0f;
+    d.each([&](int, int e, float x) {
+        const float y = ex.template y<HUGE>(x);
+        const float v = exp2_fast(y);
+        float& ss = e % 2 ? s1 : s0;
+        float& tt = e % 2 ? t1 : t0;
+        ss += v;
+        tt = __builtin_fmaf(v, fmaxf(y, kFloorY), tt);
+    });
+    *s = s0 + s1;
+    *t = t0 + t1;
+}
+
+// m, s and t of a row (t in natural units: sum e scale (x - m)) to its outputs.
+struct RowValues {
+    float m, log_s, entropy;
+    bool empty;
+    __device__ __forceinline__ RowValues(float m_, float s, float t) : m(m_) {
+        empty = m == -kInf && s == 0.0f;
+        log_s = empty ? 0.0f : logf(s);
+        entropy = empty ? 0.0f : log_s - t / s;
+    }
+    __device__ __forceinline__ float logp(float x, float scale) const {
+        return empty ? -kInf : (x - (m == -kInf ? 0.0f : m)) * scale - log_s;
+    }
+};
+
+__device__ __forceinline__ void write_values(const LogprobParams& p, int r, int64_t target,
+                                             float x_target, const RowValues& v) {
+    if (p.logprob)
+        p.logprob[r] = target < 0           ? 0.0f
+                       : target >= p.vocab ? __builtin_nanf("")
+                                           : v.logp(x_target, p.scale);
+    if (p.entropy) p.entropy[r] = v.entropy;
+    if (p.stats) {
+        p.stats[2 * (size_t)r] = v.m;
+        p.stats[2 * (size_t)r + 1] = v.log_s;
+    }
+}
+
+template <int DT, int NV, int PHASE, bool TOP>
+__global__ void __launch_bounds__(kMaxThreads) logprob_kernel(LogprobParams p) {
+    typedef typename Elem<DT>::type T;
+    extern __shared__ __attribute__((aligned(16))) uint64_t dyn[];
+    __shared__ Shared sh;
+    const int t = threadIdx.x, threads = blockDim.x, waves = threads / 64;
+    const int local = p.by_segs(blockIdx.x), seg = blockIdx.x - local * p.segs;
+    const int r = p.row0 + local;
+    const int id0 = seg * p.seg_len, len = min(p.seg_len, p.vocab - id0);
+    const T* row = static_cast<const T*>(p.x) + (size_t)r * p.ld;
+    const int64_t target = p.targets ? p.targets[r] : -1;
+    Segment<DT, NV> d;
+    d.load(row + id0, len, threads);
+    float m, log_s, entropy;
+    if constexpr (PHASE == kGrad) {
+        m = p.stats[2 * (size_t)r];
+        log_s = p.stats[2 * (size_t)r + 1];
+        entropy = p.entropy[r];
+    } else {
+        // read before anything is written: the gradient may overwrite it
+        if (t == 0 && target >= 0 && target < p.vocab) {
+            if constexpr (DT == SYMTILE_F32) sh.x_target = row[target];
+            else sh.x_target = (float)row[target];
+        }
+        const float lane_max = d.thread_max();
+        m = wave_max(lane_max);
+        if constexpr (TOP) {
+            // all waves but the one of the lowest bound hold `top` elements together
+            const float bound = wave_bound(lane_max, (p.top + waves - 2) / (waves - 1));
+            if (t % 64 == 0) sh.tau[t / 64] = bound;
+        }
+        if (t % 64 == 0) sh.m[t / 64] = m;
+        __syncthreads();
+        m = over_waves(sh.m, waves, Max());
+        const Exponent ex(m, p.scale);
+        float s, u;
+        if (ex.huge) sums<DT, NV, true>(d, ex, &s, &u);
+        else sums<DT, NV, false>(d, ex, &s, &u);
+        s = wave_sum(s);
+        u = wave_sum(u);
+        if (t % 64 == 0) {
+            sh.s[t / 64] = s;
+            sh.t[t / 64] = u;
+        }
+        __syncthreads();
+        const float back = exp2f(-ex.shift);
+        s = over_waves(sh.s, waves, Sum()) * back;
+        u = kLn2 * (over_waves(sh.t, waves, Sum()) * back - ex.shift * s);
+        float tau = -kInf;
+        bool sane = false;
+        if constexpr (TOP) {
+            float lowest = kInf;   // the lowest bound may be of a wave without elements: the next
+            tau = kInf;
+            for (int w = 0; w < waves; ++w) {
+                const float b = sh.tau[w];
+                tau = fminf(tau, fmaxf(lowest, b));
+                lowest = fminf(lowest, b);
+            }
+            sane = s == s && tau > -kInf;
+        }
+        uint64_t* keys = dyn;
+        const int cap = max(kCap, p.segs * p.top);
+        uint32_t* rank = reinterpret_cast<uint32_t*>(dyn + cap);
+        if (p.segs == 1) {
+            const RowValues v(m, s, u);
+            if (t == 0) write_values(p, r, target, sh.x_target, v);
+            if constexpr (TOP) {
+                select_top(d, lane_max, tau, sane, p.top, id0, len, sh, keys, rank,
+                           [&](int place, uint64_t key) {
+                               const size_t o = (size_t)r * p.top + place;
+                               p.top_ids[o] = key_id(key);
+                               p.top_logprobs[o] =
+                                   v.logp(ordered_value((uint32_t)(key >> 32)), p.scale);
+                           });
+            }
+            log_s = v.log_s;
+            entropy = v.entropy;
+        } else {
+            const size_t unit = (size_t)local * p.segs + seg;
+            if constexpr (TOP) {
+                const int keep = min(p.top, len);
+                uint64_t* out = p.keys + unit * p.top;
+                select_top(d, lane_max, tau, sane, keep, id0, len, sh, keys, rank,
+                           [&](int place, uint64_t key) { put(out + place, key); });
+                for (int i = keep + t; i < p.top; i += threads) put(out + i, 0ull);
+            }
+            if (t == 0) {
+                float* o = p.partials + 4 * unit;
+                put(o, m);
+                put(o + 1, s);
+                put(o + 2, u);
+            }
+            if (!arrive_last(p.counters + local, p.segs, &sh.last)) return;
+            // the row's values from its segments', by every wave
+            const float* o = p.partials + 4 * (size_t)local * p.segs;
+            float ms = -kInf, ss = 0.0f, us = 0.0f;
+            const int lane = t % 64;
+            if (lane < p.segs) {
+                ms = take(o + 4 * lane);
+                ss = take(o + 4 * lane + 1);
+                us = take(o + 4 * lane + 2);
+            }
+            m = wave_max(ms);
+            const float lower = ms == -kInf || ms == m ? 0.0f : (ms - m) * p.scale;
+            const float f = expf(lower);
+            s = wave_sum(f * ss);
+            u = wave_sum(f * __builtin_fmaf(fmaxf(lower, kFloorY), ss, us));
+            const RowValues v(m, s, u);
+            if (t == 0) write_values(p, r, target, sh.x_target, v);
+            if constexpr (TOP) {
+                // no segment's last key can be above the row's
+                const uint64_t* in = p.keys + (size_t)local * p.segs * p.top;
+                if (t == 0) {
+                    sh.n = 0;
+                    sh.bound = 0;
+                }
+                __syncthreads();
+                if (t < p.segs) {
+                    const uint64_t last = take(in + (size_t)t * p.top + p.top - 1);
+                    atomicMax(reinterpret_cast<unsigned long long*>(&sh.bound),
+                              (unsigned long long)last);
+                }
+                __syncthreads();
+                for (int i = t; i < p.segs * p.top; i += threads) {
+                    const uint64_t key = take(in + i);
+                    if (key != 0 && key >= sh.bound) keys[atomicAdd(&sh.n, 1)] = key;
+                }
+                __syncthreads();
+                rank_keys(keys, rank, sh.n, p.top, [&](int place, uint64_t key) {
+                    const size_t at = (size_t)r * p.top + place;
+                    p.top_ids[at] = key_id(key);
+                    p.top_logprobs[at] = v.logp(ordered_value((uint32_t)(key >> 32)), p.scale);
+                });
+            }
+            return;
+        }
+    }
+    if constexpr (PHASE != kValues) {
+        const Exponent ex(m, p.scale);
+        const RowGrad g = row_grad(p, r, target, m, log_s, entropy, ex);
+        T* dx = static_cast<T*>(p.dx) + (size_t)r * p.ld_grad + id0;
+        const int64_t here = target >= id0 && target < p.vocab ? target - id0 : -1;
+        if (ex.huge) write_grad<DT, NV, true>(d, dx, len, here, g, ex);
+        else write_grad<DT, NV, false>(d, dx, len, here, g, ex);
+    }
+}
+
+template <int PHASE, bool TOP>
+const void* kernel_of(int dtype, int nv) {
+    return pick(dtype, nv, [](auto d, auto n) {
+        return reinterpret_cast<const void*>(
+            &logprob_kernel<decltype(d)::value, decltype(n)::value, PHASE, TOP>);
+    });
+}
+
+// The kernels of a call, in launches whose threads fit 32 bits.
+symtile_status run(LogprobParams p, const Plan& plan, int rows, int dtype, const void* kernel,
+                   symtile_stream s, const char* what) {
+    p.segs = plan.segs;
+    p.seg_len = plan.seg_len;
+    p.by_segs = symtile_host::make_div(plan.segs);
+    const size_t lds = p.top ? (size_t)std::max(kCap, plan.segs * p.top) * 12 : 0;
+    const int most = (int)((size_t(1) << 30) / ((size_t)plan.threads * plan.segs));
+    for (int row = 0; row < rows; row += most) {
+        const int n = std::min(most, rows - row);
+        LogprobParams q = p;
+        q.row0 = row;
+        if (symtile_status st = launch(kernel, plan, n, lds, q, s, what)) return st;
+    }
+    return SYMTILE_OK;
+}
+
+}  // namespace
+
+extern "C" symtile_status symtile_logits_workspace_bytes(int device, int rows, int vocab, int dtype,
+                                                         int top, size_t* bytes) {
+    if (!bytes) return fail(SYMTILE_EINVAL, "bytes is NULL");
+    *bytes = 0;
+    if (symtile_status st = check_sizes(rows, vocab, dtype, top)) return st;
+    *bytes = make_workspace(make_plan(device, rows, vocab, dtype, top), rows, top).bytes;
+    return SYMTILE_OK;
+}
+
+extern "C" symtile_status symtile_token_logprobs(
+    int device, const void* logits, int rows, int vocab, size_t ld, int dtype, float scale,
+    const int64_t* targets, float* logprob, float* entropy, float* stats, int top,
+    int64_t* top_ids, float* top_logprobs, const float* grad_logprob, const float* grad_entropy,
+    const float* grad_lse, void* dlogits, size_t ld_grad, void* workspace, size_t workspace_bytes,
+    symtile_stream s) {
+    if (symtile_status st = check_sizes(rows, vocab, dtype, top)) return st;
+    if (symtile_status st = check_logits(logits, rows, vocab, &ld, dtype, scale)) return st;
+    if (rows && ((targets == nullptr) != (logprob == nullptr)))
+        return fail(SYMTILE_EINVAL, "targets and logprob come together");
+    if (rows && top && (!top_ids || !top_logprobs))
+        return fail(SYMTILE_EINVAL, "top needs top_ids and top_logprobs");
+    if (dlogits) {
+        if (symtile_status st = check_grad(logits, ld, dlogits, &ld_grad, rows, vocab, dtype))
+            return st;
+        if (rows && (!entropy || !stats))
+            return fail(SYMTILE_EINVAL, "dlogits needs entropy and stats");
+    } else if (grad_logprob || grad_entropy || grad_lse) {
+        return fail(SYMTILE_EINVAL, "gradients without dlogits");
+    }
+    if (grad_logprob && !targets) return fail(SYMTILE_EINVAL, "grad_logprob without targets");
+    const Plan plan = make_plan(device, rows, vocab, dtype, top);
+    const Workspace ws = make_workspace(plan, rows, top);
+    if (symtile_status st = check_workspace(workspace, workspace_bytes, ws.bytes)) return st;
+    if (rows == 0) return SYMTILE_OK;
+    LogprobParams p{};
+    p.x = logits;
+    p.dx = dlogits;
+    p.ld = ld;
+    p.ld_grad = ld_grad;
+    p.targets = targets;
+    p.logprob = logprob;
+    p.entropy = entropy;
+    p.stats = stats;
+    p.top = top;
+    p.top_ids = top_ids;
+    p.top_logprobs = top_logprobs;
+    p.g_logprob = grad_logprob;
+    p.g_entropy = grad_entropy;
+    p.g_lse = grad_lse;
+    p.vocab = vocab;
+    p.scale = scale;
+    if (ws.bytes) {
+        char* base = static_cast<char*>(workspace);
+        p.counters = reinterpret_cast<uint32_t*>(base);
+        p.partials = reinterpret_cast<float*>(base + ws.partials);
+        p.keys = reinterpret_cast<uint64_t*>(base + ws.keys);
+    }
+    OnDevice on(device);
+    if (on.status) return on.status;
+    if (dlogits && plan.segs == 1)
+        return run(p, plan, rows, dtype,
+                   top ? kernel_of<kStep, true>(dtype, plan.nv)
+                       : kernel_of<kStep, false>(dtype, plan.nv),
+                   s, "logprob_kernel launch");
+    if (symtile_status st = run(p, plan, rows, dtype,
+                                top ? kernel_of<kValues, true>(dtype, plan.nv)
+                                    : kernel_of<kValues, false>(dtype, plan.nv),
+                                s, "logprob_kernel launch"))
+        return st;
+    if (!dlogits) return SYMTILE_OK;
+    p.top = 0;
+    return run(p, plan, rows, dtype, kernel_of<kGrad, false>(dtype, plan.nv), s,
+               "logprob_kernel launch (gradient)");
+}
+
+extern "C" symtile_status symtile_token_logprobs_backward(
+    int device, const void* logits, int rows, int vocab, size_t ld, int dtype, float scale,
+    const int64_t* targets, const float* entropy, const float* stats, const float* grad_logprob,
+    const float* grad_entropy, const float* grad_lse, void* dlogits, size_t ld_grad,
+    symtile_stream s) {
+    if (symtile_status st = check_sizes(rows, vocab, dtype, 0)) return st;
+    if (symtile_status st = check_logits(logits, rows, vocab, &ld, dtype, scale)) return st;
+    if (rows && !dlogits) return fail(SYMTILE_EINVAL, "dlogits is NULL");
+    if (symtile_status st = check_grad(logits, ld, dlogits, &ld_grad, rows, vocab, dtype)) return st;
+    if (rows && (!entropy || !stats)) return fail(SYMTILE_EINVAL, "entropy or stats is NULL");
+    if (grad_logprob && !targets) return fail(SYMTILE_EINVAL, "grad_logprob without targets");
+    if (rows == 0) return SYMTILE_OK;
+    LogprobParams p{};
+    p.x = logits;
+    p.dx = dlogits;
+    p.ld = ld;
+    p.ld_grad = ld_grad;
+    p.targets = targets;
+    p.entropy = const_cast<float*>(entropy);
+    p.stats = const_cast<float*>(stats);
+    p.g_logprob = grad_logprob;
+    p.g_entropy = grad_entropy;
+    p.g_lse = grad_lse;
+    p.vocab = vocab;
+    p.scale = scale;
+    OnDevice on(device);
+    if (on.status) return on.status;
+    const Plan plan = make_plan(device, rows, vocab, dtype, 0);
+    return run(p, plan, rows, dtype, kernel_of<kGrad, false>(dtype, plan.nv), s,
+               "logprob_kernel launch (gradient)");
+}
