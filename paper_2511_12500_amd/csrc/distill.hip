@@ -155,7 +155,8 @@ __device__ __forceinline__ void gradient_constants(const DistillParams& p, int r
 }
 
 template <int DT, int NV, bool HUGE>
-__device__ __forceinline__ float rest_sum(const Segment<DT, NV>& d, const Exponent& ex) {
+__device__ __forceinline__ float rest_sum(Segment<DT, NV>& d, const Exponent& ex) {
+    d.again();
     float s0 = 0.0f, s1 = 0.0f;
     d.each([&](int, int e, float x) {
         const float v = exp2_fast(ex.template y<HUGE>(x));
@@ -165,12 +166,14 @@ __device__ __forceinline__ float rest_sum(const Segment<DT, NV>& d, const Expone
     return s0 + s1;
 }
 
-template <int DT, int NV, bool HUGE>
-__device__ __forceinline__ void write_rest(const Segment<DT, NV>& d,
+// READ: whether the registers were read in a pass before.
+template <int DT, int NV, bool HUGE, bool READ>
+__device__ __forceinline__ void write_rest(Segment<DT, NV>& d,
                                            typename Elem<DT>::type* __restrict__ dx, int len,
                                            float coef, const Exponent& ex) {
     constexpr int kVec = Elem<DT>::kVec;
     const int threads = blockDim.x;
+    if constexpr (READ) d.again();
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int at = (i * threads + (int)threadIdx.x) * kVec;
@@ -337,8 +340,8 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
             const float none[kVec] = {};
             for (int i = 0; i < NV; ++i)
                 Segment<DT, NV>::store(dx, len, (i * threads + t) * kVec, pack<DT>(none));
-        } else if (ex.huge) write_rest<DT, NV, true>(d, dx, len, coef, ex);
-        else write_rest<DT, NV, false>(d, dx, len, coef, ex);
+        } else if (ex.huge) write_rest<DT, NV, true, PHASE == kStep>(d, dx, len, coef, ex);
+        else write_rest<DT, NV, false, PHASE == kStep>(d, dx, len, coef, ex);
         symtile::wg_stores_done();   // the list's entries come after the zeros in their places
         if (first_wave) {
 #pragma unroll

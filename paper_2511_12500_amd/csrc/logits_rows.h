@@ -193,6 +193,12 @@ struct Segment {
         return r;
     }
 
+    // A vector of the segment by its first element, from memory again.
+    static __device__ __forceinline__ symtile::u32x4 fetch(const typename Elem<DT>::type* p, int len,
+                                                           int at) {
+        return at + kVec <= len ? load16(p + at) : load_part(p + at, len - at);
+    }
+
     // Vector i of the results at p: whole, or its elements inside `len`.
     static __device__ __forceinline__ void store(typename Elem<DT>::type* p, int len, int at,
                                                  const symtile::u32x4& r) {
@@ -212,6 +218,14 @@ struct Segment {
                     if (e < n) h[e] = (uint16_t)(r[e / 2] >> (16 * (e % 2)));
             }
         }
+    }
+
+    // Before another pass over the registers.  The compiler would otherwise keep
+    // the fp32 values of the pass before, twice the registers of 16-bit logits
+    // (spills with 16 vectors a thread, and half the waves with 8).
+    __device__ __forceinline__ void again() {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(v[i]));
     }
 
     template <class F>

@@ -115,8 +115,8 @@ __device__ __forceinline__ float wave_bound(float lane_max, int j) {
     return p < 0x00800000u ? -kInf : ordered_value(p);
 }
 
-// The `keep` largest of a segment's elements (keep <= len), as keys with ids from
-// `id0` on, to emit(place, key).
+// The `keep` largest of the `len` elements at `seg` (keep <= len), whose vectors
+// are in d, as keys with ids from `id0` on, to emit(place, key).
 //
 // `tau` is at or below the keep-th largest where the bounds of the waves say so;
 // usually a few more than `keep` elements reach it, and those are ranked.  Where
@@ -124,74 +124,109 @@ __device__ __forceinline__ float wave_bound(float lane_max, int j) {
 // is the keep-th largest of the threads' largest elements, and if that leaves too
 // many the keep-th largest element itself, found bit by bit; what is above the
 // bound is taken, and of the elements equal to it those of the lowest ids.
+//
+// The registers only say which vectors hold an element that reaches the bound;
+// the elements are picked from memory, where the row was just read from.  Picking
+// them from registers takes code for each (20 000 instructions with 8 vectors a
+// thread, which a single row's call spent 15 us fetching).
 template <int DT, int NV, class F>
-__device__ __forceinline__ void select_top(const Segment<DT, NV>& d, float lane_max, float tau,
-                                           bool sane, int keep, int id0, int len, Shared& sh,
-                                           uint64_t* keys, uint32_t* rank, F emit) {
-    constexpr int kVec = Elem<DT>::kVec;
+__device__ __forceinline__ void select_top(Segment<DT, NV>& d, const typename Elem<DT>::type* seg,
+                                           float tau, bool sane, int keep, int id0, int len,
+                                           Shared& sh, uint64_t* keys, uint32_t* rank, F emit) {
+    typedef Segment<DT, NV> S;
+    constexpr int kVec = S::kVec;
     const int threads = blockDim.x, waves = threads / 64, t = threadIdx.x;
-    auto at = [&](int i, int e) { return (i * threads + t) * kVec + e; };
     if (t == 0) sh.n = 0;
     __syncthreads();
-    if (sane && __ballot(lane_max >= tau)) {
-        d.each([&](int i, int e, float x) {
-            if (x >= tau) {
-                const int n = atomicAdd(&sh.n, 1);
-                if (n < kCap) keys[n] = top_key(order(x), id0 + at(i, e));
+    if (sane) {
+        uint32_t hits = 0;
+        d.again();
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float m = -kInf;
+#pragma unroll
+            for (int e = 0; e < kVec; e += 2)
+                m = max3(m, element<DT>(d.v[i], e), element<DT>(d.v[i], e + 1));
+            hits |= m >= tau ? 1u << i : 0u;
+        }
+        while (hits) {
+            const int at = ((__ffs(hits) - 1) * threads + t) * kVec;
+            hits &= hits - 1;
+            const symtile::u32x4 w = S::fetch(seg, len, at);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                const float x = element<DT>(w, e);
+                if (x >= tau) {
+                    const int n = atomicAdd(&sh.n, 1);
+                    if (n < kCap) keys[n] = top_key(order(x), id0 + at + e);
+                }
             }
-        });
+        }
     }
     __syncthreads();
     int n = sh.n;
     if (!sane || n < keep || n > max(4 * keep, 128)) {
         int step = 0;
         __syncthreads();
+        // f(element's index, its order) for this thread's elements
+        auto each = [&](auto f) {
+#pragma unroll 1
+            for (int at = t * kVec; at < len; at += threads * kVec) {
+                const symtile::u32x4 w = S::fetch(seg, len, at);
+#pragma unroll
+                for (int e = 0; e < kVec; ++e)
+                    if (at + e < len) f(at + e, order(element<DT>(w, e)));
+            }
+        };
         uint32_t mine = 0;
-        d.each([&](int i, int e, float x) {
-            if (at(i, e) < len) mine = max(mine, order(x));
-        });
+        each([&](int, uint32_t o) { mine = max(mine, o); });
         uint32_t T = 0;
+#pragma unroll 1
         for (int b = 31; b >= 0; --b) {
             const uint32_t trial = T | 1u << b;
             if ((int)block_count(mine >= trial, sh, step, waves) >= keep) T = trial;
         }
-        auto above = [&](uint32_t bound) {
+        // the number of elements above T; where ranking them would cost more than a pass over the
+        // row for each of 32 bits (in cycles), T is raised to the keep-th largest itself
+        int gt = 0;
+        bool by_bits = false;
+        for (int b = -1;;) {
+            const uint32_t bound = b < 0 ? T : (T | 1u << b) - 1;
             uint32_t c = 0;
-            d.each([&](int i, int e, float x) { c += at(i, e) < len && order(x) > bound; });
-            return (int)block_count(c, sh, step, waves);
-        };
-        int gt = above(T);
-        // ranking gt keys against a pass over the registers for each of 32 bits, in cycles
-        const float by_rank = 10.0f * (float)gt * (float)gt / (float)threads;
-        const float by_bits = 32.0f * (200.0f + 6.0f * NV * kVec * (float)waves);
-        if (gt > kCap || (gt > keep && by_rank > by_bits)) {
-            T = 0;
-            for (int b = 31; b >= 0; --b) {
-                const uint32_t trial = T | 1u << b;
-                if (above(trial - 1) >= keep) T = trial;
+            each([&](int, uint32_t o) { c += o > bound; });
+            const int above = (int)block_count(c, sh, step, waves);
+            if (b < 0) {
+                gt = above;
+                if (by_bits || gt <= keep) break;
+                const float rank_cost = 10.0f * (float)gt * (float)gt / (float)threads;
+                if (gt <= kCap && rank_cost <= 32.0f * (2000.0f + 6.0f * NV * kVec * (float)waves))
+                    break;
+                by_bits = true;
+                T = 0;
+                b = 31;
+            } else {
+                if (above >= keep) T = bound + 1;
+                --b;
             }
-            gt = above(T);
         }
         if (t == 0) sh.n = 0;
         __syncthreads();
-        d.each([&](int i, int e, float x) {
-            const uint32_t o = order(x);
-            if (at(i, e) < len && o > T) keys[atomicAdd(&sh.n, 1)] = top_key(o, id0 + at(i, e));
+        each([&](int i, uint32_t o) {
+            if (o > T) keys[atomicAdd(&sh.n, 1)] = top_key(o, id0 + i);
         });
         // elements equal to T in the order of their ids: vector by vector of all threads
         int taken = gt;
-        for (int i = 0; i < NV; ++i) {
-            if (taken >= keep) break;
-            uint32_t c = 0;
+#pragma unroll 1
+        for (int first = 0; taken < keep && first < len; first += threads * kVec) {
+            const int at = first + t * kVec;
             uint32_t tie = 0;
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                if (k != i) continue;
+            if (at < len) {
+                const symtile::u32x4 w = S::fetch(seg, len, at);
 #pragma unroll
                 for (int e = 0; e < kVec; ++e)
-                    if (at(k, e) < len && order(element<DT>(d.v[k], e)) == T) tie |= 1u << e;
+                    if (at + e < len && order(element<DT>(w, e)) == T) tie |= 1u << e;
             }
-            c = __popc(tie);
+            const uint32_t c = __popc(tie);
             uint32_t before = c;     // inclusive over the wave's lanes
 #pragma unroll
             for (int o = 1; o < 64; o *= 2) {
@@ -210,7 +245,7 @@ __device__ __forceinline__ void select_top(const Segment<DT, NV>& d, float lane_
             int place = taken + (int)(base + before - c);
             for (int e = 0; e < kVec; ++e)
                 if (tie >> e & 1) {
-                    if (place < keep) keys[place] = top_key(T, id0 + at(i, e));
+                    if (place < keep) keys[place] = top_key(T, id0 + at + e);
                     ++place;
                 }
             taken += (int)all;
@@ -242,12 +277,14 @@ __device__ __forceinline__ RowGrad row_grad(const LogprobParams& p, int r, int64
     return o;
 }
 
-template <int DT, int NV, bool HUGE>
-__device__ __forceinline__ void write_grad(const Segment<DT, NV>& d,
+// READ: whether the registers were read in a pass before.
+template <int DT, int NV, bool HUGE, bool READ>
+__device__ __forceinline__ void write_grad(Segment<DT, NV>& d,
                                            typename Elem<DT>::type* __restrict__ dx, int len,
                                            int64_t target, const RowGrad& g, const Exponent& ex) {
     constexpr int kVec = Elem<DT>::kVec;
     const int threads = blockDim.x;
+    if constexpr (READ) d.again();
     const int at_target = target >= 0 && target < len ? (int)target : -kVec;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -268,8 +305,8 @@ __device__ __forceinline__ void write_grad(const Segment<DT, NV>& d,
 }
 
 template <int DT, int NV, bool HUGE>
-__device__ __forceinline__ void sums(const Segment<DT, NV>& d, const Exponent& ex, float* s,
-                                     float* t) {
+__device__ __forceinline__ void sums(Segment<DT, NV>& d, const Exponent& ex, float* s, float* t) {
+    d.again();
     float s0 = 0.0f, s1 = 0.0f, t0 = 0.0f, t1 = 0.0f;
     d.each([&](int, int e, float x) {
         const float y = ex.template y<HUGE>(x);
@@ -377,7 +414,7 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(LogprobParams p) {
             const RowValues v(m, s, u);
             if (t == 0) write_values(p, r, target, sh.x_target, v);
             if constexpr (TOP) {
-                select_top(d, lane_max, tau, sane, p.top, id0, len, sh, keys, rank,
+                select_top(d, row + id0, tau, sane, p.top, id0, len, sh, keys, rank,
                            [&](int place, uint64_t key) {
                                const size_t o = (size_t)r * p.top + place;
                                p.top_ids[o] = key_id(key);
@@ -392,7 +429,7 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(LogprobParams p) {
             if constexpr (TOP) {
                 const int keep = min(p.top, len);
                 uint64_t* out = p.keys + unit * p.top;
-                select_top(d, lane_max, tau, sane, keep, id0, len, sh, keys, rank,
+                select_top(d, row + id0, tau, sane, keep, id0, len, sh, keys, rank,
                            [&](int place, uint64_t key) { put(out + place, key); });
                 for (int i = keep + t; i < p.top; i += threads) put(out + i, 0ull);
             }
@@ -452,8 +489,8 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(LogprobParams p) {
         const RowGrad g = row_grad(p, r, target, m, log_s, entropy, ex);
         T* dx = static_cast<T*>(p.dx) + (size_t)r * p.ld_grad + id0;
         const int64_t here = target >= id0 && target < p.vocab ? target - id0 : -1;
-        if (ex.huge) write_grad<DT, NV, true>(d, dx, len, here, g, ex);
-        else write_grad<DT, NV, false>(d, dx, len, here, g, ex);
+        if (ex.huge) write_grad<DT, NV, true, PHASE == kStep>(d, dx, len, here, g, ex);
+        else write_grad<DT, NV, false, PHASE == kStep>(d, dx, len, here, g, ex);
     }
 }
 
