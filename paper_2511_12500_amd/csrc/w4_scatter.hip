@@ -14,11 +14,12 @@
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kWaves = 8;
+constexpr int kThreads = kWaves * 64;
 constexpr int kTileN = SYMTILE_W4_TILE_N;
-constexpr int kMaxM = SYMTILE_W4_TILE_M;
-constexpr int kPerCol = kThreads / kTileN;   // threads that share a column
-constexpr int kRows = 16;                    // rows a pass over the weights serves
+constexpr int kBlockK = 128;        // weights a lane quartet's loads cover in a column
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 struct W4Params {
     const void* X;
@@ -27,69 +28,225 @@ struct W4Params {
     const uint8_t* zeros;
     const uint64_t* bases;
     uint64_t c_off, flag_off;   // of the rank's column block and its counters in a slot
-    int M, N, K, ldx, lg_group, groups, world;
-    size_t ldc;                 // elements
+    int M, N, K, ldx, groups, world;
+    int ldc;                    // elements
+};
+
+// Weights as floating point without a conversion: 4 bits placed at the top of
+// the fraction of 16.0 make 16 + q, exactly.  Two of them, from bits b and b + 16
+// of a word, take a shift and an and-or.  The offset goes out with the zero
+// point: sum x (q - z) = sum x (16 + q) + sum x (-(16 + z)), the second sum by a
+// matrix instruction too, whose right operand is one number a column and group.
+template <bool BF>
+struct Nibbles {
+    static constexpr uint32_t kMask = BF ? 0x00780078u : 0x03C003C0u;
+    static constexpr uint32_t kSixteen = BF ? 0x41804180u : 0x4C004C00u;
+    static constexpr int kUp = BF ? 3 : 6;   // where the fraction's top 4 bits start
+    // nibbles j and j + 4 of w
+    static __device__ __forceinline__ uint32_t pair(uint32_t w, int j) {
+        const int shift = kUp - 4 * j;
+        return ((shift >= 0 ? w << shift : w >> -shift) & kMask) | kSixteen;
+    }
+    static __device__ __forceinline__ uint32_t minus_offset(uint32_t zero) {
+        const uint32_t h = (kSixteen & 0xFFFFu) | 0x8000u | zero << kUp;
+        return h | h << 16;
+    }
 };
 
 template <bool BF>
-struct T16;
-template <>
-struct T16<true> { typedef __bf16 type; };
-template <>
-struct T16<false> { typedef _Float16 type; };
+__device__ __forceinline__ f32x4 mfma(symtile::u32x4 a, symtile::u32x4 b, f32x4 c) {
+    if constexpr (BF) {
+        typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a),
+                                                       __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    } else {
+        typedef _Float16 v8 __attribute__((ext_vector_type(8)));
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a),
+                                                      __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    }
+}
 
-// One workgroup per tile of 16 columns; 16 threads share a column, each takes
-// every 16th block of 32 weights.
 template <bool BF>
-__global__ void __launch_bounds__(kThreads) w4_kernel(W4Params p) {
-    typedef typename T16<BF>::type T;
-    __shared__ __attribute__((aligned(16))) T out[kMaxM][kTileN];
-    const int tile = blockIdx.x;
-    const int col = threadIdx.x / kPerCol, part = threadIdx.x % kPerCol;
-    const int n = tile * kTileN + col;
-    const T* X = static_cast<const T*>(p.X);
-    const T* scales = static_cast<const T*>(p.scales);
-    for (int m0 = 0; m0 < p.M; m0 += kRows) {
-        float acc[kRows] = {};
-        if (n < p.N) {
-            for (int k0 = part * 32; k0 < p.K; k0 += kPerCol * 32) {
-                const symtile::u32x4 w = symtile::ld16(p.q + ((size_t)n * p.K + k0) / 2);
-                const size_t g = (size_t)n * p.groups + (k0 >> p.lg_group);
-                const float sc = (float)scales[g];
-                const float z = p.zeros ? (float)(p.zeros[g] & 15) : 8.0f;
-#pragma unroll 1
-                for (int i = 0; i < 32; ++i) {
-                    const float wv = ((float)((w[i / 8] >> (4 * (i % 8))) & 15u) - z) * sc;
+__device__ __forceinline__ float scale_value(uint16_t h) {
+    if constexpr (BF) return __uint_as_float((uint32_t)h << 16);
+    else return (float)__builtin_bit_cast(_Float16, h);
+}
+
+// X[k .. k + 7] in the order in which Nibbles::pair gives weights: k and k + 4, ...
+__device__ __forceinline__ symtile::u32x4 interleave(const symtile::u32x4& x) {
+    constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
+    return symtile::u32x4{__builtin_amdgcn_perm(x[2], x[0], kLow),
+                          __builtin_amdgcn_perm(x[2], x[0], kHigh),
+                          __builtin_amdgcn_perm(x[3], x[1], kLow),
+                          __builtin_amdgcn_perm(x[3], x[1], kHigh)};
+}
+
+// Words of a 4 x 4 transposed between the four quarters of the wave: lane (n, g)
+// gets in word j what lane (n, j) had in word g.
+__device__ __forceinline__ symtile::u32x4 transpose_quarters(symtile::u32x4 w) {
+    const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+    const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+    const auto d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    return symtile::u32x4{c[0], c[1], d[0], d[1]};
+}
+
+// One block of 128 weights of 16 columns, with what it is multiplied by: lane (c =
+// lane % 16, g = lane / 16) holds column c's weights 32 g .. 32 g + 31 of the block
+// and row c's values of X that go with them.
+template <bool BF, int MT, int GROUP>
+struct Block {
+    static constexpr int kGroups = kBlockK / GROUP;
+    symtile::u32x4 w;
+    symtile::u32x4 x[MT][4];
+    uint16_t scale[kGroups];
+    uint8_t zero[kGroups];
+
+    // Of matrix instruction j: with one group a block any order of the 128 does, so
+    // each lane keeps the words it loaded; with more, words are transposed so that
+    // instruction j has the weights 32 j .. 32 j + 31.
+    static __device__ __forceinline__ int k_of(int g, int j) {
+        return GROUP == kBlockK ? 32 * g + 8 * j : 32 * j + 8 * g;
+    }
+
+    __device__ __forceinline__ void load(const W4Params& p, int n, int k0) {
+        const int lane = threadIdx.x % 64, g = lane / 16;
+        const bool whole = k0 + kBlockK <= p.K;
+        const int kw = k0 + 32 * g;
+        w = symtile::u32x4{0, 0, 0, 0};
+        if (whole || kw < p.K) w = symtile::ld16(p.q + ((size_t)n * p.K + kw) / 2);
 #pragma unroll
-                    for (int m = 0; m < kRows; ++m)
-                        if (m0 + m < p.M)
-                            acc[m] += wv * (float)X[(size_t)(m0 + m) * p.ldx + k0 + i];
+        for (int i = 0; i < MT; ++i) {
+            const int m = min(16 * i + lane % 16, p.M - 1);
+            const uint16_t* row = static_cast<const uint16_t*>(p.X) + (size_t)m * p.ldx;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = k0 + k_of(g, j);
+                x[i][j] = symtile::u32x4{0, 0, 0, 0};
+                if (whole || k < p.K) x[i][j] = symtile::ld16(row + k);
+            }
+        }
+        const size_t at = (size_t)n * p.groups + k0 / GROUP;
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+            scale[i] = 0;
+            zero[i] = 8;
+            if (whole || k0 + i * GROUP < p.K) {
+                scale[i] = static_cast<const uint16_t*>(p.scales)[at + i];
+                if (p.zeros) zero[i] = p.zeros[at + i] & 15;
+            }
+        }
+    }
+
+    __device__ __forceinline__ void multiply(f32x4 (&total)[MT]) const {
+        typedef Nibbles<BF> Q;
+        const symtile::u32x4 words = GROUP == kBlockK ? w : transpose_quarters(w);
+        f32x4 acc[MT];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = j * 32 / GROUP;      // the group
+            const uint32_t z = Q::minus_offset(zero[i]);
+            const symtile::u32x4 zs = {z, z, z, z};
+            const symtile::u32x4 ws = {Q::pair(words[j], 0), Q::pair(words[j], 1),
+                                       Q::pair(words[j], 2), Q::pair(words[j], 3)};
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                const symtile::u32x4 xs = interleave(x[t][j]);
+                if (j * 32 % GROUP == 0) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                acc[t] = mfma<BF>(xs, zs, acc[t]);
+                acc[t] = mfma<BF>(xs, ws, acc[t]);
+                if ((j + 1) * 32 % GROUP == 0) {
+                    const float sc = scale_value<BF>(scale[i]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        total[t][e] = __builtin_fmaf(sc, acc[t][e], total[t][e]);
                 }
             }
         }
+    }
+};
+
+// One workgroup per tile of 16 columns and up to 16 MT rows; its waves share the
+// blocks of K, in pairs, so that a wave reads whole 128-byte lines of its columns.
+// A wave works on U blocks while U more are on their way.
+template <bool BF, int MT, int GROUP, int U>
+__global__ void __launch_bounds__(kThreads, 2) w4_kernel(W4Params p) {
+    typedef Block<BF, MT, GROUP> B;
+    __shared__ __attribute__((aligned(16))) float red[kWaves][MT][256];
+    __shared__ __attribute__((aligned(16))) uint16_t out[16 * MT][kTileN];
+    const int tile = blockIdx.x, t = threadIdx.x, wave = t / 64, lane = t % 64;
+    const int n = min(tile * kTileN + lane % 16, p.N - 1);
+    f32x4 total[MT] = {};
+    const int blocks = (p.K + kBlockK - 1) / kBlockK;
+    // block u of the wave: pairs of blocks, kWaves pairs apart
+    auto block_of = [&](int u) { return (u / 2 * kWaves + wave) * 2 + u % 2; };
+    B a[U], b[U];
+    auto fetch = [&](B (&s)[U], int u0) {
 #pragma unroll
-        for (int m = 0; m < kRows; ++m) {
-            float a = acc[m];
+        for (int u = 0; u < U; ++u)
+            if (block_of(u0 + u) < blocks) s[u].load(p, n, block_of(u0 + u) * kBlockK);
+    };
+    auto use = [&](B (&s)[U], int u0) {
 #pragma unroll
-            for (int d = kPerCol / 2; d; d >>= 1) a += __shfl_xor(a, d);
-            if (part == 0 && m0 + m < p.M) out[m0 + m][col] = (T)a;
-        }
+        for (int u = 0; u < U; ++u)
+            if (block_of(u0 + u) < blocks) s[u].multiply(total);
+    };
+    fetch(a, 0);
+    for (int u = 0; block_of(u) < blocks; u += 2 * U) {
+        fetch(b, u + U);
+        use(a, u);
+        fetch(a, u + 2 * U);
+        use(b, u + U);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) *reinterpret_cast<f32x4*>(&red[wave][i][4 * lane]) = total[i];
+    __syncthreads();
+    for (int o = t; o < 256 * MT; o += kThreads) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) v += red[w][o / 256][o % 256];
+        // element 4 * lane + i of a tile: column lane % 16, row 4 * (lane / 16) + i
+        const int l = o % 256 / 4, m = o / 256 * 16 + l / 16 * 4 + o % 4;
+        uint16_t h;
+        if constexpr (BF) h = __builtin_bit_cast(uint16_t, (__bf16)v);
+        else h = __builtin_bit_cast(uint16_t, (_Float16)v);
+        out[m][l % 16] = h;
     }
     __syncthreads();
-    // rows of 16 columns are two chunks of 8; N is a multiple of 8
-    const int chunks = p.N - tile * kTileN >= kTileN ? 2 : 1;
-    for (int i = threadIdx.x; i < p.world * p.M * chunks; i += kThreads) {
-        const int c = i % chunks, m = i / chunks % p.M, slot = i / chunks / p.M;
-        char* dst = reinterpret_cast<char*>(p.bases[slot]) + p.c_off +
-                    ((size_t)m * p.ldc + (size_t)tile * kTileN + c * 8) * 2;
-        symtile::st16(dst, symtile::ld16(&out[m][c * 8]), false);
+    // wave s stores the tile into slot s and counts it there: its own stores'
+    // acknowledgements are all that the counter has to wait for
+    if (wave < p.world) {
+        const char* base = reinterpret_cast<const char*>(p.bases[wave]);
+        const int chunks = p.N - tile * kTileN >= kTileN ? 2 : 1;   // of 8 columns
+        const symtile::rsrc_t dst = symtile::make_rsrc(
+            base + p.c_off + (size_t)tile * kTileN * 2,
+            (uint32_t)(((size_t)(p.M - 1) * p.ldc + chunks * 8) * 2));
+        for (int i = lane; i < p.M * 2; i += 64) {
+            const int m = i / 2, c = i % 2;
+            if (c < chunks)
+                symtile::buf_st16p<symtile::kStoreWriteThrough>(
+                    symtile::ld16(&out[m][c * 8]), dst, (uint32_t)(m * p.ldc + c * 8) * 2, 0);
+        }
+        symtile::release_written_through();
+        if (lane == 0)
+            symtile::flag_signal(reinterpret_cast<uint32_t*>(
+                reinterpret_cast<char*>(p.bases[wave]) + p.flag_off) + tile);
     }
-    symtile::wg_stores_done();
-    if ((int)threadIdx.x < p.world) {
-        uint32_t* flag = reinterpret_cast<uint32_t*>(
-            reinterpret_cast<char*>(p.bases[threadIdx.x]) + p.flag_off) + tile;
-        symtile::flag_publish(flag);
-    }
+}
+
+// Rows by 16: the smallest of 1, 2 and 4 tiles that hold M.  Blocks in flight: what
+// the registers of two waves a SIMD hold.
+template <bool BF, int GROUP>
+const void* kernel_of(int M) {
+    if (M <= 16) return reinterpret_cast<const void*>(&w4_kernel<BF, 1, GROUP, 4>);
+    if (M <= 32) return reinterpret_cast<const void*>(&w4_kernel<BF, 2, GROUP, 2>);
+    return reinterpret_cast<const void*>(&w4_kernel<BF, 4, GROUP, 1>);
+}
+template <bool BF>
+const void* kernel_of(int M, int group) {
+    return group == 128  ? kernel_of<BF, 128>(M)
+           : group == 64 ? kernel_of<BF, 64>(M)
+                         : kernel_of<BF, 32>(M);
 }
 
 }  // namespace
@@ -124,6 +281,7 @@ extern "C" symtile_status symtile_w4_all_scatter(
     const size_t ldc = (size_t)world_size * N_local;
     const size_t c_bytes = (size_t)M * ldc * 2;
     const size_t flag_bytes = (size_t)world_size * tiles * 4;
+    if (c_bytes >= size_t(1) << 31) return fail(SYMTILE_EINVAL, "the gathered output exceeds 2 GiB");
     if (!symtile_host::in_slot(h, C_gathered_local, c_bytes, rank))
         return fail(SYMTILE_EINVAL, "C_gathered_local [M, world*N_local] not inside slot of rank");
     if (!symtile_host::in_slot(h, arrived_local, flag_bytes, rank))
@@ -145,14 +303,13 @@ extern "C" symtile_status symtile_w4_all_scatter(
     p.N = N_local;
     p.K = K;
     p.ldx = ldx;
-    p.lg_group = __builtin_ctz((unsigned)group);
     p.groups = (K + group - 1) / group;
     p.world = world_size;
-    p.ldc = ldc;
+    p.ldc = (int)ldc;
     int prev = -1;
     if (symtile_status st = symtile_host::set_device(h, &prev)) return st;
-    const void* kernel = dtype == SYMTILE_BF16 ? reinterpret_cast<const void*>(&w4_kernel<true>)
-                                               : reinterpret_cast<const void*>(&w4_kernel<false>);
+    const void* kernel = dtype == SYMTILE_BF16 ? kernel_of<true>(M, group)
+                                               : kernel_of<false>(M, group);
     void* args[] = {&p};
     hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)tiles), dim3(kThreads), args, 0,
                                    static_cast<hipStream_t>(s));
