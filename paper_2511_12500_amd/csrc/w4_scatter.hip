@@ -33,22 +33,25 @@ struct W4Params {
 };
 
 // Weights as floating point without a conversion: 4 bits placed at the top of
-// the fraction of 16.0 make 16 + q, exactly.  Two of them, from bits b and b + 16
-// of a word, take a shift and an and-or.  The offset goes out with the zero
+// the fraction of 16.0 make 16 + q, exactly.  The offset goes out with the zero
 // point: sum x (q - z) = sum x (16 + q) + sum x (-(16 + z)), the second sum by a
 // matrix instruction too, whose right operand is one number a column and group.
 template <bool BF>
 struct Nibbles {
     static constexpr uint32_t kMask = BF ? 0x00780078u : 0x03C003C0u;
     static constexpr uint32_t kSixteen = BF ? 0x41804180u : 0x4C004C00u;
-    static constexpr int kUp = BF ? 3 : 6;   // where the fraction's top 4 bits start
-    // nibbles j and j + 4 of w
-    static __device__ __forceinline__ uint32_t pair(uint32_t w, int j) {
-        const int shift = kUp - 4 * j;
-        return ((shift >= 0 ? w << shift : w >> -shift) & kMask) | kSixteen;
+    static constexpr int kAt = BF ? 3 : 6;   // where the fraction's top 4 bits start
+    // The weights of byte i of w (two consecutive k): the byte at the top of both
+    // halves, its low 4 bits moved into place in the lower one and its high 4 bits in
+    // the upper one, then an and-or.
+    static __device__ __forceinline__ uint32_t pair(uint32_t w, int i) {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        const uint32_t both = __builtin_amdgcn_perm(w, w, 0x000C000Cu | i << 8 | i << 24);
+        const u16x2 moved = __builtin_bit_cast(u16x2, both) >> u16x2{8 - kAt, 12 - kAt};
+        return (__builtin_bit_cast(uint32_t, moved) & kMask) | kSixteen;
     }
     static __device__ __forceinline__ uint32_t minus_offset(uint32_t zero) {
-        const uint32_t h = (kSixteen & 0xFFFFu) | 0x8000u | zero << kUp;
+        const uint32_t h = (kSixteen & 0xFFFFu) | 0x8000u | zero << kAt;
         return h | h << 16;
     }
 };
@@ -67,18 +70,9 @@ __device__ __forceinline__ f32x4 mfma(symtile::u32x4 a, symtile::u32x4 b, f32x4 
 }
 
 template <bool BF>
-__device__ __forceinline__ float scale_value(uint16_t h) {
-    if constexpr (BF) return __uint_as_float((uint32_t)h << 16);
-    else return (float)__builtin_bit_cast(_Float16, h);
-}
-
-// X[k .. k + 7] in the order in which Nibbles::pair gives weights: k and k + 4, ...
-__device__ __forceinline__ symtile::u32x4 interleave(const symtile::u32x4& x) {
-    constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
-    return symtile::u32x4{__builtin_amdgcn_perm(x[2], x[0], kLow),
-                          __builtin_amdgcn_perm(x[2], x[0], kHigh),
-                          __builtin_amdgcn_perm(x[3], x[1], kLow),
-                          __builtin_amdgcn_perm(x[3], x[1], kHigh)};
+__device__ __forceinline__ float scale_value(uint32_t h) {   // the low half
+    if constexpr (BF) return __uint_as_float(h << 16);
+    else return (float)__builtin_bit_cast(_Float16, (uint16_t)h);
 }
 
 // Words of a 4 x 4 transposed between the four quarters of the wave: lane (n, g)
@@ -91,6 +85,16 @@ __device__ __forceinline__ symtile::u32x4 transpose_quarters(symtile::u32x4 w) {
     return symtile::u32x4{c[0], c[1], d[0], d[1]};
 }
 
+// What a wave reads from: buffer resources over X, the tile's columns of weights,
+// scales and zero points, and each lane's offsets in them.  A block adds the same
+// number to every lane's offset, which is the load's scalar operand: no address
+// arithmetic a load.
+struct Source {
+    symtile::rsrc_t x, w, scales, zeros;
+    uint32_t at_x[4], at_w, at_group;   // bytes; at_group in elements
+    bool has_zeros;
+};
+
 // One block of 128 weights of 16 columns, with what it is multiplied by: lane (c =
 // lane % 16, g = lane / 16) holds column c's weights 32 g .. 32 g + 31 of the block
 // and row c's values of X that go with them.
@@ -99,64 +103,87 @@ struct Block {
     static constexpr int kGroups = kBlockK / GROUP;
     symtile::u32x4 w;
     symtile::u32x4 x[MT][4];
-    uint16_t scale[kGroups];
-    uint8_t zero[kGroups];
+    uint32_t sz;        // scale, and the zero point above it, of the lane's group
 
     // Of matrix instruction j: with one group a block any order of the 128 does, so
     // each lane keeps the words it loaded; with more, words are transposed so that
     // instruction j has the weights 32 j .. 32 j + 31.
-    static __device__ __forceinline__ int k_of(int g, int j) {
-        return GROUP == kBlockK ? 32 * g + 8 * j : 32 * j + 8 * g;
+    static constexpr int kStep = GROUP == kBlockK ? 8 : 32;       // k from j to j + 1
+    static constexpr int kQuarter = GROUP == kBlockK ? 32 : 8;    // k from g to g + 1
+
+    static __device__ __forceinline__ Source source(const W4Params& p, int tile) {
+        const int lane = threadIdx.x % 64, c = lane % 16, g = lane / 16;
+        const int n0 = tile * kTileN, cols = min(kTileN, p.N - n0);
+        const int col = min(c, cols - 1);
+        Source s;
+        s.x = symtile::make_rsrc(p.X, (uint32_t)(((p.M - 1) * p.ldx + p.K) * 2));
+        s.w = symtile::make_rsrc(p.q + (size_t)n0 * (p.K / 2), (uint32_t)(cols * (p.K / 2)));
+        s.scales = symtile::make_rsrc(static_cast<const uint16_t*>(p.scales) + (size_t)n0 * p.groups,
+                                      (uint32_t)(cols * p.groups * 2));
+        s.has_zeros = p.zeros != nullptr;
+        s.zeros = symtile::make_rsrc(p.zeros + (s.has_zeros ? (size_t)n0 * p.groups : 0),
+                                     s.has_zeros ? (uint32_t)(cols * p.groups) : 0u);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            s.at_x[i] = (uint32_t)(min(16 * i + c, p.M - 1) * p.ldx + kQuarter * g) * 2;
+        s.at_w = (uint32_t)(col * (p.K / 2) + 16 * g);
+        s.at_group = (uint32_t)(col * p.groups + g * 32 / GROUP);
+        return s;
     }
 
-    __device__ __forceinline__ void load(const W4Params& p, int n, int k0) {
-        const int lane = threadIdx.x % 64, g = lane / 16;
-        const bool whole = k0 + kBlockK <= p.K;
-        const int kw = k0 + 32 * g;
-        w = symtile::u32x4{0, 0, 0, 0};
-        if (whole || kw < p.K) w = symtile::ld16(p.q + ((size_t)n * p.K + kw) / 2);
+    // TAIL: the block that ends behind K; what is behind it is multiplied with zeros.
+    template <bool TAIL>
+    __device__ __forceinline__ void load(const Source& s, int K, int block) {
+        const int g = threadIdx.x % 64 / 16, k0 = block * kBlockK;
+        const bool in = !TAIL || k0 + 32 * g < K;
+        w = symtile::buf_ld16p<symtile::kLoadStream>(s.w, in ? s.at_w : symtile::kOOB, k0 / 2);
+        const bool group_in = !TAIL || k0 + g * 32 / GROUP * GROUP < K;
+        const uint32_t at = group_in ? s.at_group : symtile::kOOB / 2;
+        sz = __builtin_amdgcn_raw_buffer_load_b16(
+            s.scales, at * 2, __builtin_amdgcn_readfirstlane(k0 / GROUP * 2), 0);
+        uint32_t z = 8;
+        if (s.has_zeros)
+            z = __builtin_amdgcn_raw_buffer_load_b8(
+                    s.zeros, group_in ? at : symtile::kOOB, __builtin_amdgcn_readfirstlane(k0 / GROUP), 0) & 15u;
+        sz |= z << 16;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int m = min(16 * i + lane % 16, p.M - 1);
-            const uint16_t* row = static_cast<const uint16_t*>(p.X) + (size_t)m * p.ldx;
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int k = k0 + k_of(g, j);
-                x[i][j] = symtile::u32x4{0, 0, 0, 0};
-                if (whole || k < p.K) x[i][j] = symtile::ld16(row + k);
+                const bool inside = !TAIL || k0 + kStep * j + kQuarter * g < K;
+                x[i][j] = symtile::buf_ld16(
+                    s.x, inside ? s.at_x[i] + kStep * j * 2 : symtile::kOOB, k0 * 2);
             }
-        }
-        const size_t at = (size_t)n * p.groups + k0 / GROUP;
-#pragma unroll
-        for (int i = 0; i < kGroups; ++i) {
-            scale[i] = 0;
-            zero[i] = 8;
-            if (whole || k0 + i * GROUP < p.K) {
-                scale[i] = static_cast<const uint16_t*>(p.scales)[at + i];
-                if (p.zeros) zero[i] = p.zeros[at + i] & 15;
-            }
-        }
     }
 
     __device__ __forceinline__ void multiply(f32x4 (&total)[MT]) const {
         typedef Nibbles<BF> Q;
         const symtile::u32x4 words = GROUP == kBlockK ? w : transpose_quarters(w);
+        uint32_t of_group[4] = {sz, sz, sz, sz};
+        if constexpr (GROUP != kBlockK) {
+            const auto h = __builtin_amdgcn_permlane32_swap(sz, sz, false, false);
+            of_group[0] = h[0], of_group[1] = h[1];
+            if constexpr (GROUP == 32) {
+                const auto a = __builtin_amdgcn_permlane16_swap(h[0], h[0], false, false);
+                const auto b = __builtin_amdgcn_permlane16_swap(h[1], h[1], false, false);
+                of_group[0] = a[0], of_group[1] = a[1], of_group[2] = b[0], of_group[3] = b[1];
+            }
+        }
         f32x4 acc[MT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int i = j * 32 / GROUP;      // the group
-            const uint32_t z = Q::minus_offset(zero[i]);
+            const uint32_t of = of_group[j * 32 / GROUP];
+            const uint32_t z = Q::minus_offset(of >> 16);
             const symtile::u32x4 zs = {z, z, z, z};
             const symtile::u32x4 ws = {Q::pair(words[j], 0), Q::pair(words[j], 1),
                                        Q::pair(words[j], 2), Q::pair(words[j], 3)};
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
-                const symtile::u32x4 xs = interleave(x[t][j]);
                 if (j * 32 % GROUP == 0) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                acc[t] = mfma<BF>(xs, zs, acc[t]);
-                acc[t] = mfma<BF>(xs, ws, acc[t]);
+                acc[t] = mfma<BF>(x[t][j], zs, acc[t]);
+                acc[t] = mfma<BF>(x[t][j], ws, acc[t]);
                 if ((j + 1) * 32 % GROUP == 0) {
-                    const float sc = scale_value<BF>(scale[i]);
+                    const float sc = scale_value<BF>(of & 0xFFFFu);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         total[t][e] = __builtin_fmaf(sc, acc[t][e], total[t][e]);
@@ -175,16 +202,17 @@ __global__ void __launch_bounds__(kThreads, 2) w4_kernel(W4Params p) {
     __shared__ __attribute__((aligned(16))) float red[kWaves][MT][256];
     __shared__ __attribute__((aligned(16))) uint16_t out[16 * MT][kTileN];
     const int tile = blockIdx.x, t = threadIdx.x, wave = t / 64, lane = t % 64;
-    const int n = min(tile * kTileN + lane % 16, p.N - 1);
     f32x4 total[MT] = {};
-    const int blocks = (p.K + kBlockK - 1) / kBlockK;
+    const int blocks = p.K / kBlockK;
+    const Source src = B::source(p, tile);
     // block u of the wave: pairs of blocks, kWaves pairs apart
-    auto block_of = [&](int u) { return (u / 2 * kWaves + wave) * 2 + u % 2; };
+    const int w0 = __builtin_amdgcn_readfirstlane(wave);
+    auto block_of = [&](int u) { return (u / 2 * kWaves + w0) * 2 + u % 2; };
     B a[U], b[U];
     auto fetch = [&](B (&s)[U], int u0) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (block_of(u0 + u) < blocks) s[u].load(p, n, block_of(u0 + u) * kBlockK);
+            if (block_of(u0 + u) < blocks) s[u].template load<false>(src, p.K, block_of(u0 + u));
     };
     auto use = [&](B (&s)[U], int u0) {
 #pragma unroll
@@ -197,6 +225,10 @@ __global__ void __launch_bounds__(kThreads, 2) w4_kernel(W4Params p) {
         use(a, u);
         fetch(a, u + 2 * U);
         use(b, u + U);
+    }
+    if (p.K % kBlockK && w0 == kWaves - 1) {   // the wave with the fewest blocks
+        a[0].template load<true>(src, p.K, blocks);
+        a[0].multiply(total);
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i) *reinterpret_cast<f32x4*>(&red[wave][i][4 * lane]) = total[i];
@@ -271,6 +303,8 @@ extern "C" symtile_status symtile_w4_all_scatter(
     if (K % 32 || N_local % 8 || ldx % 8 || ldx < K)
         return fail(SYMTILE_EINVAL, "K must be a multiple of 32, N_local and ldx of 8, ldx >= K");
     if (M == 0 || N_local == 0) return SYMTILE_OK;
+    if ((size_t)M * ldx * 2 >= size_t(1) << 31 || (size_t)K * kTileN >= size_t(1) << 31)
+        return fail(SYMTILE_EINVAL, "X, or 16 columns of weights, exceed 2 GiB");
     if (!C_gathered_local || !arrived_local || (K && (!X || !q || !scales)))
         return fail(SYMTILE_EINVAL, "NULL pointer");
     auto misaligned = [](const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; };
