@@ -18,6 +18,7 @@ constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * 64;
 constexpr int kTileN = SYMTILE_W4_TILE_N;
 constexpr int kBlockK = 128;        // weights a lane quartet's loads cover in a column
+constexpr int kChunkK = 16384;      // weights of a column whose scales are in LDS
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -85,94 +86,89 @@ __device__ __forceinline__ symtile::u32x4 transpose_quarters(symtile::u32x4 w) {
     return symtile::u32x4{c[0], c[1], d[0], d[1]};
 }
 
-// What a wave reads from: buffer resources over X, the tile's columns of weights,
-// scales and zero points, and each lane's offsets in them.  A block adds the same
-// number to every lane's offset, which is the load's scalar operand: no address
-// arithmetic a load.
-struct Source {
-    symtile::rsrc_t x, w, scales, zeros;
-    uint32_t at_x[4], at_w, at_group;   // bytes; at_group in elements
-    bool has_zeros;
+// Scales, and zero points above them, of a tile's 16 columns for the groups of one
+// chunk of K, group by group: a column's are far from the next column's in memory
+// and every block needs one of each, so they are read once, along the columns.
+template <int GROUP>
+struct Scales {
+    uint32_t of[kChunkK / GROUP][kTileN];
+
+    __device__ __forceinline__ void load(const W4Params& p, int tile, int group0) {
+        const int n0 = tile * kTileN, cols = min(kTileN, p.N - n0);
+        const int count = min(kChunkK / GROUP, p.groups - group0);
+        // 16 threads a column: neighbours read neighbouring groups
+        const int col = min((int)threadIdx.x / 16 % kTileN, cols - 1);
+        const int part = threadIdx.x % 16 + threadIdx.x / 256 * 16;
+        const size_t at = (size_t)(n0 + col) * p.groups + group0;
+        const uint16_t* scales = static_cast<const uint16_t*>(p.scales) + at;
+        // up to the end of the last block: what is behind K is multiplied with 0 as well
+        constexpr int kPerBlock = kBlockK / GROUP;
+        const int padded = (count + kPerBlock - 1) / kPerBlock * kPerBlock;
+        for (int i = part; i < padded; i += kThreads / kTileN) {
+            uint32_t of_group = 8u << 16;
+            if (i < count) {
+                const uint32_t z = p.zeros ? p.zeros[at + i] & 15u : 8u;
+                of_group = scales[i] | z << 16;
+            }
+            of[i][threadIdx.x / 16 % kTileN] = of_group;
+        }
+    }
 };
 
-// One block of 128 weights of 16 columns, with what it is multiplied by: lane (c =
-// lane % 16, g = lane / 16) holds column c's weights 32 g .. 32 g + 31 of the block
-// and row c's values of X that go with them.
-template <bool BF, int MT, int GROUP>
-struct Block {
-    static constexpr int kGroups = kBlockK / GROUP;
-    symtile::u32x4 w;
-    symtile::u32x4 x[MT][4];
-    uint32_t sz;        // scale, and the zero point above it, of the lane's group
+// What a wave reads X and weights through: buffer resources over X and the tile's
+// columns, and each lane's offsets in them.  A block adds the same number to every
+// lane's offset, which is the load's scalar operand: no address arithmetic a load.
+template <int MT>
+struct Source {
+    symtile::rsrc_t x, w;
+    uint32_t at_x[MT], at_w;   // bytes
 
-    // Of matrix instruction j: with one group a block any order of the 128 does, so
-    // each lane keeps the words it loaded; with more, words are transposed so that
-    // instruction j has the weights 32 j .. 32 j + 31.
-    static constexpr int kStep = GROUP == kBlockK ? 8 : 32;       // k from j to j + 1
-    static constexpr int kQuarter = GROUP == kBlockK ? 32 : 8;    // k from g to g + 1
-
-    static __device__ __forceinline__ Source source(const W4Params& p, int tile) {
+    __device__ __forceinline__ Source(const W4Params& p, int tile) {
         const int lane = threadIdx.x % 64, c = lane % 16, g = lane / 16;
         const int n0 = tile * kTileN, cols = min(kTileN, p.N - n0);
-        const int col = min(c, cols - 1);
-        Source s;
-        s.x = symtile::make_rsrc(p.X, (uint32_t)(((p.M - 1) * p.ldx + p.K) * 2));
-        s.w = symtile::make_rsrc(p.q + (size_t)n0 * (p.K / 2), (uint32_t)(cols * (p.K / 2)));
-        s.scales = symtile::make_rsrc(static_cast<const uint16_t*>(p.scales) + (size_t)n0 * p.groups,
-                                      (uint32_t)(cols * p.groups * 2));
-        s.has_zeros = p.zeros != nullptr;
-        s.zeros = symtile::make_rsrc(p.zeros + (s.has_zeros ? (size_t)n0 * p.groups : 0),
-                                     s.has_zeros ? (uint32_t)(cols * p.groups) : 0u);
+        x = symtile::make_rsrc(p.X, (uint32_t)(((p.M - 1) * p.ldx + p.K) * 2));
+        w = symtile::make_rsrc(p.q + (size_t)n0 * (p.K / 2), (uint32_t)(cols * (p.K / 2)));
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-            s.at_x[i] = (uint32_t)(min(16 * i + c, p.M - 1) * p.ldx + kQuarter * g) * 2;
-        s.at_w = (uint32_t)(col * (p.K / 2) + 16 * g);
-        s.at_group = (uint32_t)(col * p.groups + g * 32 / GROUP);
-        return s;
+        for (int i = 0; i < MT; ++i) at_x[i] = (uint32_t)(min(16 * i + c, p.M - 1) * p.ldx + 8 * g) * 2;
+        at_w = (uint32_t)(min(c, cols - 1) * (p.K / 2) + 16 * g);
     }
+};
+
+// One block of 128 weights of 16 columns, with what it is multiplied by.  Lane (c =
+// lane % 16, g = lane / 16) loads column c's weights 32 g .. 32 g + 31 in one vector;
+// its words are then transposed between the quarters of the wave, so that matrix
+// instruction j has the weights 32 j .. 32 j + 31: a group's are in instructions of
+// their own, and row c's X comes in pieces of 64 bytes.  (Without the transposition
+// the pieces are 16 bytes: 64 tokens through 8192x3584 took 39 us.)
+template <bool BF, int MT, int GROUP>
+struct Block {
+    symtile::u32x4 w;
+    symtile::u32x4 x[MT][4];
 
     // TAIL: the block that ends behind K; what is behind it is multiplied with zeros.
     template <bool TAIL>
-    __device__ __forceinline__ void load(const Source& s, int K, int block) {
+    __device__ __forceinline__ void load(const Source<MT>& s, int K, int block) {
         const int g = threadIdx.x % 64 / 16, k0 = block * kBlockK;
         const bool in = !TAIL || k0 + 32 * g < K;
         w = symtile::buf_ld16p<symtile::kLoadStream>(s.w, in ? s.at_w : symtile::kOOB, k0 / 2);
-        const bool group_in = !TAIL || k0 + g * 32 / GROUP * GROUP < K;
-        const uint32_t at = group_in ? s.at_group : symtile::kOOB / 2;
-        sz = __builtin_amdgcn_raw_buffer_load_b16(
-            s.scales, at * 2, __builtin_amdgcn_readfirstlane(k0 / GROUP * 2), 0);
-        uint32_t z = 8;
-        if (s.has_zeros)
-            z = __builtin_amdgcn_raw_buffer_load_b8(
-                    s.zeros, group_in ? at : symtile::kOOB, __builtin_amdgcn_readfirstlane(k0 / GROUP), 0) & 15u;
-        sz |= z << 16;
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const bool inside = !TAIL || k0 + kStep * j + kQuarter * g < K;
-                x[i][j] = symtile::buf_ld16(
-                    s.x, inside ? s.at_x[i] + kStep * j * 2 : symtile::kOOB, k0 * 2);
+                const bool inside = !TAIL || k0 + 32 * j < K;
+                x[i][j] = symtile::buf_ld16(s.x, inside ? s.at_x[i] + 64 * j : symtile::kOOB, k0 * 2);
             }
     }
 
-    __device__ __forceinline__ void multiply(f32x4 (&total)[MT]) const {
+    __device__ __forceinline__ void multiply(f32x4 (&total)[MT], const Scales<GROUP>& scales,
+                                             int group0) const {
         typedef Nibbles<BF> Q;
-        const symtile::u32x4 words = GROUP == kBlockK ? w : transpose_quarters(w);
-        uint32_t of_group[4] = {sz, sz, sz, sz};
-        if constexpr (GROUP != kBlockK) {
-            const auto h = __builtin_amdgcn_permlane32_swap(sz, sz, false, false);
-            of_group[0] = h[0], of_group[1] = h[1];
-            if constexpr (GROUP == 32) {
-                const auto a = __builtin_amdgcn_permlane16_swap(h[0], h[0], false, false);
-                const auto b = __builtin_amdgcn_permlane16_swap(h[1], h[1], false, false);
-                of_group[0] = a[0], of_group[1] = a[1], of_group[2] = b[0], of_group[3] = b[1];
-            }
-        }
+        const symtile::u32x4 words = transpose_quarters(w);
+        const uint32_t* of_block = &scales.of[group0][threadIdx.x % 16];
         f32x4 acc[MT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t of = of_group[j * 32 / GROUP];
+            const uint32_t of = of_block[j * 32 / GROUP * kTileN];
             const uint32_t z = Q::minus_offset(of >> 16);
             const symtile::u32x4 zs = {z, z, z, z};
             const symtile::u32x4 ws = {Q::pair(words[j], 0), Q::pair(words[j], 1),
@@ -196,39 +192,47 @@ struct Block {
 // One workgroup per tile of 16 columns and up to 16 MT rows; its waves share the
 // blocks of K, in pairs, so that a wave reads whole 128-byte lines of its columns.
 // A wave works on U blocks while U more are on their way.
-template <bool BF, int MT, int GROUP, int U>
-__global__ void __launch_bounds__(kThreads, 2) w4_kernel(W4Params p) {
+template <bool BF, int MT, int GROUP, int U, int WAVES>
+__global__ void __launch_bounds__(kThreads, WAVES) w4_kernel(W4Params p) {
     typedef Block<BF, MT, GROUP> B;
     __shared__ __attribute__((aligned(16))) float red[kWaves][MT][256];
     __shared__ __attribute__((aligned(16))) uint16_t out[16 * MT][kTileN];
+    __shared__ Scales<GROUP> scales;
     const int tile = blockIdx.x, t = threadIdx.x, wave = t / 64, lane = t % 64;
-    f32x4 total[MT] = {};
-    const int blocks = p.K / kBlockK;
-    const Source src = B::source(p, tile);
-    // block u of the wave: pairs of blocks, kWaves pairs apart
     const int w0 = __builtin_amdgcn_readfirstlane(wave);
-    auto block_of = [&](int u) { return (u / 2 * kWaves + w0) * 2 + u % 2; };
-    B a[U], b[U];
-    auto fetch = [&](B (&s)[U], int u0) {
+    f32x4 total[MT] = {};
+    const Source<MT> src(p, tile);
+    for (int chunk = 0; chunk < p.K; chunk += kChunkK) {
+        const int first = chunk / kBlockK, blocks = min(p.K, chunk + kChunkK) / kBlockK;
+        // block u of the wave: pairs of blocks, kWaves pairs apart
+        auto block_of = [&](int u) { return first + (u / 2 * kWaves + w0) * 2 + u % 2; };
+        B a[U], b[U];
+        auto fetch = [&](B (&s)[U], int u0) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (block_of(u0 + u) < blocks) s[u].template load<false>(src, p.K, block_of(u0 + u));
-    };
-    auto use = [&](B (&s)[U], int u0) {
+            for (int u = 0; u < U; ++u)
+                if (block_of(u0 + u) < blocks) s[u].template load<false>(src, p.K, block_of(u0 + u));
+        };
+        auto use = [&](B (&s)[U], int u0) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (block_of(u0 + u) < blocks) s[u].multiply(total);
-    };
-    fetch(a, 0);
-    for (int u = 0; block_of(u) < blocks; u += 2 * U) {
-        fetch(b, u + U);
-        use(a, u);
-        fetch(a, u + 2 * U);
-        use(b, u + U);
-    }
-    if (p.K % kBlockK && w0 == kWaves - 1) {   // the wave with the fewest blocks
-        a[0].template load<true>(src, p.K, blocks);
-        a[0].multiply(total);
+            for (int u = 0; u < U; ++u)
+                if (block_of(u0 + u) < blocks)
+                    s[u].multiply(total, scales, (block_of(u0 + u) - first) * (kBlockK / GROUP));
+        };
+        fetch(a, 0);
+        if (chunk) __syncthreads();   // the scales before are used up
+        scales.load(p, tile, chunk / GROUP);
+        __syncthreads();
+        for (int u = 0; block_of(u) < blocks; u += 2 * U) {
+            fetch(b, u + U);
+            use(a, u);
+            fetch(a, u + 2 * U);
+            use(b, u + U);
+        }
+        if (blocks * kBlockK < min(p.K, chunk + kChunkK) && w0 == kWaves - 1) {
+            // the wave with the fewest blocks
+            a[0].template load<true>(src, p.K, blocks);
+            a[0].multiply(total, scales, (blocks - first) * (kBlockK / GROUP));
+        }
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i) *reinterpret_cast<f32x4*>(&red[wave][i][4 * lane]) = total[i];
@@ -270,9 +274,9 @@ __global__ void __launch_bounds__(kThreads, 2) w4_kernel(W4Params p) {
 // the registers of two waves a SIMD hold.
 template <bool BF, int GROUP>
 const void* kernel_of(int M) {
-    if (M <= 16) return reinterpret_cast<const void*>(&w4_kernel<BF, 1, GROUP, 4>);
-    if (M <= 32) return reinterpret_cast<const void*>(&w4_kernel<BF, 2, GROUP, 2>);
-    return reinterpret_cast<const void*>(&w4_kernel<BF, 4, GROUP, 1>);
+    if (M <= 16) return reinterpret_cast<const void*>(&w4_kernel<BF, 1, GROUP, 2, 4>);
+    if (M <= 32) return reinterpret_cast<const void*>(&w4_kernel<BF, 2, GROUP, 2, 2>);
+    return reinterpret_cast<const void*>(&w4_kernel<BF, 4, GROUP, 1, 2>);
 }
 template <bool BF>
 const void* kernel_of(int M, int group) {
