@@ -18,7 +18,7 @@ constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * 64;
 constexpr int kTileN = SYMTILE_W4_TILE_N;
 constexpr int kBlockK = 128;        // weights a lane quartet's loads cover in a column
-constexpr int kChunkK = 16384;      // weights of a column whose scales are in LDS
+constexpr int kChunkK = 8192;       // weights of a column whose scales are in LDS
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -39,23 +39,44 @@ struct W4Params {
 // matrix instruction too, whose right operand is one number a column and group.
 template <bool BF>
 struct Nibbles {
-    static constexpr uint32_t kMask = BF ? 0x00780078u : 0x03C003C0u;
     static constexpr uint32_t kSixteen = BF ? 0x41804180u : 0x4C004C00u;
     static constexpr int kAt = BF ? 3 : 6;   // where the fraction's top 4 bits start
-    // The weights of byte i of w (two consecutive k): the byte at the top of both
-    // halves, its low 4 bits moved into place in the lower one and its high 4 bits in
-    // the upper one, then an and-or.
-    static __device__ __forceinline__ uint32_t pair(uint32_t w, int i) {
+    uint32_t mask, sixteen;
+
+    // The constants in registers (one scalar, one vector): as literals they would
+    // keep the and-or from being one instruction.
+    __device__ __forceinline__ Nibbles() : mask(BF ? 0x00780078u : 0x03C003C0u), sixteen(kSixteen) {
+        asm("" : "+s"(mask));
+        asm("" : "+v"(sixteen));
+    }
+    // Weights j and j + 4 of w: two instructions, for X in that order.
+    __device__ __forceinline__ uint32_t apart(uint32_t w, int j) const {
+        const int shift = kAt - 4 * j;
+        return ((shift >= 0 ? w << shift : w >> -shift) & mask) | sixteen;
+    }
+    // Weights 2 j and 2 j + 1 of w, the byte j: at the top of both halves, its low 4
+    // bits moved into place in the lower one and its high 4 bits in the upper one;
+    // three instructions.
+    __device__ __forceinline__ uint32_t adjacent(uint32_t w, int j) const {
         typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-        const uint32_t both = __builtin_amdgcn_perm(w, w, 0x000C000Cu | i << 8 | i << 24);
+        const uint32_t both = __builtin_amdgcn_perm(w, w, 0x000C000Cu | j << 8 | j << 24);
         const u16x2 moved = __builtin_bit_cast(u16x2, both) >> u16x2{8 - kAt, 12 - kAt};
-        return (__builtin_bit_cast(uint32_t, moved) & kMask) | kSixteen;
+        return (__builtin_bit_cast(uint32_t, moved) & mask) | sixteen;
     }
     static __device__ __forceinline__ uint32_t minus_offset(uint32_t zero) {
         const uint32_t h = (kSixteen & 0xFFFFu) | 0x8000u | zero << kAt;
         return h | h << 16;
     }
 };
+
+// Eight values in the order of Nibbles::apart: k and k + 4, ...
+__device__ __forceinline__ symtile::u32x4 interleave(const symtile::u32x4& x) {
+    constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
+    return symtile::u32x4{__builtin_amdgcn_perm(x[2], x[0], kLow),
+                          __builtin_amdgcn_perm(x[2], x[0], kHigh),
+                          __builtin_amdgcn_perm(x[3], x[1], kLow),
+                          __builtin_amdgcn_perm(x[3], x[1], kHigh)};
+}
 
 template <bool BF>
 __device__ __forceinline__ f32x4 mfma(symtile::u32x4 a, symtile::u32x4 b, f32x4 c) {
@@ -115,13 +136,27 @@ struct Scales {
     }
 };
 
+// X of a wave's block in LDS: 256 bytes a row, its 16 vectors of 8 values in an
+// order of the row's own (vector v at v ^ (row % 16)), so that a matrix operand's
+// load, the same vector of 16 rows, touches every bank once.
+template <int MT>
+struct StagedX {
+    symtile::u32x4 v[16 * MT][16];
+};
+
 // What a wave reads X and weights through: buffer resources over X and the tile's
 // columns, and each lane's offsets in them.  A block adds the same number to every
 // lane's offset, which is the load's scalar operand: no address arithmetic a load.
-template <int MT>
+//
+// A lane's piece of a block exists in the blocks before `w_end` (its 32 weights) and
+// `x_end` (its 8 values): the others' offsets are set outside of the resource and
+// read as zeros, without a branch, so that the loads of several blocks are in
+// flight together.  What is behind K is multiplied with zeros of X.
+template <int XL>
 struct Source {
     symtile::rsrc_t x, w;
-    uint32_t at_x[MT], at_w;   // bytes
+    uint32_t at_x[XL], at_w;   // bytes
+    int w_end, x_end;
 
     __device__ __forceinline__ Source(const W4Params& p, int tile) {
         const int lane = threadIdx.x % 64, c = lane % 16, g = lane / 16;
@@ -129,8 +164,11 @@ struct Source {
         x = symtile::make_rsrc(p.X, (uint32_t)(((p.M - 1) * p.ldx + p.K) * 2));
         w = symtile::make_rsrc(p.q + (size_t)n0 * (p.K / 2), (uint32_t)(cols * (p.K / 2)));
 #pragma unroll
-        for (int i = 0; i < MT; ++i) at_x[i] = (uint32_t)(min(16 * i + c, p.M - 1) * p.ldx + 8 * g) * 2;
+        for (int i = 0; i < XL; ++i)
+            at_x[i] = (uint32_t)(min(4 * i + g, p.M - 1) * p.ldx + 8 * c) * 2;
         at_w = (uint32_t)(min(c, cols - 1) * (p.K / 2) + 16 * g);
+        w_end = (p.K - 32 * g + kBlockK - 1) / kBlockK;
+        x_end = (p.K - 8 * c + kBlockK - 1) / kBlockK;
     }
 };
 
@@ -138,46 +176,52 @@ struct Source {
 // lane % 16, g = lane / 16) loads column c's weights 32 g .. 32 g + 31 in one vector;
 // its words are then transposed between the quarters of the wave, so that matrix
 // instruction j has the weights 32 j .. 32 j + 31: a group's are in instructions of
-// their own, and row c's X comes in pieces of 64 bytes.  (Without the transposition
-// the pieces are 16 bytes: 64 tokens through 8192x3584 took 39 us.)
-template <bool BF, int MT, int GROUP>
+// their own.  X comes by rows, 256 bytes of four rows a load (XL of them), and takes
+// the matrix operands' layout in LDS: loading operands directly reads 64 bytes of 16
+// rows, whose distance is often a power of two, from one cache channel (64 tokens
+// through 8192x3584: 36 us).
+template <bool BF, int XL, int GROUP>
 struct Block {
+    static constexpr int MT = (XL + 3) / 4;       // tiles of 16 rows
+    static constexpr bool kApart = XL <= 4;       // X reordered for Nibbles::apart: 4 XL
+                                                  // instructions for 16 fewer on weights
     symtile::u32x4 w;
-    symtile::u32x4 x[MT][4];
+    symtile::u32x4 x[XL];    // rows 4 i + g, values 8 c .. 8 c + 7
 
-    // TAIL: the block that ends behind K; what is behind it is multiplied with zeros.
-    template <bool TAIL>
-    __device__ __forceinline__ void load(const Source<MT>& s, int K, int block) {
-        const int g = threadIdx.x % 64 / 16, k0 = block * kBlockK;
-        const bool in = !TAIL || k0 + 32 * g < K;
-        w = symtile::buf_ld16p<symtile::kLoadStream>(s.w, in ? s.at_w : symtile::kOOB, k0 / 2);
+    __device__ __forceinline__ void load(const Source<XL>& s, int block) {
+        const int k0 = block * kBlockK;
+        w = symtile::buf_ld16p<symtile::kLoadStream>(s.w, block < s.w_end ? s.at_w : symtile::kOOB,
+                                                     k0 / 2);
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bool inside = !TAIL || k0 + 32 * j < K;
-                x[i][j] = symtile::buf_ld16(s.x, inside ? s.at_x[i] + 64 * j : symtile::kOOB, k0 * 2);
-            }
+        for (int i = 0; i < XL; ++i)
+            x[i] = symtile::buf_ld16(s.x, block < s.x_end ? s.at_x[i] : symtile::kOOB, k0 * 2);
     }
 
-    __device__ __forceinline__ void multiply(f32x4 (&total)[MT], const Scales<GROUP>& scales,
-                                             int group0) const {
-        typedef Nibbles<BF> Q;
+    // `of_block`: the scales of the block's groups in this lane's column.
+    __device__ __forceinline__ void multiply(f32x4 (&total)[MT], const Nibbles<BF>& q,
+                                             const uint32_t* of_block, StagedX<MT>& staged) const {
+        const int c = threadIdx.x % 16, g = threadIdx.x % 64 / 16;
+#pragma unroll
+        for (int i = 0; i < XL; ++i)
+            staged.v[4 * i + g][c ^ (4 * i + g) % 16] = kApart ? interleave(x[i]) : x[i];
+        __builtin_amdgcn_wave_barrier();   // the wave reads what its lanes wrote
         const symtile::u32x4 words = transpose_quarters(w);
-        const uint32_t* of_block = &scales.of[group0][threadIdx.x % 16];
         f32x4 acc[MT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t of = of_block[j * 32 / GROUP * kTileN];
-            const uint32_t z = Q::minus_offset(of >> 16);
+            const uint32_t z = Nibbles<BF>::minus_offset(of >> 16);
             const symtile::u32x4 zs = {z, z, z, z};
-            const symtile::u32x4 ws = {Q::pair(words[j], 0), Q::pair(words[j], 1),
-                                       Q::pair(words[j], 2), Q::pair(words[j], 3)};
+            symtile::u32x4 ws;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                ws[i] = kApart ? q.apart(words[j], i) : q.adjacent(words[j], i);
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
+                const symtile::u32x4 xs = staged.v[16 * t + c][(4 * j + g) ^ c];
                 if (j * 32 % GROUP == 0) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                acc[t] = mfma<BF>(x[t][j], zs, acc[t]);
-                acc[t] = mfma<BF>(x[t][j], ws, acc[t]);
+                acc[t] = mfma<BF>(xs, zs, acc[t]);
+                acc[t] = mfma<BF>(xs, ws, acc[t]);
                 if ((j + 1) * 32 % GROUP == 0) {
                     const float sc = scale_value<BF>(of & 0xFFFFu);
 #pragma unroll
@@ -186,37 +230,48 @@ struct Block {
                 }
             }
         }
+        __builtin_amdgcn_wave_barrier();   // the next block's X is written after these reads
     }
 };
 
-// One workgroup per tile of 16 columns and up to 16 MT rows; its waves share the
+// One workgroup per tile of 16 columns and up to 4 XL rows; its waves share the
 // blocks of K, in pairs, so that a wave reads whole 128-byte lines of its columns.
 // A wave works on U blocks while U more are on their way.
-template <bool BF, int MT, int GROUP, int U, int WAVES>
+template <bool BF, int XL, int GROUP, int U, int WAVES>
 __global__ void __launch_bounds__(kThreads, WAVES) w4_kernel(W4Params p) {
-    typedef Block<BF, MT, GROUP> B;
-    __shared__ __attribute__((aligned(16))) float red[kWaves][MT][256];
+    typedef Block<BF, XL, GROUP> B;
+    constexpr int MT = B::MT;
+    typedef float Partial[MT][256];
+    static_assert(sizeof(Partial) <= sizeof(StagedX<MT>), "a wave's sums take its X's place");
+    __shared__ StagedX<MT> staged[kWaves];
     __shared__ __attribute__((aligned(16))) uint16_t out[16 * MT][kTileN];
     __shared__ Scales<GROUP> scales;
     const int tile = blockIdx.x, t = threadIdx.x, wave = t / 64, lane = t % 64;
     const int w0 = __builtin_amdgcn_readfirstlane(wave);
     f32x4 total[MT] = {};
-    const Source<MT> src(p, tile);
+    const Source<XL> src(p, tile);
+    const Nibbles<BF> nibbles;
     for (int chunk = 0; chunk < p.K; chunk += kChunkK) {
-        const int first = chunk / kBlockK, blocks = min(p.K, chunk + kChunkK) / kBlockK;
-        // block u of the wave: pairs of blocks, kWaves pairs apart
-        auto block_of = [&](int u) { return first + (u / 2 * kWaves + w0) * 2 + u % 2; };
+        const int first = chunk / kBlockK;
+        const int blocks = (min(p.K, chunk + kChunkK) - chunk + kBlockK - 1) / kBlockK;
+        // block u of the wave in the chunk: pairs of blocks, kWaves pairs apart
+        auto block_of = [&](int u) { return (u / 2 * kWaves + w0) * 2 + u % 2; };
         B a[U], b[U];
         auto fetch = [&](B (&s)[U], int u0) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (block_of(u0 + u) < blocks) s[u].template load<false>(src, p.K, block_of(u0 + u));
+            for (int u = 0; u < U; ++u) {
+                const int i = block_of(u0 + u);
+                // behind the chunk: a block that does not exist
+                s[u].load(src, i < blocks ? first + i : 1 << 20);
+            }
         };
         auto use = [&](B (&s)[U], int u0) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (block_of(u0 + u) < blocks)
-                    s[u].multiply(total, scales, (block_of(u0 + u) - first) * (kBlockK / GROUP));
+            for (int u = 0; u < U; ++u) {
+                const int i = min(block_of(u0 + u), blocks - 1);
+                s[u].multiply(total, nibbles, &scales.of[i * (kBlockK / GROUP)][lane % 16],
+                              staged[wave]);
+            }
         };
         fetch(a, 0);
         if (chunk) __syncthreads();   // the scales before are used up
@@ -225,22 +280,20 @@ __global__ void __launch_bounds__(kThreads, WAVES) w4_kernel(W4Params p) {
         for (int u = 0; block_of(u) < blocks; u += 2 * U) {
             fetch(b, u + U);
             use(a, u);
+            if (block_of(u + U) >= blocks) break;
             fetch(a, u + 2 * U);
             use(b, u + U);
         }
-        if (blocks * kBlockK < min(p.K, chunk + kChunkK) && w0 == kWaves - 1) {
-            // the wave with the fewest blocks
-            a[0].template load<true>(src, p.K, blocks);
-            a[0].multiply(total, scales, (blocks - first) * (kBlockK / GROUP));
-        }
     }
 #pragma unroll
-    for (int i = 0; i < MT; ++i) *reinterpret_cast<f32x4*>(&red[wave][i][4 * lane]) = total[i];
+    for (int i = 0; i < MT; ++i)
+        *reinterpret_cast<f32x4*>(&(reinterpret_cast<Partial&>(staged[wave]))[i][4 * lane]) = total[i];
     __syncthreads();
     for (int o = t; o < 256 * MT; o += kThreads) {
         float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) v += red[w][o / 256][o % 256];
+        for (int w = 0; w < kWaves; ++w)
+            v += reinterpret_cast<const Partial&>(staged[w])[o / 256][o % 256];
         // element 4 * lane + i of a tile: column lane % 16, row 4 * (lane / 16) + i
         const int l = o % 256 / 4, m = o / 256 * 16 + l / 16 * 4 + o % 4;
         uint16_t h;
@@ -270,13 +323,14 @@ __global__ void __launch_bounds__(kThreads, WAVES) w4_kernel(W4Params p) {
     }
 }
 
-// Rows by 16: the smallest of 1, 2 and 4 tiles that hold M.  Blocks in flight: what
-// the registers of two waves a SIMD hold.
+// The smallest build that holds M rows.  Blocks in flight: what the registers of two
+// workgroups a CU hold (one with over 16 rows).
 template <bool BF, int GROUP>
 const void* kernel_of(int M) {
-    if (M <= 16) return reinterpret_cast<const void*>(&w4_kernel<BF, 1, GROUP, 2, 4>);
-    if (M <= 32) return reinterpret_cast<const void*>(&w4_kernel<BF, 2, GROUP, 2, 2>);
-    return reinterpret_cast<const void*>(&w4_kernel<BF, 4, GROUP, 1, 2>);
+    if (M <= 4) return reinterpret_cast<const void*>(&w4_kernel<BF, 1, GROUP, 4, 4>);
+    if (M <= 16) return reinterpret_cast<const void*>(&w4_kernel<BF, 4, GROUP, 2, 4>);
+    if (M <= 32) return reinterpret_cast<const void*>(&w4_kernel<BF, 8, GROUP, 2, 2>);
+    return reinterpret_cast<const void*>(&w4_kernel<BF, 16, GROUP, 1, 2>);
 }
 template <bool BF>
 const void* kernel_of(int M, int group) {
