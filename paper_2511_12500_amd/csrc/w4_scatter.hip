@@ -14,8 +14,6 @@
 
 namespace {
 
-constexpr int kWaves = 8;
-constexpr int kThreads = kWaves * 64;
 constexpr int kTileN = SYMTILE_W4_TILE_N;
 constexpr int kBlockK = 128;        // weights a lane quartet's loads cover in a column
 constexpr int kChunkK = 8192;       // weights of a column whose scales are in LDS
@@ -114,6 +112,7 @@ template <int GROUP>
 struct Scales {
     uint32_t of[kChunkK / GROUP][kTileN];
 
+    template <int THREADS>
     __device__ __forceinline__ void load(const W4Params& p, int tile, int group0) {
         const int n0 = tile * kTileN, cols = min(kTileN, p.N - n0);
         const int count = min(kChunkK / GROUP, p.groups - group0);
@@ -125,7 +124,7 @@ struct Scales {
         // up to the end of the last block: what is behind K is multiplied with 0 as well
         constexpr int kPerBlock = kBlockK / GROUP;
         const int padded = (count + kPerBlock - 1) / kPerBlock * kPerBlock;
-        for (int i = part; i < padded; i += kThreads / kTileN) {
+        for (int i = part; i < padded; i += THREADS / kTileN) {
             uint32_t of_group = 8u << 16;
             if (i < count) {
                 const uint32_t z = p.zeros ? p.zeros[at + i] & 15u : 8u;
@@ -237,13 +236,14 @@ struct Block {
 // One workgroup per tile of 16 columns and up to 4 XL rows; its waves share the
 // blocks of K, in pairs, so that a wave reads whole 128-byte lines of its columns.
 // A wave works on U blocks while U more are on their way.
-template <bool BF, int XL, int GROUP, int U, int WAVES>
-__global__ void __launch_bounds__(kThreads, WAVES) w4_kernel(W4Params p) {
+template <bool BF, int XL, int GROUP, int U, int WAVES, int PER_SIMD>
+__global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
     typedef Block<BF, XL, GROUP> B;
     constexpr int MT = B::MT;
     typedef float Partial[MT][256];
     static_assert(sizeof(Partial) <= sizeof(StagedX<MT>), "a wave's sums take its X's place");
-    __shared__ StagedX<MT> staged[kWaves];
+    constexpr int kThreads = 64 * WAVES;
+    __shared__ StagedX<MT> staged[WAVES];
     __shared__ __attribute__((aligned(16))) uint16_t out[16 * MT][kTileN];
     __shared__ Scales<GROUP> scales;
     const int tile = blockIdx.x, t = threadIdx.x, wave = t / 64, lane = t % 64;
@@ -254,8 +254,8 @@ __global__ void __launch_bounds__(kThreads, WAVES) w4_kernel(W4Params p) {
     for (int chunk = 0; chunk < p.K; chunk += kChunkK) {
         const int first = chunk / kBlockK;
         const int blocks = (min(p.K, chunk + kChunkK) - chunk + kBlockK - 1) / kBlockK;
-        // block u of the wave in the chunk: pairs of blocks, kWaves pairs apart
-        auto block_of = [&](int u) { return (u / 2 * kWaves + w0) * 2 + u % 2; };
+        // block u of the wave in the chunk: pairs of blocks, WAVES pairs apart
+        auto block_of = [&](int u) { return (u / 2 * WAVES + w0) * 2 + u % 2; };
         B a[U], b[U];
         auto fetch = [&](B (&s)[U], int u0) {
 #pragma unroll
@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, WAVES) w4_kernel(W4Params p) {
         };
         fetch(a, 0);
         if (chunk) __syncthreads();   // the scales before are used up
-        scales.load(p, tile, chunk / GROUP);
+        scales.template load<kThreads>(p, tile, chunk / GROUP);
         __syncthreads();
         for (int u = 0; block_of(u) < blocks; u += 2 * U) {
             fetch(b, u + U);
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, WAVES) w4_kernel(W4Params p) {
     for (int o = t; o < 256 * MT; o += kThreads) {
         float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w)
+        for (int w = 0; w < WAVES; ++w)
             v += reinterpret_cast<const Partial&>(staged[w])[o / 256][o % 256];
         // element 4 * lane + i of a tile: column lane % 16, row 4 * (lane / 16) + i
         const int l = o % 256 / 4, m = o / 256 * 16 + l / 16 * 4 + o % 4;
@@ -302,10 +302,10 @@ __global__ void __launch_bounds__(kThreads, WAVES) w4_kernel(W4Params p) {
         out[m][l % 16] = h;
     }
     __syncthreads();
-    // wave s stores the tile into slot s and counts it there: its own stores'
+    // a wave stores the tile into a slot and counts it there: its own stores'
     // acknowledgements are all that the counter has to wait for
-    if (wave < p.world) {
-        const char* base = reinterpret_cast<const char*>(p.bases[wave]);
+    for (int slot = wave; slot < p.world; slot += WAVES) {
+        const char* base = reinterpret_cast<const char*>(p.bases[slot]);
         const int chunks = p.N - tile * kTileN >= kTileN ? 2 : 1;   // of 8 columns
         const symtile::rsrc_t dst = symtile::make_rsrc(
             base + p.c_off + (size_t)tile * kTileN * 2,
@@ -319,24 +319,32 @@ __global__ void __launch_bounds__(kThreads, WAVES) w4_kernel(W4Params p) {
         symtile::release_written_through();
         if (lane == 0)
             symtile::flag_signal(reinterpret_cast<uint32_t*>(
-                reinterpret_cast<char*>(p.bases[wave]) + p.flag_off) + tile);
+                reinterpret_cast<char*>(p.bases[slot]) + p.flag_off) + tile);
     }
 }
 
-// The smallest build that holds M rows.  Blocks in flight: what the registers of two
-// workgroups a CU hold (one with over 16 rows).
+struct Build {
+    const void* kernel;
+    int waves;
+};
+template <bool BF, int XL, int GROUP, int U, int WAVES, int PER_SIMD>
+Build build_of() {
+    return {reinterpret_cast<const void*>(&w4_kernel<BF, XL, GROUP, U, WAVES, PER_SIMD>), WAVES};
+}
+
+// The smallest build that holds M rows.
 template <bool BF, int GROUP>
-const void* kernel_of(int M) {
-    if (M <= 4) return reinterpret_cast<const void*>(&w4_kernel<BF, 1, GROUP, 4, 4>);
-    if (M <= 16) return reinterpret_cast<const void*>(&w4_kernel<BF, 4, GROUP, 2, 4>);
-    if (M <= 32) return reinterpret_cast<const void*>(&w4_kernel<BF, 8, GROUP, 2, 2>);
-    return reinterpret_cast<const void*>(&w4_kernel<BF, 16, GROUP, 1, 2>);
+Build build_for(int M, int tiles) {
+    if (M <= 4) return build_of<BF, 1, GROUP, 2, 8, 8>();
+    if (M <= 16) return build_of<BF, 4, GROUP, 2, 8, 4>();
+    if (M <= 32) return build_of<BF, 8, GROUP, 2, 8, 2>();
+    return build_of<BF, 16, GROUP, 1, 8, 2>();
 }
 template <bool BF>
-const void* kernel_of(int M, int group) {
-    return group == 128  ? kernel_of<BF, 128>(M)
-           : group == 64 ? kernel_of<BF, 64>(M)
-                         : kernel_of<BF, 32>(M);
+Build build_for(int M, int group, int tiles) {
+    return group == 128  ? build_for<BF, 128>(M, tiles)
+           : group == 64 ? build_for<BF, 64>(M, tiles)
+                         : build_for<BF, 32>(M, tiles);
 }
 
 }  // namespace
@@ -400,11 +408,11 @@ extern "C" symtile_status symtile_w4_all_scatter(
     p.ldc = (int)ldc;
     int prev = -1;
     if (symtile_status st = symtile_host::set_device(h, &prev)) return st;
-    const void* kernel = dtype == SYMTILE_BF16 ? kernel_of<true>(M, group)
-                                               : kernel_of<false>(M, group);
+    const Build build = dtype == SYMTILE_BF16 ? build_for<true>(M, group, tiles)
+                                              : build_for<false>(M, group, tiles);
     void* args[] = {&p};
-    hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)tiles), dim3(kThreads), args, 0,
-                                   static_cast<hipStream_t>(s));
+    hipError_t e = hipLaunchKernel(build.kernel, dim3((unsigned)tiles), dim3(64 * build.waves), args,
+                                   0, static_cast<hipStream_t>(s));
     if (e == hipSuccess) e = hipGetLastError();
     if (prev >= 0) (void)hipSetDevice(prev);
     return e == hipSuccess ? SYMTILE_OK : symtile_host::hip_fail(e, "w4_kernel launch");
