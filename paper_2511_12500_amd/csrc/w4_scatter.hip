@@ -105,32 +105,57 @@ __device__ __forceinline__ symtile::u32x4 transpose_quarters(symtile::u32x4 w) {
     return symtile::u32x4{c[0], c[1], d[0], d[1]};
 }
 
-// Scales, and zero points above them, of a tile's 16 columns for the groups of one
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+typedef uint8_t u8x8 __attribute__((ext_vector_type(8)));
+template <class V>
+struct __attribute__((packed, aligned(1))) Unaligned {
+    V v;
+};
+
+// Scales, and zero points above them, of NT tiles' columns for the groups of one
 // chunk of K, group by group: a column's are far from the next column's in memory
 // and every block needs one of each, so they are read once, along the columns.
-template <int GROUP>
+template <int GROUP, int NT>
 struct Scales {
-    uint32_t of[kChunkK / GROUP][kTileN];
+    uint32_t of[kChunkK / GROUP][NT * kTileN];
 
     template <int THREADS>
-    __device__ __forceinline__ void load(const W4Params& p, int tile, int group0) {
-        const int n0 = tile * kTileN, cols = min(kTileN, p.N - n0);
+    __device__ __forceinline__ void load(const W4Params& p, int n0, int group0) {
+        constexpr int kCols = NT * kTileN, kVec = 8;
+        constexpr int kMost = (kChunkK / GROUP / kVec * kCols + THREADS - 1) / THREADS;
         const int count = min(kChunkK / GROUP, p.groups - group0);
-        // 16 threads a column: neighbours read neighbouring groups
-        const int col = min((int)threadIdx.x / 16 % kTileN, cols - 1);
-        const int part = threadIdx.x % 16 + threadIdx.x / 256 * 16;
-        const size_t at = (size_t)(n0 + col) * p.groups + group0;
-        const uint16_t* scales = static_cast<const uint16_t*>(p.scales) + at;
-        // up to the end of the last block: what is behind K is multiplied with 0 as well
-        constexpr int kPerBlock = kBlockK / GROUP;
-        const int padded = (count + kPerBlock - 1) / kPerBlock * kPerBlock;
-        for (int i = part; i < padded; i += THREADS / kTileN) {
-            uint32_t of_group = 8u << 16;
-            if (i < count) {
-                const uint32_t z = p.zeros ? p.zeros[at + i] & 15u : 8u;
-                of_group = scales[i] | z << 16;
+        const int vecs = (count + kVec - 1) / kVec;     // 8 groups of a column each
+        const size_t end = (size_t)p.N * p.groups;
+        // all of a thread's loads, then their places
+        u16x8 s[kMost];
+        u8x8 z[kMost];
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            const int v = threadIdx.x + i * THREADS, col = v / vecs;
+            z[i] = u8x8{8, 8, 8, 8, 8, 8, 8, 8};
+            if (col >= kCols) continue;
+            const size_t at = (size_t)min(n0 + col, p.N - 1) * p.groups + group0 + v % vecs * kVec;
+            const uint16_t* scales = static_cast<const uint16_t*>(p.scales) + at;
+            if (at + kVec <= end) {     // what follows in the next column is not used
+                s[i] = reinterpret_cast<const Unaligned<u16x8>*>(scales)->v;
+                if (p.zeros) z[i] = reinterpret_cast<const Unaligned<u8x8>*>(p.zeros + at)->v;
+            } else {
+                for (int e = 0; e < kVec; ++e)
+                    if (at + e < end) {
+                        s[i][e] = scales[e];
+                        if (p.zeros) z[i][e] = p.zeros[at + e];
+                    }
             }
-            of[i][threadIdx.x / 16 % kTileN] = of_group;
+        }
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            const int v = threadIdx.x + i * THREADS, col = v / vecs;
+            if (col >= kCols) continue;
+            // behind the last group: multiplied with zeros of X, but with a number
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                of[v % vecs * kVec + e][col] =
+                    v % vecs * kVec + e < count ? s[i][e] | (z[i][e] & 15u) << 16 : 0u;
         }
     }
 };
@@ -151,81 +176,95 @@ struct StagedX {
 // `x_end` (its 8 values): the others' offsets are set outside of the resource and
 // read as zeros, without a branch, so that the loads of several blocks are in
 // flight together.  What is behind K is multiplied with zeros of X.
-template <int XL>
+template <int XL, int NT>
 struct Source {
     symtile::rsrc_t x, w;
-    uint32_t at_x[XL], at_w;   // bytes
+    uint32_t at_x[XL], at_w[NT];   // bytes
     int w_end, x_end;
 
-    __device__ __forceinline__ Source(const W4Params& p, int tile) {
+    __device__ __forceinline__ Source(const W4Params& p, int n0) {
         const int lane = threadIdx.x % 64, c = lane % 16, g = lane / 16;
-        const int n0 = tile * kTileN, cols = min(kTileN, p.N - n0);
+        const int cols = min(NT * kTileN, p.N - n0);
         x = symtile::make_rsrc(p.X, (uint32_t)(((p.M - 1) * p.ldx + p.K) * 2));
         w = symtile::make_rsrc(p.q + (size_t)n0 * (p.K / 2), (uint32_t)(cols * (p.K / 2)));
 #pragma unroll
         for (int i = 0; i < XL; ++i)
             at_x[i] = (uint32_t)(min(4 * i + g, p.M - 1) * p.ldx + 8 * c) * 2;
-        at_w = (uint32_t)(min(c, cols - 1) * (p.K / 2) + 16 * g);
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+            at_w[i] = (uint32_t)(min(i * kTileN + c, cols - 1) * (p.K / 2) + 16 * g);
         w_end = (p.K - 32 * g + kBlockK - 1) / kBlockK;
         x_end = (p.K - 8 * c + kBlockK - 1) / kBlockK;
     }
 };
 
-// One block of 128 weights of 16 columns, with what it is multiplied by.  Lane (c =
-// lane % 16, g = lane / 16) loads column c's weights 32 g .. 32 g + 31 in one vector;
-// its words are then transposed between the quarters of the wave, so that matrix
-// instruction j has the weights 32 j .. 32 j + 31: a group's are in instructions of
-// their own.  X comes by rows, 256 bytes of four rows a load (XL of them), and takes
-// the matrix operands' layout in LDS: loading operands directly reads 64 bytes of 16
-// rows, whose distance is often a power of two, from one cache channel (64 tokens
-// through 8192x3584: 36 us).
-template <bool BF, int XL, int GROUP>
+// One block of 128 weights of NT tiles of 16 columns, with what it is multiplied by.
+// Lane (c = lane % 16, g = lane / 16) loads column c's weights 32 g .. 32 g + 31 in
+// one vector.  With one group a block, matrix instruction j takes word j of every
+// lane; with more, the words are transposed between the quarters of the wave, so
+// that instruction j has the weights 32 j .. 32 j + 31 and a group's are in
+// instructions of their own.  X comes by rows, 256 bytes of four rows a load (XL of
+// them), and takes the matrix operands' layout in LDS: loading operands directly
+// reads 64 bytes of 16 rows, whose distance is often a power of two, from one cache
+// channel (64 tokens through 8192x3584: 36 us).
+template <bool BF, int XL, int NT, int GROUP>
 struct Block {
     static constexpr int MT = (XL + 3) / 4;       // tiles of 16 rows
-    static constexpr bool kApart = XL <= 4;       // X reordered for Nibbles::apart: 4 XL
-                                                  // instructions for 16 fewer on weights
-    symtile::u32x4 w;
+    static constexpr bool kApart = XL <= 4 * NT;  // X reordered for Nibbles::apart: 4 XL
+                                                  // instructions for 16 NT fewer on weights
+    symtile::u32x4 w[NT];
     symtile::u32x4 x[XL];    // rows 4 i + g, values 8 c .. 8 c + 7
 
-    __device__ __forceinline__ void load(const Source<XL>& s, int block) {
+    __device__ __forceinline__ void load(const Source<XL, NT>& s, int block) {
         const int k0 = block * kBlockK;
-        w = symtile::buf_ld16p<symtile::kLoadStream>(s.w, block < s.w_end ? s.at_w : symtile::kOOB,
-                                                     k0 / 2);
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+            w[i] = symtile::buf_ld16p<symtile::kLoadStream>(
+                s.w, block < s.w_end ? s.at_w[i] : symtile::kOOB, k0 / 2);
 #pragma unroll
         for (int i = 0; i < XL; ++i)
             x[i] = symtile::buf_ld16(s.x, block < s.x_end ? s.at_x[i] : symtile::kOOB, k0 * 2);
     }
 
-    // `of_block`: the scales of the block's groups in this lane's column.
-    __device__ __forceinline__ void multiply(f32x4 (&total)[MT], const Nibbles<BF>& q,
+    // `of_block`: the scales of the block's groups in this lane's column of the first tile.
+    __device__ __forceinline__ void multiply(f32x4 (&total)[NT][MT], const Nibbles<BF>& q,
                                              const uint32_t* of_block, StagedX<MT>& staged) const {
         const int c = threadIdx.x % 16, g = threadIdx.x % 64 / 16;
 #pragma unroll
         for (int i = 0; i < XL; ++i)
             staged.v[4 * i + g][c ^ (4 * i + g) % 16] = kApart ? interleave(x[i]) : x[i];
         __builtin_amdgcn_wave_barrier();   // the wave reads what its lanes wrote
-        const symtile::u32x4 words = transpose_quarters(w);
-        f32x4 acc[MT];
+        symtile::u32x4 words[NT];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) words[i] = GROUP == kBlockK ? w[i] : transpose_quarters(w[i]);
+        f32x4 acc[NT][MT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t of = of_block[j * 32 / GROUP * kTileN];
-            const uint32_t z = Nibbles<BF>::minus_offset(of >> 16);
-            const symtile::u32x4 zs = {z, z, z, z};
-            symtile::u32x4 ws;
+            symtile::u32x4 xs[MT];
+            const int v = GROUP == kBlockK ? 4 * g + j : 4 * j + g;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                ws[i] = kApart ? q.apart(words[j], i) : q.adjacent(words[j], i);
+            for (int t = 0; t < MT; ++t) xs[t] = staged.v[16 * t + c][v ^ c];
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                const symtile::u32x4 xs = staged.v[16 * t + c][(4 * j + g) ^ c];
-                if (j * 32 % GROUP == 0) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                acc[t] = mfma<BF>(xs, zs, acc[t]);
-                acc[t] = mfma<BF>(xs, ws, acc[t]);
-                if ((j + 1) * 32 % GROUP == 0) {
-                    const float sc = scale_value<BF>(of & 0xFFFFu);
+            for (int n = 0; n < NT; ++n) {
+                const uint32_t of = of_block[(j * 32 / GROUP * NT + n) * kTileN];
+                const uint32_t z = Nibbles<BF>::minus_offset(of >> 16);
+                const symtile::u32x4 zs = {z, z, z, z};
+                symtile::u32x4 ws;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        total[t][e] = __builtin_fmaf(sc, acc[t][e], total[t][e]);
+                for (int i = 0; i < 4; ++i)
+                    ws[i] = kApart ? q.apart(words[n][j], i) : q.adjacent(words[n][j], i);
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    f32x4& a = acc[n][t];
+                    if (j * 32 % GROUP == 0) a = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                    a = mfma<BF>(xs[t], zs, a);
+                    a = mfma<BF>(xs[t], ws, a);
+                    if ((j + 1) * 32 % GROUP == 0) {
+                        const float sc = scale_value<BF>(of & 0xFFFFu);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            total[n][t][e] = __builtin_fmaf(sc, a[e], total[n][t][e]);
+                    }
                 }
             }
         }
@@ -233,23 +272,22 @@ struct Block {
     }
 };
 
-// One workgroup per tile of 16 columns and up to 4 XL rows; its waves share the
+// One workgroup per NT tiles of 16 columns and up to 4 XL rows; its waves share the
 // blocks of K, in pairs, so that a wave reads whole 128-byte lines of its columns.
 // A wave works on U blocks while U more are on their way.
-template <bool BF, int XL, int GROUP, int U, int WAVES, int PER_SIMD>
+template <bool BF, int XL, int NT, int GROUP, int U, int WAVES, int PER_SIMD>
 __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
-    typedef Block<BF, XL, GROUP> B;
-    constexpr int MT = B::MT;
+    typedef Block<BF, XL, NT, GROUP> B;
+    constexpr int MT = B::MT, kThreads = 64 * WAVES;
     typedef float Partial[MT][256];
     static_assert(sizeof(Partial) <= sizeof(StagedX<MT>), "a wave's sums take its X's place");
-    constexpr int kThreads = 64 * WAVES;
     __shared__ StagedX<MT> staged[WAVES];
     __shared__ __attribute__((aligned(16))) uint16_t out[16 * MT][kTileN];
-    __shared__ Scales<GROUP> scales;
-    const int tile = blockIdx.x, t = threadIdx.x, wave = t / 64, lane = t % 64;
+    __shared__ Scales<GROUP, NT> scales;
+    const int tile0 = blockIdx.x * NT, t = threadIdx.x, wave = t / 64, lane = t % 64;
     const int w0 = __builtin_amdgcn_readfirstlane(wave);
-    f32x4 total[MT] = {};
-    const Source<XL> src(p, tile);
+    f32x4 total[NT][MT] = {};
+    const Source<XL, NT> src(p, tile0 * kTileN);
     const Nibbles<BF> nibbles;
     for (int chunk = 0; chunk < p.K; chunk += kChunkK) {
         const int first = chunk / kBlockK;
@@ -275,7 +313,7 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
         };
         fetch(a, 0);
         if (chunk) __syncthreads();   // the scales before are used up
-        scales.template load<kThreads>(p, tile, chunk / GROUP);
+        scales.template load<kThreads>(p, tile0 * kTileN, chunk / GROUP);
         __syncthreads();
         for (int u = 0; block_of(u) < blocks; u += 2 * U) {
             fetch(b, u + U);
@@ -285,60 +323,71 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
             use(b, u + U);
         }
     }
+    // the waves' sums, tile by tile
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
-        *reinterpret_cast<f32x4*>(&(reinterpret_cast<Partial&>(staged[wave]))[i][4 * lane]) = total[i];
-    __syncthreads();
-    for (int o = t; o < 256 * MT; o += kThreads) {
-        float v = 0.0f;
+    for (int n = 0; n < NT; ++n) {
+        const int tile = tile0 + n;
+        if (tile * kTileN >= p.N) break;
+        if (n) __syncthreads();   // the sums and the output of the tile before are read
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w)
-            v += reinterpret_cast<const Partial&>(staged[w])[o / 256][o % 256];
-        // element 4 * lane + i of a tile: column lane % 16, row 4 * (lane / 16) + i
-        const int l = o % 256 / 4, m = o / 256 * 16 + l / 16 * 4 + o % 4;
-        uint16_t h;
-        if constexpr (BF) h = __builtin_bit_cast(uint16_t, (__bf16)v);
-        else h = __builtin_bit_cast(uint16_t, (_Float16)v);
-        out[m][l % 16] = h;
-    }
-    __syncthreads();
-    // a wave stores the tile into a slot and counts it there: its own stores'
-    // acknowledgements are all that the counter has to wait for
-    for (int slot = wave; slot < p.world; slot += WAVES) {
-        const char* base = reinterpret_cast<const char*>(p.bases[slot]);
-        const int chunks = p.N - tile * kTileN >= kTileN ? 2 : 1;   // of 8 columns
-        const symtile::rsrc_t dst = symtile::make_rsrc(
-            base + p.c_off + (size_t)tile * kTileN * 2,
-            (uint32_t)(((size_t)(p.M - 1) * p.ldc + chunks * 8) * 2));
-        for (int i = lane; i < p.M * 2; i += 64) {
-            const int m = i / 2, c = i % 2;
-            if (c < chunks)
-                symtile::buf_st16p<symtile::kStoreWriteThrough>(
-                    symtile::ld16(&out[m][c * 8]), dst, (uint32_t)(m * p.ldc + c * 8) * 2, 0);
+        for (int i = 0; i < MT; ++i)
+            *reinterpret_cast<f32x4*>(&(reinterpret_cast<Partial&>(staged[wave]))[i][4 * lane]) =
+                total[n][i];
+        __syncthreads();
+        for (int o = t; o < 256 * MT; o += kThreads) {
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w)
+                v += reinterpret_cast<const Partial&>(staged[w])[o / 256][o % 256];
+            // element 4 * lane + i of a tile: column lane % 16, row 4 * (lane / 16) + i
+            const int l = o % 256 / 4, m = o / 256 * 16 + l / 16 * 4 + o % 4;
+            uint16_t h;
+            if constexpr (BF) h = __builtin_bit_cast(uint16_t, (__bf16)v);
+            else h = __builtin_bit_cast(uint16_t, (_Float16)v);
+            out[m][l % 16] = h;
         }
-        symtile::release_written_through();
-        if (lane == 0)
-            symtile::flag_signal(reinterpret_cast<uint32_t*>(
-                reinterpret_cast<char*>(p.bases[slot]) + p.flag_off) + tile);
+        __syncthreads();
+        // a wave stores the tile into a slot and counts it there: its own stores'
+        // acknowledgements are all that the counter has to wait for
+        for (int slot = wave; slot < p.world; slot += WAVES) {
+            char* base = reinterpret_cast<char*>(p.bases[slot]);
+            const int chunks = p.N - tile * kTileN >= kTileN ? 2 : 1;   // of 8 columns
+            const symtile::rsrc_t dst = symtile::make_rsrc(
+                base + p.c_off + (size_t)tile * kTileN * 2,
+                (uint32_t)(((size_t)(p.M - 1) * p.ldc + chunks * 8) * 2));
+            for (int i = lane; i < p.M * 2; i += 64) {
+                const int m = i / 2, c = i % 2;
+                if (c < chunks)
+                    symtile::buf_st16p<symtile::kStoreWriteThrough>(
+                        symtile::ld16(&out[m][c * 8]), dst, (uint32_t)(m * p.ldc + c * 8) * 2, 0);
+            }
+            symtile::release_written_through();
+            if (lane == 0)
+                symtile::flag_signal(reinterpret_cast<uint32_t*>(base + p.flag_off) + tile);
+        }
     }
 }
 
 struct Build {
     const void* kernel;
-    int waves;
+    int waves, tiles;   // waves and tiles of a workgroup
 };
-template <bool BF, int XL, int GROUP, int U, int WAVES, int PER_SIMD>
+template <bool BF, int XL, int NT, int GROUP, int U, int WAVES, int PER_SIMD>
 Build build_of() {
-    return {reinterpret_cast<const void*>(&w4_kernel<BF, XL, GROUP, U, WAVES, PER_SIMD>), WAVES};
+    return {reinterpret_cast<const void*>(&w4_kernel<BF, XL, NT, GROUP, U, WAVES, PER_SIMD>), WAVES,
+            NT};
 }
 
 // The smallest build that holds M rows.
 template <bool BF, int GROUP>
 Build build_for(int M, int tiles) {
-    if (M <= 4) return build_of<BF, 1, GROUP, 2, 8, 8>();
-    if (M <= 16) return build_of<BF, 4, GROUP, 2, 8, 4>();
-    if (M <= 32) return build_of<BF, 8, GROUP, 2, 8, 2>();
-    return build_of<BF, 16, GROUP, 1, 8, 2>();
+    const bool many = tiles >= 1024;
+    if (M <= 4)
+        return many ? build_of<BF, 1, 1, GROUP, 2, 4, 8>() : build_of<BF, 1, 1, GROUP, 2, 8, 8>();
+    if (M <= 16)
+        return many ? build_of<BF, 4, 2, GROUP, 1, 4, 4>() : build_of<BF, 4, 1, GROUP, 2, 8, 4>();
+    if (M <= 32) return build_of<BF, 8, 1, GROUP, 2, 8, 2>();
+    return build_of<BF, 16, 1, GROUP, 1, 8, 2>();
 }
 template <bool BF>
 Build build_for(int M, int group, int tiles) {
@@ -411,7 +460,8 @@ extern "C" symtile_status symtile_w4_all_scatter(
     const Build build = dtype == SYMTILE_BF16 ? build_for<true>(M, group, tiles)
                                               : build_for<false>(M, group, tiles);
     void* args[] = {&p};
-    hipError_t e = hipLaunchKernel(build.kernel, dim3((unsigned)tiles), dim3(64 * build.waves), args,
+    hipError_t e = hipLaunchKernel(build.kernel, dim3((unsigned)((tiles + build.tiles - 1) / build.tiles)),
+                                   dim3(64 * build.waves), args,
                                    0, static_cast<hipStream_t>(s));
     if (e == hipSuccess) e = hipGetLastError();
     if (prev >= 0) (void)hipSetDevice(prev);
