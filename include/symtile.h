@@ -603,6 +603,11 @@ symtile_status symtile_distill_topk_backward(int device, const void* logits, int
                                              const float* stats, const float* row_grad,
                                              void* dlogits, size_t ld_grad, symtile_stream s);
 
+/* Bytes of the workspace of a symtile_w4_all_scatter call on `device` with these
+ * sizes (0: none is used).  EINVAL, EUNSUPPORTED for what the call refuses. */
+symtile_status symtile_w4_workspace_bytes(int device, int M, int N_local, int K, int group,
+                                          size_t* bytes);
+
 /* Output tile of symtile_w4_all_scatter: all rows (at most 64) by 16 columns. */
 #define SYMTILE_W4_TILE_M 64
 #define SYMTILE_W4_TILE_N 16
@@ -626,13 +631,21 @@ symtile_status symtile_distill_topk_backward(int device, const void* logits, int
  *  C_gathered_local, arrived_local: as in symtile_gemm_all_scatter, with tiles of
  *           SYMTILE_W4_TILE_M x SYMTILE_W4_TILE_N: uint32 [world_size][1][ceil(N_local / 16)]
  *
+ *  workspace: device memory of symtile_w4_workspace_bytes(...) bytes, 16-byte
+ *           aligned, zero before the first call that uses it; every call leaves its
+ *           counters zero again.  NULL = K is not split over workgroups (slower
+ *           for more than 4 tokens and few columns).  Calls that share a workspace
+ *           must not overlap in time.
+ *
  * Requirements: K a multiple of 32, N_local of 8; X, q and C 16-byte aligned;
- * M = 0 or N_local = 0 launches nothing, K = 0 stores zeros.  EINVAL otherwise. */
+ * M = 0 or N_local = 0 launches nothing, K = 0 stores zeros.  EINVAL otherwise.
+ * A row of X that holds an infinity or a NaN gives NaN. */
 symtile_status symtile_w4_all_scatter(symtile_heap* h, const void* X, const uint8_t* q,
                                       const void* scales, const uint8_t* zeros,
                                       void* C_gathered_local, uint32_t* arrived_local, int M,
                                       int N_local, int K, int ldx, int group, int dtype, int rank,
-                                      int world_size, symtile_stream s);
+                                      int world_size, void* workspace, size_t workspace_bytes,
+                                      symtile_stream s);
 
 /* Rate of the realtime counter behind trace timestamps (the per-tile
  * timeline of Section 3.4, instrumentation), in kHz.  EINVAL for a bad device

@@ -22,6 +22,7 @@ _BINDING = (
     "DISTILL_RENORM", "DISTILL_REST", "TOP_MAX", "W4_TILE_M", "W4_TILE_N",
     "symtile_distill_topk", "symtile_distill_topk_backward", "symtile_logits_workspace_bytes",
     "symtile_token_logprobs", "symtile_token_logprobs_backward", "symtile_w4_all_scatter",
+    "symtile_w4_workspace_bytes",
 )
 _HEAP = ("GatheredOutput", "Heap", "current_stream")
 _HEAD = ("TokenLogprobs", "TopDistillation", "W4Weight")

@@ -106,7 +106,8 @@ def _load():
         "symtile_distill_topk_backward": [i32, vp, i32, i32, sz, i32, f32, vp, vp, i32, i32, i32,
                                           vp, vp, vp, sz, vp],
         "symtile_w4_all_scatter": [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
-                                   i32, vp],
+                                   i32, vp, sz, vp],
+        "symtile_w4_workspace_bytes": [i32, i32, i32, i32, i32, ctypes.POINTER(sz)],
         "symtile_value_exercise": [vp, i32, sz, sz, sz, i32, i32, i32, vp],
     }
     for name, args in decl.items():
@@ -349,11 +350,20 @@ def symtile_distill_topk_backward(device: int, logits: int, rows: int, vocab: in
 
 def symtile_w4_all_scatter(h: int, X: int, q: int, scales: int, zeros: int, C_gathered_local: int,
                            arrived_local: int, M: int, N_local: int, K: int, ldx: int, group: int,
-                           dtype: int, rank: int, world_size: int, stream: int = 0) -> None:
+                           dtype: int, rank: int, world_size: int, workspace: int = 0,
+                           workspace_bytes: int = 0, stream: int = 0) -> None:
     _check(lib.symtile_w4_all_scatter(_vp(h), _vp(X), _vp(q), _vp(scales), _vp(zeros),
                                       _vp(C_gathered_local), _vp(arrived_local), M, N_local, K,
-                                      ldx, group, dtype, rank, world_size, _vp(stream)),
-           "symtile_w4_all_scatter")
+                                      ldx, group, dtype, rank, world_size, _vp(workspace),
+                                      workspace_bytes, _vp(stream)), "symtile_w4_all_scatter")
+
+
+def symtile_w4_workspace_bytes(device: int, M: int, N_local: int, K: int, group: int) -> int:
+    """Bytes of the workspace of a symtile_w4_all_scatter call."""
+    out = ctypes.c_size_t()
+    _check(lib.symtile_w4_workspace_bytes(device, M, N_local, K, group, ctypes.byref(out)),
+           "symtile_w4_workspace_bytes")
+    return out.value
 
 
 def symtile_litmus_mp(h: int, data_off: int, flag_off: int, pairs: int, rounds: int,

@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <string>
 
 #include "symtile.h"
@@ -29,6 +30,11 @@ struct W4Params {
     uint64_t c_off, flag_off;   // of the rank's column block and its counters in a slot
     int M, N, K, ldx, groups, world;
     int ldc;                    // elements
+    // of the wide kernel: K in `splits` parts of `part_steps` steps each (the last may
+    // have fewer), whose sums meet in `partials`
+    int splits, part_steps;
+    uint32_t* counters;
+    float* partials;
 };
 
 // Weights as floating point without a conversion: 4 bits placed at the top of
@@ -115,26 +121,27 @@ struct __attribute__((packed, aligned(1))) Unaligned {
 // Scales, and zero points above them, of NT tiles' columns for the groups of one
 // chunk of K, group by group: a column's are far from the next column's in memory
 // and every block needs one of each, so they are read once, along the columns.
-template <int GROUP, int NT>
+template <int GROUP, int NT, int CHUNK>
 struct Scales {
-    uint32_t of[kChunkK / GROUP][NT * kTileN];
+    uint32_t of[CHUNK / GROUP][NT * kTileN];
 
+    // Groups from `group0` on.  Behind the last one stand zeros, which meet zeros of X.
     template <int THREADS>
     __device__ __forceinline__ void load(const W4Params& p, int n0, int group0) {
         constexpr int kCols = NT * kTileN, kVec = 8;
-        constexpr int kMost = (kChunkK / GROUP / kVec * kCols + THREADS - 1) / THREADS;
-        const int count = min(kChunkK / GROUP, p.groups - group0);
-        const int vecs = (count + kVec - 1) / kVec;     // 8 groups of a column each
+        constexpr int kVecs = CHUNK / GROUP / kVec;      // 8 groups of a column each
+        constexpr int kMost = (kVecs * kCols + THREADS - 1) / THREADS;
+        const int count = p.groups - group0;
         const size_t end = (size_t)p.N * p.groups;
         // all of a thread's loads, then their places
         u16x8 s[kMost];
         u8x8 z[kMost];
 #pragma unroll
         for (int i = 0; i < kMost; ++i) {
-            const int v = threadIdx.x + i * THREADS, col = v / vecs;
+            const int v = threadIdx.x + i * THREADS, col = v / kVecs, first = v % kVecs * kVec;
             z[i] = u8x8{8, 8, 8, 8, 8, 8, 8, 8};
-            if (col >= kCols) continue;
-            const size_t at = (size_t)min(n0 + col, p.N - 1) * p.groups + group0 + v % vecs * kVec;
+            if (col >= kCols || first >= count) continue;
+            const size_t at = (size_t)min(n0 + col, p.N - 1) * p.groups + group0 + first;
             const uint16_t* scales = static_cast<const uint16_t*>(p.scales) + at;
             if (at + kVec <= end) {     // what follows in the next column is not used
                 s[i] = reinterpret_cast<const Unaligned<u16x8>*>(scales)->v;
@@ -149,13 +156,11 @@ struct Scales {
         }
 #pragma unroll
         for (int i = 0; i < kMost; ++i) {
-            const int v = threadIdx.x + i * THREADS, col = v / vecs;
+            const int v = threadIdx.x + i * THREADS, col = v / kVecs, first = v % kVecs * kVec;
             if (col >= kCols) continue;
-            // behind the last group: multiplied with zeros of X, but with a number
 #pragma unroll
             for (int e = 0; e < kVec; ++e)
-                of[v % vecs * kVec + e][col] =
-                    v % vecs * kVec + e < count ? s[i][e] | (z[i][e] & 15u) << 16 : 0u;
+                of[first + e][col] = first + e < count ? s[i][e] | (z[i][e] & 15u) << 16 : 0u;
         }
     }
 };
@@ -198,12 +203,89 @@ struct Source {
     }
 };
 
-// One block of 128 weights of NT tiles of 16 columns, with what it is multiplied by.
-// Lane (c = lane % 16, g = lane / 16) loads column c's weights 32 g .. 32 g + 31 in
-// one vector.  With one group a block, matrix instruction j takes word j of every
-// lane; with more, the words are transposed between the quarters of the wave, so
-// that instruction j has the weights 32 j .. 32 j + 31 and a group's are in
-// instructions of their own.  X comes by rows, 256 bytes of four rows a load (XL of
+// A block of 128 weights of NT tiles of 16 columns times the rows of X in `staged`,
+// added to `total` with the groups' scales: `of_block` points at the first group's in
+// this lane's column of the first tile, `stride` columns before the next group's.
+// Lane (c = lane % 16, g = lane / 16) holds column c's weights 32 g .. 32 g + 31.
+// With one group a block, matrix instruction j takes word j of every lane; with
+// more, the words are transposed between the quarters of the wave, so that
+// instruction j has the weights 32 j .. 32 j + 31 and a group's are in instructions
+// of their own.
+template <bool BF, int NT, int MT, int GROUP, bool APART>
+__device__ __forceinline__ void multiply_block(f32x4 (&total)[NT][MT], const Nibbles<BF>& q,
+                                               const symtile::u32x4 (&w)[NT],
+                                               const uint32_t* of_block, int stride,
+                                               const StagedX<MT>& staged) {
+    const int c = threadIdx.x % 16, g = threadIdx.x % 64 / 16;
+    symtile::u32x4 words[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) words[i] = GROUP == kBlockK ? w[i] : transpose_quarters(w[i]);
+    f32x4 acc[NT][MT];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        symtile::u32x4 xs[MT];
+        const int v = GROUP == kBlockK ? 4 * g + j : 4 * j + g;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) xs[t] = staged.v[16 * t + c][v ^ c];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const uint32_t of = of_block[j * 32 / GROUP * stride + n * kTileN];
+            const uint32_t z = Nibbles<BF>::minus_offset(of >> 16);
+            const symtile::u32x4 zs = {z, z, z, z};
+            symtile::u32x4 ws;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                ws[i] = APART ? q.apart(words[n][j], i) : q.adjacent(words[n][j], i);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                f32x4& a = acc[n][t];
+                if (j * 32 % GROUP == 0) a = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                a = mfma<BF>(xs[t], zs, a);
+                a = mfma<BF>(xs[t], ws, a);
+                if ((j + 1) * 32 % GROUP == 0) {
+                    const float sc = scale_value<BF>(of & 0xFFFFu);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        total[n][t][e] = __builtin_fmaf(sc, a[e], total[n][t][e]);
+                }
+            }
+        }
+    }
+}
+
+// Element 4 * lane + i of a tile of sums: column lane % 16, row 4 * (lane / 16) + i.
+__device__ __forceinline__ int column_of(int element) { return element / 4 % 16; }
+__device__ __forceinline__ int row_of(int element) { return element / 64 * 4 + element % 4; }
+
+template <bool BF>
+__device__ __forceinline__ uint16_t rounded(float v) {
+    if constexpr (BF) return __builtin_bit_cast(uint16_t, (__bf16)v);
+    else return __builtin_bit_cast(uint16_t, (_Float16)v);
+}
+
+// A wave stores rows x 8 `vecs` columns of `out` (row stride `ld` values) into column
+// `col` of its slots' blocks and counts them as `tiles` tiles from `tile` on: the
+// wave's own stores' acknowledgements are all that its counters have to wait for.
+__device__ __forceinline__ void store_slots(const W4Params& p, const uint16_t* out, int ld, int col,
+                                            int vecs, int tile, int tiles, int waves) {
+    const int lane = threadIdx.x % 64;
+    for (int slot = threadIdx.x / 64; slot < p.world; slot += waves) {
+        char* base = reinterpret_cast<char*>(p.bases[slot]);
+        const symtile::rsrc_t dst = symtile::make_rsrc(
+            base + p.c_off + (size_t)col * 2, (uint32_t)(((size_t)(p.M - 1) * p.ldc + vecs * 8) * 2));
+        for (int i = lane; i < p.M * vecs; i += 64) {
+            const int m = i / vecs, v = i - m * vecs;
+            symtile::buf_st16p<symtile::kStoreWriteThrough>(
+                symtile::ld16(out + m * ld + v * 8), dst, (uint32_t)(m * p.ldc + v * 8) * 2, 0);
+        }
+        symtile::release_written_through();
+        if (lane < tiles)
+            symtile::flag_signal(reinterpret_cast<uint32_t*>(base + p.flag_off) + tile + lane);
+    }
+}
+
+// One block of 128 weights of NT tiles of 16 columns in registers, with what it is
+// multiplied by.  X comes by rows, 256 bytes of four rows a load (XL of
 // them), and takes the matrix operands' layout in LDS: loading operands directly
 // reads 64 bytes of 16 rows, whose distance is often a power of two, from one cache
 // channel (64 tokens through 8192x3584: 36 us).
@@ -226,7 +308,6 @@ struct Block {
             x[i] = symtile::buf_ld16(s.x, block < s.x_end ? s.at_x[i] : symtile::kOOB, k0 * 2);
     }
 
-    // `of_block`: the scales of the block's groups in this lane's column of the first tile.
     __device__ __forceinline__ void multiply(f32x4 (&total)[NT][MT], const Nibbles<BF>& q,
                                              const uint32_t* of_block, StagedX<MT>& staged) const {
         const int c = threadIdx.x % 16, g = threadIdx.x % 64 / 16;
@@ -234,40 +315,7 @@ struct Block {
         for (int i = 0; i < XL; ++i)
             staged.v[4 * i + g][c ^ (4 * i + g) % 16] = kApart ? interleave(x[i]) : x[i];
         __builtin_amdgcn_wave_barrier();   // the wave reads what its lanes wrote
-        symtile::u32x4 words[NT];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) words[i] = GROUP == kBlockK ? w[i] : transpose_quarters(w[i]);
-        f32x4 acc[NT][MT];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            symtile::u32x4 xs[MT];
-            const int v = GROUP == kBlockK ? 4 * g + j : 4 * j + g;
-#pragma unroll
-            for (int t = 0; t < MT; ++t) xs[t] = staged.v[16 * t + c][v ^ c];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const uint32_t of = of_block[(j * 32 / GROUP * NT + n) * kTileN];
-                const uint32_t z = Nibbles<BF>::minus_offset(of >> 16);
-                const symtile::u32x4 zs = {z, z, z, z};
-                symtile::u32x4 ws;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    ws[i] = kApart ? q.apart(words[n][j], i) : q.adjacent(words[n][j], i);
-#pragma unroll
-                for (int t = 0; t < MT; ++t) {
-                    f32x4& a = acc[n][t];
-                    if (j * 32 % GROUP == 0) a = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                    a = mfma<BF>(xs[t], zs, a);
-                    a = mfma<BF>(xs[t], ws, a);
-                    if ((j + 1) * 32 % GROUP == 0) {
-                        const float sc = scale_value<BF>(of & 0xFFFFu);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            total[n][t][e] = __builtin_fmaf(sc, a[e], total[n][t][e]);
-                    }
-                }
-            }
-        }
+        multiply_block<BF, NT, MT, GROUP, kApart>(total, q, w, of_block, NT * kTileN, staged);
         __builtin_amdgcn_wave_barrier();   // the next block's X is written after these reads
     }
 };
@@ -283,7 +331,7 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
     static_assert(sizeof(Partial) <= sizeof(StagedX<MT>), "a wave's sums take its X's place");
     __shared__ StagedX<MT> staged[WAVES];
     __shared__ __attribute__((aligned(16))) uint16_t out[16 * MT][kTileN];
-    __shared__ Scales<GROUP, NT> scales;
+    __shared__ Scales<GROUP, NT, kChunkK> scales;
     const int tile0 = blockIdx.x * NT, t = threadIdx.x, wave = t / 64, lane = t % 64;
     const int w0 = __builtin_amdgcn_readfirstlane(wave);
     f32x4 total[NT][MT] = {};
@@ -339,55 +387,223 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
 #pragma unroll
             for (int w = 0; w < WAVES; ++w)
                 v += reinterpret_cast<const Partial&>(staged[w])[o / 256][o % 256];
-            // element 4 * lane + i of a tile: column lane % 16, row 4 * (lane / 16) + i
-            const int l = o % 256 / 4, m = o / 256 * 16 + l / 16 * 4 + o % 4;
-            uint16_t h;
-            if constexpr (BF) h = __builtin_bit_cast(uint16_t, (__bf16)v);
-            else h = __builtin_bit_cast(uint16_t, (_Float16)v);
-            out[m][l % 16] = h;
+            out[o / 256 * 16 + row_of(o % 256)][column_of(o % 256)] = rounded<BF>(v);
         }
         __syncthreads();
-        // a wave stores the tile into a slot and counts it there: its own stores'
-        // acknowledgements are all that the counter has to wait for
-        for (int slot = wave; slot < p.world; slot += WAVES) {
-            char* base = reinterpret_cast<char*>(p.bases[slot]);
-            const int chunks = p.N - tile * kTileN >= kTileN ? 2 : 1;   // of 8 columns
-            const symtile::rsrc_t dst = symtile::make_rsrc(
-                base + p.c_off + (size_t)tile * kTileN * 2,
-                (uint32_t)(((size_t)(p.M - 1) * p.ldc + chunks * 8) * 2));
-            for (int i = lane; i < p.M * 2; i += 64) {
-                const int m = i / 2, c = i % 2;
-                if (c < chunks)
-                    symtile::buf_st16p<symtile::kStoreWriteThrough>(
-                        symtile::ld16(&out[m][c * 8]), dst, (uint32_t)(m * p.ldc + c * 8) * 2, 0);
-            }
-            symtile::release_written_through();
-            if (lane == 0)
-                symtile::flag_signal(reinterpret_cast<uint32_t*>(base + p.flag_off) + tile);
-        }
+        store_slots(p, &out[0][0], kTileN, tile * kTileN, p.N - tile * kTileN >= kTileN ? 2 : 1,
+                    tile, 1, WAVES);
     }
 }
 
+// ---- many rows or many columns ----------------------------------------------------
+// A workgroup takes 64 columns: four of its eight waves 16 columns each, the other
+// four the same columns' other half of every step of K.  X of a step goes through LDS
+// once for all of them, while the next step's X and weights are on their way.  (Where
+// a workgroup takes 16 columns, every workgroup reads all of X: 1 MB for 64 KB of
+// weights with 64 rows of 8192.)  Where the columns are too few for the GPU, K is
+// split over workgroups; their sums are written through to the workspace, and the
+// one that arrives last adds them in the order of K.
+constexpr int kWideTiles = 4, kWideCols = kWideTiles * kTileN, kWideThreads = 512;
+constexpr int kWideScalesK = 4096;   // weights of a column whose scales are in LDS
+
+// Blocks a step and wave, and k of a step.
+template <int MT>
+struct WideStep {
+    static constexpr int kBlocks = MT == 4 ? 1 : 2, kK = 2 * kBlocks * kBlockK;
+};
+
+template <bool BF, int MT, int GROUP>
+__global__ void __launch_bounds__(kWideThreads, MT == 4 ? 2 : 4) w4_wide_kernel(W4Params p) {
+    constexpr int CB = WideStep<MT>::kBlocks, kStepK = WideStep<MT>::kK;
+    constexpr int XV = 16 * MT * (kStepK / 8) / kWideThreads;   // vectors of X a thread and step
+    typedef float Partial[kWideTiles][MT][256];
+    struct Buffers {
+        StagedX<MT> x[2][2 * CB];
+    };
+    union Lds {
+        Buffers b;
+        struct {
+            Partial sums;
+            uint16_t out[16 * MT][kWideCols];
+        } end;
+    };
+    __shared__ Lds lds;
+    __shared__ Scales<GROUP, kWideTiles, kWideScalesK> scales;
+    __shared__ int last;
+    const int t = threadIdx.x, lane = t % 64, c = lane % 16, g = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(t / 64), tile = wave % kWideTiles;
+    const int half = wave / kWideTiles;
+    const int group = blockIdx.x / p.splits, split = blockIdx.x - group * p.splits;
+    const int n0 = group * kWideCols, cols = min(kWideCols, p.N - n0);
+    const int steps = (p.K + kStepK - 1) / kStepK;
+    const int first = split * p.part_steps, end = min(steps, first + p.part_steps);
+
+    const symtile::rsrc_t xr = symtile::make_rsrc(p.X, (uint32_t)(((p.M - 1) * p.ldx + p.K) * 2));
+    const symtile::rsrc_t wr =
+        symtile::make_rsrc(p.q + (size_t)n0 * (p.K / 2), (uint32_t)(cols * (p.K / 2)));
+    const uint32_t at_w = (uint32_t)(min(tile * kTileN + c, cols - 1) * (p.K / 2) + 16 * g);
+    const int w_end = (p.K - 32 * g + kBlockK - 1) / kBlockK;
+    // vector i of the thread: a row, and a place in the step's k
+    auto x_row = [&](int i) { return (t + i * kWideThreads) / (kStepK / 8); };
+    auto x_vec = [&](int i) { return (t + i * kWideThreads) % (kStepK / 8); };
+    uint32_t at_x[XV];
+#pragma unroll
+    for (int i = 0; i < XV; ++i) at_x[i] = (uint32_t)(min(x_row(i), p.M - 1) * p.ldx + x_vec(i) * 8) * 2;
+    // steps behind the part read nothing; offsets outside of the resources give zeros
+    auto load_x = [&](symtile::u32x4 (&x)[XV], int step) {
+        const int left = step < end ? p.K - step * kStepK : 0;
+#pragma unroll
+        for (int i = 0; i < XV; ++i)
+            x[i] = symtile::buf_ld16(xr, x_vec(i) * 8 < left ? at_x[i] : symtile::kOOB, step * kStepK * 2);
+    };
+    auto load_w = [&](symtile::u32x4 (&w)[CB], int step) {
+#pragma unroll
+        for (int i = 0; i < CB; ++i) {
+            const int block = step < end ? (step * 2 + half) * CB + i : 1 << 20;
+            w[i] = symtile::buf_ld16p<symtile::kLoadStream>(
+                wr, block < w_end ? at_w : symtile::kOOB, block * (kBlockK / 2));
+        }
+    };
+    auto stage = [&](const symtile::u32x4 (&x)[XV], int buffer) {
+#pragma unroll
+        for (int i = 0; i < XV; ++i) {
+            const int row = x_row(i), vec = x_vec(i);
+            lds.b.x[buffer][vec / 16].v[row][vec % 16 ^ row % 16] = interleave(x[i]);
+        }
+    };
+    f32x4 total[1][MT] = {};
+    const Nibbles<BF> nibbles;
+    symtile::u32x4 x[XV], w0[CB], w1[CB];
+    int staged_from = first;   // the step whose scales are the first in LDS
+    auto use = [&](const symtile::u32x4 (&w)[CB], int step, int buffer) {
+#pragma unroll
+        for (int i = 0; i < CB; ++i) {
+            const symtile::u32x4 one[1] = {w[i]};
+            const int block = half * CB + i;
+            const int of = ((step - staged_from) * 2 * CB + block) * (kBlockK / GROUP);
+            multiply_block<BF, 1, MT, GROUP, true>(total, nibbles, one,
+                                                   &scales.of[of][tile * kTileN + c], kWideCols,
+                                                   lds.b.x[buffer][block]);
+        }
+    };
+    // one step: `w` holds its weights and the buffer its X; `x` the next step's
+    auto advance = [&](symtile::u32x4 (&w)[CB], int step, int buffer) {
+        if (step - staged_from == kWideScalesK / kStepK) {
+            staged_from = step;
+            scales.template load<kWideThreads>(p, n0, step * (kStepK / GROUP));
+            __syncthreads();
+        }
+        use(w, step, buffer);
+        load_w(w, step + 2);
+        stage(x, buffer ^ 1);
+        load_x(x, step + 2);
+        __syncthreads();
+    };
+    if (first < end) {
+        load_x(x, first);
+        load_w(w0, first);
+        load_w(w1, first + 1);
+        scales.template load<kWideThreads>(p, n0, first * (kStepK / GROUP));
+        stage(x, 0);
+        load_x(x, first + 1);
+        __syncthreads();
+        for (int step = first; step < end; step += 2) {
+            advance(w0, step, 0);
+            if (step + 1 >= end) break;
+            advance(w1, step + 1, 1);
+        }
+    }
+    // the two halves' sums
+    if (half == 1) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            *reinterpret_cast<f32x4*>(&lds.end.sums[tile][i][4 * lane]) = total[0][i];
+    }
+    __syncthreads();
+    if (half == 0) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            total[0][i] += *reinterpret_cast<const f32x4*>(&lds.end.sums[tile][i][4 * lane]);
+    }
+    if (p.splits > 1) {
+        // [column group][split][tile][row tile][4 * lane + i]
+        constexpr int kPart = kWideTiles * MT * 256;
+        float* mine = p.partials + ((size_t)blockIdx.x * kWideTiles + tile) * MT * 256;
+        const symtile::rsrc_t to = symtile::make_rsrc(mine, MT * 1024);
+        if (half == 0) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                symtile::buf_st16p<symtile::kStoreWriteThrough>(
+                    __builtin_bit_cast(symtile::u32x4, total[0][i]), to, (uint32_t)(i * 1024 + lane * 16), 0);
+        }
+        symtile::wg_stores_done();
+        if (t == 0) {
+            symtile::release_written_through();
+            const uint32_t before = symtile::atomic_add<__ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT>(
+                p.counters + group, 1u);
+            last = before == (uint32_t)p.splits - 1;
+            if (last)
+                __hip_atomic_store(symtile::global_ptr(p.counters + group), 0u, __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (!last) return;
+        symtile::acquire_coherent_reads();
+        if (half == 0) {
+            const symtile::rsrc_t from = symtile::make_rsrc(
+                p.partials + ((size_t)group * p.splits * kWideTiles + tile) * MT * 256,
+                (uint32_t)(((p.splits - 1) * kPart + MT * 256) * 4));
+#pragma unroll
+            for (int i = 0; i < MT; ++i) total[0][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int s = 0; s < p.splits; ++s) {
+                f32x4 part[MT];
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    part[i] = __builtin_bit_cast(
+                        f32x4, symtile::buf_ld16p<symtile::kLoadCoherent>(
+                                   from, (uint32_t)(i * 1024 + lane * 16), s * kPart * 4));
+#pragma unroll
+                for (int i = 0; i < MT; ++i) total[0][i] += part[i];
+            }
+        }
+    }
+    if (half == 0) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                lds.end.out[16 * i + 4 * g + e][tile * kTileN + c] = rounded<BF>(total[0][i][e]);
+    }
+    __syncthreads();
+    store_slots(p, &lds.end.out[0][0], kWideCols, n0, cols / 8, group * kWideTiles,
+                (cols + kTileN - 1) / kTileN, kWideThreads / 64);
+}
+
+// ---- host ------------------------------------------------------------------------------
 struct Build {
     const void* kernel;
     int waves, tiles;   // waves and tiles of a workgroup
+    int step_k;         // of the wide kernel; 0 = the other one
 };
 template <bool BF, int XL, int NT, int GROUP, int U, int WAVES, int PER_SIMD>
 Build build_of() {
     return {reinterpret_cast<const void*>(&w4_kernel<BF, XL, NT, GROUP, U, WAVES, PER_SIMD>), WAVES,
-            NT};
+            NT, 0};
+}
+template <bool BF, int MT, int GROUP>
+Build wide_of() {
+    return {reinterpret_cast<const void*>(&w4_wide_kernel<BF, MT, GROUP>), kWideThreads / 64,
+            kWideTiles, WideStep<MT>::kK};
 }
 
-// The smallest build that holds M rows.
 template <bool BF, int GROUP>
 Build build_for(int M, int tiles) {
     const bool many = tiles >= 1024;
     if (M <= 4)
         return many ? build_of<BF, 1, 1, GROUP, 2, 4, 8>() : build_of<BF, 1, 1, GROUP, 2, 8, 8>();
-    if (M <= 16)
-        return many ? build_of<BF, 4, 2, GROUP, 1, 4, 4>() : build_of<BF, 4, 1, GROUP, 2, 8, 4>();
-    if (M <= 32) return build_of<BF, 8, 1, GROUP, 2, 8, 2>();
-    return build_of<BF, 16, 1, GROUP, 1, 8, 2>();
+    if (M <= 16) return wide_of<BF, 1, GROUP>();
+    if (M <= 32) return wide_of<BF, 2, GROUP>();
+    return wide_of<BF, 4, GROUP>();
 }
 template <bool BF>
 Build build_for(int M, int group, int tiles) {
@@ -396,37 +612,76 @@ Build build_for(int M, int group, int tiles) {
                          : build_for<BF, 32>(M, tiles);
 }
 
+int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+// Parts that K is split into: as many as give every CU one workgroup, of two steps at
+// least.
+int splits_of(int device, const Build& b, int N, int K) {
+    if (!b.step_k) return 1;
+    const int cus = std::max(1, symtile_host::cu_count(device));
+    const int groups = ceil_div(N, kWideCols), steps = ceil_div(K, b.step_k);
+    return std::max(1, std::min(cus / groups, steps / 2));
+}
+
+size_t counter_bytes(int N) { return ((size_t)ceil_div(N, kWideCols) * 4 + 255) / 256 * 256; }
+
+size_t workspace_bytes_of(const Build& b, int splits, int M, int N) {
+    if (splits <= 1) return 0;
+    const size_t rows = M <= 16 ? 16 : M <= 32 ? 32 : 64;
+    return counter_bytes(N) + (size_t)ceil_div(N, kWideCols) * splits * rows * kWideCols * 4;
+}
+
+// What the calls refuse about sizes.
+symtile_status check_sizes(int M, int N, int K, int group) {
+    using symtile_host::fail;
+    if (M < 0 || N < 0 || K < 0) return fail(SYMTILE_EINVAL, "negative size");
+    if (M > SYMTILE_W4_TILE_M)
+        return fail(SYMTILE_EUNSUPPORTED, "M exceeds " + std::to_string(SYMTILE_W4_TILE_M) + " tokens");
+    if (group != 32 && group != 64 && group != 128)
+        return fail(SYMTILE_EINVAL, "group must be 32, 64 or 128");
+    if (K % 32 || N % 8) return fail(SYMTILE_EINVAL, "K must be a multiple of 32, N_local of 8");
+    if ((size_t)K * kWideCols / 2 >= size_t(1) << 31)
+        return fail(SYMTILE_EINVAL, "64 columns of weights exceed 2 GiB");
+    return SYMTILE_OK;
+}
+
 }  // namespace
+
+extern "C" symtile_status symtile_w4_workspace_bytes(int device, int M, int N_local, int K,
+                                                     int group, size_t* bytes) {
+    if (!bytes) return symtile_host::fail(SYMTILE_EINVAL, "bytes is NULL");
+    *bytes = 0;
+    if (symtile_status st = check_sizes(M, N_local, K, group)) return st;
+    if (M == 0 || N_local == 0) return SYMTILE_OK;
+    const Build b = build_for<true>(M, group, ceil_div(N_local, kTileN));
+    *bytes = workspace_bytes_of(b, splits_of(device, b, N_local, K), M, N_local);
+    return SYMTILE_OK;
+}
 
 extern "C" symtile_status symtile_w4_all_scatter(
     symtile_heap* h, const void* X, const uint8_t* q, const void* scales, const uint8_t* zeros,
     void* C_gathered_local, uint32_t* arrived_local, int M, int N_local, int K, int ldx, int group,
-    int dtype, int rank, int world_size, symtile_stream s) {
+    int dtype, int rank, int world_size, void* workspace, size_t workspace_bytes,
+    symtile_stream s) {
     using symtile_host::fail;
     if (!h) return fail(SYMTILE_EINVAL, "heap is NULL");
     if (dtype != SYMTILE_F16 && dtype != SYMTILE_BF16)
         return fail(SYMTILE_EUNSUPPORTED, "dtype must be SYMTILE_F16 or SYMTILE_BF16");
     if (world_size != h->world) return fail(SYMTILE_EINVAL, "world_size differs from the heap's");
     if (rank < 0 || rank >= world_size) return fail(SYMTILE_EINVAL, "rank out of range");
-    if (M < 0 || N_local < 0 || K < 0) return fail(SYMTILE_EINVAL, "negative size");
-    if (M > SYMTILE_W4_TILE_M)
-        return fail(SYMTILE_EUNSUPPORTED,
-                    "M exceeds " + std::to_string(SYMTILE_W4_TILE_M) + " tokens");
-    if (group != 32 && group != 64 && group != 128)
-        return fail(SYMTILE_EINVAL, "group must be 32, 64 or 128");
+    if (symtile_status st = check_sizes(M, N_local, K, group)) return st;
     if (ldx == 0) ldx = K;
-    if (K % 32 || N_local % 8 || ldx % 8 || ldx < K)
-        return fail(SYMTILE_EINVAL, "K must be a multiple of 32, N_local and ldx of 8, ldx >= K");
+    if (ldx % 8 || ldx < K) return fail(SYMTILE_EINVAL, "ldx must be a multiple of 8 and >= K");
+    if ((size_t)M * ldx * 2 >= size_t(1) << 31) return fail(SYMTILE_EINVAL, "X exceeds 2 GiB");
     if (M == 0 || N_local == 0) return SYMTILE_OK;
-    if ((size_t)M * ldx * 2 >= size_t(1) << 31 || (size_t)K * kTileN >= size_t(1) << 31)
-        return fail(SYMTILE_EINVAL, "X, or 16 columns of weights, exceed 2 GiB");
     if (!C_gathered_local || !arrived_local || (K && (!X || !q || !scales)))
         return fail(SYMTILE_EINVAL, "NULL pointer");
     auto misaligned = [](const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; };
     if (misaligned(X, 16) || misaligned(q, 16) || misaligned(C_gathered_local, 16) ||
-        misaligned(arrived_local, 4) || misaligned(scales, 2))
-        return fail(SYMTILE_EINVAL, "X, q and C must be 16-byte aligned, counters 4, scales 2");
-    const int tiles = (N_local + SYMTILE_W4_TILE_N - 1) / SYMTILE_W4_TILE_N;
+        misaligned(arrived_local, 4) || misaligned(scales, 2) || misaligned(workspace, 16))
+        return fail(SYMTILE_EINVAL,
+                    "X, q, C and the workspace must be 16-byte aligned, counters 4, scales 2");
+    const int tiles = ceil_div(N_local, kTileN);
     const size_t ldc = (size_t)world_size * N_local;
     const size_t c_bytes = (size_t)M * ldc * 2;
     const size_t flag_bytes = (size_t)world_size * tiles * 4;
@@ -439,6 +694,12 @@ extern "C" symtile_status symtile_w4_all_scatter(
     const uint64_t f0 = reinterpret_cast<uint64_t>(arrived_local);
     if (c0 < f0 + flag_bytes && f0 < c0 + c_bytes)
         return fail(SYMTILE_EINVAL, "arrived_local overlaps C_gathered_local");
+    const Build build = dtype == SYMTILE_BF16 ? build_for<true>(M, group, tiles)
+                                              : build_for<false>(M, group, tiles);
+    int splits = workspace ? splits_of(h->device, build, N_local, K) : 1;
+    const size_t need = workspace_bytes_of(build, splits, M, N_local);
+    if (workspace && workspace_bytes < need)
+        return fail(SYMTILE_EINVAL, "workspace of " + std::to_string(need) + " bytes needed");
 
     W4Params p{};
     p.X = X;
@@ -452,17 +713,22 @@ extern "C" symtile_status symtile_w4_all_scatter(
     p.N = N_local;
     p.K = K;
     p.ldx = ldx;
-    p.groups = (K + group - 1) / group;
+    p.groups = ceil_div(K, group);
     p.world = world_size;
     p.ldc = (int)ldc;
+    p.part_steps = build.step_k ? ceil_div(ceil_div(K, build.step_k), splits) : 0;
+    if (p.part_steps) splits = ceil_div(ceil_div(K, build.step_k), p.part_steps);   // none empty
+    p.splits = splits;
+    if (splits > 1) {
+        p.counters = static_cast<uint32_t*>(workspace);
+        p.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + counter_bytes(N_local));
+    }
     int prev = -1;
     if (symtile_status st = symtile_host::set_device(h, &prev)) return st;
-    const Build build = dtype == SYMTILE_BF16 ? build_for<true>(M, group, tiles)
-                                              : build_for<false>(M, group, tiles);
     void* args[] = {&p};
-    hipError_t e = hipLaunchKernel(build.kernel, dim3((unsigned)((tiles + build.tiles - 1) / build.tiles)),
-                                   dim3(64 * build.waves), args,
-                                   0, static_cast<hipStream_t>(s));
+    const unsigned wgs = (unsigned)ceil_div(tiles, build.tiles) * (unsigned)splits;
+    hipError_t e = hipLaunchKernel(build.kernel, dim3(wgs), dim3(64 * build.waves), args, 0,
+                                   static_cast<hipStream_t>(s));
     if (e == hipSuccess) e = hipGetLastError();
     if (prev >= 0) (void)hipSetDevice(prev);
     return e == hipSuccess ? SYMTILE_OK : symtile_host::hip_fail(e, "w4_kernel launch");

@@ -138,6 +138,7 @@ class GatheredOutput:
         self.ready_epoch = 0     # value of every ready counter after the last WG_SPEC call
         self.ws = None           # split-K workspace (uint8 device tensor), grown on demand
         self.ws_seen = heap.failed_barriers   # failed barriers already answered by a reset
+        self.ws_w4 = {}          # run_w4's workspace (uint8 device tensor or None) per (K, group)
         # per-call constants, computed once (run() is on the host's launch path):
         # the output's and counters' addresses per rank, the workspace size per
         # slice count, and one config struct filled in by every call
@@ -248,12 +249,23 @@ class GatheredOutput:
         if st:
             B._check(st, "symtile_gemm_all_scatter")
 
+    def _workspace_w4(self, K: int, group: int) -> torch.Tensor | None:
+        """run_w4's workspace for this K (None where it needs none): zeroed, kept
+        and reused by later calls, each of which leaves its counters at zero."""
+        if (K, group) not in self.ws_w4:
+            need = B.symtile_w4_workspace_bytes(self.heap.device, self.M, self.N_local, K, group)
+            self.ws_w4[K, group] = (torch.zeros(need, dtype=torch.uint8, device=self.heap.mem.device)
+                                    if need else None)
+        return self.ws_w4[K, group]
+
     def run_w4(self, X: torch.Tensor, weight, rank: int, stream: int | None = None) -> None:
         """The call of rank ``rank`` for a few tokens X [M, K] and its shard of
         4-bit weights (``W4Weight`` of N_local columns): the product lands in
         the same places and counts the same arrivals as ``run``'s, in tiles of
         W4_TILE_M x W4_TILE_N, which this object must have been made with.
-        Enqueued on the stream, asynchronous; it can be captured in a graph."""
+        Enqueued on the stream, asynchronous; calls on one object must not
+        overlap in time.  It can be captured in a graph; make one eager call first
+        so that its workspace exists."""
         if X.dtype != self.dtype or weight.dtype != self.dtype:
             raise TypeError("X and the weight's scales must have the output dtype")
         if not X.is_cuda or X.dim() != 2 or X.stride(1) != 1:
@@ -267,9 +279,11 @@ class GatheredOutput:
         if ptrs is None:
             ptrs = self._ptrs[rank] = (self.heap.ptr(rank, self.c_off),
                                        self.heap.ptr(rank, self.flag_off))
+        ws = self._workspace_w4(K, weight.group)
         st = B.lib.symtile_w4_all_scatter(
             self.heap.handle, X.data_ptr(), *weight.pointers, ptrs[0], ptrs[1], M, self.N_local, K,
             X.stride(0) if M > 1 and K else 0, weight.group, self._dt, rank, self.heap.world,
+            None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
             current_stream(self.heap.device) if stream is None else stream)
         if st:
             B._check(st, "symtile_w4_all_scatter")

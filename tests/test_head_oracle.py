@@ -131,7 +131,7 @@ def test_workspace_query_refuses():
 def test_w4_without_a_heap_is_refused():
     import paper_2511_12500_amd as pkg
     assert pkg.lib.symtile_w4_all_scatter(None, P, P, P, None, P, P, 1, 16, 32, 0, 32, 2, 0, 1,
-                                          None) == -1
+                                          None, 0, None) == -1
     assert b"NULL" in ctypes.string_at(pkg.lib.symtile_last_error())
 
 
