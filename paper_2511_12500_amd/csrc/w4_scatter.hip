@@ -118,49 +118,59 @@ struct __attribute__((packed, aligned(1))) Unaligned {
     V v;
 };
 
-// Scales, and zero points above them, of NT tiles' columns for the groups of one
-// chunk of K, group by group: a column's are far from the next column's in memory
-// and every block needs one of each, so they are read once, along the columns.
-template <int GROUP, int NT, int CHUNK>
+// Scales, and zero points above them, of NT tiles' columns for the groups of CHUNK
+// weights from group `group0` on, group by group: a column's are far from the next
+// column's in memory and every block needs one of each, so they are read once, along
+// the columns.  fetch() asks for them, without a branch, so that loads may follow
+// that place() does not wait for; place() puts them into LDS.  Behind the last group
+// stand zeros, which meet zeros of X.
+template <int GROUP, int NT, int CHUNK, int THREADS>
 struct Scales {
-    uint32_t of[CHUNK / GROUP][NT * kTileN];
+    static constexpr int kCols = NT * kTileN, kVec = 8, kGroups = CHUNK / GROUP;
+    static constexpr int kVecs = kGroups / kVec;      // 8 groups of a column each
+    static constexpr int kMost = (kVecs * kCols + THREADS - 1) / THREADS;
+    typedef uint32_t Table[kGroups][kCols];
+    u16x8 s[kMost];
+    u8x8 z[kMost];
 
-    // Groups from `group0` on.  Behind the last one stand zeros, which meet zeros of X.
-    template <int THREADS>
-    __device__ __forceinline__ void load(const W4Params& p, int n0, int group0) {
-        constexpr int kCols = NT * kTileN, kVec = 8;
-        constexpr int kVecs = CHUNK / GROUP / kVec;      // 8 groups of a column each
-        constexpr int kMost = (kVecs * kCols + THREADS - 1) / THREADS;
-        const int count = p.groups - group0;
-        const size_t end = (size_t)p.N * p.groups;
-        // all of a thread's loads, then their places
-        u16x8 s[kMost];
-        u8x8 z[kMost];
+    // Vector i of the thread is the 8 groups from `first` on in column `col`; the
+    // last ones of the array come from the 8 before its end (there are 8 columns).
+    __device__ __forceinline__ size_t at(const W4Params& p, int n0, int group0, int i, int* col,
+                                         int* first) const {
+        const int v = threadIdx.x + i * THREADS;
+        *col = v / kVecs;
+        *first = v % kVecs * kVec;
+        const size_t at = (size_t)min(n0 + *col, p.N - 1) * p.groups + group0 + *first;
+        const size_t most = (size_t)p.N * p.groups - kVec;
+        if (at > most) *first -= (int)(at - most);
+        return at > most ? most : at;
+    }
+    __device__ __forceinline__ void fetch(const W4Params& p, int n0, int group0) {
+        // without zero points any bytes of the scales are read in their place
+        const uint8_t* zeros = p.zeros ? p.zeros : static_cast<const uint8_t*>(p.scales);
 #pragma unroll
         for (int i = 0; i < kMost; ++i) {
-            const int v = threadIdx.x + i * THREADS, col = v / kVecs, first = v % kVecs * kVec;
-            z[i] = u8x8{8, 8, 8, 8, 8, 8, 8, 8};
-            if (col >= kCols || first >= count) continue;
-            const size_t at = (size_t)min(n0 + col, p.N - 1) * p.groups + group0 + first;
-            const uint16_t* scales = static_cast<const uint16_t*>(p.scales) + at;
-            if (at + kVec <= end) {     // what follows in the next column is not used
-                s[i] = reinterpret_cast<const Unaligned<u16x8>*>(scales)->v;
-                if (p.zeros) z[i] = reinterpret_cast<const Unaligned<u8x8>*>(p.zeros + at)->v;
-            } else {
-                for (int e = 0; e < kVec; ++e)
-                    if (at + e < end) {
-                        s[i][e] = scales[e];
-                        if (p.zeros) z[i][e] = p.zeros[at + e];
-                    }
-            }
+            int col, first;
+            const size_t from = at(p, n0, group0, i, &col, &first);
+            s[i] = reinterpret_cast<const Unaligned<u16x8>*>(static_cast<const uint16_t*>(p.scales) +
+                                                             from)->v;
+            z[i] = reinterpret_cast<const Unaligned<u8x8>*>(zeros + from)->v;
         }
+    }
+    __device__ __forceinline__ void place(const W4Params& p, int n0, int group0, Table& of) const {
+        const int count = p.groups - group0;
 #pragma unroll
         for (int i = 0; i < kMost; ++i) {
-            const int v = threadIdx.x + i * THREADS, col = v / kVecs, first = v % kVecs * kVec;
+            int col, first;
+            at(p, n0, group0, i, &col, &first);
+            const int begin = (threadIdx.x + i * THREADS) % kVecs * kVec;
             if (col >= kCols) continue;
 #pragma unroll
-            for (int e = 0; e < kVec; ++e)
-                of[first + e][col] = first + e < count ? s[i][e] | (z[i][e] & 15u) << 16 : 0u;
+            for (int e = 0; e < kVec; ++e) {
+                const uint32_t zero = p.zeros ? z[i][e] & 15u : 8u;
+                if (first + e >= begin && first + e < count) of[first + e][col] = s[i][e] | zero << 16;
+                if (begin + e >= count) of[begin + e][col] = 0u;
+            }
         }
     }
 };
@@ -331,7 +341,8 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
     static_assert(sizeof(Partial) <= sizeof(StagedX<MT>), "a wave's sums take its X's place");
     __shared__ StagedX<MT> staged[WAVES];
     __shared__ __attribute__((aligned(16))) uint16_t out[16 * MT][kTileN];
-    __shared__ Scales<GROUP, NT, kChunkK> scales;
+    typedef Scales<GROUP, NT, kChunkK, kThreads> S;
+    __shared__ typename S::Table scales;
     const int tile0 = blockIdx.x * NT, t = threadIdx.x, wave = t / 64, lane = t % 64;
     const int w0 = __builtin_amdgcn_readfirstlane(wave);
     f32x4 total[NT][MT] = {};
@@ -355,13 +366,15 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int i = min(block_of(u0 + u), blocks - 1);
-                s[u].multiply(total, nibbles, &scales.of[i * (kBlockK / GROUP)][lane % 16],
+                s[u].multiply(total, nibbles, &scales[i * (kBlockK / GROUP)][lane % 16],
                               staged[wave]);
             }
         };
+        S s;
+        s.fetch(p, tile0 * kTileN, chunk / GROUP);
         fetch(a, 0);
         if (chunk) __syncthreads();   // the scales before are used up
-        scales.template load<kThreads>(p, tile0 * kTileN, chunk / GROUP);
+        s.place(p, tile0 * kTileN, chunk / GROUP, scales);
         __syncthreads();
         for (int u = 0; block_of(u) < blocks; u += 2 * U) {
             fetch(b, u + U);
@@ -406,15 +419,17 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
 constexpr int kWideTiles = 4, kWideCols = kWideTiles * kTileN, kWideThreads = 512;
 constexpr int kWideScalesK = 4096;   // weights of a column whose scales are in LDS
 
-// Blocks a step and wave, and k of a step.
+// Blocks a step and wave, k of a step, and how many steps ahead X and weights are
+// asked for.
 template <int MT>
 struct WideStep {
     static constexpr int kBlocks = MT == 4 ? 1 : 2, kK = 2 * kBlocks * kBlockK;
+    static constexpr int kAhead = 2;
 };
 
 template <bool BF, int MT, int GROUP>
-__global__ void __launch_bounds__(kWideThreads, MT == 4 ? 2 : 4) w4_wide_kernel(W4Params p) {
-    constexpr int CB = WideStep<MT>::kBlocks, kStepK = WideStep<MT>::kK;
+__global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(W4Params p) {
+    constexpr int CB = WideStep<MT>::kBlocks, kStepK = WideStep<MT>::kK, D = WideStep<MT>::kAhead;
     constexpr int XV = 16 * MT * (kStepK / 8) / kWideThreads;   // vectors of X a thread and step
     typedef float Partial[kWideTiles][MT][256];
     struct Buffers {
@@ -428,7 +443,8 @@ __global__ void __launch_bounds__(kWideThreads, MT == 4 ? 2 : 4) w4_wide_kernel(
         } end;
     };
     __shared__ Lds lds;
-    __shared__ Scales<GROUP, kWideTiles, kWideScalesK> scales;
+    typedef Scales<GROUP, kWideTiles, kWideScalesK, kWideThreads> S;
+    __shared__ typename S::Table scales;
     __shared__ int last;
     const int t = threadIdx.x, lane = t % 64, c = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(t / 64), tile = wave % kWideTiles;
@@ -473,44 +489,54 @@ __global__ void __launch_bounds__(kWideThreads, MT == 4 ? 2 : 4) w4_wide_kernel(
     };
     f32x4 total[1][MT] = {};
     const Nibbles<BF> nibbles;
-    symtile::u32x4 x[XV], w0[CB], w1[CB];
-    int staged_from = first;   // the step whose scales are the first in LDS
-    auto use = [&](const symtile::u32x4 (&w)[CB], int step, int buffer) {
+    symtile::u32x4 x[D][XV], w[D][CB];   // rings: of step s in place (s - first) % D
+    auto use = [&](const symtile::u32x4 (&w)[CB], int step, int buffer) {   // step in the table
 #pragma unroll
         for (int i = 0; i < CB; ++i) {
             const symtile::u32x4 one[1] = {w[i]};
             const int block = half * CB + i;
-            const int of = ((step - staged_from) * 2 * CB + block) * (kBlockK / GROUP);
+            const int of = (step * 2 * CB + block) * (kBlockK / GROUP);
             multiply_block<BF, 1, MT, GROUP, true>(total, nibbles, one,
-                                                   &scales.of[of][tile * kTileN + c], kWideCols,
+                                                   &scales[of][tile * kTileN + c], kWideCols,
                                                    lds.b.x[buffer][block]);
         }
     };
-    // one step: `w` holds its weights and the buffer its X; `x` the next step's
-    auto advance = [&](symtile::u32x4 (&w)[CB], int step, int buffer) {
-        if (step - staged_from == kWideScalesK / kStepK) {
-            staged_from = step;
-            scales.template load<kWideThreads>(p, n0, step * (kStepK / GROUP));
-            __syncthreads();
-        }
-        use(w, step, buffer);
-        load_w(w, step + 2);
-        stage(x, buffer ^ 1);
-        load_x(x, step + 2);
-        __syncthreads();
-    };
     if (first < end) {
-        load_x(x, first);
-        load_w(w0, first);
-        load_w(w1, first + 1);
-        scales.template load<kWideThreads>(p, n0, first * (kStepK / GROUP));
-        stage(x, 0);
-        load_x(x, first + 1);
+        S s;
+        s.fetch(p, n0, first * (kStepK / GROUP));
+#pragma unroll
+        for (int i = 0; i < D; ++i) {
+            load_x(x[i], first + i);
+            load_w(w[i], first + i);
+        }
+        s.place(p, n0, first * (kStepK / GROUP), scales);
+        stage(x[0], 0);
+        load_x(x[0], first + D);
         __syncthreads();
-        for (int step = first; step < end; step += 2) {
-            advance(w0, step, 0);
-            if (step + 1 >= end) break;
-            advance(w1, step + 1, 1);
+        // the steps whose scales are in LDS; inside, nothing may make the compiler wait for
+        // all loads (a branch with loads of its own in the loop did: 19.9 us for 64 tokens
+        // through 8192x3584)
+        constexpr int kTableSteps = kWideScalesK / kStepK;
+        static_assert(kTableSteps % D == 0, "the rings keep their places");
+        for (int base = first; base < end; base += kTableSteps) {
+            if (base != first) {
+                s.fetch(p, n0, base * (kStepK / GROUP));
+                s.place(p, n0, base * (kStepK / GROUP), scales);
+                __syncthreads();
+            }
+            const int stop = min(end, base + kTableSteps);
+            for (int from = base; from < stop; from += D) {
+#pragma unroll
+                for (int i = 0; i < D; ++i) {
+                    const int step = from + i, buffer = (step - first) & 1;
+                    if (step >= stop) break;
+                    use(w[i], step - base, buffer);
+                    load_w(w[i], step + D);
+                    stage(x[(i + 1) % D], buffer ^ 1);
+                    load_x(x[(i + 1) % D], step + 1 + D);
+                    __syncthreads();
+                }
+            }
         }
     }
     // the two halves' sums
