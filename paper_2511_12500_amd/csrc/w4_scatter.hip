@@ -4,6 +4,7 @@
 //
 // C[m, n] = sum_k X[m, k] (q[n, k] - zero[n, k / group]) scale[n, k / group].
 #include <hip/hip_runtime.h>
+#include <stddef.h>
 #include <stdint.h>
 
 #include <algorithm>
@@ -37,39 +38,46 @@ struct W4Params {
     float* partials;
 };
 
-// Weights as floating point without a conversion: 4 bits placed at the top of
-// the fraction of 16.0 make 16 + q, exactly.  The offset goes out with the zero
-// point: sum x (q - z) = sum x (16 + q) + sum x (-(16 + z)), the second sum by a
-// matrix instruction too, whose right operand is one number a column and group.
+// Weights as floating point without a conversion: 4 bits in the fraction of a power
+// of two are 16 + q (bfloat16) or 64 + q (float16), exactly.  The offset goes out with
+// the zero point: sum x (q - z) = sum x (16 + q) + sum x (-(16 + z)), the second sum by
+// a matrix instruction too, whose right operand is one number a column and group.
 template <bool BF>
 struct Nibbles {
-    static constexpr uint32_t kSixteen = BF ? 0x41804180u : 0x4C004C00u;
-    static constexpr int kAt = BF ? 3 : 6;   // where the fraction's top 4 bits start
-    uint32_t mask, sixteen;
+    static constexpr uint32_t kBase = BF ? 0x4180u : 0x5400u;
+    static constexpr int kAt = BF ? 3 : 4;   // where the 4 bits start
+    uint32_t mask, base;
 
     // The constants in registers (one scalar, one vector): as literals they would
     // keep the and-or from being one instruction.
-    __device__ __forceinline__ Nibbles() : mask(BF ? 0x00780078u : 0x03C003C0u), sixteen(kSixteen) {
+    __device__ __forceinline__ Nibbles()
+        : mask((0xFu << kAt) * 0x10001u), base(kBase * 0x10001u) {
         asm("" : "+s"(mask));
-        asm("" : "+v"(sixteen));
+        asm("" : "+v"(base));
     }
-    // Weights j and j + 4 of w: two instructions, for X in that order.
-    __device__ __forceinline__ uint32_t apart(uint32_t w, int j) const {
-        const int shift = kAt - 4 * j;
-        return ((shift >= 0 ? w << shift : w >> -shift) & mask) | sixteen;
+    static __device__ __forceinline__ uint32_t shifted(uint32_t w, int left) {
+        return left >= 0 ? w << left : w >> -left;
     }
-    // Weights 2 j and 2 j + 1 of w, the byte j: at the top of both halves, its low 4
-    // bits moved into place in the lower one and its high 4 bits in the upper one;
-    // three instructions.
-    __device__ __forceinline__ uint32_t adjacent(uint32_t w, int j) const {
-        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-        const uint32_t both = __builtin_amdgcn_perm(w, w, 0x000C000Cu | j << 8 | j << 24);
-        const u16x2 moved = __builtin_bit_cast(u16x2, both) >> u16x2{8 - kAt, 12 - kAt};
-        return (__builtin_bit_cast(uint32_t, moved) & mask) | sixteen;
+    // The 8 weights of a word in pairs, weights j and j + 4 in dword j, for X in that
+    // order: two instructions a pair.
+    __device__ __forceinline__ symtile::u32x4 apart(uint32_t w) const {
+        symtile::u32x4 r;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = (shifted(w, kAt - 4 * j) & mask) | base;
+        return r;
+    }
+    // Weights 2 j and 2 j + 1 in dword j: the even and the odd ones of the word are
+    // moved into place within their bytes, then a byte of each and an and-or a pair.
+    __device__ __forceinline__ symtile::u32x4 adjacent(uint32_t w) const {
+        const uint32_t even = w << kAt, odd = shifted(w, kAt - 4);
+        symtile::u32x4 r;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            r[j] = (__builtin_amdgcn_perm(odd, even, 0x0C040C00u + 0x00010001u * j) & mask) | base;
+        return r;
     }
     static __device__ __forceinline__ uint32_t minus_offset(uint32_t zero) {
-        const uint32_t h = (kSixteen & 0xFFFFu) | 0x8000u | zero << kAt;
-        return h | h << 16;
+        return (kBase | 0x8000u | zero << kAt) * 0x10001u;
     }
 };
 
@@ -242,10 +250,7 @@ __device__ __forceinline__ void multiply_block(f32x4 (&total)[NT][MT], const Nib
             const uint32_t of = of_block[j * 32 / GROUP * stride + n * kTileN];
             const uint32_t z = Nibbles<BF>::minus_offset(of >> 16);
             const symtile::u32x4 zs = {z, z, z, z};
-            symtile::u32x4 ws;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                ws[i] = APART ? q.apart(words[n][j], i) : q.adjacent(words[n][j], i);
+            const symtile::u32x4 ws = APART ? q.apart(words[n][j]) : q.adjacent(words[n][j]);
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
                 f32x4& a = acc[n][t];
@@ -408,44 +413,50 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
     }
 }
 
-// ---- many rows or many columns ----------------------------------------------------
+// ---- over 4 rows -------------------------------------------------------------------
 // A workgroup takes 64 columns: four of its eight waves 16 columns each, the other
-// four the same columns' other half of every step of K.  X of a step goes through LDS
-// once for all of them, while the next step's X and weights are on their way.  (Where
-// a workgroup takes 16 columns, every workgroup reads all of X: 1 MB for 64 KB of
-// weights with 64 rows of 8192.)  Where the columns are too few for the GPU, K is
-// split over workgroups; their sums are written through to the workspace, and the
-// one that arrives last adds them in the order of K.
+// four the same columns' other half of every step of K.  X of a step goes to LDS once
+// for all of them.  (Where a workgroup takes 16 columns, every workgroup reads all of
+// X: 1 MB for 64 KB of weights with 64 rows of 8192.)  X and weights go straight into
+// a ring of stages in LDS, waited for by count, so that later steps' loads stay in
+// flight across the barriers; held in registers, the compiler waits for them where
+// it moves registers (64 tokens through 8192x3584: 19.0 us).  Where the columns are
+// too few for the GPU, K is split over workgroups; their sums are written through to
+// the workspace, and the one that arrives last adds them in the order of K.
 constexpr int kWideTiles = 4, kWideCols = kWideTiles * kTileN, kWideThreads = 512;
-constexpr int kWideScalesK = 4096;   // weights of a column whose scales are in LDS
+constexpr int kWideGroups = 64;      // groups of a column whose scales are in LDS
 
-// Blocks a step and wave, k of a step, and how many steps ahead X and weights are
-// asked for.
+// Blocks a step and wave, k of a step, and stages of the ring.
 template <int MT>
 struct WideStep {
-    static constexpr int kBlocks = MT == 4 ? 1 : 2, kK = 2 * kBlocks * kBlockK;
-    static constexpr int kAhead = 2;
+    static constexpr int kBlocks = MT == 2 ? 2 : 1, kK = 2 * kBlocks * kBlockK;
+    static constexpr int kStages = MT == 1 ? 3 : 2;
 };
+
+// s_waitcnt immediate: at most n vector-memory operations outstanding, no LDS ones
+// (gfx9 encoding: vmcnt 3:0 and 15:14, expcnt 6:4, lgkmcnt 11:8).
+constexpr int wait_loads(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4); }
 
 template <bool BF, int MT, int GROUP>
 __global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(W4Params p) {
-    constexpr int CB = WideStep<MT>::kBlocks, kStepK = WideStep<MT>::kK, D = WideStep<MT>::kAhead;
-    constexpr int XV = 16 * MT * (kStepK / 8) / kWideThreads;   // vectors of X a thread and step
+    constexpr int CB = WideStep<MT>::kBlocks, kStepK = WideStep<MT>::kK;
+    constexpr int kStages = WideStep<MT>::kStages;
+    constexpr int XL = CB * MT, kLoads = XL + CB;    // loads of 1 KB a wave and step
     typedef float Partial[kWideTiles][MT][256];
-    struct Buffers {
-        StagedX<MT> x[2][2 * CB];
+    typedef Scales<GROUP, kWideTiles, kWideGroups * GROUP, kWideThreads> S;
+    struct Stage {
+        StagedX<MT> x[2 * CB];
+        symtile::u32x4 w[kWideThreads / 64][CB][64];
     };
     union Lds {
-        Buffers b;
+        Stage ring[kStages];
         struct {
             Partial sums;
             uint16_t out[16 * MT][kWideCols];
         } end;
     };
-    __shared__ Lds lds;
-    typedef Scales<GROUP, kWideTiles, kWideScalesK, kWideThreads> S;
+    __shared__ __attribute__((aligned(16))) Lds lds;
     __shared__ typename S::Table scales;
-    __shared__ int last;
     const int t = threadIdx.x, lane = t % 64, c = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(t / 64), tile = wave % kWideTiles;
     const int half = wave / kWideTiles;
@@ -453,91 +464,86 @@ __global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(
     const int n0 = group * kWideCols, cols = min(kWideCols, p.N - n0);
     const int steps = (p.K + kStepK - 1) / kStepK;
     const int first = split * p.part_steps, end = min(steps, first + p.part_steps);
+    const int end_k = min(p.K, end * kStepK);
 
-    const symtile::rsrc_t xr = symtile::make_rsrc(p.X, (uint32_t)(((p.M - 1) * p.ldx + p.K) * 2));
-    const symtile::rsrc_t wr =
-        symtile::make_rsrc(p.q + (size_t)n0 * (p.K / 2), (uint32_t)(cols * (p.K / 2)));
-    const uint32_t at_w = (uint32_t)(min(tile * kTileN + c, cols - 1) * (p.K / 2) + 16 * g);
-    const int w_end = (p.K - 32 * g + kBlockK - 1) / kBlockK;
-    // vector i of the thread: a row, and a place in the step's k
-    auto x_row = [&](int i) { return (t + i * kWideThreads) / (kStepK / 8); };
-    auto x_vec = [&](int i) { return (t + i * kWideThreads) % (kStepK / 8); };
-    uint32_t at_x[XV];
+    const symtile::i32x4_t xr =
+        symtile::make_rsrc_words(p.X, (uint32_t)(((p.M - 1) * p.ldx + p.K) * 2));
+    const symtile::i32x4_t wr =
+        symtile::make_rsrc_words(p.q + (size_t)n0 * (p.K / 2), (uint32_t)(cols * (p.K / 2)));
+    // The lane's vector of weights in block i of the wave's half of a step, and of X in
+    // the wave's loads: load u fills four rows of one block of LDS, whose place c
+    // holds the row's vector c ^ (row % 16).
+    const uint32_t at_w = (uint32_t)(min(tile * kTileN + c, cols - 1) * (p.K / 2) + 16 * g) +
+                          half * CB * (kBlockK / 2);
+    const int k_w = half * CB * kBlockK + 32 * g;
+    uint32_t at_x[XL], to_x[XL];
+    int k_x[XL];
 #pragma unroll
-    for (int i = 0; i < XV; ++i) at_x[i] = (uint32_t)(min(x_row(i), p.M - 1) * p.ldx + x_vec(i) * 8) * 2;
-    // steps behind the part read nothing; offsets outside of the resources give zeros
-    auto load_x = [&](symtile::u32x4 (&x)[XV], int step) {
-        const int left = step < end ? p.K - step * kStepK : 0;
+    for (int u = 0; u < XL; ++u) {
+        const int load = wave + u * (kWideThreads / 64), block = load / (4 * MT);
+        const int row = load % (4 * MT) * 4 + g;
+        k_x[u] = block * kBlockK + 8 * (c ^ row % 16);
+        at_x[u] = (uint32_t)(min(row, p.M - 1) * p.ldx + k_x[u]) * 2;
+        to_x[u] = (uint32_t)(load * 1024);
+    }
+    const uint32_t lds0 = symtile::lds_addr(&lds);
+    const uint32_t to_w = (uint32_t)(offsetof(Stage, w) + wave * CB * 1024);
+    // what is behind the part's end is read from outside of the resources: zeros
+    auto load = [&](int step, int stage) {
+        const int k0 = step * kStepK;
+        const uint32_t to = lds0 + stage * (uint32_t)sizeof(Stage);
 #pragma unroll
-        for (int i = 0; i < XV; ++i)
-            x[i] = symtile::buf_ld16(xr, x_vec(i) * 8 < left ? at_x[i] : symtile::kOOB, step * kStepK * 2);
-    };
-    auto load_w = [&](symtile::u32x4 (&w)[CB], int step) {
+        for (int i = 0; i < CB; ++i)
+            symtile::buf_ld16_lds_async(
+                wr, to + to_w + i * 1024,
+                (at_w + i * (kBlockK / 2)) | ((uint32_t)(end_k - 1 - k0 - k_w - i * kBlockK) & symtile::kOOB),
+                k0 / 2);
 #pragma unroll
-        for (int i = 0; i < CB; ++i) {
-            const int block = step < end ? (step * 2 + half) * CB + i : 1 << 20;
-            w[i] = symtile::buf_ld16p<symtile::kLoadStream>(
-                wr, block < w_end ? at_w : symtile::kOOB, block * (kBlockK / 2));
-        }
-    };
-    auto stage = [&](const symtile::u32x4 (&x)[XV], int buffer) {
-#pragma unroll
-        for (int i = 0; i < XV; ++i) {
-            const int row = x_row(i), vec = x_vec(i);
-            lds.b.x[buffer][vec / 16].v[row][vec % 16 ^ row % 16] = interleave(x[i]);
-        }
+        for (int u = 0; u < XL; ++u)
+            symtile::buf_ld16_lds_async(
+                xr, to + to_x[u], at_x[u] | ((uint32_t)(end_k - 1 - k0 - k_x[u]) & symtile::kOOB), k0 * 2);
     };
     f32x4 total[1][MT] = {};
     const Nibbles<BF> nibbles;
-    symtile::u32x4 x[D][XV], w[D][CB];   // rings: of step s in place (s - first) % D
-    auto use = [&](const symtile::u32x4 (&w)[CB], int step, int buffer) {   // step in the table
-#pragma unroll
-        for (int i = 0; i < CB; ++i) {
-            const symtile::u32x4 one[1] = {w[i]};
-            const int block = half * CB + i;
-            const int of = (step * 2 * CB + block) * (kBlockK / GROUP);
-            multiply_block<BF, 1, MT, GROUP, true>(total, nibbles, one,
-                                                   &scales[of][tile * kTileN + c], kWideCols,
-                                                   lds.b.x[buffer][block]);
-        }
-    };
     if (first < end) {
         S s;
         s.fetch(p, n0, first * (kStepK / GROUP));
 #pragma unroll
-        for (int i = 0; i < D; ++i) {
-            load_x(x[i], first + i);
-            load_w(w[i], first + i);
-        }
+        for (int i = 0; i < kStages - 1; ++i) load(first + i, i);
         s.place(p, n0, first * (kStepK / GROUP), scales);
-        stage(x[0], 0);
-        load_x(x[0], first + D);
-        __syncthreads();
-        // the steps whose scales are in LDS; inside, nothing may make the compiler wait for
-        // all loads (a branch with loads of its own in the loop did: 19.9 us for 64 tokens
-        // through 8192x3584)
-        constexpr int kTableSteps = kWideScalesK / kStepK;
-        static_assert(kTableSteps % D == 0, "the rings keep their places");
+        int stage = 0, next = kStages - 1;
+        constexpr int kTableSteps = kWideGroups * GROUP / kStepK;   // whose scales are in LDS
         for (int base = first; base < end; base += kTableSteps) {
             if (base != first) {
                 s.fetch(p, n0, base * (kStepK / GROUP));
+                __syncthreads();   // the scales before are used up
                 s.place(p, n0, base * (kStepK / GROUP), scales);
-                __syncthreads();
             }
             const int stop = min(end, base + kTableSteps);
-            for (int from = base; from < stop; from += D) {
+            for (int step = base; step < stop; ++step) {
+                // this step's loads are there, for all waves; the step's before is used up
+                __builtin_amdgcn_s_waitcnt(wait_loads((kStages - 2) * kLoads));
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                load(step + kStages - 1, next);
+                const Stage& now = lds.ring[stage];
 #pragma unroll
-                for (int i = 0; i < D; ++i) {
-                    const int step = from + i, buffer = (step - first) & 1;
-                    if (step >= stop) break;
-                    use(w[i], step - base, buffer);
-                    load_w(w[i], step + D);
-                    stage(x[(i + 1) % D], buffer ^ 1);
-                    load_x(x[(i + 1) % D], step + 1 + D);
-                    __syncthreads();
+                for (int i = 0; i < CB; ++i) {
+                    const symtile::u32x4 w[1] = {now.w[wave][i][lane]};
+                    const int block = half * CB + i;
+                    const int of = ((step - base) * 2 * CB + block) * (kBlockK / GROUP);
+                    multiply_block<BF, 1, MT, GROUP, false>(total, nibbles, w,
+                                                            &scales[of][tile * kTileN + c],
+                                                            kWideCols, now.x[block]);
                 }
+                stage = stage + 1 == kStages ? 0 : stage + 1;
+                next = next + 1 == kStages ? 0 : next + 1;
             }
         }
+        // the ring's place is the sums' from here on
+        __builtin_amdgcn_s_waitcnt(wait_loads(0));
+        __syncthreads();
     }
     // the two halves' sums
     if (half == 1) {
@@ -567,13 +573,14 @@ __global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(
             symtile::release_written_through();
             const uint32_t before = symtile::atomic_add<__ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT>(
                 p.counters + group, 1u);
-            last = before == (uint32_t)p.splits - 1;
+            const bool last = before == (uint32_t)p.splits - 1;
+            scales[0][0] = last;   // (the scales are used up)
             if (last)
                 __hip_atomic_store(symtile::global_ptr(p.counters + group), 0u, __ATOMIC_RELAXED,
                                    __HIP_MEMORY_SCOPE_AGENT);
         }
         __syncthreads();
-        if (!last) return;
+        if (!scales[0][0]) return;
         symtile::acquire_coherent_reads();
         if (half == 0) {
             const symtile::rsrc_t from = symtile::make_rsrc(
@@ -622,29 +629,35 @@ Build wide_of() {
             kWideTiles, WideStep<MT>::kK};
 }
 
+// Up to 4 rows: one tile a workgroup, of 8 waves while every tile has a CU of its own
+// (8192x3584, 224 tiles: 8.7 us against 9.5 with 4), else of 4, so that more
+// workgroups overlap their beginnings and ends (8192x6144, 384 tiles: 11.2 against
+// 13.0 us with 8; 8192x28672: 33 against 40).  Up to 16 rows the 8 waves while every
+// tile has a CU (8192x3584: 11.2 us against the wide kernel's 11.8; 8192x5120, 320
+// tiles: 18.8 against 12.6).
 template <bool BF, int GROUP>
-Build build_for(int M, int tiles) {
-    const bool many = tiles >= 1024;
+Build build_for(int M, int tiles, int cus) {
     if (M <= 4)
-        return many ? build_of<BF, 1, 1, GROUP, 2, 4, 8>() : build_of<BF, 1, 1, GROUP, 2, 8, 8>();
+        return tiles > cus ? build_of<BF, 1, 1, GROUP, 2, 4, 8>()
+                                : build_of<BF, 1, 1, GROUP, 2, 8, 8>();
+    if (M <= 16 && tiles <= cus) return build_of<BF, 4, 1, GROUP, 2, 8, 4>();
     if (M <= 16) return wide_of<BF, 1, GROUP>();
     if (M <= 32) return wide_of<BF, 2, GROUP>();
     return wide_of<BF, 4, GROUP>();
 }
 template <bool BF>
-Build build_for(int M, int group, int tiles) {
-    return group == 128  ? build_for<BF, 128>(M, tiles)
-           : group == 64 ? build_for<BF, 64>(M, tiles)
-                         : build_for<BF, 32>(M, tiles);
+Build build_for(int M, int group, int tiles, int cus) {
+    return group == 128  ? build_for<BF, 128>(M, tiles, cus)
+           : group == 64 ? build_for<BF, 64>(M, tiles, cus)
+                         : build_for<BF, 32>(M, tiles, cus);
 }
 
 int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // Parts that K is split into: as many as give every CU one workgroup, of two steps at
 // least.
-int splits_of(int device, const Build& b, int N, int K) {
+int splits_of(int cus, const Build& b, int N, int K) {
     if (!b.step_k) return 1;
-    const int cus = std::max(1, symtile_host::cu_count(device));
     const int groups = ceil_div(N, kWideCols), steps = ceil_div(K, b.step_k);
     return std::max(1, std::min(cus / groups, steps / 2));
 }
@@ -679,8 +692,9 @@ extern "C" symtile_status symtile_w4_workspace_bytes(int device, int M, int N_lo
     *bytes = 0;
     if (symtile_status st = check_sizes(M, N_local, K, group)) return st;
     if (M == 0 || N_local == 0) return SYMTILE_OK;
-    const Build b = build_for<true>(M, group, ceil_div(N_local, kTileN));
-    *bytes = workspace_bytes_of(b, splits_of(device, b, N_local, K), M, N_local);
+    const int cus = std::max(1, symtile_host::cu_count(device));
+    const Build b = build_for<true>(M, group, ceil_div(N_local, kTileN), cus);
+    *bytes = workspace_bytes_of(b, splits_of(cus, b, N_local, K), M, N_local);
     return SYMTILE_OK;
 }
 
@@ -720,9 +734,10 @@ extern "C" symtile_status symtile_w4_all_scatter(
     const uint64_t f0 = reinterpret_cast<uint64_t>(arrived_local);
     if (c0 < f0 + flag_bytes && f0 < c0 + c_bytes)
         return fail(SYMTILE_EINVAL, "arrived_local overlaps C_gathered_local");
-    const Build build = dtype == SYMTILE_BF16 ? build_for<true>(M, group, tiles)
-                                              : build_for<false>(M, group, tiles);
-    int splits = workspace ? splits_of(h->device, build, N_local, K) : 1;
+    const int cus = std::max(1, symtile_host::cu_count(h->device));
+    const Build build = dtype == SYMTILE_BF16 ? build_for<true>(M, group, tiles, cus)
+                                              : build_for<false>(M, group, tiles, cus);
+    int splits = workspace ? splits_of(cus, build, N_local, K) : 1;
     const size_t need = workspace_bytes_of(build, splits, M, N_local);
     if (workspace && workspace_bytes < need)
         return fail(SYMTILE_EINVAL, "workspace of " + std::to_string(need) + " bytes needed");
