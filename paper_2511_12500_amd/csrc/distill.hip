@@ -266,7 +266,8 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
         }
         __syncthreads();
     } else {
-        m_rest = wave_max(d.thread_max());
+        float vec_max[NV];
+        m_rest = wave_max(d.thread_max(vec_max));
         if (t % 64 == 0) l.m[t / 64] = m_rest;
         __syncthreads();
         m_rest = over_waves(l.m, waves, Max());

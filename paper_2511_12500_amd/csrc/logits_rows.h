@@ -236,13 +236,17 @@ struct Segment {
             for (int e = 0; e < kVec; ++e) f(i, e, element<DT>(v[i], e));
     }
 
-    __device__ __forceinline__ float thread_max() const {
+    // The largest element of each vector, and of all.
+    __device__ __forceinline__ float thread_max(float (&vec)[NV]) const {
         float m = -kInf;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+            vec[i] = -kInf;
 #pragma unroll
             for (int e = 0; e < kVec; e += 2)
-                m = max3(m, element<DT>(v[i], e), element<DT>(v[i], e + 1));
+                vec[i] = max3(vec[i], element<DT>(v[i], e), element<DT>(v[i], e + 1));
+            m = max3(m, vec[i], vec[i]);
+        }
         return m;
     }
 };

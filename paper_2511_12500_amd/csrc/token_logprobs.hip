@@ -16,6 +16,7 @@ namespace {
 using namespace logits;
 
 constexpr int kCap = 1024;          // candidates for the top entries of a segment
+constexpr int kCapVecs = 256;       // vectors that hold the candidates in the usual case
 
 enum Phase { kValues, kStep, kGrad };   // the values, both (whole rows), the gradient
 
@@ -40,8 +41,23 @@ struct Shared {
     float m[kMaxWaves], s[kMaxWaves], t[kMaxWaves], tau[kMaxWaves];
     uint32_t count[2][kMaxWaves];
     float x_target;
-    int n, last;
+    int n, vecs, last;
     uint64_t bound;
+};
+
+// Dynamic LDS of the top entries: keys, and the vectors that hold the candidates.
+struct TopLds {
+    uint64_t* keys;
+    symtile::u32x4* vec;
+    int* at;               // first element of each
+    static size_t bytes(int segs, int top) {
+        return (size_t)std::max(kCap, segs * top) * 8 + kCapVecs * 20;
+    }
+    __device__ __forceinline__ TopLds(void* base, int segs, int top) {
+        vec = static_cast<symtile::u32x4*>(base);
+        at = reinterpret_cast<int*>(vec + kCapVecs);
+        keys = reinterpret_cast<uint64_t*>(at + kCapVecs);
+    }
 };
 
 // ---- the order of the top entries ------------------------------------------------
@@ -76,34 +92,35 @@ __device__ __forceinline__ uint32_t block_count(uint32_t c, Shared& sh, int& ste
 }
 
 // n distinct keys in LDS; calls emit(place, key) for the `keep` largest.  The
-// place is the number of larger keys, counted by as many threads a key as there
-// are.
+// place is the number of larger keys, counted by up to 16 neighbouring threads a key.
 template <class F>
-__device__ __forceinline__ void rank_keys(const uint64_t* keys, uint32_t* rank, int n, int keep,
-                                          F emit) {
-    const int threads = blockDim.x;
-    for (int i = threadIdx.x; i < n; i += threads) rank[i] = 0;
-    __syncthreads();
-    int parts = 1;
-    while (2 * parts * n <= threads) parts *= 2;
-    const int per = (n + parts - 1) / parts;
-    for (int at = threadIdx.x; at < n * parts; at += threads) {
-        const int i = at % n, first = at / n * per;
-        const uint64_t mine = keys[i];
+__device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int keep, F emit) {
+    const int threads = blockDim.x, t = threadIdx.x;
+    int lg = 0;
+    while (lg < 4 && n << (lg + 1) <= threads) ++lg;
+    const int part = t & ((1 << lg) - 1);
+    for (int i = t >> lg; i - (t >> lg) < n; i += threads >> lg) {
+        const uint64_t mine = i < n ? keys[i] : ~0ull;
         uint32_t c = 0;
-        for (int j = first; j < min(first + per, n); ++j) c += keys[j] > mine;
-        if (c) atomicAdd(&rank[i], c);
+        for (int j = part; j < n; j += 1 << lg) c += keys[j] > mine;
+        for (int o = 1; o < 1 << lg; o *= 2) c += __shfl_xor(c, o);
+        if (part == 0 && i < n && (int)c < keep) emit((int)c, mine);
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += threads)
-        if ((int)rank[i] < keep) emit((int)rank[i], keys[i]);
 }
 
 // A bound for the wave's share of the top entries: the j-th largest of its
-// lanes' largest logits, to 16 bits of their order (rounded down); -inf where
-// there is none.
+// lanes' largest logits (or a lower one); -inf where there is none.
 __device__ __forceinline__ float wave_bound(float lane_max, int j) {
     if (j > 64) return -kInf;
+    if (j <= 6) {       // take away the largest j - 1 times (equal ones together)
+        float m = wave_max(lane_max);
+        for (int i = 1; i < j; ++i) {
+            lane_max = lane_max == m ? -kInf : lane_max;
+            m = wave_max(lane_max);
+        }
+        return m;
+    }
+    // bit by bit, to 16 bits of their order (rounded down)
     const uint32_t o = order(lane_max);
     uint32_t p = 0;
 #pragma unroll
@@ -115,57 +132,75 @@ __device__ __forceinline__ float wave_bound(float lane_max, int j) {
     return p < 0x00800000u ? -kInf : ordered_value(p);
 }
 
-// The `keep` largest of the `len` elements at `seg` (keep <= len), whose vectors
-// are in d, as keys with ids from `id0` on, to emit(place, key).
+// The second lowest of the waves' bounds: the lowest may be of a wave without
+// elements, and all others hold `top` elements that reach theirs together.
+__device__ __forceinline__ float row_bound(const float* tau, int waves) {
+    float lowest = kInf, bound = kInf;
+    for (int w = 0; w < waves; ++w) {
+        const float b = tau[w];
+        bound = fminf(bound, fmaxf(lowest, b));
+        lowest = fminf(lowest, b);
+    }
+    return bound;
+}
+
+// The thread's vectors that hold an element which reaches the bound, into LDS
+// (sh.vecs is zero before and counts them).
+template <int DT, int NV>
+__device__ __forceinline__ void stage_candidates(const Segment<DT, NV>& d, const float* vec_max,
+                                                 float tau, Shared& sh, const TopLds& top) {
+    uint32_t hits = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) hits |= vec_max[i] >= tau ? 1u << i : 0u;
+    if (!hits) return;
+    int place = atomicAdd(&sh.vecs, __popc(hits));
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (hits >> i & 1) {
+            if (place < kCapVecs) {
+                top.vec[place] = d.v[i];
+                top.at[place] = (i * (int)blockDim.x + (int)threadIdx.x) * Elem<DT>::kVec;
+            }
+            ++place;
+        }
+}
+
+// The `keep` largest of the `len` elements at `seg` (keep <= len), as keys with ids
+// from `id0` on, to emit(place, key).  All threads call it after a barrier behind
+// stage_candidates (if `sane`).
 //
 // `tau` is at or below the keep-th largest where the bounds of the waves say so;
 // usually a few more than `keep` elements reach it, and those are ranked.  Where
 // too many do (ties, a row that is mostly masked, sorted rows, a NaN) the bound
 // is the keep-th largest of the threads' largest elements, and if that leaves too
 // many the keep-th largest element itself, found bit by bit; what is above the
-// bound is taken, and of the elements equal to it those of the lowest ids.
-//
-// The registers only say which vectors hold an element that reaches the bound;
-// the elements are picked from memory, where the row was just read from.  Picking
-// them from registers takes code for each (20 000 instructions with 8 vectors a
-// thread, which a single row's call spent 15 us fetching).
+// bound is taken, and of the elements equal to it those of the lowest ids.  This
+// second way reads the segment from memory again: it is rare, and from registers it
+// takes code for each element (20 000 instructions with 8 vectors a thread, which a
+// single row's call spent 15 us fetching).
 template <int DT, int NV, class F>
-__device__ __forceinline__ void select_top(Segment<DT, NV>& d, const typename Elem<DT>::type* seg,
-                                           float tau, bool sane, int keep, int id0, int len,
-                                           Shared& sh, uint64_t* keys, uint32_t* rank, F emit) {
+__device__ __forceinline__ void select_top(const typename Elem<DT>::type* seg, float tau, bool sane,
+                                           int keep, int id0, int len, Shared& sh,
+                                           const TopLds& top, F emit) {
     typedef Segment<DT, NV> S;
     constexpr int kVec = S::kVec;
     const int threads = blockDim.x, waves = threads / 64, t = threadIdx.x;
-    if (t == 0) sh.n = 0;
-    __syncthreads();
-    if (sane) {
-        uint32_t hits = 0;
-        d.again();
+    uint64_t* keys = top.keys;
+    const int vecs = sane ? sh.vecs : 0;
+    if (vecs <= kCapVecs) {
+        for (int i = t; i < vecs * kVec; i += threads) {
+            const int e = i % kVec;
+            const symtile::u32x4 w = top.vec[i / kVec];
+            // (element() takes its place as a constant)
+            float x = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float m = -kInf;
-#pragma unroll
-            for (int e = 0; e < kVec; e += 2)
-                m = max3(m, element<DT>(d.v[i], e), element<DT>(d.v[i], e + 1));
-            hits |= m >= tau ? 1u << i : 0u;
-        }
-        while (hits) {
-            const int at = ((__ffs(hits) - 1) * threads + t) * kVec;
-            hits &= hits - 1;
-            const symtile::u32x4 w = S::fetch(seg, len, at);
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                const float x = element<DT>(w, e);
-                if (x >= tau) {
-                    const int n = atomicAdd(&sh.n, 1);
-                    if (n < kCap) keys[n] = top_key(order(x), id0 + at + e);
-                }
-            }
+            for (int k = 0; k < kVec; ++k) x = e == k ? element<DT>(w, k) : x;
+            if (x >= tau) keys[atomicAdd(&sh.n, 1) % kCap] = top_key(order(x), id0 + top.at[i / kVec] + e);
         }
     }
     __syncthreads();
     int n = sh.n;
-    if (!sane || n < keep || n > max(4 * keep, 128)) {
+    if (!sane || vecs > kCapVecs || n < keep || n > max(4 * keep, 128)) {
         int step = 0;
         __syncthreads();
         // f(element's index, its order) for this thread's elements
@@ -253,7 +288,7 @@ __device__ __forceinline__ void select_top(Segment<DT, NV>& d, const typename El
         n = max(gt, keep);
         __syncthreads();
     }
-    rank_keys(keys, rank, n, keep, emit);
+    rank_keys(keys, n, keep, emit);
 }
 
 // What the gradient of a row needs of it.
@@ -371,16 +406,23 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(LogprobParams p) {
             if constexpr (DT == SYMTILE_F32) sh.x_target = row[target];
             else sh.x_target = (float)row[target];
         }
-        const float lane_max = d.thread_max();
+        float vec_max[NV];
+        const float lane_max = d.thread_max(vec_max);
         m = wave_max(lane_max);
         if constexpr (TOP) {
-            // all waves but the one of the lowest bound hold `top` elements together
             const float bound = wave_bound(lane_max, (p.top + waves - 2) / (waves - 1));
             if (t % 64 == 0) sh.tau[t / 64] = bound;
+            if (t == 0) sh.n = sh.vecs = 0;
         }
         if (t % 64 == 0) sh.m[t / 64] = m;
         __syncthreads();
         m = over_waves(sh.m, waves, Max());
+        const TopLds top(dyn, p.segs, p.top);
+        float tau = -kInf;
+        if constexpr (TOP) {
+            tau = row_bound(sh.tau, waves);
+            if (tau > -kInf) stage_candidates(d, vec_max, tau, sh, top);
+        }
         const Exponent ex(m, p.scale);
         float s, u;
         if (ex.huge) sums<DT, NV, true>(d, ex, &s, &u);
@@ -395,26 +437,12 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(LogprobParams p) {
         const float back = exp2f(-ex.shift);
         s = over_waves(sh.s, waves, Sum()) * back;
         u = kLn2 * (over_waves(sh.t, waves, Sum()) * back - ex.shift * s);
-        float tau = -kInf;
-        bool sane = false;
-        if constexpr (TOP) {
-            float lowest = kInf;   // the lowest bound may be of a wave without elements: the next
-            tau = kInf;
-            for (int w = 0; w < waves; ++w) {
-                const float b = sh.tau[w];
-                tau = fminf(tau, fmaxf(lowest, b));
-                lowest = fminf(lowest, b);
-            }
-            sane = s == s && tau > -kInf;
-        }
-        uint64_t* keys = dyn;
-        const int cap = max(kCap, p.segs * p.top);
-        uint32_t* rank = reinterpret_cast<uint32_t*>(dyn + cap);
+        const bool sane = s == s && tau > -kInf;
         if (p.segs == 1) {
             const RowValues v(m, s, u);
             if (t == 0) write_values(p, r, target, sh.x_target, v);
             if constexpr (TOP) {
-                select_top(d, row + id0, tau, sane, p.top, id0, len, sh, keys, rank,
+                select_top<DT, NV>(row + id0, tau, sane, p.top, id0, len, sh, top,
                            [&](int place, uint64_t key) {
                                const size_t o = (size_t)r * p.top + place;
                                p.top_ids[o] = key_id(key);
@@ -429,7 +457,7 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(LogprobParams p) {
             if constexpr (TOP) {
                 const int keep = min(p.top, len);
                 uint64_t* out = p.keys + unit * p.top;
-                select_top(d, row + id0, tau, sane, keep, id0, len, sh, keys, rank,
+                select_top<DT, NV>(row + id0, tau, sane, keep, id0, len, sh, top,
                            [&](int place, uint64_t key) { put(out + place, key); });
                 for (int i = keep + t; i < p.top; i += threads) put(out + i, 0ull);
             }
@@ -472,10 +500,10 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(LogprobParams p) {
                 __syncthreads();
                 for (int i = t; i < p.segs * p.top; i += threads) {
                     const uint64_t key = take(in + i);
-                    if (key != 0 && key >= sh.bound) keys[atomicAdd(&sh.n, 1)] = key;
+                    if (key != 0 && key >= sh.bound) top.keys[atomicAdd(&sh.n, 1)] = key;
                 }
                 __syncthreads();
-                rank_keys(keys, rank, sh.n, p.top, [&](int place, uint64_t key) {
+                rank_keys(top.keys, sh.n, p.top, [&](int place, uint64_t key) {
                     const size_t at = (size_t)r * p.top + place;
                     p.top_ids[at] = key_id(key);
                     p.top_logprobs[at] = v.logp(ordered_value((uint32_t)(key >> 32)), p.scale);
@@ -508,7 +536,7 @@ symtile_status run(LogprobParams p, const Plan& plan, int rows, int dtype, const
     p.segs = plan.segs;
     p.seg_len = plan.seg_len;
     p.by_segs = symtile_host::make_div(plan.segs);
-    const size_t lds = p.top ? (size_t)std::max(kCap, plan.segs * p.top) * 12 : 0;
+    const size_t lds = p.top ? TopLds::bytes(plan.segs, p.top) : 0;
     const int most = (int)((size_t(1) << 30) / ((size_t)plan.threads * plan.segs));
     for (int row = 0; row < rows; row += most) {
         const int n = std::min(most, rows - row);
