@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
         m_rest = wave_max(d.thread_max(vec_max));
         if (t % 64 == 0) l.m[t / 64] = m_rest;
         __syncthreads();
-        m_rest = over_waves(l.m, waves, Max());
+        m_rest = waves_max(l.m, waves);
         const Exponent ex(m_rest, p.scale);
         float s = ex.huge ? rest_sum<DT, NV, true>(d, ex) : rest_sum<DT, NV, false>(d, ex);
         s = wave_sum(s);
@@ -278,10 +278,11 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
         if (first_wave) teacher(p, en, l);
         __syncthreads();
         if (p.segs > 1) {
+            const float sum = waves_sum(l.s, waves) * exp2f(-ex.shift);
             if (t == 0) {
                 float* o = p.partials + 4 * ((size_t)local * p.segs + seg);
                 put(o, m_rest);
-                put(o + 1, over_waves(l.s, waves, Sum()) * exp2f(-ex.shift));
+                put(o + 1, sum);
             }
             if (!arrive_last(p.counters + local, p.segs, &l.last)) return;
         }
@@ -296,7 +297,7 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
                 s_rest = wave_sum(ms == -kInf || ms == m_rest ? ss
                                                               : ss * expf((ms - m_rest) * p.scale));
             } else {
-                s_rest = over_waves(l.s, waves, Sum()) * exp2f(-ex.shift);
+                s_rest = waves_sum(l.s, waves) * exp2f(-ex.shift);
             }
             const float x0 = en.first[0] ? en.x[0] : -kInf, x1 = en.first[1] ? en.x[1] : -kInf;
             const float m = max3(m_rest, wave_max(max3(x0, x1, x1)), -kInf);

@@ -108,17 +108,31 @@ __device__ __forceinline__ float dpp(float v) {
     return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), CTRL, 0xF, 0xF, true));
 }
 template <class F>
-__device__ __forceinline__ float wave_reduce(float v, F f) {
-    v = f(v, dpp<0xB1>(v));    // quad_perm 1 0 3 2
-    v = f(v, dpp<0x4E>(v));    // quad_perm 2 3 0 1
-    v = f(v, dpp<0x141>(v));   // row_half_mirror
-    v = f(v, dpp<0x140>(v));   // row_mirror
+__device__ __forceinline__ float quad_reduce(float v, F f) {
+    v = f(v, dpp<0xB1>(v));       // quad_perm 1 0 3 2
+    return f(v, dpp<0x4E>(v));    // quad_perm 2 3 0 1
+}
+template <class F>
+__device__ __forceinline__ float row_of_quads(float v, F f) {
+    v = f(v, dpp<0x141>(v));      // row_half_mirror
+    return f(v, dpp<0x140>(v));   // row_mirror
+}
+template <class F>
+__device__ __forceinline__ float wave_of_rows(float v, F f) {
     const uint32_t u = __float_as_uint(v);
     const auto rows = __builtin_amdgcn_permlane16_swap(u, u, false, false);
     v = f(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
     const uint32_t w = __float_as_uint(v);
     const auto halves = __builtin_amdgcn_permlane32_swap(w, w, false, false);
     return f(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+}
+template <class F>
+__device__ __forceinline__ float row_reduce(float v, F f) {
+    return row_of_quads(quad_reduce(v, f), f);
+}
+template <class F>
+__device__ __forceinline__ float wave_reduce(float v, F f) {
+    return wave_of_rows(row_reduce(v, f), f);
 }
 struct Max {
     __device__ __forceinline__ float operator()(float a, float b) const { return max3(a, b, b); }
@@ -135,12 +149,21 @@ __device__ __forceinline__ uint32_t wave_sum_u32(uint32_t v) {
     return v;
 }
 
-// Over the workgroup's `waves` wave results in LDS.
+// Over the workgroup's `waves` (at most 16) wave results in LDS: every row of 16
+// lanes reads and reduces them (one after the other they took a thousand cycles a
+// row of logits).
+static_assert(kMaxWaves == 16, "a row of lanes holds the waves' results");
 template <class F>
-__device__ __forceinline__ float over_waves(const float* lds, int waves, F f) {
-    float v = lds[0];
-    for (int w = 1; w < waves; ++w) v = f(v, lds[w]);
-    return v;
+__device__ __forceinline__ float over_waves(const float* lds, int waves, float none, F f) {
+    const int l = threadIdx.x % 16;
+    const float v = lds[l];
+    return row_reduce(l < waves ? v : none, f);
+}
+__device__ __forceinline__ float waves_max(const float* lds, int waves) {
+    return over_waves(lds, waves, -kInf, Max());
+}
+__device__ __forceinline__ float waves_sum(const float* lds, int waves) {
+    return over_waves(lds, waves, 0.0f, Sum());
 }
 
 // ---- a segment in registers ----------------------------------------------------

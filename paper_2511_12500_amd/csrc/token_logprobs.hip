@@ -38,7 +38,8 @@ struct LogprobParams {
 };
 
 struct Shared {
-    float m[kMaxWaves], s[kMaxWaves], t[kMaxWaves], tau[kMaxWaves];
+    float m[kMaxWaves], s[kMaxWaves], t[kMaxWaves];
+    float tau;
     uint32_t count[2][kMaxWaves];
     float x_target;
     int n, vecs, last;
@@ -46,8 +47,12 @@ struct Shared {
 };
 
 // Dynamic LDS of the top entries: keys, and the vectors that hold the candidates.
+// Before there are keys, groups' largest logits stand in their place.
 struct TopLds {
-    uint64_t* keys;
+    union {
+        uint64_t* keys;
+        float* groups;
+    };
     symtile::u32x4* vec;
     int* at;               // first element of each
     static size_t bytes(int segs, int top) {
@@ -108,40 +113,33 @@ __device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int keep,
     }
 }
 
-// A bound for the wave's share of the top entries: the j-th largest of its
-// lanes' largest logits (or a lower one); -inf where there is none.
-__device__ __forceinline__ float wave_bound(float lane_max, int j) {
-    if (j > 64) return -kInf;
-    if (j <= 6) {       // take away the largest j - 1 times (equal ones together)
-        float m = wave_max(lane_max);
-        for (int i = 1; i < j; ++i) {
-            lane_max = lane_max == m ? -kInf : lane_max;
-            m = wave_max(lane_max);
-        }
-        return m;
+// The bound for the top entries: the `top`-th largest of the largest logits of groups
+// of lanes, which as many elements reach as there are groups above it, and hardly
+// more.  Groups are rows of 16 lanes, quads or single lanes, so that there are some
+// more than `top` of them.
+__device__ __forceinline__ int group_lanes(int top, int waves) {
+    return top <= 3 * waves ? 16 : top <= 14 * waves ? 4 : 1;
+}
+// By the first wave; not above the `top`-th largest, -inf where fewer groups have one.
+__device__ __forceinline__ float groups_bound(const float* groups, int n, int top) {
+    const int lane = threadIdx.x;
+    if (n <= 64) {      // how many are larger than mine?
+        const float v = lane < n ? groups[lane] : -kInf;
+        int c = 0;
+        for (int j = 0; j < n; ++j)
+            c += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), j)) > v;
+        return -wave_max(lane < n && c < top ? -v : -kInf);
     }
     // bit by bit, to 16 bits of their order (rounded down)
-    const uint32_t o = order(lane_max);
     uint32_t p = 0;
-#pragma unroll
     for (int b = 31; b >= 16; --b) {
         const uint32_t trial = p | 1u << b;
-        const int n = __popcll(__ballot(o >= trial));
-        p = n >= j ? trial : p;
+        int c = 0;
+        for (int i = lane; i - lane < n; i += 64)
+            c += __popcll(__ballot(i < n && order(groups[i]) >= trial));
+        p = c >= top ? trial : p;
     }
     return p < 0x00800000u ? -kInf : ordered_value(p);
-}
-
-// The second lowest of the waves' bounds: the lowest may be of a wave without
-// elements, and all others hold `top` elements that reach theirs together.
-__device__ __forceinline__ float row_bound(const float* tau, int waves) {
-    float lowest = kInf, bound = kInf;
-    for (int w = 0; w < waves; ++w) {
-        const float b = tau[w];
-        bound = fminf(bound, fmaxf(lowest, b));
-        lowest = fminf(lowest, b);
-    }
-    return bound;
 }
 
 // The thread's vectors that hold an element which reaches the bound, into LDS
@@ -169,8 +167,8 @@ __device__ __forceinline__ void stage_candidates(const Segment<DT, NV>& d, const
 // from `id0` on, to emit(place, key).  All threads call it after a barrier behind
 // stage_candidates (if `sane`).
 //
-// `tau` is at or below the keep-th largest where the bounds of the waves say so;
-// usually a few more than `keep` elements reach it, and those are ranked.  Where
+// `tau` is at or below the keep-th largest; usually a few more than `keep` elements
+// reach it, and those are ranked.  Where
 // too many do (ties, a row that is mostly masked, sorted rows, a NaN) the bound
 // is the keep-th largest of the threads' largest elements, and if that leaves too
 // many the keep-th largest element itself, found bit by bit; what is above the
@@ -408,20 +406,26 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(LogprobParams p) {
         }
         float vec_max[NV];
         const float lane_max = d.thread_max(vec_max);
-        m = wave_max(lane_max);
+        const TopLds top(dyn, p.segs, p.top);
         if constexpr (TOP) {
-            const float bound = wave_bound(lane_max, (p.top + waves - 2) / (waves - 1));
-            if (t % 64 == 0) sh.tau[t / 64] = bound;
+            const float quad = quad_reduce(lane_max, Max()), line = row_of_quads(quad, Max());
+            m = wave_of_rows(line, Max());
+            const int group = group_lanes(p.top, waves);
+            if (t % group == 0)
+                top.groups[t / group] = group == 16 ? line : group == 4 ? quad : lane_max;
             if (t == 0) sh.n = sh.vecs = 0;
+        } else {
+            m = wave_max(lane_max);
         }
         if (t % 64 == 0) sh.m[t / 64] = m;
         __syncthreads();
-        m = over_waves(sh.m, waves, Max());
-        const TopLds top(dyn, p.segs, p.top);
-        float tau = -kInf;
+        m = waves_max(sh.m, waves);
         if constexpr (TOP) {
-            tau = row_bound(sh.tau, waves);
-            if (tau > -kInf) stage_candidates(d, vec_max, tau, sh, top);
+            if (t < 64) {
+                const float bound =
+                    groups_bound(top.groups, threads / group_lanes(p.top, waves), p.top);
+                if (t == 0) sh.tau = bound;
+            }
         }
         const Exponent ex(m, p.scale);
         float s, u;
@@ -434,9 +438,15 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(LogprobParams p) {
             sh.t[t / 64] = u;
         }
         __syncthreads();
+        float tau = -kInf;
+        if constexpr (TOP) {
+            tau = sh.tau;
+            if (tau > -kInf) stage_candidates(d, vec_max, tau, sh, top);
+        }
         const float back = exp2f(-ex.shift);
-        s = over_waves(sh.s, waves, Sum()) * back;
-        u = kLn2 * (over_waves(sh.t, waves, Sum()) * back - ex.shift * s);
+        s = waves_sum(sh.s, waves) * back;
+        u = kLn2 * (waves_sum(sh.t, waves) * back - ex.shift * s);
+        if constexpr (TOP) __syncthreads();
         const bool sane = s == s && tau > -kInf;
         if (p.segs == 1) {
             const RowValues v(m, s, u);
