@@ -367,19 +367,18 @@ const void* kernel_of(int dtype, int nv) {
     });
 }
 
-// The kernels of a call, in launches whose threads fit 32 bits.
-symtile_status run(DistillParams p, const Plan& plan, int rows, const void* kernel,
+// A kernel over rows first .. first + rows - 1, in launches whose threads fit 32 bits.
+symtile_status run(DistillParams p, const Plan& plan, int first, int rows, const void* kernel,
                    symtile_stream s, const char* what) {
     p.segs = plan.segs;
     p.seg_len = plan.seg_len;
     p.by_segs = symtile_host::make_div(plan.segs);
     const size_t lds = (size_t)(plan.seg_len + 31) / 32 * 4;
-    const int most = (int)((size_t(1) << 30) / ((size_t)plan.threads * plan.segs));
+    const int most = rows_a_launch(plan);
     for (int row = 0; row < rows; row += most) {
-        const int n = std::min(most, rows - row);
-        DistillParams q = p;
-        q.row0 = row;
-        if (symtile_status st = launch(kernel, plan, n, lds, q, s, what)) return st;
+        p.row0 = first + row;
+        if (symtile_status st = launch(kernel, plan, std::min(most, rows - row), lds, p, s, what))
+            return st;
     }
     return SYMTILE_OK;
 }
@@ -419,7 +418,7 @@ extern "C" symtile_status symtile_distill_topk(int device, const void* logits, i
     } else if (row_grad) {
         return fail(SYMTILE_EINVAL, "row_grad without dlogits");
     }
-    const Plan plan = make_plan(device, rows, vocab, dtype, 0);
+    const Plan plan = make_plan(vocab, dtype, dlogits != nullptr);
     const Workspace ws = make_workspace(plan, rows, 0);
     if (symtile_status st = check_workspace(workspace, workspace_bytes, ws.bytes)) return st;
     if (rows == 0) return SYMTILE_OK;
@@ -446,10 +445,11 @@ extern "C" symtile_status symtile_distill_topk(int device, const void* logits, i
     if (on.status) return on.status;
     const char* what = "distill_kernel launch";
     if (dlogits && plan.segs == 1)
-        return run(p, plan, rows, kernel_of<kStep>(dtype, plan.nv), s, what);
-    if (symtile_status st = run(p, plan, rows, kernel_of<kValues>(dtype, plan.nv), s, what)) return st;
+        return run(p, plan, 0, rows, kernel_of<kStep>(dtype, plan.nv), s, what);
+    if (symtile_status st = run(p, plan, 0, rows, kernel_of<kValues>(dtype, plan.nv), s, what))
+        return st;
     if (!dlogits) return SYMTILE_OK;
-    return run(p, plan, rows, kernel_of<kGrad>(dtype, plan.nv), s, what);
+    return run(p, plan, 0, rows, kernel_of<kGrad>(dtype, plan.nv), s, what);
 }
 
 extern "C" symtile_status symtile_distill_topk_backward(
@@ -479,7 +479,7 @@ extern "C" symtile_status symtile_distill_topk_backward(
     p.scale = scale;
     OnDevice on(device);
     if (on.status) return on.status;
-    const Plan plan = make_plan(device, rows, vocab, dtype, 0);
-    return run(p, plan, rows, kernel_of<kGrad>(dtype, plan.nv), s,
+    const Plan plan = make_plan(vocab, dtype, true);
+    return run(p, plan, 0, rows, kernel_of<kGrad>(dtype, plan.nv), s,
                "distill_kernel launch (gradient)");
 }

@@ -353,20 +353,25 @@ inline void shape(int n, int* nv, int* threads) {
     *threads = std::min(kMaxThreads, std::max(128, (n + *nv * 64 - 1) / (*nv * 64) * 64));
 }
 
-inline Plan make_plan(int device, int rows, int vocab, int dtype, int top) {
+// Values alone take segments of at most 4096 vectors (512 threads of 8), several
+// workgroups a CU, so that one's loads go on under another's sums (333x100003 fp32:
+// 28 us, with segments of 16384 38).  With a gradient a row that one workgroup holds
+// (16384 vectors) stays whole, since it is read once then.
+inline Plan make_plan(int vocab, int dtype, bool grad) {
     const int vec = dtype == SYMTILE_F32 ? 4 : 8;
     const int n = (vocab + vec - 1) / vec;
-    const int capacity = 16 * kMaxThreads;
-    int segs = (n + capacity - 1) / capacity;
-    (void)device;
-    (void)rows;
-    (void)top;
+    const int most = grad && n <= 16 * kMaxThreads ? 16 * kMaxThreads : 4096;
+    const int segs = (n + most - 1) / most;
     Plan p;
     const int per = (n + segs - 1) / segs;
     p.segs = (n + per - 1) / per;
     p.seg_len = per * vec;
     shape(per, &p.nv, &p.threads);
     return p;
+}
+
+inline int rows_a_launch(const Plan& p) {
+    return (int)((size_t(1) << 30) / ((size_t)p.threads * p.segs));
 }
 
 // Workspace of split rows: a counter per row, then 4 floats per segment, then

@@ -107,7 +107,17 @@ __device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int keep,
     for (int i = t >> lg; i - (t >> lg) < n; i += threads >> lg) {
         const uint64_t mine = i < n ? keys[i] : ~0ull;
         uint32_t c = 0;
-        for (int j = part; j < n; j += 1 << lg) c += keys[j] > mine;
+        // eight at a time: one after the other, each would wait for its own read
+        for (int j = part; j < n; j += 8 << lg) {
+            uint64_t k[8];
+#pragma unroll
+            for (int o = 0; o < 8; ++o) {
+                const int at = j + (o << lg);
+                k[o] = at < n ? keys[at] : 0;
+            }
+#pragma unroll
+            for (int o = 0; o < 8; ++o) c += k[o] > mine;
+        }
         for (int o = 1; o < 1 << lg; o *= 2) c += __shfl_xor(c, o);
         if (part == 0 && i < n && (int)c < keep) emit((int)c, mine);
     }
@@ -131,12 +141,20 @@ __device__ __forceinline__ float groups_bound(const float* groups, int n, int to
         return -wave_max(lane < n && c < top ? -v : -kInf);
     }
     // bit by bit, to 16 bits of their order (rounded down)
+    constexpr int kEach = kMaxThreads / 64;
+    uint32_t v[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) v[i] = lane + 64 * i < n ? order(groups[lane + 64 * i]) : 0;
     uint32_t p = 0;
+#pragma unroll 1
     for (int b = 31; b >= 16; --b) {
         const uint32_t trial = p | 1u << b;
         int c = 0;
-        for (int i = lane; i - lane < n; i += 64)
-            c += __popcll(__ballot(i < n && order(groups[i]) >= trial));
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if (64 * i >= n) break;
+            c += __popcll(__ballot(v[i] >= trial));
+        }
         p = c >= top ? trial : p;
     }
     return p < 0x00800000u ? -kInf : ordered_value(p);
@@ -495,17 +513,17 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(LogprobParams p) {
             const RowValues v(m, s, u);
             if (t == 0) write_values(p, r, target, sh.x_target, v);
             if constexpr (TOP) {
-                // no segment's last key can be above the row's
+                // `top` keys are at or above the lowest of the segments' j-th, j = ceil(top / segs)
                 const uint64_t* in = p.keys + (size_t)local * p.segs * p.top;
                 if (t == 0) {
                     sh.n = 0;
-                    sh.bound = 0;
+                    sh.bound = ~0ull;
                 }
                 __syncthreads();
                 if (t < p.segs) {
-                    const uint64_t last = take(in + (size_t)t * p.top + p.top - 1);
-                    atomicMax(reinterpret_cast<unsigned long long*>(&sh.bound),
-                              (unsigned long long)last);
+                    const int j = (p.top + p.segs - 1) / p.segs;
+                    atomicMin(reinterpret_cast<unsigned long long*>(&sh.bound),
+                              (unsigned long long)take(in + (size_t)t * p.top + j - 1));
                 }
                 __syncthreads();
                 for (int i = t; i < p.segs * p.top; i += threads) {
@@ -540,19 +558,18 @@ const void* kernel_of(int dtype, int nv) {
     });
 }
 
-// The kernels of a call, in launches whose threads fit 32 bits.
-symtile_status run(LogprobParams p, const Plan& plan, int rows, int dtype, const void* kernel,
+// A kernel over rows first .. first + rows - 1, in launches whose threads fit 32 bits.
+symtile_status run(LogprobParams p, const Plan& plan, int first, int rows, const void* kernel,
                    symtile_stream s, const char* what) {
     p.segs = plan.segs;
     p.seg_len = plan.seg_len;
     p.by_segs = symtile_host::make_div(plan.segs);
     const size_t lds = p.top ? TopLds::bytes(plan.segs, p.top) : 0;
-    const int most = (int)((size_t(1) << 30) / ((size_t)plan.threads * plan.segs));
+    const int most = rows_a_launch(plan);
     for (int row = 0; row < rows; row += most) {
-        const int n = std::min(most, rows - row);
-        LogprobParams q = p;
-        q.row0 = row;
-        if (symtile_status st = launch(kernel, plan, n, lds, q, s, what)) return st;
+        p.row0 = first + row;
+        if (symtile_status st = launch(kernel, plan, std::min(most, rows - row), lds, p, s, what))
+            return st;
     }
     return SYMTILE_OK;
 }
@@ -564,7 +581,7 @@ extern "C" symtile_status symtile_logits_workspace_bytes(int device, int rows, i
     if (!bytes) return fail(SYMTILE_EINVAL, "bytes is NULL");
     *bytes = 0;
     if (symtile_status st = check_sizes(rows, vocab, dtype, top)) return st;
-    *bytes = make_workspace(make_plan(device, rows, vocab, dtype, top), rows, top).bytes;
+    *bytes = make_workspace(make_plan(vocab, dtype, false), rows, top).bytes;
     return SYMTILE_OK;
 }
 
@@ -589,7 +606,7 @@ extern "C" symtile_status symtile_token_logprobs(
         return fail(SYMTILE_EINVAL, "gradients without dlogits");
     }
     if (grad_logprob && !targets) return fail(SYMTILE_EINVAL, "grad_logprob without targets");
-    const Plan plan = make_plan(device, rows, vocab, dtype, top);
+    const Plan plan = make_plan(vocab, dtype, dlogits != nullptr);
     const Workspace ws = make_workspace(plan, rows, top);
     if (symtile_status st = check_workspace(workspace, workspace_bytes, ws.bytes)) return st;
     if (rows == 0) return SYMTILE_OK;
@@ -619,18 +636,18 @@ extern "C" symtile_status symtile_token_logprobs(
     OnDevice on(device);
     if (on.status) return on.status;
     if (dlogits && plan.segs == 1)
-        return run(p, plan, rows, dtype,
+        return run(p, plan, 0, rows,
                    top ? kernel_of<kStep, true>(dtype, plan.nv)
                        : kernel_of<kStep, false>(dtype, plan.nv),
                    s, "logprob_kernel launch");
-    if (symtile_status st = run(p, plan, rows, dtype,
+    if (symtile_status st = run(p, plan, 0, rows,
                                 top ? kernel_of<kValues, true>(dtype, plan.nv)
                                     : kernel_of<kValues, false>(dtype, plan.nv),
                                 s, "logprob_kernel launch"))
         return st;
     if (!dlogits) return SYMTILE_OK;
     p.top = 0;
-    return run(p, plan, rows, dtype, kernel_of<kGrad, false>(dtype, plan.nv), s,
+    return run(p, plan, 0, rows, kernel_of<kGrad, false>(dtype, plan.nv), s,
                "logprob_kernel launch (gradient)");
 }
 
@@ -661,7 +678,7 @@ extern "C" symtile_status symtile_token_logprobs_backward(
     p.scale = scale;
     OnDevice on(device);
     if (on.status) return on.status;
-    const Plan plan = make_plan(device, rows, vocab, dtype, 0);
-    return run(p, plan, rows, dtype, kernel_of<kGrad, false>(dtype, plan.nv), s,
+    const Plan plan = make_plan(vocab, dtype, false);
+    return run(p, plan, 0, rows, kernel_of<kGrad, false>(dtype, plan.nv), s,
                "logprob_kernel launch (gradient)");
 }
