@@ -11,7 +11,8 @@
 //
 // Listed tokens are found through a bit for each token of the segment in LDS, and
 // their logits replaced by -inf in registers: they drop out of the sums, and the
-// gradient's main pass writes 0 there, which the list's threads overwrite.
+// gradient's main pass writes 0 there.  The thread that wrote it overwrites it: every
+// thread has a chain of the list's entries in its vectors.
 #include "logits_rows.h"
 #include "symtile_device.h"
 
@@ -42,11 +43,14 @@ struct DistillParams {
 struct __attribute__((aligned(16))) List {
     int id[kMaxK];
     float q[kMaxK];
+    float x[kMaxK];            // the student's logit
+    float q_id[kMaxK];         // sum of q over the entries of the id; -1: not the first of them
+    int next[kMaxK];           // the chains
     float m[kMaxWaves], s[kMaxWaves];
     float sum_q, q_rest;
     float coef, all;           // of the gradient
     float g, m_all, log_s;
-    int bad, some, last, zero;
+    int bad, some, repeated, last, zero;
 };
 
 __device__ __forceinline__ float teacher_value(const DistillParams& p, size_t i) {
@@ -60,9 +64,8 @@ __device__ __forceinline__ float teacher_value(const DistillParams& p, size_t i)
 // What the first wave knows of the list: lane l holds entries l and l + 64.
 struct Entries {
     int id[2];
-    float value[2], x[2], q[2], log_q[2];
+    float value[2], x[2], q[2], log_q[2], q_id[2];
     bool first[2];      // the first entry of its id
-    float q_id[2];      // sum of q over the entries of this id
 };
 
 // Sum in 64 bits: the rest's probability is what the list's leaves of 1.
@@ -72,21 +75,19 @@ __device__ __forceinline__ double wave_sum64(double v) {
     return v;
 }
 
-// The teacher's probabilities, by the first wave.
-__device__ __forceinline__ void teacher(const DistillParams& p, Entries& e, List& l) {
+// The teacher's probabilities, by the first wave.  `search`: look for entries that
+// name the same id (they count once in the student's sum, together in q).
+__device__ __forceinline__ void teacher(const DistillParams& p, Entries& e, List& l, bool search) {
     const int lane = threadIdx.x;
     float sum_q = 0.0f, q_rest = 0.0f;
     const bool some = l.some != 0;
     if (p.mode == SYMTILE_DISTILL_REST) {
-        double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const double q = e.id[i] != -1 ? exp((double)e.value[i]) : 0.0;
+            e.q[i] = e.id[i] != -1 ? expf(e.value[i]) : 0.0f;
             e.log_q[i] = e.value[i];
-            e.q[i] = (float)q;
-            sum += q;
         }
-        sum = wave_sum64(sum);
+        const double sum = wave_sum64((double)e.q[0] + (double)e.q[1]);
         sum_q = (float)sum;
         q_rest = some ? fmaxf((float)(1.0 - sum), 0.0f) : 0.0f;
     } else {
@@ -106,27 +107,34 @@ __device__ __forceinline__ void teacher(const DistillParams& p, Entries& e, List
         }
         sum_q = wave_sum(e.q[0] + e.q[1]);
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) l.q[lane + 64 * i] = e.q[i];
     if (lane == 0) {
         l.sum_q = sum_q;
         l.q_rest = q_rest;
     }
-    __builtin_amdgcn_wave_barrier();   // the wave reads what its lanes wrote
-    // entries that name one id count once in the student's sum, together in q
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int j = lane + 64 * i;
         e.first[i] = e.id[i] >= 0;
-        e.q_id[i] = 0.0f;
-        if (e.id[i] >= 0) {
-            for (int o = 0; o < p.k; ++o)
+        e.q_id[i] = e.q[i];
+        l.q[lane + 64 * i] = e.q[i];
+    }
+    __builtin_amdgcn_wave_barrier();   // the wave reads what its lanes wrote
+    if (search) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int j = lane + 64 * i;
+            float sum = 0.0f;
+#pragma unroll 4
+            for (int o = 0; o < kMaxK; ++o)     // (behind the list stand absent ones)
                 if (l.id[o] == e.id[i]) {
-                    e.q_id[i] += l.q[o];
+                    sum += l.q[o];
                     if (o < j) e.first[i] = false;
                 }
+            e.q_id[i] = sum;
         }
     }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) l.q_id[lane + 64 * i] = e.first[i] ? e.q_id[i] : -1.0f;
+    __builtin_amdgcn_wave_barrier();
 }
 
 // The row's constants of the gradient, by every lane of the first wave.
@@ -197,6 +205,8 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
     const int r = p.row0 + local;
     const int id0 = seg * p.seg_len, len = min(p.seg_len, p.vocab - id0);
     const T* row = static_cast<const T*>(p.x) + (size_t)r * p.ld;
+    const int words = (p.seg_len + 31) / 32;
+    int* chain = reinterpret_cast<int*>(bits + words);   // a thread's first entry, -1: none
     // the list first: its tokens' logits wait for the ids
     Entries en;
     int64_t wide[2] = {-1, -1};
@@ -213,30 +223,46 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
     }
     Segment<DT, NV> d;
     d.load(row + id0, len, threads);
-    for (int i = t; i < (p.seg_len + 31) / 32; i += threads) bits[i] = 0;
+    for (int i = t; i < words; i += threads) bits[i] = 0;
+    if constexpr (PHASE != kValues) chain[t] = -1;
     __syncthreads();
     if (first_wave) {
-        bool bad = false, some = false;
+        bool bad = false, some = false, repeated = false;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
+            const int j = t + 64 * i;
             en.id[i] = wide[i] < 0 ? -1 : wide[i] >= p.vocab ? -2 : (int)wide[i];
             if (en.id[i] == -1) en.value[i] = -kInf;
             bad |= en.id[i] == -2;
             some |= en.id[i] != -1;
-            l.id[t + 64 * i] = en.id[i];
-            const unsigned in = (unsigned)(en.id[i] - id0);
-            if (en.id[i] >= 0 && in < (unsigned)len) atomicOr(&bits[in / 32], 1u << in % 32);
+            l.id[j] = en.id[i];
             // read before anything is written: the gradient may overwrite it
             en.x[i] = en.id[i] >= 0 ? (float)row[en.id[i]] : -kInf;
+            const unsigned in = (unsigned)(en.id[i] - id0);
+            if (en.id[i] >= 0 && in < (unsigned)len) {
+                repeated |= atomicOr(&bits[in / 32], 1u << in % 32) >> in % 32 & 1u;
+                if constexpr (PHASE != kValues)
+                    l.next[j] = atomicExch(&chain[in / kVec % (unsigned)threads], j);
+            }
         }
         bad = __any(bad);
         some = __any(some);
+        repeated = __any(repeated);
         if (t == 0) {
             l.bad = bad;
             l.some = some;
+            l.repeated = repeated;
         }
     }
     __syncthreads();
+    if (first_wave) {
+        // of a split row's loss all entries count, also those of other segments
+        teacher(p, en, l, l.repeated || (PHASE == kValues && p.segs > 1));
+        if constexpr (PHASE != kValues) {
+            l.x[t] = en.x[0];
+            l.x[t + 64] = en.x[1];
+        }
+    }
     const uint8_t* bytes = reinterpret_cast<const uint8_t*>(bits);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -260,10 +286,7 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
     if constexpr (PHASE == kGrad) {
         const float* st = p.stats + 4 * (size_t)r;
         m_rest = st[2];
-        if (first_wave) {
-            teacher(p, en, l);
-            gradient_constants(p, r, l, st[0], st[1], m_rest, st[3]);
-        }
+        if (first_wave) gradient_constants(p, r, l, st[0], st[1], m_rest, st[3]);
         __syncthreads();
     } else {
         float vec_max[NV];
@@ -275,7 +298,6 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
         float s = ex.huge ? rest_sum<DT, NV, true>(d, ex) : rest_sum<DT, NV, false>(d, ex);
         s = wave_sum(s);
         if (t % 64 == 0) l.s[t / 64] = s;
-        if (first_wave) teacher(p, en, l);
         __syncthreads();
         if (p.segs > 1) {
             const float sum = waves_sum(l.s, waves) * exp2f(-ex.shift);
@@ -286,30 +308,36 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
             }
             if (!arrive_last(p.counters + local, p.segs, &l.last)) return;
         }
+        float ms = 0.0f, m = 0.0f, log_s = 0.0f, log_rest = 0.0f;
+        bool empty = false;
         if (first_wave) {
             float s_rest;
             if (p.segs > 1) {
                 const float* o = p.partials + 4 * (size_t)local * p.segs;
                 const bool there = t < p.segs;
-                const float ms = there ? take(o + 4 * t) : -kInf;
-                const float ss = there ? take(o + 4 * t + 1) : 0.0f;
-                m_rest = wave_max(ms);
-                s_rest = wave_sum(ms == -kInf || ms == m_rest ? ss
-                                                              : ss * expf((ms - m_rest) * p.scale));
+                const float mine = there ? take(o + 4 * t) : -kInf;
+                const float sum = there ? take(o + 4 * t + 1) : 0.0f;
+                m_rest = wave_max(mine);
+                s_rest = wave_sum(mine == -kInf || mine == m_rest
+                                      ? sum
+                                      : sum * expf((mine - m_rest) * p.scale));
             } else {
                 s_rest = waves_sum(l.s, waves) * exp2f(-ex.shift);
             }
             const float x0 = en.first[0] ? en.x[0] : -kInf, x1 = en.first[1] ? en.x[1] : -kInf;
-            const float m = max3(m_rest, wave_max(max3(x0, x1, x1)), -kInf);
-            const float ms = m == -kInf ? 0.0f : m;
+            m = max3(m_rest, wave_max(max3(x0, x1, x1)), -kInf);
+            ms = m == -kInf ? 0.0f : m;
             const float s_list = wave_sum((en.first[0] ? expf((en.x[0] - ms) * p.scale) : 0.0f) +
                                           (en.first[1] ? expf((en.x[1] - ms) * p.scale) : 0.0f));
             const float s_all =
                 s_list + (m_rest == -kInf ? s_rest : s_rest * expf((m_rest - ms) * p.scale));
-            const bool empty = m == -kInf && s_all == 0.0f;
-            const bool bad = l.bad != 0;
-            const float log_s = bad ? __builtin_nanf("") : empty ? 0.0f : logf(s_all);
-            const float log_rest = m_rest == -kInf && s_rest == 0.0f ? 0.0f : logf(s_rest);
+            empty = m == -kInf && s_all == 0.0f;
+            log_s = l.bad ? __builtin_nanf("") : empty ? 0.0f : logf(s_all);
+            log_rest = m_rest == -kInf && s_rest == 0.0f ? 0.0f : logf(s_rest);
+            if constexpr (PHASE == kStep) gradient_constants(p, r, l, m, log_s, m_rest, log_rest);
+        }
+        if constexpr (PHASE == kStep) __syncthreads();
+        if (first_wave) {   // the loss, while the other waves go on
             float term = 0.0f;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -321,7 +349,7 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
             const float q_rest = l.q_rest;
             if (q_rest > 0.0f && m_rest != -kInf)
                 loss += q_rest * (logf(q_rest) - ((m_rest - ms) * p.scale + log_rest - log_s));
-            if (bad) loss = __builtin_nanf("");
+            if (l.bad) loss = __builtin_nanf("");
             if (t == 0) {
                 p.loss[r] = loss;
                 if (p.stats) {
@@ -329,10 +357,7 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
                     o[0] = m, o[1] = log_s, o[2] = m_rest, o[3] = log_rest;
                 }
             }
-            if constexpr (PHASE == kStep) gradient_constants(p, r, l, m, log_s, m_rest, log_rest);
         }
-        if constexpr (PHASE == kValues) return;
-        __syncthreads();
     }
     if constexpr (PHASE != kValues) {
         T* dx = static_cast<T*>(p.dx) + (size_t)r * p.ld_grad + id0;
@@ -344,17 +369,11 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
                 Segment<DT, NV>::store(dx, len, (i * threads + t) * kVec, pack<DT>(none));
         } else if (ex.huge) write_rest<DT, NV, true, PHASE == kStep>(d, dx, len, coef, ex);
         else write_rest<DT, NV, false, PHASE == kStep>(d, dx, len, coef, ex);
-        symtile::wg_stores_done();   // the list's entries come after the zeros in their places
-        if (first_wave) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const unsigned in = (unsigned)(en.id[i] - id0);
-                if (!en.first[i] || in >= (unsigned)len) continue;
-                const float pj =
-                    en.x[i] == -kInf ? 0.0f : expf((en.x[i] - l.m_all) * p.scale - l.log_s);
-                const float v = l.g * (l.all * pj - en.q_id[i]);
-                dx[in] = (T)v;
-            }
+        for (int j = chain[t]; j >= 0; j = l.next[j]) {
+            if (l.q_id[j] < 0.0f) continue;
+            const float x = l.x[j];
+            const float pj = x == -kInf ? 0.0f : expf((x - l.m_all) * p.scale - l.log_s);
+            dx[l.id[j] - id0] = (T)(l.g * (l.all * pj - l.q_id[j]));
         }
     }
 }
@@ -373,7 +392,7 @@ symtile_status run(DistillParams p, const Plan& plan, int first, int rows, const
     p.segs = plan.segs;
     p.seg_len = plan.seg_len;
     p.by_segs = symtile_host::make_div(plan.segs);
-    const size_t lds = (size_t)(plan.seg_len + 31) / 32 * 4;
+    const size_t lds = (size_t)(plan.seg_len + 31) / 32 * 4 + (size_t)plan.threads * 4;
     const int most = rows_a_launch(plan);
     for (int row = 0; row < rows; row += most) {
         p.row0 = first + row;
@@ -418,7 +437,7 @@ extern "C" symtile_status symtile_distill_topk(int device, const void* logits, i
     } else if (row_grad) {
         return fail(SYMTILE_EINVAL, "row_grad without dlogits");
     }
-    const Plan plan = make_plan(vocab, dtype, dlogits != nullptr);
+    const Plan plan = make_plan(device, rows, vocab, dtype, dlogits != nullptr);
     const Workspace ws = make_workspace(plan, rows, 0);
     if (symtile_status st = check_workspace(workspace, workspace_bytes, ws.bytes)) return st;
     if (rows == 0) return SYMTILE_OK;
@@ -479,7 +498,7 @@ extern "C" symtile_status symtile_distill_topk_backward(
     p.scale = scale;
     OnDevice on(device);
     if (on.status) return on.status;
-    const Plan plan = make_plan(vocab, dtype, true);
+    const Plan plan = make_plan(device, rows, vocab, dtype, true);
     return run(p, plan, 0, rows, kernel_of<kGrad>(dtype, plan.nv), s,
                "distill_kernel launch (gradient)");
 }

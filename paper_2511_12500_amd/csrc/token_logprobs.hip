@@ -107,16 +107,16 @@ __device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int keep,
     for (int i = t >> lg; i - (t >> lg) < n; i += threads >> lg) {
         const uint64_t mine = i < n ? keys[i] : ~0ull;
         uint32_t c = 0;
-        // eight at a time: one after the other, each would wait for its own read
-        for (int j = part; j < n; j += 8 << lg) {
-            uint64_t k[8];
+        // four at a time: one after the other, each would wait for its own read
+        for (int j = part; j < n; j += 4 << lg) {
+            uint64_t k[4];
 #pragma unroll
-            for (int o = 0; o < 8; ++o) {
+            for (int o = 0; o < 4; ++o) {
                 const int at = j + (o << lg);
                 k[o] = at < n ? keys[at] : 0;
             }
 #pragma unroll
-            for (int o = 0; o < 8; ++o) c += k[o] > mine;
+            for (int o = 0; o < 4; ++o) c += k[o] > mine;
         }
         for (int o = 1; o < 1 << lg; o *= 2) c += __shfl_xor(c, o);
         if (part == 0 && i < n && (int)c < keep) emit((int)c, mine);
@@ -136,8 +136,10 @@ __device__ __forceinline__ float groups_bound(const float* groups, int n, int to
     if (n <= 64) {      // how many are larger than mine?
         const float v = lane < n ? groups[lane] : -kInf;
         int c = 0;
-        for (int j = 0; j < n; ++j)
-            c += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), j)) > v;
+        for (int j = 0; j < n; j += 4)      // (the lanes from n on hold -inf)
+#pragma unroll
+            for (int o = 0; o < 4; ++o)
+                c += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), j + o)) > v;
         return -wave_max(lane < n && c < top ? -v : -kInf);
     }
     // bit by bit, to 16 bits of their order (rounded down)
@@ -581,7 +583,7 @@ extern "C" symtile_status symtile_logits_workspace_bytes(int device, int rows, i
     if (!bytes) return fail(SYMTILE_EINVAL, "bytes is NULL");
     *bytes = 0;
     if (symtile_status st = check_sizes(rows, vocab, dtype, top)) return st;
-    *bytes = make_workspace(make_plan(vocab, dtype, false), rows, top).bytes;
+    *bytes = make_workspace(make_plan(device, rows, vocab, dtype, false), rows, top).bytes;
     return SYMTILE_OK;
 }
 
@@ -606,7 +608,7 @@ extern "C" symtile_status symtile_token_logprobs(
         return fail(SYMTILE_EINVAL, "gradients without dlogits");
     }
     if (grad_logprob && !targets) return fail(SYMTILE_EINVAL, "grad_logprob without targets");
-    const Plan plan = make_plan(vocab, dtype, dlogits != nullptr);
+    const Plan plan = make_plan(device, rows, vocab, dtype, dlogits != nullptr);
     const Workspace ws = make_workspace(plan, rows, top);
     if (symtile_status st = check_workspace(workspace, workspace_bytes, ws.bytes)) return st;
     if (rows == 0) return SYMTILE_OK;
@@ -678,7 +680,7 @@ extern "C" symtile_status symtile_token_logprobs_backward(
     p.scale = scale;
     OnDevice on(device);
     if (on.status) return on.status;
-    const Plan plan = make_plan(vocab, dtype, false);
+    const Plan plan = make_plan(device, rows, vocab, dtype, false);
     return run(p, plan, 0, rows, kernel_of<kGrad, false>(dtype, plan.nv), s,
                "logprob_kernel launch (gradient)");
 }
