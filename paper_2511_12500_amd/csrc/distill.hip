@@ -68,7 +68,8 @@ struct Entries {
     bool first[2];      // the first entry of its id
 };
 
-// Sum in 64 bits: the rest's probability is what the list's leaves of 1.
+// In 64 bits, as the list's exponentials are: the rest's probability is what they
+// leave of 1.
 __device__ __forceinline__ double wave_sum64(double v) {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
@@ -82,12 +83,15 @@ __device__ __forceinline__ void teacher(const DistillParams& p, Entries& e, List
     float sum_q = 0.0f, q_rest = 0.0f;
     const bool some = l.some != 0;
     if (p.mode == SYMTILE_DISTILL_REST) {
+        double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            e.q[i] = e.id[i] != -1 ? expf(e.value[i]) : 0.0f;
+            const double q = e.id[i] != -1 ? exp((double)e.value[i]) : 0.0;
+            e.q[i] = (float)q;
             e.log_q[i] = e.value[i];
+            sum += q;
         }
-        const double sum = wave_sum64((double)e.q[0] + (double)e.q[1]);
+        sum = wave_sum64(sum);
         sum_q = (float)sum;
         q_rest = some ? fmaxf((float)(1.0 - sum), 0.0f) : 0.0f;
     } else {
@@ -308,7 +312,7 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
             }
             if (!arrive_last(p.counters + local, p.segs, &l.last)) return;
         }
-        float ms = 0.0f, m = 0.0f, log_s = 0.0f, log_rest = 0.0f;
+        float ms = 0.0f, m = 0.0f, log_s = 0.0f, log_rest = 0.0f, log_p_rest = 0.0f;
         bool empty = false;
         if (first_wave) {
             float s_rest;
@@ -329,11 +333,17 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
             ms = m == -kInf ? 0.0f : m;
             const float s_list = wave_sum((en.first[0] ? expf((en.x[0] - ms) * p.scale) : 0.0f) +
                                           (en.first[1] ? expf((en.x[1] - ms) * p.scale) : 0.0f));
-            const float s_all =
-                s_list + (m_rest == -kInf ? s_rest : s_rest * expf((m_rest - ms) * p.scale));
+            const float s_part =
+                m_rest == -kInf ? s_rest : s_rest * expf((m_rest - ms) * p.scale);
+            const float s_all = s_list + s_part;
             empty = m == -kInf && s_all == 0.0f;
             log_s = l.bad ? __builtin_nanf("") : empty ? 0.0f : logf(s_all);
             log_rest = m_rest == -kInf && s_rest == 0.0f ? 0.0f : logf(s_rest);
+            // log p_R from the ratio, unless that vanishes: the logarithms' difference would
+            // carry their own roundings into a loss that is small against them
+            const float share = s_part / s_all;
+            log_p_rest = share > 1e-30f ? logf(share)
+                                        : (m_rest - ms) * p.scale + log_rest - log_s;
             if constexpr (PHASE == kStep) gradient_constants(p, r, l, m, log_s, m_rest, log_rest);
         }
         if constexpr (PHASE == kStep) __syncthreads();
@@ -348,7 +358,7 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
             float loss = wave_sum(term);
             const float q_rest = l.q_rest;
             if (q_rest > 0.0f && m_rest != -kInf)
-                loss += q_rest * (logf(q_rest) - ((m_rest - ms) * p.scale + log_rest - log_s));
+                loss += q_rest * (logf(q_rest) - log_p_rest);
             if (l.bad) loss = __builtin_nanf("");
             if (t == 0) {
                 p.loss[r] = loss;
