@@ -335,6 +335,11 @@ __device__ __forceinline__ bool arrive_last(uint32_t* counter, int segs, int* ld
 }
 
 // ---- host: how rows are laid out over workgroups -------------------------------------
+// At most 32 segments a row: a wave joins them, and with SYMTILE_TOP_MAX keys each
+// their keys fit LDS; SYMTILE_VOCAB_MAX is what 32 segments of 16384 vectors hold.
+constexpr int kMaxSegments = 32;
+static_assert(SYMTILE_VOCAB_MAX <= kMaxSegments * 16 * kMaxThreads * 4, "a row fits its segments");
+
 // segs workgroups a row, each of `threads` threads with nv vectors of 16 bytes,
 // of seg_len elements (the last may have fewer).
 struct Plan {
@@ -365,7 +370,9 @@ inline void shape(int n, bool alone, int* nv, int* threads) {
 inline Plan make_plan(int device, int rows, int vocab, int dtype, bool grad) {
     const int vec = dtype == SYMTILE_F32 ? 4 : 8;
     const int n = (vocab + vec - 1) / vec;
-    const int most = grad && n <= 16 * kMaxThreads ? 16 * kMaxThreads : 4096;
+    const int most = grad && n <= 16 * kMaxThreads
+                         ? 16 * kMaxThreads
+                         : std::max(4096, (n + kMaxSegments - 1) / kMaxSegments);
     const int segs = (n + most - 1) / most;
     Plan p;
     const int per = (n + segs - 1) / segs;

@@ -164,6 +164,51 @@ def test_logprobs_of_long_and_many_rows(dtype, rows, vocab, top):
         check_logprobs(op, x, targets, np.float32(0.9).item(), top)
 
 
+@pytest.mark.parametrize("dtype,vocab", [("f32", 1 << 21), ("bf16", 1 << 21), ("f32", 1300007)])
+def test_the_longest_rows(dtype, vocab):
+    """As many segments as a row can have: values, top entries, both gradients."""
+    pkg = sym()
+    x = normal_rows(2, vocab, dtype, 3)
+    x[1, 5:] = -INF                                     # all but the first segment's are masked
+    targets = torch.tensor([vocab - 1, 2])
+    g = [torch.randn((2,), generator=gen(k)) for k in range(3)]
+    op = pkg.TokenLogprobs(2, vocab, TD[dtype], top=128)
+    dl = torch.empty((2, vocab), dtype=TD[dtype], device="cuda")
+    op.run(x.cuda(), targets.cuda(), dl, *[t.cuda() for t in g])
+    check_logprobs(op, x, targets, 1.0, 128)
+    check_logprob_grad(dl, x, targets, 1.0, g, dtype)
+    ids, values = op.top_ids.cpu(), op.top_logprobs.cpu()
+    kd = pkg.TopDistillation(2, vocab, TD[dtype], 128, rest=True)
+    kd.run(x.cuda(), ids.cuda(), values.cuda(), g[0].cuda(), dl)
+    check_distill(kd.loss, dl, x, ids, values, 1.0, True, g[0], dtype)
+    with pytest.raises(pkg.SymtileError):
+        pkg.TokenLogprobs(1, (1 << 21) + 1, TD[dtype])
+
+
+def test_rows_past_32_bits():
+    """The third row starts 2^32 elements into its memory."""
+    pkg = sym()
+    ld, vocab = 1 << 31, 1000
+    mem = torch.empty(2 * ld + vocab, dtype=torch.bfloat16, device="cuda")
+    dx = mem.as_strided((3, vocab), (ld, 1))
+    x = normal_rows(3, vocab, "bf16", 3)
+    dx.copy_(x)
+    targets = torch.tensor([5, 999, 0])
+    g = [torch.randn((3,), generator=gen(k)) for k in range(3)]
+    op = pkg.TokenLogprobs(3, vocab, torch.bfloat16, top=7)
+    dl = torch.empty((3, vocab), dtype=torch.bfloat16, device="cuda")
+    op.run(dx, targets.cuda(), dl, *[t.cuda() for t in g])
+    check_logprobs(op, x, targets, 1.0, 7)
+    check_logprob_grad(dl, x, targets, 1.0, g, "bf16")
+    op.backward(dx, targets.cuda(), dx, *[t.cuda() for t in g])          # in place
+    check_logprob_grad(dx, x, targets, 1.0, g, "bf16")
+    dx.copy_(x)
+    ids, values = teacher_list(x, 9, 4, False)
+    kd = pkg.TopDistillation(3, vocab, torch.bfloat16, 9)
+    kd.run(dx, ids.cuda(), values.cuda(), g[0].cuda(), dx)
+    check_distill(kd.loss, dx, x, ids, values, 1.0, False, g[0], "bf16")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("vocab", [40000, 70000])
 def test_long_special_rows(dtype, vocab):

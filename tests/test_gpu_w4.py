@@ -126,6 +126,54 @@ def test_products(shape, dtype, zeros):
     c.check(rank, expected(*t, group), dtype, walk(t[0], t[2], K), calls=2)
 
 
+BUILDS = [  # long columns and many tiles: every build and its rest at the ends of K and N
+    (1, 16416, 24, 2, 0, 32), (2, 24640, 40, 1, 0, 128), (4, 544, 4360, 2, 1, 64), (3, 8224, 4104, 1, 0, 128),
+    (16, 16416, 40, 2, 1, 64), (9, 544, 4360, 2, 0, 32), (16, 8224, 4104, 1, 0, 128), (13, 20512, 4104, 1, 0, 64),
+    (20, 16416, 72, 2, 0, 32), (32, 8224, 136, 1, 0, 128), (17, 160, 4360, 1, 0, 64), (50, 12320, 104, 2, 1, 128),
+    (64, 8224, 4104, 1, 0, 64), (33, 24640, 24, 1, 0, 32)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("shape", BUILDS, ids=lambda s: "m%d_k%d_n%d_w%d_r%d_g%d" % s)
+def test_long_columns_and_many_tiles(shape, dtype):
+    M, K, N, world, rank, group = shape
+    t = inputs(M, K, N, dtype, group, True, M + K + N)
+    want, bound = expected(*t, group), walk(t[0], t[2], K)
+    c = Call(M, N, world, dtype, t, group)
+    for calls in (1, 2):                 # the second runs on what the first left in the workspace
+        c.out.C_all().view(torch.int16).fill_(-1)
+        c.run(rank)
+        c.check(rank, want, dtype, bound, calls=calls)
+
+
+@pytest.mark.parametrize("M,K,N", [(24, 2048, 136), (64, 8192, 200)])
+def test_without_a_workspace(M, K, N):
+    """The C call without a workspace does not split K; a workspace too small is refused."""
+    pkg = sym()
+    t = inputs(M, K, N, "bf16", 64, True, 3, whole=True)
+    c = Call(M, N, 2, "bf16", t, 64)
+    args = [c.heap.handle, c.X.data_ptr(), c.w.q.data_ptr(), c.w.scales.data_ptr(), c.w.zeros.data_ptr(),
+            c.heap.ptr(1, c.out.c_off), c.heap.ptr(1, c.out.flag_off), M, N, K, 0, 64, pkg.BF16, 1, 2]
+    need = pkg.symtile_w4_workspace_bytes(0, M, N, K, 64)
+    assert need > 0 and need % 16 == 0
+    ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    with pytest.raises(pkg.SymtileError) as e:
+        pkg.symtile_w4_all_scatter(*args, ws.data_ptr(), need - 1, pkg.current_stream())
+    assert e.value.name == "EINVAL"
+    with pytest.raises(pkg.SymtileError):
+        pkg.symtile_w4_all_scatter(*args, ws.data_ptr() + 8, need, pkg.current_stream())
+    pkg.symtile_w4_all_scatter(*args, stream=pkg.current_stream())
+    c.check(1, expected(*t, 64), "bf16", None)
+    for bad in ((0, -1, N, K, 64), (0, M, N, 48, 64), (0, M, 12, K, 64), (0, M, N, K, 96)):
+        with pytest.raises(pkg.SymtileError) as e:
+            pkg.symtile_w4_workspace_bytes(*bad)
+        assert e.value.name == "EINVAL", bad
+    with pytest.raises(pkg.SymtileError) as e:
+        pkg.symtile_w4_workspace_bytes(0, 65, N, K, 64)
+    assert e.value.name == "EUNSUPPORTED"
+    assert pkg.symtile_w4_workspace_bytes(0, 0, N, K, 64) == 0
+
+
 @pytest.mark.parametrize("M,dtype", [(1, "bf16"), (16, "f16"), (64, "bf16")])
 def test_the_large_layer(M, dtype):
     K, N, world, rank, group = 8192, 3584, 8, 3, 128
