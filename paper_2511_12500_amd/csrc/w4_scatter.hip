@@ -278,18 +278,32 @@ __device__ __forceinline__ uint16_t rounded(float v) {
     else return __builtin_bit_cast(uint16_t, (_Float16)v);
 }
 
+// The bases of the slots that a wave stores into, asked for where the kernel begins.
+template <int WAVES>
+__device__ __forceinline__ void slot_bases(const W4Params& p, uint64_t* bases) {
+    static_assert(SYMTILE_MAX_WORLD % WAVES == 0 && WAVES <= SYMTILE_MAX_WORLD, "slots by waves");
+#pragma unroll
+    for (int i = 0; i < SYMTILE_MAX_WORLD / WAVES; ++i)
+        bases[i] = p.bases[min((int)threadIdx.x / 64 + i * WAVES, p.world - 1)];
+}
+
 // A wave stores rows x 8 `vecs` columns of `out` (row stride `ld` values) into column
 // `col` of its slots' blocks and counts them as `tiles` tiles from `tile` on: the
 // wave's own stores' acknowledgements are all that its counters have to wait for.
-__device__ __forceinline__ void store_slots(const W4Params& p, const uint16_t* out, int ld, int col,
-                                            int vecs, int tile, int tiles, int waves) {
+// `bases`: see slot_bases.
+template <int WAVES>
+__device__ __forceinline__ void store_slots(const W4Params& p, const uint64_t* bases,
+                                            const uint16_t* out, int ld, int col, int vecs,
+                                            int tile, int tiles) {
     const int lane = threadIdx.x % 64;
-    for (int slot = threadIdx.x / 64; slot < p.world; slot += waves) {
-        char* base = reinterpret_cast<char*>(p.bases[slot]);
+#pragma unroll
+    for (int i = 0; i < SYMTILE_MAX_WORLD / WAVES; ++i) {
+        if ((int)threadIdx.x / 64 + i * WAVES >= p.world) break;
+        char* base = reinterpret_cast<char*>(bases[i]);
         const symtile::rsrc_t dst = symtile::make_rsrc(
             base + p.c_off + (size_t)col * 2, (uint32_t)(((size_t)(p.M - 1) * p.ldc + vecs * 8) * 2));
-        for (int i = lane; i < p.M * vecs; i += 64) {
-            const int m = i / vecs, v = i - m * vecs;
+        for (int e = lane; e < p.M * vecs; e += 64) {
+            const int m = e / vecs, v = e - m * vecs;
             symtile::buf_st16p<symtile::kStoreWriteThrough>(
                 symtile::ld16(out + m * ld + v * 8), dst, (uint32_t)(m * p.ldc + v * 8) * 2, 0);
         }
@@ -337,7 +351,7 @@ struct Block {
 
 // One workgroup per NT tiles of 16 columns and up to 4 XL rows; its waves share the
 // blocks of K, in pairs, so that a wave reads whole 128-byte lines of its columns.
-// A wave works on U blocks while U more are on their way.
+// A wave works on U blocks while U to 2 U more are on their way.
 template <bool BF, int XL, int NT, int GROUP, int U, int WAVES, int PER_SIMD>
 __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
     typedef Block<BF, XL, NT, GROUP> B;
@@ -350,6 +364,8 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
     __shared__ typename S::Table scales;
     const int tile0 = blockIdx.x * NT, t = threadIdx.x, wave = t / 64, lane = t % 64;
     const int w0 = __builtin_amdgcn_readfirstlane(wave);
+    uint64_t bases[SYMTILE_MAX_WORLD / WAVES];
+    slot_bases<WAVES>(p, bases);
     f32x4 total[NT][MT] = {};
     const Source<XL, NT> src(p, tile0 * kTileN);
     const Nibbles<BF> nibbles;
@@ -378,15 +394,16 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
         S s;
         s.fetch(p, tile0 * kTileN, chunk / GROUP);
         fetch(a, 0);
+        fetch(b, U);
         if (chunk) __syncthreads();   // the scales before are used up
         s.place(p, tile0 * kTileN, chunk / GROUP, scales);
         __syncthreads();
         for (int u = 0; block_of(u) < blocks; u += 2 * U) {
-            fetch(b, u + U);
             use(a, u);
-            if (block_of(u + U) >= blocks) break;
             fetch(a, u + 2 * U);
+            if (block_of(u + U) >= blocks) break;
             use(b, u + U);
+            fetch(b, u + 3 * U);
         }
     }
     // the waves' sums, tile by tile
@@ -408,8 +425,8 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
             out[o / 256 * 16 + row_of(o % 256)][column_of(o % 256)] = rounded<BF>(v);
         }
         __syncthreads();
-        store_slots(p, &out[0][0], kTileN, tile * kTileN, p.N - tile * kTileN >= kTileN ? 2 : 1,
-                    tile, 1, WAVES);
+        store_slots<WAVES>(p, bases, &out[0][0], kTileN, tile * kTileN,
+                           p.N - tile * kTileN >= kTileN ? 2 : 1, tile, 1);
     }
 }
 
@@ -465,6 +482,8 @@ __global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(
     const int steps = (p.K + kStepK - 1) / kStepK;
     const int first = split * p.part_steps, end = min(steps, first + p.part_steps);
     const int end_k = min(p.K, end * kStepK);
+    uint64_t bases[1];
+    slot_bases<kWideThreads / 64>(p, bases);
 
     const symtile::i32x4_t xr =
         symtile::make_rsrc_words(p.X, (uint32_t)(((p.M - 1) * p.ldx + p.K) * 2));
@@ -608,8 +627,8 @@ __global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(
                 lds.end.out[16 * i + 4 * g + e][tile * kTileN + c] = rounded<BF>(total[0][i][e]);
     }
     __syncthreads();
-    store_slots(p, &lds.end.out[0][0], kWideCols, n0, cols / 8, group * kWideTiles,
-                (cols + kTileN - 1) / kTileN, kWideThreads / 64);
+    store_slots<kWideThreads / 64>(p, bases, &lds.end.out[0][0], kWideCols, n0, cols / 8,
+                                   group * kWideTiles, (cols + kTileN - 1) / kTileN);
 }
 
 // ---- host ------------------------------------------------------------------------------
@@ -639,8 +658,8 @@ template <bool BF, int GROUP>
 Build build_for(int M, int tiles, int cus) {
     if (M <= 4)
         return tiles > cus ? build_of<BF, 1, 1, GROUP, 2, 4, 8>()
-                                : build_of<BF, 1, 1, GROUP, 2, 8, 8>();
-    if (M <= 16 && tiles <= cus) return build_of<BF, 4, 1, GROUP, 2, 8, 4>();
+                                : build_of<BF, 1, 1, GROUP, 2, 8, 4>();
+    if (M <= 16 && tiles <= cus) return build_of<BF, 4, 1, GROUP, 1, 8, 2>();
     if (M <= 16) return wide_of<BF, 1, GROUP>();
     if (M <= 32) return wide_of<BF, 2, GROUP>();
     return wide_of<BF, 4, GROUP>();

@@ -45,7 +45,7 @@ def _matrix(t: torch.Tensor, name: str, rows: int, cols: int, dtype: torch.dtype
     """Row stride in elements of a device matrix with contiguous rows."""
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if not t.is_cuda or tuple(t.shape) != (rows, cols):
+    if not t.is_cuda or t.shape != (rows, cols):
         raise ValueError(f"{name} must be a [{rows}, {cols}] device tensor")
     if cols > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must have contiguous rows")
@@ -61,7 +61,7 @@ def _vector(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.dtype)
         return None
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if not t.is_cuda or tuple(t.shape) != shape or not t.is_contiguous():
+    if not t.is_cuda or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous device tensor {list(shape)}")
     return t.data_ptr()
 
