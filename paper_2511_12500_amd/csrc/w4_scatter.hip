@@ -199,70 +199,61 @@ struct StagedX {
 // `x_end` (its 8 values): the others' offsets are set outside of the resource and
 // read as zeros, without a branch, so that the loads of several blocks are in
 // flight together.  What is behind K is multiplied with zeros of X.
-template <int XL, int NT>
+template <int XL>
 struct Source {
     symtile::rsrc_t x, w;
-    uint32_t at_x[XL], at_w[NT];   // bytes
+    uint32_t at_x[XL], at_w;   // bytes
     int w_end, x_end;
 
     __device__ __forceinline__ Source(const W4Params& p, int n0) {
         const int lane = threadIdx.x % 64, c = lane % 16, g = lane / 16;
-        const int cols = min(NT * kTileN, p.N - n0);
+        const int cols = min(kTileN, p.N - n0);
         x = symtile::make_rsrc(p.X, (uint32_t)(((p.M - 1) * p.ldx + p.K) * 2));
         w = symtile::make_rsrc(p.q + (size_t)n0 * (p.K / 2), (uint32_t)(cols * (p.K / 2)));
 #pragma unroll
         for (int i = 0; i < XL; ++i)
             at_x[i] = (uint32_t)(min(4 * i + g, p.M - 1) * p.ldx + 8 * c) * 2;
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-            at_w[i] = (uint32_t)(min(i * kTileN + c, cols - 1) * (p.K / 2) + 16 * g);
+        at_w = (uint32_t)(min(c, cols - 1) * (p.K / 2) + 16 * g);
         w_end = (p.K - 32 * g + kBlockK - 1) / kBlockK;
         x_end = (p.K - 8 * c + kBlockK - 1) / kBlockK;
     }
 };
 
-// A block of 128 weights of NT tiles of 16 columns times the rows of X in `staged`,
-// added to `total` with the groups' scales: `of_block` points at the first group's in
-// this lane's column of the first tile, `stride` columns before the next group's.
-// Lane (c = lane % 16, g = lane / 16) holds column c's weights 32 g .. 32 g + 31.
-// With one group a block, matrix instruction j takes word j of every lane; with
-// more, the words are transposed between the quarters of the wave, so that
-// instruction j has the weights 32 j .. 32 j + 31 and a group's are in instructions
-// of their own.
-template <bool BF, int NT, int MT, int GROUP, bool APART>
-__device__ __forceinline__ void multiply_block(f32x4 (&total)[NT][MT], const Nibbles<BF>& q,
-                                               const symtile::u32x4 (&w)[NT],
-                                               const uint32_t* of_block, int stride,
-                                               const StagedX<MT>& staged) {
+// A block of 128 weights of 16 columns times the rows of X in `staged`, added to
+// `total` with the groups' scales: `of_block` points at the first group's in this
+// lane's column, `stride` columns before the next group's.  Lane (c = lane % 16,
+// g = lane / 16) holds column c's weights 32 g .. 32 g + 31.  With one group a block,
+// matrix instruction j takes word j of every lane; with more, the words are transposed
+// between the quarters of the wave, so that instruction j has the weights
+// 32 j .. 32 j + 31 and a group's are in instructions of their own.  APART: X is in the
+// order of Nibbles::apart.
+template <bool BF, int MT, int GROUP, bool APART>
+__device__ __forceinline__ void multiply_block(f32x4 (&total)[MT], const Nibbles<BF>& q,
+                                               const symtile::u32x4& w, const uint32_t* of_block,
+                                               int stride, const StagedX<MT>& staged) {
     const int c = threadIdx.x % 16, g = threadIdx.x % 64 / 16;
-    symtile::u32x4 words[NT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) words[i] = GROUP == kBlockK ? w[i] : transpose_quarters(w[i]);
-    f32x4 acc[NT][MT];
+    const symtile::u32x4 words = GROUP == kBlockK ? w : transpose_quarters(w);
+    f32x4 acc[MT];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         symtile::u32x4 xs[MT];
         const int v = GROUP == kBlockK ? 4 * g + j : 4 * j + g;
 #pragma unroll
         for (int t = 0; t < MT; ++t) xs[t] = staged.v[16 * t + c][v ^ c];
+        const uint32_t of = of_block[j * 32 / GROUP * stride];
+        const uint32_t z = Nibbles<BF>::minus_offset(of >> 16);
+        const symtile::u32x4 zs = {z, z, z, z};
+        const symtile::u32x4 ws = APART ? q.apart(words[j]) : q.adjacent(words[j]);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const uint32_t of = of_block[j * 32 / GROUP * stride + n * kTileN];
-            const uint32_t z = Nibbles<BF>::minus_offset(of >> 16);
-            const symtile::u32x4 zs = {z, z, z, z};
-            const symtile::u32x4 ws = APART ? q.apart(words[n][j]) : q.adjacent(words[n][j]);
+        for (int t = 0; t < MT; ++t) {
+            f32x4& a = acc[t];
+            if (j * 32 % GROUP == 0) a = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            a = mfma<BF>(xs[t], zs, a);
+            a = mfma<BF>(xs[t], ws, a);
+            if ((j + 1) * 32 % GROUP == 0) {
+                const float sc = scale_value<BF>(of & 0xFFFFu);
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                f32x4& a = acc[n][t];
-                if (j * 32 % GROUP == 0) a = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                a = mfma<BF>(xs[t], zs, a);
-                a = mfma<BF>(xs[t], ws, a);
-                if ((j + 1) * 32 % GROUP == 0) {
-                    const float sc = scale_value<BF>(of & 0xFFFFu);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        total[n][t][e] = __builtin_fmaf(sc, a[e], total[n][t][e]);
-                }
+                for (int e = 0; e < 4; ++e) total[t][e] = __builtin_fmaf(sc, a[e], total[t][e]);
             }
         }
     }
@@ -313,61 +304,63 @@ __device__ __forceinline__ void store_slots(const W4Params& p, const uint64_t* b
     }
 }
 
-// One block of 128 weights of NT tiles of 16 columns in registers, with what it is
-// multiplied by.  X comes by rows, 256 bytes of four rows a load (XL of
-// them), and takes the matrix operands' layout in LDS: loading operands directly
-// reads 64 bytes of 16 rows, whose distance is often a power of two, from one cache
-// channel (64 tokens through 8192x3584: 36 us).
-template <bool BF, int XL, int NT, int GROUP>
+// ---- up to 16 rows -----------------------------------------------------------------
+// One block of 128 weights of 16 columns in registers, with what it is multiplied by.
+// X comes by rows, 256 bytes of four rows a load (XL of them), and takes the matrix
+// operands' layout in LDS: loading operands directly reads 64 bytes of 16 rows, whose
+// distance is often a power of two, from one cache channel.
+template <bool BF, int XL, int GROUP>
 struct Block {
-    static constexpr int MT = (XL + 3) / 4;       // tiles of 16 rows
-    static constexpr bool kApart = XL <= 4 * NT;  // X reordered for Nibbles::apart: 4 XL
-                                                  // instructions for 16 NT fewer on weights
-    symtile::u32x4 w[NT];
+    static_assert(XL <= 4, "one tile of 16 rows");
+    symtile::u32x4 w;
     symtile::u32x4 x[XL];    // rows 4 i + g, values 8 c .. 8 c + 7
 
-    __device__ __forceinline__ void load(const Source<XL, NT>& s, int block) {
+    __device__ __forceinline__ void load(const Source<XL>& s, int block) {
         const int k0 = block * kBlockK;
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-            w[i] = symtile::buf_ld16p<symtile::kLoadStream>(
-                s.w, block < s.w_end ? s.at_w[i] : symtile::kOOB, k0 / 2);
+        w = symtile::buf_ld16p<symtile::kLoadStream>(
+            s.w, block < s.w_end ? s.at_w : symtile::kOOB, k0 / 2);
 #pragma unroll
         for (int i = 0; i < XL; ++i)
             x[i] = symtile::buf_ld16(s.x, block < s.x_end ? s.at_x[i] : symtile::kOOB, k0 * 2);
     }
 
-    __device__ __forceinline__ void multiply(f32x4 (&total)[NT][MT], const Nibbles<BF>& q,
-                                             const uint32_t* of_block, StagedX<MT>& staged) const {
+    // X in the order of Nibbles::apart: 4 XL instructions a block for 16 fewer on weights.
+    __device__ __forceinline__ void multiply(f32x4 (&total)[1], const Nibbles<BF>& q,
+                                             const uint32_t* of_block, StagedX<1>& staged) const {
         const int c = threadIdx.x % 16, g = threadIdx.x % 64 / 16;
 #pragma unroll
         for (int i = 0; i < XL; ++i)
-            staged.v[4 * i + g][c ^ (4 * i + g) % 16] = kApart ? interleave(x[i]) : x[i];
+            staged.v[4 * i + g][c ^ (4 * i + g)] = interleave(x[i]);
         __builtin_amdgcn_wave_barrier();   // the wave reads what its lanes wrote
-        multiply_block<BF, NT, MT, GROUP, kApart>(total, q, w, of_block, NT * kTileN, staged);
+        multiply_block<BF, 1, GROUP, true>(total, q, w, of_block, kTileN, staged);
         __builtin_amdgcn_wave_barrier();   // the next block's X is written after these reads
     }
 };
 
-// One workgroup per NT tiles of 16 columns and up to 4 XL rows; its waves share the
-// blocks of K, in pairs, so that a wave reads whole 128-byte lines of its columns.
-// A wave works on U blocks while U to 2 U more are on their way.
-template <bool BF, int XL, int NT, int GROUP, int U, int WAVES, int PER_SIMD>
+// One workgroup per 16 columns and up to 4 XL rows; its waves share the blocks of K, in
+// pairs, so that a wave reads whole 128-byte lines of its columns.  A wave works on U
+// blocks while U to 2 U more are on their way.
+//
+// Bound by the weights' bytes on a long N (one row through 8192x28672: @A@ us, 3.7 TB/s)
+// and by latency on a short one (8192x3584: 7.2 us, of which an empty kernel takes 2.9):
+// so the loads of the first 2 U blocks are asked for before the scales, whose place in
+// LDS is a barrier, and with them the slots' addresses.
+template <bool BF, int XL, int GROUP, int U, int WAVES, int PER_SIMD>
 __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
-    typedef Block<BF, XL, NT, GROUP> B;
-    constexpr int MT = B::MT, kThreads = 64 * WAVES;
-    typedef float Partial[MT][256];
-    static_assert(sizeof(Partial) <= sizeof(StagedX<MT>), "a wave's sums take its X's place");
-    __shared__ StagedX<MT> staged[WAVES];
-    __shared__ __attribute__((aligned(16))) uint16_t out[16 * MT][kTileN];
-    typedef Scales<GROUP, NT, kChunkK, kThreads> S;
+    typedef Block<BF, XL, GROUP> B;
+    constexpr int kThreads = 64 * WAVES;
+    typedef float Partial[256];
+    static_assert(sizeof(Partial) <= sizeof(StagedX<1>), "a wave's sums take its X's place");
+    __shared__ StagedX<1> staged[WAVES];
+    __shared__ __attribute__((aligned(16))) uint16_t out[16][kTileN];
+    typedef Scales<GROUP, 1, kChunkK, kThreads> S;
     __shared__ typename S::Table scales;
-    const int tile0 = blockIdx.x * NT, t = threadIdx.x, wave = t / 64, lane = t % 64;
+    const int tile = blockIdx.x, t = threadIdx.x, wave = t / 64, lane = t % 64;
     const int w0 = __builtin_amdgcn_readfirstlane(wave);
     uint64_t bases[SYMTILE_MAX_WORLD / WAVES];
     slot_bases<WAVES>(p, bases);
-    f32x4 total[NT][MT] = {};
-    const Source<XL, NT> src(p, tile0 * kTileN);
+    f32x4 total[1] = {};
+    const Source<XL> src(p, tile * kTileN);
     const Nibbles<BF> nibbles;
     for (int chunk = 0; chunk < p.K; chunk += kChunkK) {
         const int first = chunk / kBlockK;
@@ -392,11 +385,11 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
             }
         };
         S s;
-        s.fetch(p, tile0 * kTileN, chunk / GROUP);
+        s.fetch(p, tile * kTileN, chunk / GROUP);
         fetch(a, 0);
         fetch(b, U);
         if (chunk) __syncthreads();   // the scales before are used up
-        s.place(p, tile0 * kTileN, chunk / GROUP, scales);
+        s.place(p, tile * kTileN, chunk / GROUP, scales);
         __syncthreads();
         for (int u = 0; block_of(u) < blocks; u += 2 * U) {
             use(a, u);
@@ -406,31 +399,21 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
             fetch(b, u + 3 * U);
         }
     }
-    // the waves' sums, tile by tile
+    // the waves' sums, in the order of the waves
+    *reinterpret_cast<f32x4*>(&reinterpret_cast<Partial&>(staged[wave])[4 * lane]) = total[0];
+    __syncthreads();
+    if (t < 256) {
+        float v = 0.0f;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int tile = tile0 + n;
-        if (tile * kTileN >= p.N) break;
-        if (n) __syncthreads();   // the sums and the output of the tile before are read
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-            *reinterpret_cast<f32x4*>(&(reinterpret_cast<Partial&>(staged[wave]))[i][4 * lane]) =
-                total[n][i];
-        __syncthreads();
-        for (int o = t; o < 256 * MT; o += kThreads) {
-            float v = 0.0f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w)
-                v += reinterpret_cast<const Partial&>(staged[w])[o / 256][o % 256];
-            out[o / 256 * 16 + row_of(o % 256)][column_of(o % 256)] = rounded<BF>(v);
-        }
-        __syncthreads();
-        store_slots<WAVES>(p, bases, &out[0][0], kTileN, tile * kTileN,
-                           p.N - tile * kTileN >= kTileN ? 2 : 1, tile, 1);
+        for (int w = 0; w < WAVES; ++w) v += reinterpret_cast<const Partial&>(staged[w])[t];
+        out[row_of(t)][column_of(t)] = rounded<BF>(v);
     }
+    __syncthreads();
+    store_slots<WAVES>(p, bases, &out[0][0], kTileN, tile * kTileN,
+                       p.N - tile * kTileN >= kTileN ? 2 : 1, tile, 1);
 }
 
-// ---- over 4 rows -------------------------------------------------------------------
+// ---- up to 64 rows -----------------------------------------------------------------
 // A workgroup takes 64 columns: four of its eight waves 16 columns each, the other
 // four the same columns' other half of every step of K.  X of a step goes to LDS once
 // for all of them.  (Where a workgroup takes 16 columns, every workgroup reads all of
@@ -522,7 +505,7 @@ __global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(
             symtile::buf_ld16_lds_async(
                 xr, to + to_x[u], at_x[u] | ((uint32_t)(end_k - 1 - k0 - k_x[u]) & symtile::kOOB), k0 * 2);
     };
-    f32x4 total[1][MT] = {};
+    f32x4 total[MT] = {};
     const Nibbles<BF> nibbles;
     if (first < end) {
         S s;
@@ -549,12 +532,11 @@ __global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(
                 const Stage& now = lds.ring[stage];
 #pragma unroll
                 for (int i = 0; i < CB; ++i) {
-                    const symtile::u32x4 w[1] = {now.w[wave][i][lane]};
                     const int block = half * CB + i;
                     const int of = ((step - base) * 2 * CB + block) * (kBlockK / GROUP);
-                    multiply_block<BF, 1, MT, GROUP, false>(total, nibbles, w,
-                                                            &scales[of][tile * kTileN + c],
-                                                            kWideCols, now.x[block]);
+                    multiply_block<BF, MT, GROUP, false>(total, nibbles, now.w[wave][i][lane],
+                                                         &scales[of][tile * kTileN + c],
+                                                         kWideCols, now.x[block]);
                 }
                 stage = stage + 1 == kStages ? 0 : stage + 1;
                 next = next + 1 == kStages ? 0 : next + 1;
@@ -568,13 +550,13 @@ __global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(
     if (half == 1) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
-            *reinterpret_cast<f32x4*>(&lds.end.sums[tile][i][4 * lane]) = total[0][i];
+            *reinterpret_cast<f32x4*>(&lds.end.sums[tile][i][4 * lane]) = total[i];
     }
     __syncthreads();
     if (half == 0) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
-            total[0][i] += *reinterpret_cast<const f32x4*>(&lds.end.sums[tile][i][4 * lane]);
+            total[i] += *reinterpret_cast<const f32x4*>(&lds.end.sums[tile][i][4 * lane]);
     }
     if (p.splits > 1) {
         // [column group][split][tile][row tile][4 * lane + i]
@@ -585,7 +567,7 @@ __global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(
 #pragma unroll
             for (int i = 0; i < MT; ++i)
                 symtile::buf_st16p<symtile::kStoreWriteThrough>(
-                    __builtin_bit_cast(symtile::u32x4, total[0][i]), to, (uint32_t)(i * 1024 + lane * 16), 0);
+                    __builtin_bit_cast(symtile::u32x4, total[i]), to, (uint32_t)(i * 1024 + lane * 16), 0);
         }
         symtile::wg_stores_done();
         if (t == 0) {
@@ -606,7 +588,7 @@ __global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(
                 p.partials + ((size_t)group * p.splits * kWideTiles + tile) * MT * 256,
                 (uint32_t)(((p.splits - 1) * kPart + MT * 256) * 4));
 #pragma unroll
-            for (int i = 0; i < MT; ++i) total[0][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int i = 0; i < MT; ++i) total[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             for (int s = 0; s < p.splits; ++s) {
                 f32x4 part[MT];
 #pragma unroll
@@ -615,7 +597,7 @@ __global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(
                         f32x4, symtile::buf_ld16p<symtile::kLoadCoherent>(
                                    from, (uint32_t)(i * 1024 + lane * 16), s * kPart * 4));
 #pragma unroll
-                for (int i = 0; i < MT; ++i) total[0][i] += part[i];
+                for (int i = 0; i < MT; ++i) total[i] += part[i];
             }
         }
     }
@@ -624,7 +606,7 @@ __global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                lds.end.out[16 * i + 4 * g + e][tile * kTileN + c] = rounded<BF>(total[0][i][e]);
+                lds.end.out[16 * i + 4 * g + e][tile * kTileN + c] = rounded<BF>(total[i][e]);
     }
     __syncthreads();
     store_slots<kWideThreads / 64>(p, bases, &lds.end.out[0][0], kWideCols, n0, cols / 8,
@@ -637,10 +619,10 @@ struct Build {
     int waves, tiles;   // waves and tiles of a workgroup
     int step_k;         // of the wide kernel; 0 = the other one
 };
-template <bool BF, int XL, int NT, int GROUP, int U, int WAVES, int PER_SIMD>
+template <bool BF, int XL, int GROUP, int U, int WAVES, int PER_SIMD>
 Build build_of() {
-    return {reinterpret_cast<const void*>(&w4_kernel<BF, XL, NT, GROUP, U, WAVES, PER_SIMD>), WAVES,
-            NT, 0};
+    return {reinterpret_cast<const void*>(&w4_kernel<BF, XL, GROUP, U, WAVES, PER_SIMD>), WAVES, 1,
+            0};
 }
 template <bool BF, int MT, int GROUP>
 Build wide_of() {
@@ -657,9 +639,9 @@ Build wide_of() {
 template <bool BF, int GROUP>
 Build build_for(int M, int tiles, int cus) {
     if (M <= 4)
-        return tiles > cus ? build_of<BF, 1, 1, GROUP, 2, 4, 8>()
-                                : build_of<BF, 1, 1, GROUP, 2, 8, 4>();
-    if (M <= 16 && tiles <= cus) return build_of<BF, 4, 1, GROUP, 1, 8, 2>();
+        return tiles > cus ? build_of<BF, 1, GROUP, 2, 4, 8>()
+                                : build_of<BF, 1, GROUP, 2, 8, 4>();
+    if (M <= 16 && tiles <= cus) return build_of<BF, 4, GROUP, 1, 8, 2>();
     if (M <= 16) return wide_of<BF, 1, GROUP>();
     if (M <= 32) return wide_of<BF, 2, GROUP>();
     return wide_of<BF, 4, GROUP>();
