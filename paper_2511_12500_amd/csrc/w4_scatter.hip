@@ -589,15 +589,23 @@ __global__ void __launch_bounds__(kWideThreads, MT == 1 ? 4 : 2) w4_wide_kernel(
                 (uint32_t)(((p.splits - 1) * kPart + MT * 256) * 4));
 #pragma unroll
             for (int i = 0; i < MT; ++i) total[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            for (int s = 0; s < p.splits; ++s) {
-                f32x4 part[MT];
+            // four parts' loads in flight together; parts that are not there are zeros
+            for (int s0 = 0; s0 < p.splits; s0 += 4) {
+                f32x4 part[4][MT];
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
-                    part[i] = __builtin_bit_cast(
-                        f32x4, symtile::buf_ld16p<symtile::kLoadCoherent>(
-                                   from, (uint32_t)(i * 1024 + lane * 16), s * kPart * 4));
+                for (int s = 0; s < 4; ++s)
 #pragma unroll
-                for (int i = 0; i < MT; ++i) total[i] += part[i];
+                    for (int i = 0; i < MT; ++i)
+                        part[s][i] = __builtin_bit_cast(
+                            f32x4, symtile::buf_ld16p<symtile::kLoadCoherent>(
+                                       from,
+                                       s0 + s < p.splits ? (uint32_t)(i * 1024 + lane * 16)
+                                                         : symtile::kOOB,
+                                       (s0 + s) * kPart * 4));
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) total[i] += part[s][i];
             }
         }
     }
