@@ -15,6 +15,7 @@ namespace {
 
 using namespace logits;
 
+typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 constexpr int kCap = 1024;          // candidates for the top entries of a segment
 constexpr int kCapVecs = 256;       // vectors that hold the candidates in the usual case
 
@@ -47,16 +48,18 @@ struct Shared {
 };
 
 // Dynamic LDS of the top entries: keys, and the vectors that hold the candidates.
-// Before there are keys, groups' largest logits stand in their place.
+// Before there are keys, groups' largest logits stand in their place.  Behind the keys zeros fill up a step of all
+// threads that count for one key.
 struct TopLds {
+    static constexpr int kPad = 32;
     union {
         uint64_t* keys;
-        float* groups;
+        uint32_t* groups;
     };
     symtile::u32x4* vec;
     int* at;               // first element of each
     static size_t bytes(int segs, int top) {
-        return (size_t)std::max(kCap, segs * top) * 8 + kCapVecs * 20;
+        return (size_t)(std::max(kCap, segs * top) + kPad) * 8 + kCapVecs * 20;
     }
     __device__ __forceinline__ TopLds(void* base, int segs, int top) {
         vec = static_cast<symtile::u32x4*>(base);
@@ -96,91 +99,105 @@ __device__ __forceinline__ uint32_t block_count(uint32_t c, Shared& sh, int& ste
     return n;
 }
 
+// Sum over `lanes` (1, 2, 4, 8 or 16) neighbouring lanes that begin at a multiple of them.
+__device__ __forceinline__ uint32_t sum_lanes(uint32_t c, int lanes) {
+    auto add = [](uint32_t v, float o) { return v + __float_as_uint(o); };
+    if (lanes > 1) c = add(c, dpp<0xB1>(__uint_as_float(c)));
+    if (lanes > 2) c = add(c, dpp<0x4E>(__uint_as_float(c)));
+    if (lanes > 4) c = add(c, dpp<0x141>(__uint_as_float(c)));
+    if (lanes > 8) c = add(c, dpp<0x140>(__uint_as_float(c)));
+    return c;
+}
+
 // n distinct keys in LDS; calls emit(place, key) for the `keep` largest.  The
-// place is the number of larger keys, counted by up to 16 neighbouring threads a key.
+// place is the number of larger keys, counted by up to 16 neighbouring threads a key,
+// two keys a read.  All threads call it after a barrier behind the last key.
 template <class F>
-__device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int keep, F emit) {
+__device__ __forceinline__ void rank_keys(uint64_t* keys, int n, int keep, F emit) {
     const int threads = blockDim.x, t = threadIdx.x;
+    if (t < TopLds::kPad) keys[n + t] = 0;
+    __syncthreads();
     int lg = 0;
     while (lg < 4 && n << (lg + 1) <= threads) ++lg;
-    const int part = t & ((1 << lg) - 1);
+    const int lanes = 1 << lg, part = t & (lanes - 1);
     for (int i = t >> lg; i - (t >> lg) < n; i += threads >> lg) {
         const uint64_t mine = i < n ? keys[i] : ~0ull;
         uint32_t c = 0;
-        // four at a time: one after the other, each would wait for its own read
-        for (int j = part; j < n; j += 4 << lg) {
-            uint64_t k[4];
-#pragma unroll
-            for (int o = 0; o < 4; ++o) {
-                const int at = j + (o << lg);
-                k[o] = at < n ? keys[at] : 0;
-            }
-#pragma unroll
-            for (int o = 0; o < 4; ++o) c += k[o] > mine;
+        const u64x2* pairs = reinterpret_cast<const u64x2*>(keys) + part;
+        // unrolled: one after the other, each would wait for its own read
+#pragma unroll 4
+        for (int left = n; left > 0; left -= 2 * lanes, pairs += lanes) {
+            const u64x2 k = *pairs;
+            c += k[0] > mine;
+            c += k[1] > mine;
         }
-        for (int o = 1; o < 1 << lg; o *= 2) c += __shfl_xor(c, o);
+        c = sum_lanes(c, lanes);
         if (part == 0 && i < n && (int)c < keep) emit((int)c, mine);
     }
 }
 
 // The bound for the top entries: the `top`-th largest of the largest logits of groups
 // of lanes, which as many elements reach as there are groups above it, and hardly
-// more.  Groups are rows of 16 lanes, quads or single lanes, so that there are some
-// more than `top` of them.
+// more.  Groups are rows of 16 lanes, quads, pairs or single lanes, so that there are
+// some more than `top` of them.
 __device__ __forceinline__ int group_lanes(int top, int waves) {
-    return top <= 3 * waves ? 16 : top <= 14 * waves ? 4 : 1;
+    return top <= 3 * waves ? 16 : top <= 14 * waves ? 4 : top <= 28 * waves ? 2 : 1;
 }
-// By the first wave; not above the `top`-th largest, -inf where fewer groups have one.
-__device__ __forceinline__ float groups_bound(const float* groups, int n, int top) {
-    const int lane = threadIdx.x;
-    if (n <= 64) {      // how many are larger than mine?
-        const float v = lane < n ? groups[lane] : -kInf;
-        int c = 0;
-        for (int j = 0; j < n; j += 4)      // (the lanes from n on hold -inf)
+// A group's largest logit in the order of the top entries, to the bits that its index
+// leaves: distinct, so that exactly one group is the top-th.
+constexpr uint32_t kIndexBits = kMaxThreads - 1;
+__device__ __forceinline__ uint32_t group_key(float largest, int index) {
+    return (order(largest) & ~kIndexBits) | (uint32_t)index;
+}
+// The group's lanes count the groups above its own, `mine`, four a read; the group that
+// is the top-th sets sh.tau (-inf before).  All threads' work, and two instructions a
+// group: the selection is bound by the instructions of all of its steps (4096 rows of
+// 28672 bf16: @C@).
+__device__ __forceinline__ void find_bound(const uint32_t* groups, uint32_t mine, int group, int top,
+                                           Shared& sh) {
+    const int t = threadIdx.x, quads = (int)blockDim.x / group / 4, part = t % group;
+    uint32_t above = 0;
+#pragma unroll 4
+    for (int i = part; i < quads; i += group) {
+        const symtile::u32x4 g = reinterpret_cast<const symtile::u32x4*>(groups)[i];
 #pragma unroll
-            for (int o = 0; o < 4; ++o)
-                c += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), j + o)) > v;
-        return -wave_max(lane < n && c < top ? -v : -kInf);
+        for (int e = 0; e < 4; ++e) above += g[e] > mine;
     }
-    // bit by bit, to 16 bits of their order (rounded down)
-    constexpr int kEach = kMaxThreads / 64;
-    uint32_t v[kEach];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) v[i] = lane + 64 * i < n ? order(groups[lane + 64 * i]) : 0;
-    uint32_t p = 0;
-#pragma unroll 1
-    for (int b = 31; b >= 16; --b) {
-        const uint32_t trial = p | 1u << b;
-        int c = 0;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            if (64 * i >= n) break;
-            c += __popcll(__ballot(v[i] >= trial));
-        }
-        p = c >= top ? trial : p;
-    }
-    return p < 0x00800000u ? -kInf : ordered_value(p);
+    above = sum_lanes(above, group);
+    // 0x00800000: the lowest finite number's place
+    if (part == 0 && (int)above == top - 1 && mine >= 0x00800000u)
+        sh.tau = ordered_value(mine & ~kIndexBits);
 }
 
 // The thread's vectors that hold an element which reaches the bound, into LDS
-// (sh.vecs is zero before and counts them).
+// (sh.vecs is zero before and counts them).  Counted by scalar instructions, with one
+// addition to sh.vecs a wave.
 template <int DT, int NV>
 __device__ __forceinline__ void stage_candidates(const Segment<DT, NV>& d, const float* vec_max,
                                                  float tau, Shared& sh, const TopLds& top) {
-    uint32_t hits = 0;
+    uint64_t hits[NV];
+    int all = 0;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) hits |= vec_max[i] >= tau ? 1u << i : 0u;
-    if (!hits) return;
-    int place = atomicAdd(&sh.vecs, __popc(hits));
+    for (int i = 0; i < NV; ++i) {
+        hits[i] = __ballot(vec_max[i] >= tau);
+        all += __popcll(hits[i]);
+    }
+    if (!all) return;
+    int base = 0;
+    if (threadIdx.x % 64 == 0) base = atomicAdd(&sh.vecs, all);
+    base = __builtin_amdgcn_readfirstlane(base);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if (hits >> i & 1) {
-            if (place < kCapVecs) {
-                top.vec[place] = d.v[i];
-                top.at[place] = (i * (int)blockDim.x + (int)threadIdx.x) * Elem<DT>::kVec;
-            }
-            ++place;
+    for (int i = 0; i < NV; ++i) {
+        if (!hits[i]) continue;
+        const int place = base + (int)__builtin_amdgcn_mbcnt_hi(
+                                     (uint32_t)(hits[i] >> 32),
+                                     __builtin_amdgcn_mbcnt_lo((uint32_t)hits[i], 0));
+        if (vec_max[i] >= tau && place < kCapVecs) {
+            top.vec[place] = d.v[i];
+            top.at[place] = (i * (int)blockDim.x + (int)threadIdx.x) * Elem<DT>::kVec;
         }
+        base += __popcll(hits[i]);
+    }
 }
 
 // The `keep` largest of the `len` elements at `seg` (keep <= len), as keys with ids
@@ -427,26 +444,26 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(LogprobParams p) {
         float vec_max[NV];
         const float lane_max = d.thread_max(vec_max);
         const TopLds top(dyn, p.segs, p.top);
+        const int group = TOP ? group_lanes(p.top, waves) : 0;
+        uint32_t group_best = 0;
         if constexpr (TOP) {
-            const float quad = quad_reduce(lane_max, Max()), line = row_of_quads(quad, Max());
+            const float pair = Max()(lane_max, dpp<0xB1>(lane_max));
+            const float quad = Max()(pair, dpp<0x4E>(pair)), line = row_of_quads(quad, Max());
             m = wave_of_rows(line, Max());
-            const int group = group_lanes(p.top, waves);
-            if (t % group == 0)
-                top.groups[t / group] = group == 16 ? line : group == 4 ? quad : lane_max;
-            if (t == 0) sh.n = sh.vecs = 0;
+            group_best = group_key(
+                group == 16 ? line : group == 4 ? quad : group == 2 ? pair : lane_max, t / group);
+            if (t % group == 0) top.groups[t / group] = group_best;
+            if (t == 0) {
+                sh.n = sh.vecs = 0;
+                sh.tau = -kInf;
+            }
         } else {
             m = wave_max(lane_max);
         }
         if (t % 64 == 0) sh.m[t / 64] = m;
         __syncthreads();
         m = waves_max(sh.m, waves);
-        if constexpr (TOP) {
-            if (t < 64) {
-                const float bound =
-                    groups_bound(top.groups, threads / group_lanes(p.top, waves), p.top);
-                if (t == 0) sh.tau = bound;
-            }
-        }
+        if constexpr (TOP) find_bound(top.groups, group_best, group, p.top, sh);
         const Exponent ex(m, p.scale);
         float s, u;
         if (ex.huge) sums<DT, NV, true>(d, ex, &s, &u);
