@@ -152,7 +152,7 @@ __device__ __forceinline__ uint32_t group_key(float largest, int index) {
 // The group's lanes count the groups above its own, `mine`, four a read; the group that
 // is the top-th sets sh.tau (-inf before).  All threads' work, and two instructions a
 // group: the selection is bound by the instructions of all of its steps (4096 rows of
-// 28672 bf16: @C@).
+// 28672 bf16: 46 us without top entries, 57 with 20 and 65 with 64 of them).
 __device__ __forceinline__ void find_bound(const uint32_t* groups, uint32_t mine, int group, int top,
                                            Shared& sh) {
     const int t = threadIdx.x, quads = (int)blockDim.x / group / 4, part = t % group;

@@ -341,12 +341,12 @@ struct Block {
 // pairs, so that a wave reads whole 128-byte lines of its columns.  A wave works on U
 // blocks while U to 2 U more are on their way.
 //
-// Bound by the weights' bytes on a long N (one row through 8192x28672: @A@ us, 3.7 TB/s)
-// and by latency on a short one (8192x3584: 7.2 us, of which an empty kernel takes 2.9):
+// Bound by the weights' bytes on a long N (one row through 8192x28672: 33 us, 3.7 TB/s)
+// and by latency on a short one (8192x3584: 7.1 us, of which an empty kernel takes 2.9):
 // so the loads of the first 2 U blocks are asked for before the scales, whose place in
 // LDS is a barrier, and with them the slots' addresses.
-template <bool BF, int XL, int GROUP, int U, int WAVES, int PER_SIMD>
-__global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
+template <bool BF, int XL, int GROUP, int U, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 4) w4_kernel(W4Params p) {
     typedef Block<BF, XL, GROUP> B;
     constexpr int kThreads = 64 * WAVES;
     typedef float Partial[256];
@@ -420,9 +420,16 @@ __global__ void __launch_bounds__(64 * WAVES, PER_SIMD) w4_kernel(W4Params p) {
 // X: 1 MB for 64 KB of weights with 64 rows of 8192.)  X and weights go straight into
 // a ring of stages in LDS, waited for by count, so that later steps' loads stay in
 // flight across the barriers; held in registers, the compiler waits for them where
-// it moves registers (64 tokens through 8192x3584: 19.0 us).  Where the columns are
-// too few for the GPU, K is split over workgroups; their sums are written through to
-// the workspace, and the one that arrives last adds them in the order of K.
+// it moves registers (64 rows through 8192x3584: 19.0 us against 17.9).  Where the
+// columns are too few for the GPU, K is split over workgroups; their sums are written
+// through to the workspace, and the one that arrives last adds them in the order of K.
+//
+// 64 rows through 8192x3584 take 17.4 us: about 8.5 are there whatever K is (the
+// kernel's beginning, the partial sums' way through memory, the stores into 8 slots
+// and their acknowledgement); in the K loop matrix instructions and LDS reads wait for
+// each other (without the zero points' matrix instructions 16.0 us, with a quarter of
+// the reads of X 15.6, without both 15.5).  16 rows through 8192x28672: 39 us,
+// 3.2 TB/s of weights.
 constexpr int kWideTiles = 4, kWideCols = kWideTiles * kTileN, kWideThreads = 512;
 constexpr int kWideGroups = 64;      // groups of a column whose scales are in LDS
 
@@ -627,10 +634,9 @@ struct Build {
     int waves, tiles;   // waves and tiles of a workgroup
     int step_k;         // of the wide kernel; 0 = the other one
 };
-template <bool BF, int XL, int GROUP, int U, int WAVES, int PER_SIMD>
+template <bool BF, int XL, int GROUP, int U, int WAVES>
 Build build_of() {
-    return {reinterpret_cast<const void*>(&w4_kernel<BF, XL, GROUP, U, WAVES, PER_SIMD>), WAVES, 1,
-            0};
+    return {reinterpret_cast<const void*>(&w4_kernel<BF, XL, GROUP, U, WAVES>), WAVES, 1, 0};
 }
 template <bool BF, int MT, int GROUP>
 Build wide_of() {
@@ -639,17 +645,17 @@ Build wide_of() {
 }
 
 // Up to 4 rows: one tile a workgroup, of 8 waves while every tile has a CU of its own
-// (8192x3584, 224 tiles: 8.7 us against 9.5 with 4), else of 4, so that more
-// workgroups overlap their beginnings and ends (8192x6144, 384 tiles: 11.2 against
-// 13.0 us with 8; 8192x28672: 33 against 40).  Up to 16 rows the 8 waves while every
-// tile has a CU (8192x3584: 11.2 us against the wide kernel's 11.8; 8192x5120, 320
-// tiles: 18.8 against 12.6).
+// (8192x3584, 224 tiles: 7.1 us against 9.0 with 4), else of 4, so that more
+// workgroups overlap their beginnings and ends (8192x28672: 33 against 35 us with 8;
+// 8192x5120, 320 tiles: the same).  Up to 16 rows the 8 waves too while every tile has
+// a CU (8192x3584: 10.2 us against the wide kernel's 11.7, 4096x1024 5.6 against 9.6),
+// not beyond (8192x5120: 17.7 against 12.1).
 template <bool BF, int GROUP>
 Build build_for(int M, int tiles, int cus) {
     if (M <= 4)
-        return tiles > cus ? build_of<BF, 1, GROUP, 2, 4, 8>()
-                                : build_of<BF, 1, GROUP, 2, 8, 4>();
-    if (M <= 16 && tiles <= cus) return build_of<BF, 4, GROUP, 1, 8, 2>();
+        return tiles > cus ? build_of<BF, 1, GROUP, 2, 4>()
+                                : build_of<BF, 1, GROUP, 2, 8>();
+    if (M <= 16 && tiles <= cus) return build_of<BF, 4, GROUP, 1, 8>();
     if (M <= 16) return wide_of<BF, 1, GROUP>();
     if (M <= 32) return wide_of<BF, 2, GROUP>();
     return wide_of<BF, 4, GROUP>();
@@ -664,7 +670,7 @@ Build build_for(int M, int group, int tiles, int cus) {
 int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // Parts that K is split into: as many as give every CU one workgroup, of two steps at
-// least.
+// least (a part's way through memory costs 3 us).
 int splits_of(int cus, const Build& b, int N, int K) {
     if (!b.step_k) return 1;
     const int groups = ceil_div(N, kWideCols), steps = ceil_div(K, b.step_k);
