@@ -634,7 +634,7 @@ symtile_status symtile_w4_workspace_bytes(int device, int M, int N_local, int K,
  *  workspace: device memory of symtile_w4_workspace_bytes(...) bytes, 16-byte
  *           aligned, zero before the first call that uses it; every call leaves its
  *           counters zero again.  NULL = K is not split over workgroups (slower
- *           for more than 4 tokens and few columns).  Calls that share a workspace
+ *           where that needs a workspace: more than 16 tokens and few columns).  Calls that share a workspace
  *           must not overlap in time.
  *
  * Requirements: K a multiple of 32, N_local of 8; X, q and C 16-byte aligned;

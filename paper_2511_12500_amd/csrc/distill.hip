@@ -197,6 +197,12 @@ __device__ __forceinline__ void write_rest(Segment<DT, NV>& d,
     }
 }
 
+// A workgroup per row or segment; its logits come once from memory.  Memory bounds it:
+// loss and gradient of 4096 rows of 28672 in bfloat16 94 us (5.0 TB/s), of 1000 rows of
+// 50001 in float32 97 us (4.1 TB/s).  Where one workgroup of 1024 threads fills a CU
+// (1024 rows of 131072 bfloat16: 130 us, 4.1 TB/s) loading, sums and storing of a row
+// follow each other with nothing beside them; in segments the logits would be read
+// twice.  64 rows of 8192 take 4.2 us, an empty kernel 2.9.
 template <int DT, int NV, int PHASE>
 __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
     typedef typename Elem<DT>::type T;

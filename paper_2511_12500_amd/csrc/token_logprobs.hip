@@ -424,6 +424,14 @@ constexpr int waves_of(int nv, int phase, bool top) {
     return nv == 8 && phase == kValues && top ? 8 : 4;
 }
 
+// A workgroup per row or segment.  Its logits come once from memory, and the passes
+// over them (largest, sums, candidates, gradient) take them from registers.  With 4096
+// rows of 28672 in bfloat16 memory bounds it: the log probabilities alone 45 us (5.2
+// TB/s), with the gradient in the same pass 91 us (5.2 TB/s); the gradient in a call of
+// its own reads the logits again (2048x32000 float16, both calls: 79 us).  With top
+// entries the selection's instructions and barriers are on top of that, and a split
+// row's join (333x100003 float32: 28 us, with 64 entries 47).  A single row takes 6.4 us:
+// one load, six barriers, one store, of which an empty kernel takes 2.9.
 template <int DT, int NV, int PHASE, bool TOP>
 __global__ void __launch_bounds__(kMaxThreads, waves_of(NV, PHASE, TOP)) logprob_kernel(LogprobParams p) {
     typedef typename Elem<DT>::type T;
