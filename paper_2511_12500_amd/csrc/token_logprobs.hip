@@ -522,6 +522,10 @@ __global__ void __launch_bounds__(kMaxThreads, waves_of(NV, PHASE, TOP)) logprob
                 select_top<DT, NV>(row + id0, tau, sane, keep, id0, len, sh, top,
                            [&](int place, uint64_t key) { put(out + place, key); });
                 for (int i = keep + t; i < p.top; i += threads) put(out + i, 0ull);
+                if (t == 0) {      // (read before the barrier in rank_keys)
+                    sh.n = 0;
+                    sh.bound = ~0ull;
+                }
             }
             if (t == 0) {
                 float* o = p.partials + 4 * unit;
@@ -532,6 +536,14 @@ __global__ void __launch_bounds__(kMaxThreads, waves_of(NV, PHASE, TOP)) logprob
             if (!arrive_last(p.counters + local, p.segs, &sh.last)) return;
             // the row's values from its segments', by every wave
             const float* o = p.partials + 4 * (size_t)local * p.segs;
+            // (all loads asked for together: each is a way to memory and back)
+            const uint64_t* in = p.keys + (size_t)local * p.segs * p.top;
+            uint64_t first_key = 0, bound = ~0ull;
+            if constexpr (TOP) {
+                // `top` keys are at or above the lowest of the segments' j-th, j = ceil(top / segs)
+                if (t < p.segs * p.top) first_key = take(in + t);
+                if (t < p.segs) bound = take(in + (size_t)t * p.top + (p.top + p.segs - 1) / p.segs - 1);
+            }
             float ms = -kInf, ss = 0.0f, us = 0.0f;
             const int lane = t % 64;
             if (lane < p.segs) {
@@ -547,21 +559,12 @@ __global__ void __launch_bounds__(kMaxThreads, waves_of(NV, PHASE, TOP)) logprob
             const RowValues v(m, s, u);
             if (t == 0) write_values(p, r, target, sh.x_target, v);
             if constexpr (TOP) {
-                // `top` keys are at or above the lowest of the segments' j-th, j = ceil(top / segs)
-                const uint64_t* in = p.keys + (size_t)local * p.segs * p.top;
-                if (t == 0) {
-                    sh.n = 0;
-                    sh.bound = ~0ull;
-                }
-                __syncthreads();
-                if (t < p.segs) {
-                    const int j = (p.top + p.segs - 1) / p.segs;
+                if (t < p.segs)
                     atomicMin(reinterpret_cast<unsigned long long*>(&sh.bound),
-                              (unsigned long long)take(in + (size_t)t * p.top + j - 1));
-                }
+                              (unsigned long long)bound);
                 __syncthreads();
                 for (int i = t; i < p.segs * p.top; i += threads) {
-                    const uint64_t key = take(in + i);
+                    const uint64_t key = i == t ? first_key : take(in + i);
                     if (key != 0 && key >= sh.bound) top.keys[atomicAdd(&sh.n, 1)] = key;
                 }
                 __syncthreads();
