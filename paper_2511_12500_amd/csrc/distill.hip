@@ -453,7 +453,7 @@ extern "C" symtile_status symtile_distill_topk(int device, const void* logits, i
     } else if (row_grad) {
         return fail(SYMTILE_EINVAL, "row_grad without dlogits");
     }
-    const Plan plan = make_plan(device, rows, vocab, dtype, dlogits != nullptr);
+    const Plan plan = make_plan(device, rows, vocab, dtype, dlogits != nullptr, 0);
     const Workspace ws = make_workspace(plan, rows, 0);
     if (symtile_status st = check_workspace(workspace, workspace_bytes, ws.bytes)) return st;
     if (rows == 0) return SYMTILE_OK;
@@ -514,7 +514,7 @@ extern "C" symtile_status symtile_distill_topk_backward(
     p.scale = scale;
     OnDevice on(device);
     if (on.status) return on.status;
-    const Plan plan = make_plan(device, rows, vocab, dtype, true);
+    const Plan plan = make_plan(device, rows, vocab, dtype, true, 0);
     return run(p, plan, 0, rows, kernel_of<kGrad>(dtype, plan.nv), s,
                "distill_kernel launch (gradient)");
 }

@@ -363,22 +363,33 @@ inline void shape(int n, bool alone, int* nv, int* threads) {
     *threads = std::min(kMaxThreads, std::max(128, (n + *nv * 64 - 1) / (*nv * 64) * 64));
 }
 
-// Values alone take segments of at most 4096 vectors (512 threads of 8), several
-// workgroups a CU, so that one's loads go on under another's sums (333x100003 fp32:
-// 28 us, with segments of 16384 38).  With a gradient a row that one workgroup holds
-// (16384 vectors) stays whole, since it is read once then.
-inline Plan make_plan(int device, int rows, int vocab, int dtype, bool grad) {
+// Values alone take rows of more than 4096 vectors (512 threads of 8) in segments,
+// several workgroups a CU, so that one's loads go on under another's sums (333x100003
+// fp32: 28 us, with segments of 16384 vectors 38).  Segments of at most 2048 vectors: in
+// smaller workgroups fewer waves wait at a barrier (2000x50257 fp32 with 20 entries 100
+// us, 115 with 4096; 1000x65537 bf16 alone 32, 37).  4096 where more than 32 entries
+// make a segment's own selection and the join dear (1024x131072 bf16 with 64 79 us, 89
+// with 2048), in rows of more than 16384 vectors (distillation of 200x300000 fp32, loss
+// and gradient, 193 us, 229 with 32 segments), and where only those leave every
+// workgroup a CU (64x100003 bf16 with 20 11.6 us against 13.7).  With a gradient a row that one workgroup holds (16384
+// vectors) stays whole, since it is read once then.
+inline Plan make_plan(int device, int rows, int vocab, int dtype, bool grad, int top) {
     const int vec = dtype == SYMTILE_F32 ? 4 : 8;
     const int n = (vocab + vec - 1) / vec;
-    const int most = grad && n <= 16 * kMaxThreads
-                         ? 16 * kMaxThreads
-                         : std::max(4096, (n + kMaxSegments - 1) / kMaxSegments);
+    const size_t cus = (size_t)symtile_host::cu_count(device);
+    auto workgroups = [&](int most) { return (size_t)rows * ((n + most - 1) / most); };
+    int most = 4096;
+    if (n > most && n <= 16 * kMaxThreads && top <= 32 &&
+        !(workgroups(4096) <= cus && workgroups(2048) > cus))
+        most = 2048;
+    most = grad && n <= 16 * kMaxThreads ? 16 * kMaxThreads
+                                         : std::max(most, (n + kMaxSegments - 1) / kMaxSegments);
     const int segs = (n + most - 1) / most;
     Plan p;
     const int per = (n + segs - 1) / segs;
     p.segs = (n + per - 1) / per;
     p.seg_len = per * vec;
-    shape(per, (size_t)rows * p.segs <= (size_t)symtile_host::cu_count(device), &p.nv, &p.threads);
+    shape(per, (size_t)rows * p.segs <= cus, &p.nv, &p.threads);
     return p;
 }
 

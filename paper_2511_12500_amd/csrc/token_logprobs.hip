@@ -618,7 +618,7 @@ extern "C" symtile_status symtile_logits_workspace_bytes(int device, int rows, i
     if (!bytes) return fail(SYMTILE_EINVAL, "bytes is NULL");
     *bytes = 0;
     if (symtile_status st = check_sizes(rows, vocab, dtype, top)) return st;
-    *bytes = make_workspace(make_plan(device, rows, vocab, dtype, false), rows, top).bytes;
+    *bytes = make_workspace(make_plan(device, rows, vocab, dtype, false, top), rows, top).bytes;
     return SYMTILE_OK;
 }
 
@@ -643,7 +643,7 @@ extern "C" symtile_status symtile_token_logprobs(
         return fail(SYMTILE_EINVAL, "gradients without dlogits");
     }
     if (grad_logprob && !targets) return fail(SYMTILE_EINVAL, "grad_logprob without targets");
-    const Plan plan = make_plan(device, rows, vocab, dtype, dlogits != nullptr);
+    const Plan plan = make_plan(device, rows, vocab, dtype, dlogits != nullptr, top);
     const Workspace ws = make_workspace(plan, rows, top);
     if (symtile_status st = check_workspace(workspace, workspace_bytes, ws.bytes)) return st;
     if (rows == 0) return SYMTILE_OK;
@@ -715,7 +715,7 @@ extern "C" symtile_status symtile_token_logprobs_backward(
     p.scale = scale;
     OnDevice on(device);
     if (on.status) return on.status;
-    const Plan plan = make_plan(device, rows, vocab, dtype, false);
+    const Plan plan = make_plan(device, rows, vocab, dtype, false, 0);
     return run(p, plan, 0, rows, kernel_of<kGrad, false>(dtype, plan.nv), s,
                "logprob_kernel launch (gradient)");
 }
