@@ -371,8 +371,8 @@ inline void shape(int n, bool alone, int* nv, int* threads) {
 // make a segment's own selection and the join dear (1024x131072 bf16 with 64 79 us, 89
 // with 2048), in rows of more than 16384 vectors (distillation of 200x300000 fp32, loss
 // and gradient, 193 us, 229 with 32 segments), and where only those leave every
-// workgroup a CU (64x100003 bf16 with 20 11.6 us against 13.7).  With a gradient a row that one workgroup holds (16384
-// vectors) stays whole, since it is read once then.
+// workgroup a CU (64x100003 bf16 with 20 11.6 us against 13.7).  With a gradient a row
+// that one workgroup holds (16384 vectors) stays whole, since it is read once then.
 inline Plan make_plan(int device, int rows, int vocab, int dtype, bool grad, int top) {
     const int vec = dtype == SYMTILE_F32 ? 4 : 8;
     const int n = (vocab + vec - 1) / vec;
