@@ -276,22 +276,24 @@ struct Segment {
 
 // The exponent of a logit in base 2: y = c (x - m) with c = scale * log2(e), as
 // one fused multiply-add x * c - o.  o = m * c is rounded, which moves every y by
-// the same r = m * c - o (`shift`), to be taken out of what is made of them.
-// Where the product with a huge logit (a mask at the type's lowest value)
-// overflows, the difference comes first and r = 0.
+// the same r = m * c - o (`shift`), to be taken out of what is made of them.  r is
+// up to half a unit in o's last place, so from kHugeExponent on, where that is more
+// than 1/8 (and 2^r would soon pass the numbers' range: a row that is masked at -1e10),
+// and where c is infinite, the difference comes first and r = 0.
+constexpr float kHugeExponent = 0x1p22f;
 struct Exponent {
-    float c, o, m, shift;
+    float scale, c, o, m, shift;
     bool huge;
-    __device__ __forceinline__ Exponent(float largest, float scale) {
+    __host__ __device__ __forceinline__ Exponent(float largest, float scale_) : scale(scale_) {
         m = largest == -kInf ? 0.0f : largest;
         c = scale * kLog2e;
         o = m * c;
-        huge = !(fabsf(o) < 1e30f && fabsf(m) < 1e30f);
+        huge = !(fabsf(o) < kHugeExponent);
         shift = huge ? 0.0f : __builtin_fmaf(m, c, -o);
     }
     template <bool HUGE>
-    __device__ __forceinline__ float y(float x) const {
-        return HUGE ? (x - m) * c : __builtin_fmaf(x, c, -o);
+    __host__ __device__ __forceinline__ float y(float x) const {
+        return HUGE ? (x - m) * scale * kLog2e : __builtin_fmaf(x, c, -o);
     }
 };
 // Where exp2 has long vanished, and a product with its zero must not be a NaN.

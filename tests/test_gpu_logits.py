@@ -590,3 +590,86 @@ def test_zero_rows():
     op.run(torch.empty((0, 100), dtype=torch.bfloat16, device="cuda"),
            torch.empty(0, dtype=torch.int64, device="cuda"))
     assert op.logprob.numel() == 0
+
+
+# ---- large finite masks ------------------------------------------------------------
+
+MASKS = [-1e8, -1e9, -1e10, -1e12, -1e20, -1e29, 1e10]
+
+
+def masked_rows(vocab, dtype, mask, seed):
+    """Rows of the mask alone, with its last third masked (the last segment of a row that is
+    split, the first one's where it is the largest), with one token left, and without it."""
+    x = normal_rows(4, vocab, dtype, seed).float()
+    x[0] = mask
+    x[1, vocab - vocab // 3:] = mask
+    one = x[2, vocab // 2].clone()
+    x[2] = mask
+    x[2, vocab // 2] = one
+    return x.to(TD[dtype])
+
+
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("dtype,vocab", [("bf16", 1000), ("f32", 1001), ("bf16", 131072), ("f32", 70001)])
+def test_rows_with_large_finite_masks(dtype, vocab, mask):
+    pkg = sym()
+    x = masked_rows(vocab, dtype, mask, 3)
+    targets = torch.tensor([7, 11, vocab // 2, vocab - 1])
+    g = [torch.randn((4,), generator=gen(k)) for k in range(3)]
+    for scale in (1.0, np.float32(0.7).item(), 2.0):
+        op = pkg.TokenLogprobs(4, vocab, TD[dtype], top=9, scale=scale)
+        op.run(x.cuda(), targets.cuda())
+        check_logprobs(op, x, targets, scale, 9)
+        dl = torch.full((4, vocab), 5.0, dtype=TD[dtype], device="cuda")
+        op.backward(x.cuda(), targets.cuda(), dl, *[t.cuda() for t in g])
+        check_logprob_grad(dl, x, targets, scale, g, dtype)
+        dl.fill_(5.0)
+        op.run(x.cuda(), targets.cuda(), dl, *[t.cuda() for t in g])
+        check_logprobs(op, x, targets, scale, 9)
+        check_logprob_grad(dl, x, targets, scale, g, dtype)
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("dtype,vocab", [("bf16", 1000), ("f32", 1001), ("bf16", 131072), ("f32", 70001)])
+def test_distillation_with_large_finite_masks(dtype, vocab, mask, rest):
+    """As above, and with every token outside the list masked (the last row)."""
+    pkg = sym()
+    k = 16
+    x = masked_rows(vocab, dtype, mask, 5)
+    ids, values = teacher_list(x, k, 7, rest)
+    ids = torch.where(ids < 0, torch.arange(k) * (vocab // k), ids)
+    x = torch.cat([x, torch.full((1, vocab), mask).to(TD[dtype])])
+    x[4, ids[3]] = normal_rows(1, k, dtype, 9)[0]
+    ids, values = torch.cat([ids, ids[3:]]), torch.cat([values, values[3:]])
+    g = torch.rand((5,), generator=gen(1)) + 0.5
+    for scale in (1.0,) if rest else (1.0, np.float32(0.7).item(), 2.0):
+        kd = pkg.TopDistillation(5, vocab, TD[dtype], k, scale=scale, rest=rest)
+        kd.run(x.cuda(), ids.cuda(), values.cuda())
+        check_distill(kd.loss, None, x, ids, values, scale, rest, g, dtype)
+        back = torch.full((5, vocab), 5.0, dtype=TD[dtype], device="cuda")
+        kd.backward(x.cuda(), ids.cuda(), values.cuda(), g.cuda(), back)
+        check_distill(kd.loss, back, x, ids, values, scale, rest, g, dtype)
+        back.fill_(5.0)
+        kd.run(x.cuda(), ids.cuda(), values.cuda(), g.cuda(), back)
+        check_distill(kd.loss, back, x, ids, values, scale, rest, g, dtype)
+
+
+@pytest.mark.parametrize("scale", [1e-38, 1e-30, 1e30, 3e38])
+def test_extreme_scales(scale):
+    """Products of the scale that pass the range of fp32 either way."""
+    pkg = sym()
+    scale = np.float32(scale).item()
+    x = torch.randn((3, 300), generator=gen(2)) * (1.0 if scale > 1 else 3e37)
+    x[0] = 0.0
+    x[1, 5:] = -1.0 if scale > 1 else -1e38
+    targets = torch.tensor([3, 4, 5])
+    op = pkg.TokenLogprobs(3, 300, torch.float32, top=5, scale=scale)
+    op.run(x.cuda(), targets.cuda())
+    check_logprobs(op, x, targets, scale, 5)
+    ids, values = teacher_list(x, 5, 7, False)
+    ids[2] = torch.arange(5)
+    values = torch.zeros_like(values)
+    kd = pkg.TopDistillation(3, 300, torch.float32, 5, scale=scale)
+    kd.run(x.cuda(), ids.cuda(), values.cuda())
+    check_distill(kd.loss, None, x, ids, values, scale, False, torch.ones(3), "f32")
