@@ -497,8 +497,8 @@ symtile_status symtile_gemm_all_scatter_noalloc(symtile_heap* h, const void* A,
  * split over workgroups where there are too few to fill the GPU, and the parts
  * of a row meet there.  0 where no row is split.  The workspace is 16-byte
  * aligned device memory that must be zero before the first call that uses it;
- * every call leaves its counters zero again, so calls of other sizes may
- * follow.  Calls that share a workspace must not overlap in time.  EINVAL for
+ * every call leaves its counters, its first 64 KiB, zero again, so calls of other
+ * sizes and of the other operator may follow.  Calls that share a workspace must not overlap in time.  EINVAL for
  * what the calls refuse. */
 symtile_status symtile_logits_workspace_bytes(int device, int rows, int vocab, int dtype, int top,
                                               size_t* bytes);

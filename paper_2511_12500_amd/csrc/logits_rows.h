@@ -395,20 +395,22 @@ inline Plan make_plan(int device, int rows, int vocab, int dtype, bool grad, int
     return p;
 }
 
+// Threads that fit 32 bits, and a counter for every split row.
 inline int rows_a_launch(const Plan& p) {
-    return (int)((size_t(1) << 30) / ((size_t)p.threads * p.segs));
+    const int most = (int)((size_t(1) << 30) / ((size_t)p.threads * p.segs));
+    return p.segs > 1 ? std::min(most, symtile_host::kWorkspaceCounters) : most;
 }
 
-// Workspace of split rows: a counter per row, then 4 floats per segment, then
-// `top` 64-bit keys per segment.
+// Workspace of a launch's split rows: counters, one per row, then 4 floats per segment,
+// then `top` 64-bit keys per segment.
 struct Workspace {
     size_t partials, keys, bytes;
 };
 inline Workspace make_workspace(const Plan& p, int rows, int top) {
     Workspace w{};
     if (p.segs <= 1 || rows == 0) return w;
-    const size_t units = (size_t)rows * p.segs;
-    w.partials = ((size_t)rows * 4 + 255) / 256 * 256;
+    const size_t units = (size_t)std::min(rows, rows_a_launch(p)) * p.segs;
+    w.partials = (size_t)symtile_host::kWorkspaceCounters * 4;
     w.keys = w.partials + units * 16;
     w.bytes = w.keys + units * (size_t)top * 8;
     return w;

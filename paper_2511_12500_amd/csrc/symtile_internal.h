@@ -74,6 +74,10 @@ symtile_status set_device(const symtile_heap* h, int* previous);
 
 int cu_count(int device);
 
+// The counters at the start of a workspace whose calls leave them at zero.  As large
+// for every call, so that no call's data lies where another's counters are.
+constexpr int kWorkspaceCounters = 16384;
+
 // The heap's second stream and its fork/join events, created on first use on
 // the heap's device (which must be current).
 symtile_status aux_stream(symtile_heap* h);

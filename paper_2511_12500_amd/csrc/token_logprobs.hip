@@ -595,7 +595,7 @@ const void* kernel_of(int dtype, int nv) {
     });
 }
 
-// A kernel over rows first .. first + rows - 1, in launches whose threads fit 32 bits.
+// A kernel over rows first .. first + rows - 1, in launches of rows_a_launch().
 symtile_status run(LogprobParams p, const Plan& plan, int first, int rows, const void* kernel,
                    symtile_stream s, const char* what) {
     p.segs = plan.segs;

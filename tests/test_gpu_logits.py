@@ -673,3 +673,71 @@ def test_extreme_scales(scale):
     kd = pkg.TopDistillation(3, 300, torch.float32, 5, scale=scale)
     kd.run(x.cuda(), ids.cuda(), values.cuda())
     check_distill(kd.loss, None, x, ids, values, scale, False, torch.ones(3), "f32")
+
+
+# ---- workspaces --------------------------------------------------------------------
+
+
+def c_logprobs(ws, x, targets, top, grad=None):
+    """The C call on a workspace of the test's own; outputs filled with a pattern before."""
+    pkg = sym()
+    rows, vocab = x.shape
+    new = lambda *s, dtype=torch.float32: torch.full(s, -7, dtype=dtype, device="cuda")  # noqa: E731
+    out = [new(rows), new(rows), new(rows, 2), new(rows, top, dtype=torch.int64), new(rows, top)]
+    dt = {torch.bfloat16: pkg.BF16, torch.float16: pkg.F16, torch.float32: pkg.F32}[x.dtype]
+    pkg.symtile_token_logprobs(0, x.data_ptr(), rows, vocab, 0, dt, 1.0, targets.data_ptr(),
+                               *[t.data_ptr() for t in out[:3]], top, out[3].data_ptr(),
+                               out[4].data_ptr(), workspace=ws.data_ptr(), workspace_bytes=ws.numel(),
+                               stream=pkg.current_stream())
+
+    class Outputs:
+        logprob, entropy, stats, top_ids, top_logprobs = out
+    return Outputs
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_workspace_for_calls_of_all_sizes(dtype):
+    """One row, many rows, other lengths, other operators, one after another."""
+    pkg = sym()
+    dt = {"bf16": pkg.BF16, "f32": pkg.F32}[dtype]
+    sizes = [(1, 131072, 128), (128, 65544, 9), (1, 131072, 128), (300, 40000, 0), (2, 1 << 20, 100),
+             (700, 33000, 3), (1, 131072, 0), (70, 131072, 1)]
+    need = max(pkg.symtile_logits_workspace_bytes(0, r, v, dt, t) for r, v, t in sizes)
+    ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    for rows, vocab, top in sizes:
+        x = normal_rows(rows, vocab, dtype, rows + vocab)
+        targets = torch.randint(0, vocab, (rows,), generator=gen(1))
+        got = c_logprobs(ws, x.cuda(), targets.cuda(), top)
+        check_logprobs(got, x[:2], targets, 1.0, top) if rows < 3 else None
+        own = pkg.TokenLogprobs(rows, vocab, TD[dtype], top=top)
+        own.run(x.cuda(), targets.cuda())
+        for name in ("logprob", "entropy", "stats", "top_ids", "top_logprobs"):
+            assert torch.equal(getattr(got, name), getattr(own, name)), (rows, vocab, top, name)
+        ids, values = torch.randint(0, vocab, (rows, 8), generator=gen(2)), torch.zeros(rows, 8)
+        loss = torch.full((rows,), -7.0, device="cuda")
+        dx, di, dv = x.cuda(), ids.cuda(), values.cuda()
+        pkg.symtile_distill_topk(0, dx.data_ptr(), rows, vocab, 0, dt, 1.0, di.data_ptr(), dv.data_ptr(),
+                                 pkg.F32, 8, pkg.DISTILL_RENORM, loss.data_ptr(), workspace=ws.data_ptr(),
+                                 workspace_bytes=ws.numel(), stream=pkg.current_stream())
+        kd = pkg.TopDistillation(rows, vocab, TD[dtype], 8)
+        kd.run(dx, di, dv)
+        assert torch.equal(loss, kd.loss), (rows, vocab)
+
+
+def test_more_split_rows_than_counters():
+    """Rows in several launches: every row is joined, and the counters end at zero."""
+    pkg = sym()
+    rows, vocab = 20001, 16400                     # fp32: 4100 vectors, two segments or more
+    need = pkg.symtile_logits_workspace_bytes(0, rows, vocab, pkg.F32, 3)
+    assert need > 0
+    ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    row = torch.randn((vocab,), generator=gen(5))
+    x = row.cuda().repeat(rows, 1)
+    at = torch.arange(rows, device="cuda") % vocab
+    x[torch.arange(rows, device="cuda"), at] = 9.0 + torch.arange(rows, device="cuda") / rows
+    for _ in range(2):
+        got = c_logprobs(ws, x, at, 3)
+        assert torch.equal(got.top_ids[:, 0], at)
+        want = torch.log_softmax(x[::997].double(), 1).gather(1, at[::997, None])[:, 0]
+        assert float((got.logprob[::997].double() - want).abs().max()) < O.log_bound(row.numpy(), 1.0) + 64 * O.U
+        assert bool((got.logprob == got.top_logprobs[:, 0]).all()) and bool((got.entropy > 0).all())
