@@ -633,8 +633,9 @@ symtile_status symtile_w4_workspace_bytes(int device, int M, int N_local, int K,
  *
  *  workspace: device memory of symtile_w4_workspace_bytes(...) bytes, 16-byte
  *           aligned, zero before the first call that uses it; every call leaves its
- *           counters zero again.  NULL = K is not split over workgroups (slower
- *           where that needs a workspace: more than 16 tokens and few columns).  Calls that share a workspace
+ *           counters, its first 64 KiB, zero again, so calls of other sizes may
+ *           follow.  NULL = K is not split over workgroups (slower where that needs a
+ *           workspace: more than 16 tokens and few columns).  Calls that share a workspace
  *           must not overlap in time.
  *
  * Requirements: K a multiple of 32, N_local of 8; X, q and C 16-byte aligned;

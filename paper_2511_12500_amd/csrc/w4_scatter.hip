@@ -674,15 +674,17 @@ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 int splits_of(int cus, const Build& b, int N, int K) {
     if (!b.step_k) return 1;
     const int groups = ceil_div(N, kWideCols), steps = ceil_div(K, b.step_k);
+    if (groups > symtile_host::kWorkspaceCounters) return 1;
     return std::max(1, std::min(cus / groups, steps / 2));
 }
 
-size_t counter_bytes(int N) { return ((size_t)ceil_div(N, kWideCols) * 4 + 255) / 256 * 256; }
+// Counters, one per group of columns, then the partial sums.
+constexpr size_t kCounterBytes = (size_t)symtile_host::kWorkspaceCounters * 4;
 
 size_t workspace_bytes_of(const Build& b, int splits, int M, int N) {
     if (splits <= 1) return 0;
     const size_t rows = M <= 16 ? 16 : M <= 32 ? 32 : 64;
-    return counter_bytes(N) + (size_t)ceil_div(N, kWideCols) * splits * rows * kWideCols * 4;
+    return kCounterBytes + (size_t)ceil_div(N, kWideCols) * splits * rows * kWideCols * 4;
 }
 
 // What the calls refuse about sizes.
@@ -777,7 +779,7 @@ extern "C" symtile_status symtile_w4_all_scatter(
     p.splits = splits;
     if (splits > 1) {
         p.counters = static_cast<uint32_t*>(workspace);
-        p.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + counter_bytes(N_local));
+        p.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes);
     }
     int prev = -1;
     if (symtile_status st = symtile_host::set_device(h, &prev)) return st;

@@ -286,3 +286,18 @@ def test_refusals():
             pkg.W4Weight(*bad, group=32)
     with pytest.raises(ValueError):
         pkg.W4Weight(w.q, w.scales, None, 48)
+
+
+def test_one_workspace_for_calls_of_all_sizes():
+    """Few columns, many, few again, with other M, on one workspace of the C call."""
+    pkg = sym()
+    sizes = [(64, 8192, 3584), (64, 8192, 8192), (20, 4096, 40), (16, 8192, 6000), (33, 8192, 8000), (64, 8192, 3584)]
+    need = max(pkg.symtile_w4_workspace_bytes(0, M, N, K, 128) for M, K, N in sizes)
+    ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    for M, K, N in sizes:
+        t = inputs(M, K, N, "bf16", 128, True, M + N)
+        c = Call(M, N, 1, "bf16", t, 128)
+        pkg.symtile_w4_all_scatter(c.heap.handle, c.X.data_ptr(), *c.w.pointers, c.heap.ptr(0, c.out.c_off),
+                                   c.heap.ptr(0, c.out.flag_off), M, N, K, 0, 128, pkg.BF16, 0, 1,
+                                   ws.data_ptr(), ws.numel(), pkg.current_stream())
+        c.check(0, expected(*t, 128), "bf16", walk(t[0], t[2], K))
