@@ -4,6 +4,7 @@ returns tensors living in the heap), and the symmetric buffers of one
 GEMM + All-Scatter problem.  Argument marshalling only."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 
 import torch
@@ -25,6 +26,15 @@ def current_stream(device: int | None = None) -> int:
     if _raw_stream is not None:
         return _raw_stream(torch.cuda.current_device() if device is None else device)
     return torch.cuda.current_stream(device).cuda_stream
+
+
+def launching(stream: int | None, device: int):
+    """Context in which torch allocates and fills on the stream that a call is
+    launched on (``stream``; None: the current one), so that a workspace is
+    zero when the call's kernels begin, whatever other streams do."""
+    if stream is None or stream == current_stream(device):
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device))
 
 
 class Heap:
@@ -249,13 +259,15 @@ class GatheredOutput:
         if st:
             B._check(st, "symtile_gemm_all_scatter")
 
-    def _workspace_w4(self, K: int, group: int) -> torch.Tensor | None:
-        """run_w4's workspace for this K (None where it needs none): zeroed, kept
-        and reused by later calls, each of which leaves its counters at zero."""
+    def _workspace_w4(self, K: int, group: int, stream: int | None) -> torch.Tensor | None:
+        """run_w4's workspace for this K (None where it needs none): zeroed on
+        the first call's stream, kept and reused by later calls, each of which
+        leaves its counters at zero."""
         if (K, group) not in self.ws_w4:
             need = B.symtile_w4_workspace_bytes(self.heap.device, self.M, self.N_local, K, group)
-            self.ws_w4[K, group] = (torch.zeros(need, dtype=torch.uint8, device=self.heap.mem.device)
-                                    if need else None)
+            with launching(stream, self.heap.device):
+                self.ws_w4[K, group] = (torch.zeros(need, dtype=torch.uint8,
+                                                    device=self.heap.mem.device) if need else None)
         return self.ws_w4[K, group]
 
     def run_w4(self, X: torch.Tensor, weight, rank: int, stream: int | None = None) -> None:
@@ -279,7 +291,7 @@ class GatheredOutput:
         if ptrs is None:
             ptrs = self._ptrs[rank] = (self.heap.ptr(rank, self.c_off),
                                        self.heap.ptr(rank, self.flag_off))
-        ws = self._workspace_w4(K, weight.group)
+        ws = self._workspace_w4(K, weight.group, stream)
         st = B.lib.symtile_w4_all_scatter(
             self.heap.handle, X.data_ptr(), *weight.pointers, ptrs[0], ptrs[1], M, self.N_local, K,
             X.stride(0) if M > 1 and K else 0, weight.group, self._dt, rank, self.heap.world,

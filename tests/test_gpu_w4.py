@@ -301,3 +301,47 @@ def test_one_workspace_for_calls_of_all_sizes():
                                    c.heap.ptr(0, c.out.flag_off), M, N, K, 0, 128, pkg.BF16, 0, 1,
                                    ws.data_ptr(), ws.numel(), pkg.current_stream())
         c.check(0, expected(*t, 128), "bf16", walk(t[0], t[2], K))
+
+
+@pytest.mark.parametrize("M,K,N", [(64, 8192, 200), (16, 2048, 4360)])
+def test_the_first_call_on_another_stream(M, K, N):
+    """stream= for the first call, whose workspace is made in it, while torch's current stream is
+    busy and the memory of the workspace held other values before; then replays of a graph."""
+    pkg = sym()
+    t = inputs(M, K, N, "bf16", 64, True, 1)
+    want, bound = expected(*t, 64), walk(t[0], t[2], K)
+    c = Call(M, N, 2, "bf16", t, 64)
+    need = pkg.symtile_w4_workspace_bytes(0, M, N, K, 64)
+    assert need > 0
+    side = torch.cuda.Stream()
+    for s in (torch.cuda.current_stream(), side):        # what a new workspace of either may get
+        with torch.cuda.stream(s):
+            dirty = torch.full((need,), 3, dtype=torch.uint8, device="cuda")
+            del dirty
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    c.run(1, stream=side.cuda_stream)
+    side.synchronize()
+    early = c.out.C(1).clone()
+    c.check(1, want, "bf16", bound)
+    assert torch.equal(early.view(torch.int16), c.out.C(1).view(torch.int16))
+    c.run(1)                                             # the same workspace on the current stream
+    c.check(1, want, "bf16", bound, calls=2)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.run(1)
+    for i in range(4):
+        c.out.C_all().view(torch.int16).fill_(-1)
+        graph.replay()
+        torch.cuda.synchronize()
+        c.check(1, want, "bf16", bound, calls=3 + i)
+
+
+def test_the_first_call_on_the_null_stream_beside_another():
+    t = inputs(64, 8192, 200, "bf16", 64, True, 1)
+    c = Call(64, 200, 2, "bf16", t, 64)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        torch.cuda._sleep(20_000_000)
+        c.run(1, stream=0)
+    c.check(1, expected(*t, 64), "bf16", walk(t[0], t[2], 8192))
