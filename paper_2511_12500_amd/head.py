@@ -80,6 +80,10 @@ class _Rows:
         self._dt = _DTYPES[dtype]
         need = B.symtile_logits_workspace_bytes(device, rows, vocab, self._dt, top)
         self.ws = torch.zeros(need, dtype=torch.uint8, device=f"cuda:{device}") if need else None
+        if need and not torch.cuda.is_current_stream_capturing():
+            # the calls may come on any stream, and find the workspace zero on each (a
+            # capture's calls follow the zeroing in it)
+            torch.cuda.current_stream(device).synchronize()
         self._ws = (self.ws.data_ptr(), need) if need else (None, 0)
 
     def _new(self, *shape, dtype=torch.float32) -> torch.Tensor:

@@ -741,3 +741,48 @@ def test_more_split_rows_than_counters():
         want = torch.log_softmax(x[::997].double(), 1).gather(1, at[::997, None])[:, 0]
         assert float((got.logprob[::997].double() - want).abs().max()) < O.log_bound(row.numpy(), 1.0) + 64 * O.U
         assert bool((got.logprob == got.top_logprobs[:, 0]).all()) and bool((got.entropy > 0).all())
+
+
+def test_the_first_call_on_another_stream():
+    """stream= for the first call, right after the object was made while torch's current stream is
+    busy and the memory of the workspace held other values before."""
+    pkg = sym()
+    rows, vocab = 3, 131072
+    x = normal_rows(rows, vocab, "bf16", 3)
+    targets = torch.randint(0, vocab, (rows,), generator=gen(4))
+    ids, values = teacher_list(x, 9, 3, False)
+    dx, dt, di, dv = x.cuda(), targets.cuda(), ids.cuda(), values.cuda()
+    side = torch.cuda.Stream()
+    for make in ("logprobs", "distill"):
+        need = pkg.symtile_logits_workspace_bytes(0, rows, vocab, pkg.BF16, 9 if make == "logprobs" else 0)
+        assert need > 0
+        dirty = torch.full((need,), 3, dtype=torch.uint8, device="cuda")
+        del dirty
+        torch.cuda.synchronize()
+        torch.cuda._sleep(200_000_000)
+        if make == "logprobs":
+            op = pkg.TokenLogprobs(rows, vocab, torch.bfloat16, top=9)
+            op.run(dx, dt, stream=side.cuda_stream)
+        else:
+            op = pkg.TopDistillation(rows, vocab, torch.bfloat16, 9)
+            op.run(dx, di, dv, stream=side.cuda_stream)
+        torch.cuda.synchronize()
+        if make == "logprobs":
+            check_logprobs(op, x, targets, 1.0, 9)
+        else:
+            check_distill(op.loss, None, x, ids, values, 1.0, False, torch.ones(rows), "bf16")
+
+
+def test_an_object_made_while_a_graph_is_captured():
+    pkg = sym()
+    x = normal_rows(2, 131072, "bf16", 3)
+    dx, targets = x.cuda(), torch.tensor([5, 7])
+    dt = targets.cuda()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        op = pkg.TokenLogprobs(2, 131072, torch.bfloat16, top=3)
+        op.run(dx, dt)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        check_logprobs(op, x, targets, 1.0, 3)
