@@ -174,10 +174,11 @@ class GatheredOutput:
         return self.heap.slots_view(self.flag_off, (self.heap.world, self.tiles_m, self.tiles_n),
                                     torch.int32)
 
-    def workspace(self, split_k: int) -> torch.Tensor | None:
+    def workspace(self, split_k: int, stream: int | None = None) -> torch.Tensor | None:
         """The split-K workspace for ``split_k`` slices (None when split_k <= 1):
-        a zeroed uint8 device tensor, kept and reused by later calls (each call
-        leaves its counters at zero), replaced by a larger one when needed."""
+        a uint8 device tensor, zeroed on ``stream`` (default: the current one),
+        kept and reused by later calls (each call leaves its counters at zero),
+        replaced by a larger one when needed."""
         need = self._ws_need.get(split_k)
         if need is None:
             need = self._ws_need[split_k] = B.symtile_gas_workspace_bytes(
@@ -186,9 +187,11 @@ class GatheredOutput:
             return None
         if self.ws is None or self.ws.numel() < need:
             self.ws = None
-            self.ws = torch.zeros(need, dtype=torch.uint8, device=self.heap.mem.device)
+            with launching(stream, self.heap.device):
+                self.ws = torch.zeros(need, dtype=torch.uint8, device=self.heap.mem.device)
         elif self.ws_seen != self.heap.failed_barriers:
-            self.ws.zero_()      # a timed-out call may have left its counters non-zero
+            with launching(stream, self.heap.device):
+                self.ws.zero_()  # a timed-out call may have left its counters non-zero
         self.ws_seen = self.heap.failed_barriers
         return self.ws
 
@@ -249,7 +252,7 @@ class GatheredOutput:
         cfg.trace = trace.data_ptr() if trace is not None else None
         cfg.split_k, cfg.split_reduce = split_k, split_reduce
         cfg.workspace, cfg.workspace_bytes = None, 0
-        ws = self.workspace(split_k) if split_k > 1 else None
+        ws = self.workspace(split_k, stream) if split_k > 1 else None
         if ws is not None:               # None: no tiles, nothing to keep
             cfg.workspace, cfg.workspace_bytes = ws.data_ptr(), ws.numel()
         st = B.lib.symtile_gemm_all_scatter(

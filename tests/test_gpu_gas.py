@@ -1124,3 +1124,25 @@ def test_banded_64x64_grid_larger_than_resident():
         heaps.append(u16(p.out.C_all()).copy())
         assert np.all(_ws_counters(p) == 0)
     assert np.array_equal(heaps[0], heaps[1])
+
+
+def test_a_split_k_workspace_made_for_another_stream():
+    """stream= for the first split-K call, whose workspace is made in it, while torch's current
+    stream is busy and the memory of the workspace held other values before."""
+    pkg = sym()
+    M, K, N = 256, 1024, 256
+    p = Problem(2, M, N, K, "bf16", 256, 256, seed=11)
+    need = pkg.symtile_gas_workspace_bytes(M, N, 256, 256, 4)
+    assert need > 0
+    side = torch.cuda.Stream()
+    for s in (torch.cuda.current_stream(), side):
+        with torch.cuda.stream(s):
+            dirty = torch.full((need,), 3, dtype=torch.uint8, device="cuda")
+            del dirty
+    p.sentinel()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    p.run(1, pkg.FUSED_SEQ, split_k=4, split_reduce=pkg.SPLIT_REDUCE_LAST, stream=side.cuda_stream)
+    p.heap.barrier(side.cuda_stream)
+    p.barrier()
+    check_gathered(p, {1: oracle_block(p.A, p.shards[1], "bf16")})
