@@ -288,6 +288,8 @@ class GatheredOutput:
         M, K = X.shape
         if M != self.M or weight.N != self.N_local or weight.K != K:
             raise ValueError("shape mismatch")
+        if M > 1 and X.stride(0) < K:
+            raise ValueError("rows of X must not overlap")
         if (self.tile_m, self.tile_n) != (B.W4_TILE_M, B.W4_TILE_N):
             raise ValueError("the output must be made with W4_TILE_M x W4_TILE_N tiles")
         ptrs = self._ptrs.get(rank)

@@ -345,3 +345,17 @@ def test_the_first_call_on_the_null_stream_beside_another():
         torch.cuda._sleep(20_000_000)
         c.run(1, stream=0)
     c.check(1, expected(*t, 64), "bf16", walk(t[0], t[2], 8192))
+
+
+def test_one_row_expanded_to_several_is_refused():
+    """Rows without a distance between them are not rows K apart."""
+    t = inputs(3, 64, 16, "bf16", 32, True, 1)
+    c = Call(3, 16, 2, "bf16", t, 32)
+    with pytest.raises(ValueError):
+        c.out.run_w4(c.X[:1].expand(3, 64), c.w, 0)
+    with pytest.raises(ValueError):
+        c.out.run_w4(c.X.flatten()[:128].as_strided((3, 64), (32, 1)), c.w, 0)
+    one = inputs(1, 64, 16, "bf16", 32, True, 1)
+    c = Call(1, 16, 2, "bf16", one, 32)
+    c.out.run_w4(c.X.expand(1, 64), c.w, 1)          # a single row has no distance
+    c.check(1, expected(*one, 32), "bf16", walk(one[0], one[2], 64))
