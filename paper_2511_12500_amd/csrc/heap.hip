@@ -248,8 +248,10 @@ int cu_count(int device) {
         if (n > 0) return n;
     }
     int n = 0;
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess)
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess) {
+        (void)hipGetLastError();   // not the next call's
         return 0;
+    }
     if (device >= 0 && device < 64) known[device].store(n, std::memory_order_relaxed);
     return n;
 }

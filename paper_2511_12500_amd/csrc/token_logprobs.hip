@@ -618,6 +618,8 @@ extern "C" symtile_status symtile_logits_workspace_bytes(int device, int rows, i
     if (!bytes) return fail(SYMTILE_EINVAL, "bytes is NULL");
     *bytes = 0;
     if (symtile_status st = check_sizes(rows, vocab, dtype, top)) return st;
+    if (symtile_host::cu_count(device) <= 0)
+        return fail(SYMTILE_EINVAL, "device " + std::to_string(device) + " out of range");
     *bytes = make_workspace(make_plan(device, rows, vocab, dtype, false, top), rows, top).bytes;
     return SYMTILE_OK;
 }

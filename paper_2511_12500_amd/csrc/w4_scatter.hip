@@ -708,8 +708,10 @@ extern "C" symtile_status symtile_w4_workspace_bytes(int device, int M, int N_lo
     if (!bytes) return symtile_host::fail(SYMTILE_EINVAL, "bytes is NULL");
     *bytes = 0;
     if (symtile_status st = check_sizes(M, N_local, K, group)) return st;
+    const int cus = symtile_host::cu_count(device);
+    if (cus <= 0)
+        return symtile_host::fail(SYMTILE_EINVAL, "device " + std::to_string(device) + " out of range");
     if (M == 0 || N_local == 0) return SYMTILE_OK;
-    const int cus = std::max(1, symtile_host::cu_count(device));
     const Build b = build_for<true>(M, group, ceil_div(N_local, kTileN), cus);
     *bytes = workspace_bytes_of(b, splits_of(cus, b, N_local, K), M, N_local);
     return SYMTILE_OK;

@@ -786,3 +786,19 @@ def test_an_object_made_while_a_graph_is_captured():
         graph.replay()
         torch.cuda.synchronize()
         check_logprobs(op, x, targets, 1.0, 3)
+
+
+def test_a_device_that_does_not_exist_is_refused():
+    """The size queries refuse it as the calls do, and leave nothing behind for the next call."""
+    pkg = sym()
+    for query in (lambda d: pkg.symtile_logits_workspace_bytes(d, 4, 131072, pkg.BF16, 5),
+                  lambda d: pkg.symtile_w4_workspace_bytes(d, 64, 200, 8192, 64)):
+        assert query(0) > 0
+        for device in (99, -1):
+            with pytest.raises(pkg.SymtileError) as e:
+                query(device)
+            assert e.value.name == "EINVAL" and "device" in str(e.value)
+            x = normal_rows(2, 100, "bf16", 1)
+            op = pkg.TokenLogprobs(2, 100, torch.bfloat16)
+            op.run(x.cuda(), torch.zeros(2, dtype=torch.int64, device="cuda"))
+            check_logprobs(op, x, [0, 0], 1.0, 0)
