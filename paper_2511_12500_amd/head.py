@@ -34,19 +34,22 @@ class W4Weight:
         tensors = [q, scales] + ([] if zeros is None else [zeros])
         if any(tuple(t.shape) != shape for t in tensors[1:]):
             raise ValueError(f"scales and zeros must be {list(shape)}")
-        if not all(t.is_cuda and t.is_contiguous() for t in tensors):
-            raise ValueError("q, scales and zeros must be contiguous device tensors")
+        self.device = q.get_device()
+        if not all(t.is_cuda and t.get_device() == self.device and t.is_contiguous()
+                   for t in tensors):
+            raise ValueError("q, scales and zeros must be contiguous tensors on one GPU")
         self.q, self.scales, self.zeros = q, scales, zeros
         self.pointers = (q.data_ptr(), scales.data_ptr(),
                          None if zeros is None else zeros.data_ptr())
 
 
-def _matrix(t: torch.Tensor, name: str, rows: int, cols: int, dtype: torch.dtype) -> int:
-    """Row stride in elements of a device matrix with contiguous rows."""
+def _matrix(t: torch.Tensor, name: str, rows: int, cols: int, dtype: torch.dtype,
+            device: int) -> int:
+    """Row stride in elements of a matrix on the device with contiguous rows."""
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if not t.is_cuda or t.shape != (rows, cols):
-        raise ValueError(f"{name} must be a [{rows}, {cols}] device tensor")
+    if t.get_device() != device or t.shape != (rows, cols):
+        raise ValueError(f"{name} must be a [{rows}, {cols}] tensor on cuda:{device}")
     if cols > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must have contiguous rows")
     ld = t.stride(0) if rows > 1 else cols
@@ -55,14 +58,14 @@ def _matrix(t: torch.Tensor, name: str, rows: int, cols: int, dtype: torch.dtype
     return ld
 
 
-def _vector(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.dtype):
-    """Address of a contiguous device tensor (None for None)."""
+def _vector(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.dtype, device: int):
+    """Address of a contiguous tensor on the device (None for None)."""
     if t is None:
         return None
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if not t.is_cuda or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous device tensor {list(shape)}")
+    if t.get_device() != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor {list(shape)} on cuda:{device}")
     return t.data_ptr()
 
 
@@ -90,9 +93,9 @@ class _Rows:
         return torch.empty(shape, dtype=dtype, device=f"cuda:{self.device}")
 
     def _matrices(self, logits, dlogits):
-        ld = _matrix(logits, "logits", self.rows, self.vocab, self.dtype)
+        ld = _matrix(logits, "logits", self.rows, self.vocab, self.dtype, self.device)
         ld_grad = 0 if dlogits is None else _matrix(dlogits, "dlogits", self.rows, self.vocab,
-                                                    self.dtype)
+                                                    self.dtype, self.device)
         return ld, ld_grad
 
     def _stream(self, stream):
@@ -124,7 +127,7 @@ class TokenLogprobs(_Rows):
         return self.stats[:, 0] * self.scale + self.stats[:, 1]
 
     def _grads(self, *grads):
-        return [_vector(g, n, (self.rows,), torch.float32)
+        return [_vector(g, n, (self.rows,), torch.float32, self.device)
                 for g, n in zip(grads, ("grad_logprob", "grad_entropy", "grad_lse"))]
 
     def run(self, logits: torch.Tensor, targets: torch.Tensor | None = None,
@@ -139,7 +142,7 @@ class TokenLogprobs(_Rows):
         fp32 [rows] ``grad_*`` (None: zero), for losses whose weights are known
         before the call; it may be ``logits`` itself."""
         ld, ld_grad = self._matrices(logits, dlogits)
-        t = _vector(targets, "targets", (self.rows,), torch.int64)
+        t = _vector(targets, "targets", (self.rows,), torch.int64, self.device)
         st = B.lib.symtile_token_logprobs(
             self.device, logits.data_ptr(), self.rows, self.vocab, ld, self._dt, self.scale, t,
             None if t is None else self.logprob.data_ptr(), *self._out,
@@ -159,9 +162,9 @@ class TokenLogprobs(_Rows):
         ld, ld_grad = self._matrices(logits, dlogits)
         st = B.lib.symtile_token_logprobs_backward(
             self.device, logits.data_ptr(), self.rows, self.vocab, ld, self._dt, self.scale,
-            _vector(targets, "targets", (self.rows,), torch.int64), self._out[0], self._out[1],
-            *self._grads(grad_logprob, grad_entropy, grad_lse), dlogits.data_ptr(), ld_grad,
-            self._stream(stream))
+            _vector(targets, "targets", (self.rows,), torch.int64, self.device), self._out[0],
+            self._out[1], *self._grads(grad_logprob, grad_entropy, grad_lse), dlogits.data_ptr(),
+            ld_grad, self._stream(stream))
         if st:
             B._check(st, "symtile_token_logprobs_backward")
 
@@ -182,8 +185,8 @@ class TopDistillation(_Rows):
     def _list(self, ids, values):
         if values.dtype not in _DTYPES:
             raise TypeError("values must be float16, bfloat16 or float32")
-        return (_vector(ids, "ids", (self.rows, self.k), torch.int64),
-                _vector(values, "values", (self.rows, self.k), values.dtype),
+        return (_vector(ids, "ids", (self.rows, self.k), torch.int64, self.device),
+                _vector(values, "values", (self.rows, self.k), values.dtype, self.device),
                 _DTYPES[values.dtype], self.k, self.mode)
 
     def run(self, logits: torch.Tensor, ids: torch.Tensor, values: torch.Tensor,
@@ -197,7 +200,7 @@ class TopDistillation(_Rows):
         st = B.lib.symtile_distill_topk(
             self.device, logits.data_ptr(), self.rows, self.vocab, ld, self._dt, self.scale,
             *self._list(ids, values), self.loss.data_ptr(), self.stats.data_ptr(),
-            _vector(row_grad, "row_grad", (self.rows,), torch.float32),
+            _vector(row_grad, "row_grad", (self.rows,), torch.float32, self.device),
             None if dlogits is None else dlogits.data_ptr(), ld_grad, *self._ws,
             self._stream(stream))
         if st:
@@ -211,7 +214,7 @@ class TopDistillation(_Rows):
         st = B.lib.symtile_distill_topk_backward(
             self.device, logits.data_ptr(), self.rows, self.vocab, ld, self._dt, self.scale,
             *self._list(ids, values), self.stats.data_ptr(),
-            _vector(row_grad, "row_grad", (self.rows,), torch.float32), dlogits.data_ptr(),
-            ld_grad, self._stream(stream))
+            _vector(row_grad, "row_grad", (self.rows,), torch.float32, self.device),
+            dlogits.data_ptr(), ld_grad, self._stream(stream))
         if st:
             B._check(st, "symtile_distill_topk_backward")

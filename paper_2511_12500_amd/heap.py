@@ -283,8 +283,10 @@ class GatheredOutput:
         so that its workspace exists."""
         if X.dtype != self.dtype or weight.dtype != self.dtype:
             raise TypeError("X and the weight's scales must have the output dtype")
-        if not X.is_cuda or X.dim() != 2 or X.stride(1) != 1:
-            raise ValueError("X must be a device matrix with contiguous rows")
+        device = self.heap.device
+        if X.get_device() != device or X.dim() != 2 or X.stride(1) != 1 or weight.device != device:
+            raise ValueError("X must be a matrix with contiguous rows, it and the weight on "
+                             f"cuda:{device}")
         M, K = X.shape
         if M != self.M or weight.N != self.N_local or weight.K != K:
             raise ValueError("shape mismatch")
