@@ -197,6 +197,9 @@ struct Segment {
         }
     }
 
+    // (Parts of vectors are of the elements' own type: other code reads and writes
+    // the same elements alone, and through another type the compiler need not keep
+    // the order.)
     static __device__ __forceinline__ symtile::u32x4 load_part(const typename Elem<DT>::type* p,
                                                                int n) {
         const uint32_t none = Elem<DT>::kMasked;
@@ -204,14 +207,15 @@ struct Segment {
         if constexpr (DT == SYMTILE_F32) {
 #pragma unroll
             for (int e = 0; e < 3; ++e)
-                if (e < n) r[e] = reinterpret_cast<const uint32_t*>(p)[e];
+                if (e < n) r[e] = __float_as_uint(p[e]);
         } else {
-            const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
             for (int e = 0; e < 7; ++e)
-                if (e < n)
-                    r[e / 2] = e % 2 ? (r[e / 2] & 0xFFFFu) | (uint32_t)h[e] << 16
-                                     : (r[e / 2] & 0xFFFF0000u) | h[e];
+                if (e < n) {
+                    const uint32_t h = __builtin_bit_cast(uint16_t, p[e]);
+                    r[e / 2] = e % 2 ? (r[e / 2] & 0xFFFFu) | h << 16
+                                     : (r[e / 2] & 0xFFFF0000u) | h;
+                }
         }
         return r;
     }
@@ -230,15 +234,15 @@ struct Segment {
         } else if (at < len) {
             const int n = len - at;
             if constexpr (DT == SYMTILE_F32) {
-                uint32_t* w = reinterpret_cast<uint32_t*>(p + at);
 #pragma unroll
                 for (int e = 0; e < 3; ++e)
-                    if (e < n) w[e] = r[e];
+                    if (e < n) p[at + e] = __uint_as_float(r[e]);
             } else {
-                uint16_t* h = reinterpret_cast<uint16_t*>(p + at);
 #pragma unroll
                 for (int e = 0; e < 7; ++e)
-                    if (e < n) h[e] = (uint16_t)(r[e / 2] >> (16 * (e % 2)));
+                    if (e < n)
+                        p[at + e] = __builtin_bit_cast(typename Elem<DT>::type,
+                                                       (uint16_t)(r[e / 2] >> (16 * (e % 2))));
             }
         }
     }
