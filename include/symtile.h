@@ -493,13 +493,15 @@ symtile_status symtile_gemm_all_scatter_noalloc(symtile_heap* h, const void* A,
 #define SYMTILE_VOCAB_MAX (1 << 21)
 
 /* Bytes of the workspace of a symtile_token_logprobs (top) or
- * symtile_distill_topk (top = 0) call on `device` with these sizes: rows are
- * split over workgroups where there are too few to fill the GPU, and the parts
- * of a row meet there.  0 where no row is split.  The workspace is 16-byte
- * aligned device memory that must be zero before the first call that uses it;
- * every call leaves its counters, its first 64 KiB, zero again, so calls of other
- * sizes and of the other operator may follow.  Calls that share a workspace must not overlap in time.  EINVAL for
- * what the calls refuse. */
+ * symtile_distill_topk (top = 0) call on `device` with these sizes.  Rows of more
+ * than 4096 vectors of 16 bytes (with a gradient in the call: more than 16384) are
+ * split over workgroups, however many rows there are, and the parts of a row meet in
+ * the workspace: 16 + 8 * top bytes a part, of up to 16384 rows at a time.  0 where
+ * no row is split.  The workspace is 16-byte aligned device memory that must be zero
+ * before the first call that uses it; every call leaves its counters, its first 64
+ * KiB, zero again, so calls of other sizes and of the other operator may follow.
+ * Calls that share a workspace must not overlap in time.  EINVAL for what the calls
+ * refuse. */
 symtile_status symtile_logits_workspace_bytes(int device, int rows, int vocab, int dtype, int top,
                                               size_t* bytes);
 
@@ -519,7 +521,8 @@ symtile_status symtile_logits_workspace_bytes(int device, int rows, int vocab, i
  *   dlogits_v = scale * (p_v * (grad_lse - grad_logprob)
  *                        - p_v * (logp_v + entropy) * grad_entropy
  *                        + (v = target ? grad_logprob : 0)).
- * A logit of -inf is a masked token: p = 0, gradient 0.  In a row with nothing
+ * A logit of -inf is a masked token: p = 0, gradient 0 (but for the target's own
+ * term; its logprob is -inf).  In a row with nothing
  * else logprob is -inf, entropy 0, stats (-inf, 0), the top entries are ids
  * 0, 1, ... at -inf, and the gradient is 0.  A row with a NaN or +inf gives NaN
  * (a NaN counts as the largest logit).  Sums are held in fp32; the gradient is
@@ -634,9 +637,9 @@ symtile_status symtile_w4_workspace_bytes(int device, int M, int N_local, int K,
  *  workspace: device memory of symtile_w4_workspace_bytes(...) bytes, 16-byte
  *           aligned, zero before the first call that uses it; every call leaves its
  *           counters, its first 64 KiB, zero again, so calls of other sizes may
- *           follow.  NULL = K is not split over workgroups (slower where that needs a
- *           workspace: more than 16 tokens and few columns).  Calls that share a workspace
- *           must not overlap in time.
+ *           follow.  NULL = K is not split over workgroups, which is slower wherever
+ *           the size is not 0 (over 4 tokens through a few thousand columns).  Calls
+ *           that share a workspace must not overlap in time.
  *
  * Requirements: K a multiple of 32, N_local of 8; X, q and C 16-byte aligned;
  * M = 0 or N_local = 0 launches nothing, K = 0 stores zeros.  EINVAL otherwise.

@@ -199,10 +199,15 @@ __device__ __forceinline__ void write_rest(Segment<DT, NV>& d,
 
 // A workgroup per row or segment; its logits come once from memory.  Memory bounds it:
 // loss and gradient of 4096 rows of 28672 in bfloat16 94 us (5.0 TB/s), of 1000 rows of
-// 50001 in float32 97 us (4.1 TB/s).  Where one workgroup of 1024 threads fills a CU
-// (1024 rows of 131072 bfloat16: 130 us, 4.1 TB/s) loading, sums and storing of a row
+// 50001 in float32 100 us (4.0 TB/s).  Where one workgroup of 1024 threads fills a CU
+// (1024 rows of 131072 bfloat16: 135 us, 4.0 TB/s) loading, sums and storing of a row
 // follow each other with nothing beside them; in segments the logits would be read
-// twice.  64 rows of 8192 take 4.2 us, an empty kernel 2.9.
+// twice.  64 rows of 8192 take 4.3 us, an empty kernel 2.9.
+// The loss alone of rows that are split is bound by the list instead, since every
+// segment takes it anew (exponentials, search for repeated ids, the listed logits) ahead
+// of a barrier: 1024 rows of 131072 bfloat16 124 us, 1000 of 50257 float32 102 us, where
+// token_logprobs takes 53 and 40 for the same logits; whole rows, 4096 of 28672
+// bfloat16: 48 us (5.0 TB/s).
 template <int DT, int NV, int PHASE>
 __global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p) {
     typedef typename Elem<DT>::type T;

@@ -48,8 +48,8 @@ struct Shared {
 };
 
 // Dynamic LDS of the top entries: keys, and the vectors that hold the candidates.
-// Before there are keys, groups' largest logits stand in their place.  Behind the keys zeros fill up a step of all
-// threads that count for one key.
+// Before there are keys, groups' largest logits stand in their place.  Behind the keys
+// zeros fill up a step of all threads that count for one key.
 struct TopLds {
     static constexpr int kPad = 32;
     union {
@@ -428,7 +428,7 @@ constexpr int waves_of(int nv, int phase, bool top) {
 // over them (largest, sums, candidates, gradient) take them from registers.  With 4096
 // rows of 28672 in bfloat16 memory bounds it: the log probabilities alone 45 us (5.2
 // TB/s), with the gradient in the same pass 91 us (5.2 TB/s); the gradient in a call of
-// its own reads the logits again (2048x32000 float16, both calls: 79 us).  With top
+// its own reads the logits again (2048x32000 float16, both calls: 80 us).  With top
 // entries the selection's instructions and barriers are on top of that, and a split
 // row's join (333x100003 float32: 28 us, with 64 entries 47).  A single row takes 6.4 us:
 // one load, six barriers, one store, of which an empty kernel takes 2.9.

@@ -424,12 +424,12 @@ __global__ void __launch_bounds__(64 * WAVES, 4) w4_kernel(W4Params p) {
 // columns are too few for the GPU, K is split over workgroups; their sums are written
 // through to the workspace, and the one that arrives last adds them in the order of K.
 //
-// 64 rows through 8192x3584 take 17.4 us: about 8.5 are there whatever K is (the
-// kernel's beginning, the partial sums' way through memory, the stores into 8 slots
-// and their acknowledgement); in the K loop matrix instructions and LDS reads wait for
-// each other (without the zero points' matrix instructions 16.0 us, with a quarter of
-// the reads of X 15.6, without both 15.5).  16 rows through 8192x28672: 39 us,
-// 3.2 TB/s of weights.
+// 64 rows through 8192x3584 take 17.4 us in the first milliseconds of such calls, 16.2
+// after 20 ms: about 8.5 are there whatever K is (the kernel's beginning, the partial
+// sums' way through memory, the stores into 8 slots and their acknowledgement); in the K
+// loop matrix instructions and LDS reads wait for each other (of the 17.4 us without the
+// zero points' matrix instructions 16.0, with a quarter of the reads of X 15.6, without
+// both 15.5).  16 rows through 8192x28672: 36 us, 3.5 TB/s of weights.
 constexpr int kWideTiles = 4, kWideCols = kWideTiles * kTileN, kWideThreads = 512;
 constexpr int kWideGroups = 64;      // groups of a column whose scales are in LDS
 

@@ -71,8 +71,9 @@ def _vector(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.dtype,
 
 class _Rows:
     """What the operators over rows of logits share: sizes, type and the
-    workspace, which a call needs where there are few rows.  Calls on one object
-    must not overlap in time."""
+    workspace, which a call needs where rows are long enough to be split (more
+    than 4096 vectors of 16 bytes).  Calls on one object must not overlap in
+    time."""
 
     def __init__(self, rows: int, vocab: int, dtype: torch.dtype, top: int, scale: float,
                  device: int):
