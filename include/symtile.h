@@ -651,6 +651,184 @@ symtile_status symtile_w4_all_scatter(symtile_heap* h, const void* X, const uint
                                       int world_size, void* workspace, size_t workspace_bytes,
                                       symtile_stream s);
 
+/* ---- a model's two ends: microscaled 4-bit product, draft verification, embedding ----
+ *
+ * What a step of speculative decoding and of training puts through a
+ * vocabulary-parallel model's ends beside the calls above.  The paper has none of
+ * them.
+ *
+ * A matrix in blocks of 32 values along a row: row r of `rows` holds K/2 bytes of
+ * 4-bit elements, two consecutive k to a byte, the even one in the low bits, and K/32
+ * bytes of scales, both rows next to each other.  An element is a sign (bit 3), two
+ * bits of exponent and one of fraction: 0, 0.5, 1, 1.5, 2, 3, 4, 6; a scale b stands for
+ * 2^(b - 127), 255 for NaN (the microscaling formats' fp4 e2m1 with e8m0). */
+
+/* Quantises x: a block's scale is the power of two of its largest magnitude, less two
+ * (2^-127 at least; 2^-127 where all are zero), an element the nearest value of x over
+ * the scale, of two as near the one whose fraction bit is 0, and 6 beyond it (a magnitude
+ * between 6 and 8 times the scale).  A block with a NaN or an infinity gets scale 255 and
+ * elements 0.
+ *
+ *  x        device [rows, cols] of dtype (SYMTILE_F16, SYMTILE_BF16, SYMTILE_F32), row
+ *           stride ld (0 = cols); rows may start at any multiple of the element size
+ *  q        device uint8 [rows, cols/2], 16-byte aligned
+ *  scales   device uint8 [rows, cols/32]
+ *  values   device [rows, cols] of dtype, row stride ld_values (0 = cols): what the
+ *           elements stand for (rounded once to dtype; NaN under scale 255); NULL = not
+ *           wanted.  May be x itself (same address and stride).
+ * cols is a multiple of 32; no other arguments may overlap.  EINVAL otherwise; rows = 0
+ * or cols = 0 launches nothing. */
+symtile_status symtile_mx4_quantise(int device, const void* x, int rows, int cols, size_t ld,
+                                    int dtype, uint8_t* q, uint8_t* scales, void* values,
+                                    size_t ld_values, symtile_stream s);
+
+/* Tile of symtile_mx4_all_scatter's arrival counters. */
+#define SYMTILE_MX4_TILE_M 64
+#define SYMTILE_MX4_TILE_N 16
+
+/* Bytes of the workspace of a symtile_mx4_all_scatter call on `device` with these
+ * sizes (0: none is used).  EINVAL for what the call refuses. */
+symtile_status symtile_mx4_workspace_bytes(int device, int M, int N_local, int K, size_t* bytes);
+
+/* Rank `rank`'s share of a column-parallel layer whose tokens and weights are both
+ * matrices in blocks: C_r[m, n] = sum over the blocks b of a row of 2^(xs[m, b] +
+ * ws[n, b] - 254) sum_k x[m, k] w[n, k], with fp32 accumulators (products are exact;
+ * partial sums below the smallest normal number may become zero), rounded once to dtype
+ * (SYMTILE_F16, SYMTILE_BF16) and stored into column block `rank` of the gathered
+ * output in every slot; after a tile's data the arrival counter of (rank, tile row,
+ * tile column) in that slot is incremented with release semantics at agent scope, as
+ * symtile_gemm_all_scatter does.  A NaN scale makes its row's or column's results NaN.
+ *
+ *  x, x_scales   the tokens [M, K]; q, scales: the weights [N_local, K], row n those of
+ *                output column n.  Elements 16-byte aligned.
+ *  C_gathered_local, arrived_local: as in symtile_gemm_all_scatter, with tiles of
+ *                SYMTILE_MX4_TILE_M x SYMTILE_MX4_TILE_N: uint32
+ *                [world_size][ceil(M / 64)][ceil(N_local / 16)]
+ *  workspace     as in symtile_w4_all_scatter: device memory of
+ *                symtile_mx4_workspace_bytes(...) bytes, 16-byte aligned, zero before the
+ *                first call that uses it, its first 64 KiB left at zero by every call;
+ *                NULL = K is not split over workgroups.  Calls that share one must not
+ *                overlap in time.
+ *
+ * Requirements: K a multiple of 32 (at most 4194304), N_local of 8, M at most 2097152,
+ * world_size * N_local at most 4194304; C 16-byte aligned; M = 0 or N_local = 0 launches
+ * nothing, K = 0 stores zeros.  EINVAL otherwise. */
+symtile_status symtile_mx4_all_scatter(symtile_heap* h, const uint8_t* x, const uint8_t* x_scales,
+                                       const uint8_t* q, const uint8_t* scales,
+                                       void* C_gathered_local, uint32_t* arrived_local, int M,
+                                       int N_local, int K, int dtype, int rank, int world_size,
+                                       void* workspace, size_t workspace_bytes, symtile_stream s);
+
+/* Most drafted tokens of a sequence in symtile_verify_draft. */
+#define SYMTILE_DRAFT_MAX 32
+
+/* Bytes of the workspace of a symtile_verify_draft call on `device` with these sizes:
+ * 16-byte aligned device memory that must be zero before the first call that uses it;
+ * every call leaves its counters, its first 64 KiB, zero again, so calls of other sizes
+ * and of the other operators may follow.  Calls that share a workspace must not overlap
+ * in time.  EINVAL for what the call refuses. */
+symtile_status symtile_verify_workspace_bytes(int device, int sequences, int drafted, int vocab,
+                                              int dtype, size_t* bytes);
+
+/* Verification of drafted tokens.  A sequence b has up to `drafted` = k drafted tokens
+ * d_i = ids[b, i], ending at its first negative one (n_b of them), and k + 1 rows of
+ * target logits: p_i = softmax(scale * logits[b * (k + 1) + i]) is the target's
+ * distribution at position i given the drafted tokens before it.  q_i is the draft's:
+ * softmax(draft_scale * draft_logits[b * k + i]), or, without draft logits, 1 for d_i and
+ * 0 for all others.
+ *   With noise: the first a positions i < n_b with uniforms[b, i] * q_i(d_i) < p_i(d_i)
+ * are accepted.  At position a the token is drawn from w = max(0, p_a - q_a) if a < n_b,
+ * else from w = p_a (also where no token has p_a > q_a): the token with w_v > 0 of the
+ * largest w_v / noise[b, v], of equal ones the lowest.  For uniforms in [0, 1) and noise
+ * of independent exponential numbers (positive, normal) the tokens then follow the target.
+ *   Without noise (greedy): the first a positions where d_i is the token of the largest
+ * logit (the lowest of equal ones) are accepted, and that token of position a follows.
+ *   tokens[b]  = d_0 .. d_{a-1}, the token of position a, then -1;
+ *   accepted[b] = a;
+ *   logprob[b, i] = log p_i of tokens[b, i] for i <= a, 0 behind.
+ * A logit of -inf is a masked token.  Where the target's row has no distribution (a NaN
+ * or +inf, or nothing above -inf) the position is not accepted and token a is -1 with
+ * logprob 0; a drafted token whose draft row has none is not accepted and the next one is
+ * drawn from p_a; an id >= vocab has p = 0.  The decision is made in 64 bits from the rows'
+ * fp32 sums, the draw in fp32.
+ *
+ *  logits       device [sequences * (drafted + 1), vocab], row stride ld (0 = vocab)
+ *               elements of dtype, as in symtile_token_logprobs
+ *  ids          device int64 [sequences, drafted]
+ *  draft_logits device [sequences * drafted, vocab] of dtype, row stride ld_draft; NULL =
+ *               the drafted tokens alone
+ *  uniforms     device fp32 [sequences, drafted]
+ *  noise        device fp32 [sequences, vocab], row stride ld_noise (0 = vocab); NULL =
+ *               greedy (uniforms and draft_logits NULL then)
+ *  tokens       device int64 [sequences, drafted + 1]
+ *  accepted     device int64 [sequences]
+ *  logprob      device fp32 [sequences, drafted + 1]
+ *  drafted      0 .. SYMTILE_DRAFT_MAX; vocab 1 .. SYMTILE_VOCAB_MAX
+ * EINVAL for anything else; sequences = 0 launches nothing. */
+symtile_status symtile_verify_draft(int device, const void* logits, int sequences, int drafted,
+                                    int vocab, size_t ld, int dtype, float scale,
+                                    const int64_t* ids, const void* draft_logits, size_t ld_draft,
+                                    float draft_scale, const float* uniforms, const float* noise,
+                                    size_t ld_noise, int64_t* tokens, int64_t* accepted,
+                                    float* logprob, void* workspace, size_t workspace_bytes,
+                                    symtile_stream s);
+
+/* Tile of symtile_embed_all_scatter's arrival counters: 16 tokens by 2048 bytes of a row
+ * (1024 columns of 16 bits, 512 of 32). */
+#define SYMTILE_EMBED_TILE_M 16
+#define SYMTILE_EMBED_TILE_BYTES 2048
+
+/* Rank `rank`'s share of the lookup of T tokens in a table whose rows are sharded over
+ * the ranks: for every token with first <= tokens[t] < first + rows,
+ * row t of the output = scale * table[tokens[t] - first] (one fp32 product, rounded once
+ * to dtype) is stored into every slot.  Rows of negative tokens (padding) are zero, stored
+ * by rank 0; all others are left as they were.  After its part of a tile of
+ * SYMTILE_EMBED_TILE_M tokens by SYMTILE_EMBED_TILE_BYTES, which may be none of its rows,
+ * the arrival counter of (rank, tile row, tile column) in every slot is incremented with
+ * release semantics at agent scope: a tile is whole in a slot when all ranks' counters
+ * say so.
+ *
+ *  tokens        device int64 [T]
+ *  table         device [rows, D] of dtype (SYMTILE_F16, SYMTILE_BF16, SYMTILE_F32), row
+ *                stride ld (0 = D); rows 16-byte aligned
+ *  rows_local    address inside slot `rank` of the output [T, D] of dtype; the same
+ *                offset is written in every slot; 16-byte aligned
+ *  arrived_local address inside slot `rank` of the counters uint32
+ *                [world_size][ceil(T / 16)][ceil(D * element size / 2048)]
+ *  D             a multiple of 8; scale finite; rows 0 .. SYMTILE_VOCAB_MAX
+ * EINVAL otherwise; T = 0 or D = 0 launches nothing. */
+symtile_status symtile_embed_all_scatter(symtile_heap* h, const int64_t* tokens, int T,
+                                         const void* table, int rows, int D, size_t ld, int dtype,
+                                         int64_t first, float scale, void* rows_local,
+                                         uint32_t* arrived_local, int rank, int world_size,
+                                         symtile_stream s);
+
+/* Bytes of the workspace of a symtile_embed_backward call on `device` for T tokens of D
+ * columns: 16-byte aligned device memory of any contents.  Calls that share a workspace
+ * must not overlap in time.  EINVAL for what the call refuses. */
+symtile_status symtile_embed_workspace_bytes(int device, int T, int D, size_t* bytes);
+
+/* The gradient of a table's shard: for every row v of `rows`
+ *   dtable[v] = scale * sum over t with tokens[t] = first + v of drows[t],
+ * in the order of t within each 32 tokens of sorted ids and then of those, with fp32 sums,
+ * so results do not depend on timing; with accumulate = 1 added to what dtable[v] holds
+ * (in fp32, rounded once to table_dtype) and rows without a token left alone, else those
+ * are zero.  Other tokens (other ranks', padding) are not read.
+ *
+ *  tokens       device int64 [T]
+ *  drows        device [T, D] of dtype, row stride ld (0 = D); rows 16-byte aligned
+ *  dtable       device [rows, D] of table_dtype, row stride ld_table (0 = D); rows 16-byte
+ *               aligned; does not overlap drows
+ *  workspace    see symtile_embed_workspace_bytes; may be NULL where that is 0
+ *  dtype and table_dtype are any of the three types; D a multiple of 8; scale finite;
+ *  rows 0 .. SYMTILE_VOCAB_MAX.
+ * EINVAL otherwise; T = 0 zeroes dtable (accumulate = 0) or launches nothing. */
+symtile_status symtile_embed_backward(int device, const int64_t* tokens, int T, const void* drows,
+                                      int D, size_t ld, int dtype, int64_t first, int rows,
+                                      float scale, void* dtable, size_t ld_table, int table_dtype,
+                                      int accumulate, void* workspace, size_t workspace_bytes,
+                                      symtile_stream s);
+
 /* Rate of the realtime counter behind trace timestamps (the per-tile
  * timeline of Section 3.4, instrumentation), in kHz.  EINVAL for a bad device
  * or NULL khz. */

@@ -23,9 +23,14 @@ _BINDING = (
     "symtile_distill_topk", "symtile_distill_topk_backward", "symtile_logits_workspace_bytes",
     "symtile_token_logprobs", "symtile_token_logprobs_backward", "symtile_w4_all_scatter",
     "symtile_w4_workspace_bytes",
+    "DRAFT_MAX", "EMBED_TILE_BYTES", "EMBED_TILE_M", "MX4_TILE_M", "MX4_TILE_N",
+    "symtile_embed_all_scatter", "symtile_embed_backward", "symtile_embed_workspace_bytes",
+    "symtile_mx4_all_scatter", "symtile_mx4_quantise", "symtile_mx4_workspace_bytes",
+    "symtile_verify_draft", "symtile_verify_workspace_bytes",
 )
-_HEAP = ("GatheredOutput", "Heap", "current_stream")
-_HEAD = ("TokenLogprobs", "TopDistillation", "W4Weight")
+_HEAP = ("GatheredOutput", "GatheredRows", "Heap", "current_stream")
+_HEAD = ("DraftVerification", "EmbeddingGrad", "MX4Matrix", "TokenLogprobs", "TopDistillation",
+         "W4Weight")
 
 __all__ = list(_BINDING + _HEAP + _HEAD)
 

@@ -14,6 +14,9 @@ PUT, GET = 0, 1
 DISTILL_RENORM, DISTILL_REST = 0, 1
 TOP_MAX = 128                             # SYMTILE_TOP_MAX
 W4_TILE_M, W4_TILE_N = 64, 16             # SYMTILE_W4_TILE_M, SYMTILE_W4_TILE_N
+MX4_TILE_M, MX4_TILE_N = 64, 16           # SYMTILE_MX4_TILE_M, SYMTILE_MX4_TILE_N
+DRAFT_MAX = 32                            # SYMTILE_DRAFT_MAX
+EMBED_TILE_M, EMBED_TILE_BYTES = 16, 2048  # SYMTILE_EMBED_TILE_M, SYMTILE_EMBED_TILE_BYTES
 LOAD, STORE = 0, 1
 ATOMIC_OPS = {"add": 0, "xchg": 1, "cas": 2, "and": 3, "or": 4, "xor": 5, "min": 6, "max": 7}
 SEMS = {"relaxed": 0, "acquire": 1, "release": 2, "acq_rel": 3}
@@ -67,7 +70,7 @@ def _load():
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2511_12500_amd.build`")
     L = ctypes.CDLL(LIB_PATH)
     vp, sz, i32, u32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_uint32
-    f32 = ctypes.c_float
+    f32, i64 = ctypes.c_float, ctypes.c_int64
     pvp = ctypes.POINTER(ctypes.c_void_p)
     decl = {
         "symtile_heap_create": [i32, i32, sz, pvp],
@@ -108,6 +111,18 @@ def _load():
         "symtile_w4_all_scatter": [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
                                    i32, vp, sz, vp],
         "symtile_w4_workspace_bytes": [i32, i32, i32, i32, i32, ctypes.POINTER(sz)],
+        "symtile_mx4_quantise": [i32, vp, i32, i32, sz, i32, vp, vp, vp, sz, vp],
+        "symtile_mx4_workspace_bytes": [i32, i32, i32, i32, ctypes.POINTER(sz)],
+        "symtile_mx4_all_scatter": [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp,
+                                    sz, vp],
+        "symtile_verify_workspace_bytes": [i32, i32, i32, i32, i32, ctypes.POINTER(sz)],
+        "symtile_verify_draft": [i32, vp, i32, i32, i32, sz, i32, f32, vp, vp, sz, f32, vp, vp, sz,
+                                 vp, vp, vp, vp, sz, vp],
+        "symtile_embed_all_scatter": [vp, vp, i32, vp, i32, i32, sz, i32, i64, f32, vp, vp, i32,
+                                      i32, vp],
+        "symtile_embed_workspace_bytes": [i32, i32, i32, ctypes.POINTER(sz)],
+        "symtile_embed_backward": [i32, vp, i32, vp, i32, sz, i32, i64, i32, f32, vp, sz, i32, i32,
+                                   vp, sz, vp],
         "symtile_value_exercise": [vp, i32, sz, sz, sz, i32, i32, i32, vp],
     }
     for name, args in decl.items():
@@ -364,6 +379,79 @@ def symtile_w4_workspace_bytes(device: int, M: int, N_local: int, K: int, group:
     _check(lib.symtile_w4_workspace_bytes(device, M, N_local, K, group, ctypes.byref(out)),
            "symtile_w4_workspace_bytes")
     return out.value
+
+
+def symtile_mx4_quantise(device: int, x: int, rows: int, cols: int, ld: int, dtype: int, q: int,
+                         scales: int, values: int = 0, ld_values: int = 0, stream: int = 0) -> None:
+    _check(lib.symtile_mx4_quantise(device, _vp(x), rows, cols, ld, dtype, _vp(q), _vp(scales),
+                                    _vp(values), ld_values, _vp(stream)), "symtile_mx4_quantise")
+
+
+def symtile_mx4_workspace_bytes(device: int, M: int, N_local: int, K: int) -> int:
+    """Bytes of the workspace of a symtile_mx4_all_scatter call."""
+    out = ctypes.c_size_t()
+    _check(lib.symtile_mx4_workspace_bytes(device, M, N_local, K, ctypes.byref(out)),
+           "symtile_mx4_workspace_bytes")
+    return out.value
+
+
+def symtile_mx4_all_scatter(h: int, x: int, x_scales: int, q: int, scales: int,
+                            C_gathered_local: int, arrived_local: int, M: int, N_local: int,
+                            K: int, dtype: int, rank: int, world_size: int, workspace: int = 0,
+                            workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib.symtile_mx4_all_scatter(_vp(h), _vp(x), _vp(x_scales), _vp(q), _vp(scales),
+                                       _vp(C_gathered_local), _vp(arrived_local), M, N_local, K,
+                                       dtype, rank, world_size, _vp(workspace), workspace_bytes,
+                                       _vp(stream)), "symtile_mx4_all_scatter")
+
+
+def symtile_verify_workspace_bytes(device: int, sequences: int, drafted: int, vocab: int,
+                                   dtype: int) -> int:
+    """Bytes of the workspace of a symtile_verify_draft call."""
+    out = ctypes.c_size_t()
+    _check(lib.symtile_verify_workspace_bytes(device, sequences, drafted, vocab, dtype,
+                                              ctypes.byref(out)),
+           "symtile_verify_workspace_bytes")
+    return out.value
+
+
+def symtile_verify_draft(device: int, logits: int, sequences: int, drafted: int, vocab: int,
+                         ld: int, dtype: int, scale: float, ids: int, draft_logits: int,
+                         ld_draft: int, draft_scale: float, uniforms: int, noise: int,
+                         ld_noise: int, tokens: int, accepted: int, logprob: int, workspace: int,
+                         workspace_bytes: int, stream: int = 0) -> None:
+    _check(lib.symtile_verify_draft(device, _vp(logits), sequences, drafted, vocab, ld, dtype,
+                                    scale, _vp(ids), _vp(draft_logits), ld_draft, draft_scale,
+                                    _vp(uniforms), _vp(noise), ld_noise, _vp(tokens),
+                                    _vp(accepted), _vp(logprob), _vp(workspace), workspace_bytes,
+                                    _vp(stream)), "symtile_verify_draft")
+
+
+def symtile_embed_all_scatter(h: int, tokens: int, T: int, table: int, rows: int, D: int, ld: int,
+                              dtype: int, first: int, scale: float, rows_local: int,
+                              arrived_local: int, rank: int, world_size: int,
+                              stream: int = 0) -> None:
+    _check(lib.symtile_embed_all_scatter(_vp(h), _vp(tokens), T, _vp(table), rows, D, ld, dtype,
+                                         first, scale, _vp(rows_local), _vp(arrived_local), rank,
+                                         world_size, _vp(stream)), "symtile_embed_all_scatter")
+
+
+def symtile_embed_workspace_bytes(device: int, T: int, D: int) -> int:
+    """Bytes of the workspace of a symtile_embed_backward call."""
+    out = ctypes.c_size_t()
+    _check(lib.symtile_embed_workspace_bytes(device, T, D, ctypes.byref(out)),
+           "symtile_embed_workspace_bytes")
+    return out.value
+
+
+def symtile_embed_backward(device: int, tokens: int, T: int, drows: int, D: int, ld: int,
+                           dtype: int, first: int, rows: int, scale: float, dtable: int,
+                           ld_table: int, table_dtype: int, accumulate: int = 0,
+                           workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib.symtile_embed_backward(device, _vp(tokens), T, _vp(drows), D, ld, dtype, first,
+                                      rows, scale, _vp(dtable), ld_table, table_dtype, accumulate,
+                                      _vp(workspace), workspace_bytes, _vp(stream)),
+           "symtile_embed_backward")
 
 
 def symtile_litmus_mp(h: int, data_off: int, flag_off: int, pairs: int, rounds: int,

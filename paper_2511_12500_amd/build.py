@@ -17,7 +17,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OBJDIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libsymtile.so")
-SOURCES = ["heap.hip", "tile_copy.hip", "gemm_all_scatter.hip", "token_logprobs.hip", "distill.hip", "w4_scatter.hip"]
+SOURCES = ["heap.hip", "tile_copy.hip", "gemm_all_scatter.hip", "token_logprobs.hip", "distill.hip", "w4_scatter.hip",
+           "mx4.hip", "verify_draft.hip", "embedding.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

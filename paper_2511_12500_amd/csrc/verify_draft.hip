@@ -1,0 +1,449 @@
+// Verification of drafted tokens against the target's probabilities, from rows of
+// logits and given random numbers.
+//
+// With p_i and q_i the target's and the draft's probabilities of a sequence's
+// position i, its first positions with u_i q_i(d_i) < p_i(d_i) are accepted.  At the
+// first other one, a, the token is drawn from w_v = max(0, p_a(v) - q_a(v)) by a race
+// of exponential times: the largest w_v / noise_v.  One kernel reads all rows for their
+// largest logits and sums; the other one decides (every workgroup of a sequence for
+// itself) and reads the rows of position a once more.
+#include "logits_rows.h"
+#include "symtile_device.h"
+
+namespace {
+
+using namespace logits;
+using symtile::u32x4;
+
+enum Mode { kGreedy, kTokens, kDraft };   // drafts without and with their logits
+
+// A segment's part of a row's numbers: the largest logit, the sum of exp(scale (x - m))
+// and, greedy, the lowest id of the largest.
+struct __attribute__((aligned(16))) Part {
+    float m, s;
+    uint32_t best;
+    uint32_t unused;
+};
+
+struct VerifyParams {
+    const void *x, *y;          // target and draft logits
+    size_t ldx, ldy, ldn;
+    const int64_t* ids;
+    const float *uniforms, *noise;
+    int64_t *tokens, *accepted;
+    float* logprob;
+    Part* parts;                // [sequence][row][segment]
+    uint32_t* counters;         // one a sequence
+    uint64_t* keys;             // [sequence][segment][2]
+    symtile_host::Div by_segs, by_rows, by_draw;
+    int seq0, k, rows, vocab;   // rows of a sequence: k + 1 target ones, then k draft ones
+    int segs, seg_len;          // of the first kernel
+    int draw_segs, draw_len;    // of the second
+    float scale, draft_scale;
+};
+
+template <int DT>
+__device__ __forceinline__ const typename Elem<DT>::type* row_of(const VerifyParams& p, int seq,
+                                                                 int r) {
+    typedef typename Elem<DT>::type T;
+    const size_t at = (size_t)p.seq0 + seq;
+    return r <= p.k ? static_cast<const T*>(p.x) + (at * (p.k + 1) + r) * p.ldx
+                    : static_cast<const T*>(p.y) + (at * p.k + (r - p.k - 1)) * p.ldy;
+}
+
+// ---- largest logits and sums ---------------------------------------------------------------
+template <int DT, int NV, bool HUGE>
+__device__ __forceinline__ float sum_of(Segment<DT, NV>& d, const Exponent& ex) {
+    d.again();
+    float s0 = 0.0f, s1 = 0.0f;
+    d.each([&](int, int e, float x) {
+        (e % 2 ? s1 : s0) += exp2_fast(ex.template y<HUGE>(x));
+    });
+    return s0 + s1;
+}
+
+template <int DT, int NV, bool GREEDY>
+__global__ void __launch_bounds__(kMaxThreads) verify_sums_kernel(VerifyParams p) {
+    __shared__ float m_of[kMaxWaves], s_of[kMaxWaves];
+    __shared__ uint32_t best_of[kMaxWaves];
+    const int threads = blockDim.x, waves = threads / 64, t = threadIdx.x;
+    const int unit = blockIdx.x, row = p.by_segs(unit), seg = unit - row * p.segs;
+    const int seq = p.by_rows(row), r = row - seq * p.rows;
+    const int begin = seg * p.seg_len, len = min(p.seg_len, p.vocab - begin);
+    const float scale = r <= p.k ? p.scale : p.draft_scale;
+    Segment<DT, NV> d;
+    d.load(row_of<DT>(p, seq, r) + begin, len, threads);
+    float vec[NV];
+    const float mine = wave_max(d.thread_max(vec));
+    if (t % 64 == 0) m_of[t / 64] = mine;
+    __syncthreads();
+    const float m = waves_max(m_of, waves);
+    const Exponent ex(m, scale);
+    const float sum = wave_sum(ex.huge ? sum_of<DT, NV, true>(d, ex) : sum_of<DT, NV, false>(d, ex));
+    uint32_t best = 0xFFFFFFFFu;
+    if constexpr (GREEDY) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = Segment<DT, NV>::kVec - 1; e >= 0; --e)
+                if (element<DT>(d.v[i], e) == m) {
+                    const uint32_t at = (i * threads + t) * Segment<DT, NV>::kVec + e;
+                    if ((int)at < len) best = min(best, begin + at);
+                }
+#pragma unroll
+        for (int o = 32; o; o >>= 1) best = min(best, (uint32_t)__shfl_xor(best, o));
+        if (t % 64 == 0) best_of[t / 64] = best;
+    }
+    if (t % 64 == 0) s_of[t / 64] = sum;
+    __syncthreads();
+    if (t < 64) {
+        const float s = waves_sum(s_of, waves) * exp2f(-ex.shift);
+        if constexpr (GREEDY)
+            for (int w = 0; w < waves; ++w) best = min(best, best_of[w]);
+        if (t == 0) p.parts[unit] = Part{m, s, best, 0u};
+    }
+}
+
+// ---- the decision and the draw ------------------------------------------------------------
+// A row's numbers from its parts'; a row without a distribution (a NaN or +inf, or nothing
+// above -inf) has s not positive and finite.
+struct RowStat {
+    float m;
+    double s;
+    uint32_t best;
+    __device__ __forceinline__ bool good() const { return s > 0.0 && s < (double)kInf; }
+};
+
+__device__ __forceinline__ RowStat join(const Part* parts, int segs, float scale) {
+    RowStat r{-kInf, 0.0, 0xFFFFFFFFu};
+    for (int i = 0; i < segs; ++i) r.m = fmaxf(r.m, parts[i].m);
+    for (int i = 0; i < segs; ++i) {
+        const Part q = parts[i];
+        // (a segment at -inf alone has s = 0; beside a NaN sum nothing else matters)
+        r.s += q.m == -kInf ? (double)q.s
+                            : (double)q.s * exp((double)(q.m - r.m) * (double)scale);
+        if (q.m == r.m) r.best = min(r.best, q.best);
+    }
+    return r;
+}
+
+// Larger is better: scores as whole numbers, among equal ones the lower id; 0 = none.
+__device__ __forceinline__ uint64_t race_key(float score, uint32_t id) {
+    return (uint64_t)(__float_as_uint(score) + 1u) << 32 | (0xFFFFFFFFu - id);
+}
+
+__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        const uint64_t u = __shfl_xor((unsigned long long)v, o);
+        v = u > v ? u : v;
+    }
+    return v;
+}
+
+struct Shared {
+    RowStat stat[2 * SYMTILE_DRAFT_MAX + 1];
+    uint64_t best[kMaxWaves], any[kMaxWaves];
+    int accepted;
+    bool drafted;      // position `accepted` has a drafted token, which was not accepted
+    int last;
+};
+
+// The target's log probability of a token at position i.
+template <int DT>
+__device__ __forceinline__ float logprob_of(const VerifyParams& p, const Shared& sh, int seq, int i,
+                                            int64_t id) {
+    const float x = (float)row_of<DT>(p, seq, i)[id];
+    return (float)((double)(x - sh.stat[i].m) * (double)p.scale - log(sh.stat[i].s));
+}
+
+// Which positions are accepted; by the workgroup's first wave.
+template <int DT, int MODE>
+__device__ __forceinline__ void decide(const VerifyParams& p, int seq, Shared& sh) {
+    const int lane = threadIdx.x;
+    const size_t at = ((size_t)p.seq0 + seq) * p.k;
+    const bool in = lane < p.k;
+    const int64_t id = in ? p.ids[at + lane] : -1;
+    bool good = false;
+    if (in && id >= 0 && id < p.vocab && sh.stat[lane].good()) {
+        if constexpr (MODE == kGreedy) {
+            good = (uint32_t)id == sh.stat[lane].best;
+        } else {
+            const RowStat& a = sh.stat[lane];
+            const double px = exp((double)((float)row_of<DT>(p, seq, lane)[id] - a.m) * (double)p.scale) / a.s;
+            double qx = 1.0;
+            if constexpr (MODE == kDraft) {
+                const RowStat& b = sh.stat[p.k + 1 + lane];
+                qx = exp((double)((float)row_of<DT>(p, seq, p.k + 1 + lane)[id] - b.m) *
+                         (double)p.draft_scale) / b.s;
+                if (!b.good()) qx = (double)kInf;
+            }
+            // (u = 0 and q = inf give a NaN: not accepted)
+            good = (double)p.uniforms[at + lane] * qx < px;
+        }
+    }
+    const uint64_t mask = __ballot(good), given = __ballot(in && id >= 0);
+    if (lane == 0) {
+        // a draft ends at its first absent token
+        sh.accepted = __builtin_ctzll(~(mask & given));
+        sh.drafted = given >> sh.accepted & 1;
+    }
+}
+
+template <int DT, int MODE>
+__device__ __forceinline__ void finish(const VerifyParams& p, int seq, const Shared& sh,
+                                       int64_t token) {
+    const int i = threadIdx.x;
+    if (i > p.k) return;
+    const size_t at = (size_t)p.seq0 + seq;
+    const int a = sh.accepted;
+    const int64_t id = i < a ? p.ids[at * p.k + i] : i == a ? token : -1;
+    p.tokens[at * (p.k + 1) + i] = id;
+    p.logprob[at * (p.k + 1) + i] = id >= 0 ? logprob_of<DT>(p, sh, seq, i, id) : 0.0f;
+    if (i == 0) p.accepted[at] = a;
+}
+
+// The exponentials of a row's elements, over their sum.
+struct Weights {
+    Exponent ex;
+    float inv;
+    __device__ __forceinline__ Weights(const RowStat& r, float scale)
+        : ex(r.m, scale), inv((float)(exp2(-(double)ex.shift) / r.s)) {}
+    __device__ __forceinline__ float operator()(float x) const {
+        return exp2_fast(ex.huge ? ex.y<true>(x) : ex.y<false>(x)) * inv;
+    }
+};
+
+constexpr int kDrawThreads = 256;
+
+template <int DT, int MODE>
+__global__ void __launch_bounds__(kDrawThreads) verify_draw_kernel(VerifyParams p) {
+    constexpr int kVec = Elem<DT>::kVec;
+    __shared__ Shared sh;
+    const int t = threadIdx.x, unit = blockIdx.x;
+    const int seq = p.by_draw(unit), seg = unit - seq * p.draw_segs;
+    for (int r = t; r < p.rows; r += kDrawThreads)
+        sh.stat[r] = join(p.parts + ((size_t)seq * p.rows + r) * p.segs, p.segs,
+                          r <= p.k ? p.scale : p.draft_scale);
+    __syncthreads();
+    if (t < 64) decide<DT, MODE>(p, seq, sh);
+    __syncthreads();
+    const int a = sh.accepted;
+    const bool valid = sh.stat[a].good();
+    if constexpr (MODE == kGreedy) {
+        finish<DT, MODE>(p, seq, sh, valid ? (int64_t)sh.stat[a].best : -1);
+        return;
+    }
+    if (!valid) {          // (the same for all of the sequence's workgroups)
+        if (seg == 0) finish<DT, MODE>(p, seq, sh, -1);
+        return;
+    }
+    // a position with a drafted token, and the draft's own distribution
+    const bool less = MODE == kDraft && sh.drafted && sh.stat[p.k + 1 + a].good();
+    const int64_t out = MODE == kTokens && sh.drafted ? p.ids[((size_t)p.seq0 + seq) * p.k + a] : -1;
+    const Weights wp(sh.stat[a], p.scale);
+    const Weights wq(less ? sh.stat[p.k + 1 + a] : sh.stat[a], less ? p.draft_scale : p.scale);
+    const int begin = seg * p.draw_len, len = min(p.draw_len, p.vocab - begin);
+    typedef typename Elem<DT>::type T;
+    const T* x = row_of<DT>(p, seq, a) + begin;
+    const T* y = less ? row_of<DT>(p, seq, p.k + 1 + a) + begin : x;
+    const float* noise = p.noise + ((size_t)p.seq0 + seq) * p.ldn + begin;
+    uint64_t best = 0, any = 0;
+    for (int at = t * kVec; at < len; at += kDrawThreads * kVec) {
+        const u32x4 xv = Segment<DT, 1>::fetch(x, len, at), yv = Segment<DT, 1>::fetch(y, len, at);
+        u32x4 nv[kVec / 4];
+#pragma unroll
+        for (int i = 0; i < kVec / 4; ++i)
+            nv[i] = Segment<SYMTILE_F32, 1>::fetch(noise, len, at + 4 * i < len ? at + 4 * i : at);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+            const uint32_t id = begin + at + e;
+            const float pv = wp(element<DT>(xv, e));
+            float wv = pv;
+            if (less) wv -= wq(element<DT>(yv, e));
+            if (MODE == kTokens && (int64_t)id == out) wv = 0.0f;
+            const float over = __builtin_amdgcn_rcpf(__uint_as_float(nv[e / 4][e % 4]));
+            const float score = wv * over, plain = pv * over;
+            // (a NaN, from noise that is none, is no candidate)
+            if (at + e < len) {
+                if (wv > 0.0f && score >= 0.0f) best = max(best, race_key(score, id));
+                if (pv > 0.0f && plain >= 0.0f) any = max(any, race_key(plain, id));
+            }
+        }
+    }
+    best = wave_max_u64(best);
+    any = wave_max_u64(any);
+    if (t % 64 == 0) {
+        sh.best[t / 64] = best;
+        sh.any[t / 64] = any;
+    }
+    __syncthreads();
+    if (t == 0) {
+        for (int w = 1; w < kDrawThreads / 64; ++w) {
+            best = max(best, sh.best[w]);
+            any = max(any, sh.any[w]);
+        }
+        sh.best[0] = best;
+        sh.any[0] = any;
+    }
+    if (p.draw_segs > 1) {
+        if (t == 0) {
+            put(p.keys + (size_t)unit * 2, best);
+            put(p.keys + (size_t)unit * 2 + 1, any);
+        }
+        if (!arrive_last(p.counters + seq, p.draw_segs, &sh.last)) return;
+        best = any = 0;
+        if (t < 64) {
+            for (int i = t; i < p.draw_segs; i += 64) {
+                best = max(best, take(p.keys + ((size_t)seq * p.draw_segs + i) * 2));
+                any = max(any, take(p.keys + ((size_t)seq * p.draw_segs + i) * 2 + 1));
+            }
+            best = wave_max_u64(best);
+            any = wave_max_u64(any);
+            if (t == 0) {
+                sh.best[0] = best;
+                sh.any[0] = any;
+            }
+        }
+    }
+    __syncthreads();
+    // where no token has p > q, one is drawn from p
+    const uint64_t key = sh.best[0] ? sh.best[0] : sh.any[0];
+    finish<DT, MODE>(p, seq, sh, key ? (int64_t)(0xFFFFFFFFu - (uint32_t)key) : -1);
+}
+
+// ---- host ------------------------------------------------------------------------------------
+struct VerifyPlan {
+    Plan sums;
+    int draw_segs, draw_len, launch;      // sequences of a launch
+    size_t parts, keys, bytes;            // of the workspace
+};
+
+VerifyPlan verify_plan(int device, int sequences, int k, int vocab, int dtype) {
+    VerifyPlan v{};
+    const int rows = 2 * k + 1;
+    v.launch = std::max(1, std::min(sequences, symtile_host::kWorkspaceCounters / rows));
+    v.sums = make_plan(device, v.launch * rows, vocab, dtype, false, 0);
+    const int vec = dtype == SYMTILE_F32 ? 4 : 8, n = (vocab + vec - 1) / vec;
+    const int cus = std::max(1, symtile_host::cu_count(device));
+    // as many as give every CU two workgroups, of two vectors a thread at least
+    const int want = std::max(1, 2 * cus / v.launch);
+    const int segs = std::min({want, (n + 2 * kDrawThreads - 1) / (2 * kDrawThreads), 64});
+    const int per = (n + segs - 1) / segs;
+    v.draw_segs = (n + per - 1) / per;
+    v.draw_len = per * vec;
+    v.parts = (size_t)symtile_host::kWorkspaceCounters * 4;
+    v.keys = v.parts + (size_t)v.launch * rows * v.sums.segs * sizeof(Part);
+    v.bytes = v.keys + (size_t)v.launch * v.draw_segs * 16;
+    return v;
+}
+
+symtile_status check_verify(int sequences, int k, int vocab, int dtype) {
+    if (sequences < 0) return fail(SYMTILE_EINVAL, "sequences < 0");
+    if (k < 0 || k > SYMTILE_DRAFT_MAX)
+        return fail(SYMTILE_EINVAL, "drafted must be in 0 .. " + std::to_string(SYMTILE_DRAFT_MAX));
+    if (sequences > (1 << 24)) return fail(SYMTILE_EINVAL, "sequences exceed 16777216");
+    return check_sizes(sequences, vocab, dtype, 0);
+}
+
+template <int MODE>
+const void* draw_kernel_of(int dtype) {
+    switch (dtype) {
+        case SYMTILE_F16: return reinterpret_cast<const void*>(&verify_draw_kernel<SYMTILE_F16, MODE>);
+        case SYMTILE_BF16: return reinterpret_cast<const void*>(&verify_draw_kernel<SYMTILE_BF16, MODE>);
+        default: return reinterpret_cast<const void*>(&verify_draw_kernel<SYMTILE_F32, MODE>);
+    }
+}
+
+}  // namespace
+
+extern "C" symtile_status symtile_verify_workspace_bytes(int device, int sequences, int drafted,
+                                                         int vocab, int dtype, size_t* bytes) {
+    if (!bytes) return fail(SYMTILE_EINVAL, "bytes is NULL");
+    *bytes = 0;
+    if (symtile_status st = check_verify(sequences, drafted, vocab, dtype)) return st;
+    if (symtile_host::cu_count(device) <= 0)
+        return fail(SYMTILE_EINVAL, "device " + std::to_string(device) + " out of range");
+    if (sequences) *bytes = verify_plan(device, sequences, drafted, vocab, dtype).bytes;
+    return SYMTILE_OK;
+}
+
+extern "C" symtile_status symtile_verify_draft(
+    int device, const void* logits, int sequences, int drafted, int vocab, size_t ld, int dtype,
+    float scale, const int64_t* ids, const void* draft_logits, size_t ld_draft, float draft_scale,
+    const float* uniforms, const float* noise, size_t ld_noise, int64_t* tokens, int64_t* accepted,
+    float* logprob, void* workspace, size_t workspace_bytes, symtile_stream s) {
+    if (symtile_status st = check_verify(sequences, drafted, vocab, dtype)) return st;
+    if ((size_t)sequences * (drafted + 1) > (size_t(1) << 30))
+        return fail(SYMTILE_EINVAL, "sequences * (drafted + 1) exceeds 1073741824 rows");
+    if (symtile_status st = check_logits(logits, sequences * (drafted + 1), vocab, &ld, dtype, scale))
+        return st;
+    if (ld_noise == 0) ld_noise = (size_t)vocab;
+    if (!noise && (uniforms || draft_logits))
+        return fail(SYMTILE_EINVAL, "uniforms and draft_logits come with noise");
+    if (draft_logits) {
+        if (symtile_status st = check_logits(draft_logits, sequences * drafted, vocab, &ld_draft,
+                                             dtype, draft_scale))
+            return st;
+    }
+    if (noise && ld_noise < (size_t)vocab) return fail(SYMTILE_EINVAL, "ld_noise smaller than vocab");
+    if (sequences == 0) return SYMTILE_OK;
+    if (noise && ld_noise > (SIZE_MAX >> 3) / (size_t)sequences)
+        return fail(SYMTILE_EINVAL, "noise exceeds the address space");
+    if (noise && drafted && !uniforms) return fail(SYMTILE_EINVAL, "noise comes with uniforms");
+    if ((drafted && !ids) || !tokens || !accepted || !logprob)
+        return fail(SYMTILE_EINVAL, "NULL pointer");
+    const VerifyPlan plan = verify_plan(device, sequences, drafted, vocab, dtype);
+    if (symtile_status st = check_workspace(workspace, workspace_bytes, plan.bytes)) return st;
+    const bool draft = draft_logits && drafted;
+    VerifyParams p{};
+    p.x = logits;
+    p.y = draft_logits;
+    p.ldx = ld;
+    p.ldy = ld_draft;
+    p.ldn = ld_noise;
+    p.ids = ids;
+    p.uniforms = uniforms;
+    p.noise = noise;
+    p.tokens = tokens;
+    p.accepted = accepted;
+    p.logprob = logprob;
+    char* base = static_cast<char*>(workspace);
+    p.counters = reinterpret_cast<uint32_t*>(base);
+    p.parts = reinterpret_cast<Part*>(base + plan.parts);
+    p.keys = reinterpret_cast<uint64_t*>(base + plan.keys);
+    p.k = drafted;
+    p.rows = draft ? 2 * drafted + 1 : drafted + 1;
+    p.vocab = vocab;
+    p.segs = plan.sums.segs;
+    p.seg_len = plan.sums.seg_len;
+    p.draw_segs = noise ? plan.draw_segs : 1;
+    p.draw_len = plan.draw_len;
+    p.scale = scale;
+    p.draft_scale = draft_scale;
+    p.by_segs = symtile_host::make_div(p.segs);
+    p.by_rows = symtile_host::make_div(p.rows);
+    p.by_draw = symtile_host::make_div(p.draw_segs);
+    const void* sums = pick(dtype, plan.sums.nv, [&](auto d, auto nv) -> const void* {
+        constexpr int DT = decltype(d)::value, NV = decltype(nv)::value;
+        return noise ? reinterpret_cast<const void*>(&verify_sums_kernel<DT, NV, false>)
+                     : reinterpret_cast<const void*>(&verify_sums_kernel<DT, NV, true>);
+    });
+    const void* draw = !noise ? draw_kernel_of<kGreedy>(dtype)
+                       : draft ? draw_kernel_of<kDraft>(dtype)
+                               : draw_kernel_of<kTokens>(dtype);
+    OnDevice on(device);
+    if (on.status) return on.status;
+    for (int seq0 = 0; seq0 < sequences; seq0 += plan.launch) {
+        const int n = std::min(plan.launch, sequences - seq0);
+        p.seq0 = seq0;
+        if (symtile_status st = launch(sums, plan.sums, n * p.rows, 0, p, s, "verify_sums_kernel launch"))
+            return st;
+        void* args[] = {&p};
+        hipError_t e = hipLaunchKernel(draw, dim3((unsigned)n * (unsigned)p.draw_segs),
+                                       dim3(kDrawThreads), args, 0, static_cast<hipStream_t>(s));
+        if (e == hipSuccess) e = hipGetLastError();
+        if (e != hipSuccess) return symtile_host::hip_fail(e, "verify_draw_kernel launch");
+    }
+    return SYMTILE_OK;
+}

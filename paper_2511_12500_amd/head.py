@@ -1,6 +1,8 @@
-"""Host-side conveniences over the C ABI for the output head: a shard of 4-bit
-weights, and the outputs and workspace of token log probabilities and of the
-distillation loss over rows of logits.  Argument marshalling only."""
+"""Host-side conveniences over the C ABI for a vocabulary-parallel model's two
+ends: shards of 4-bit weights, the outputs and workspace of token log
+probabilities, of the distillation loss and of the verification of drafted
+tokens over rows of logits, and of the embedding's gradient.  Argument
+marshalling only."""
 from __future__ import annotations
 
 import torch
@@ -41,6 +43,53 @@ class W4Weight:
         self.q, self.scales, self.zeros = q, scales, zeros
         self.pointers = (q.data_ptr(), scales.data_ptr(),
                          None if zeros is None else zeros.data_ptr())
+
+
+class MX4Matrix:
+    """A matrix [rows, K] in blocks of 32 values along a row that share a power of
+    two and hold 4-bit floating-point elements (fp4 e2m1 with e8m0 scales): the
+    weights of a shard, row n those of output column n, or a few thousand tokens.
+
+    ``q``: uint8 [rows, K/2], two consecutive k to a byte, the even one in the low
+    bits; ``scales``: uint8 [rows, K/32].  The tensors are kept, not copied."""
+
+    def __init__(self, q: torch.Tensor, scales: torch.Tensor):
+        if q.dtype != torch.uint8 or scales.dtype != torch.uint8 or q.dim() != 2:
+            raise TypeError("q must be a uint8 matrix, scales uint8")
+        self.rows, self.K = q.shape[0], 2 * q.shape[1]
+        if self.K % 32 or tuple(scales.shape) != (self.rows, self.K // 32):
+            raise ValueError("q must be [rows, K/2] with K a multiple of 32, scales [rows, K/32]")
+        self.device = q.get_device()
+        if not all(t.is_cuda and t.get_device() == self.device and t.is_contiguous()
+                   for t in (q, scales)):
+            raise ValueError("q and scales must be contiguous tensors on one GPU")
+        self.q, self.scales = q, scales
+        self.pointers = (q.data_ptr(), scales.data_ptr())
+
+    @classmethod
+    def empty(cls, rows: int, K: int, device: int = 0) -> "MX4Matrix":
+        """A matrix to be written by ``quantise``."""
+        if rows < 0 or K < 0 or K % 32:
+            raise ValueError("K must be a multiple of 32")
+        return cls(torch.empty((rows, K // 2), dtype=torch.uint8, device=f"cuda:{device}"),
+                   torch.empty((rows, K // 32), dtype=torch.uint8, device=f"cuda:{device}"))
+
+    def quantise(self, x: torch.Tensor, values: torch.Tensor | None = None,
+                 stream: int | None = None) -> None:
+        """Writes x [rows, K] (16 or 32 bits, contiguous rows any distance apart)
+        into this matrix; enqueued on the stream, asynchronous.  ``values``: also
+        what the elements stand for, in x's type; it may be ``x`` itself."""
+        if x.dtype not in _DTYPES:
+            raise TypeError("x must be float16, bfloat16 or float32")
+        ld = _matrix(x, "x", self.rows, self.K, x.dtype, self.device)
+        ld_values = 0 if values is None else _matrix(values, "values", self.rows, self.K, x.dtype,
+                                                     self.device)
+        st = B.lib.symtile_mx4_quantise(
+            self.device, x.data_ptr(), self.rows, self.K, ld, _DTYPES[x.dtype], *self.pointers,
+            None if values is None else values.data_ptr(), ld_values,
+            current_stream(self.device) if stream is None else stream)
+        if st:
+            B._check(st, "symtile_mx4_quantise")
 
 
 def _matrix(t: torch.Tensor, name: str, rows: int, cols: int, dtype: torch.dtype,
@@ -219,3 +268,98 @@ class TopDistillation(_Rows):
             dlogits.data_ptr(), ld_grad, self._stream(stream))
         if st:
             B._check(st, "symtile_distill_topk_backward")
+
+
+class DraftVerification:
+    """Drafted tokens of ``sequences`` sequences, up to ``drafted`` each, accepted
+    or replaced by the target's probabilities softmax(``scale`` * logits).
+
+    Outputs, written by every call: ``tokens`` (int64 [sequences, drafted + 1]:
+    the accepted tokens, the one that follows them, then -1), ``accepted`` (int64
+    [sequences], how many were) and ``logprob`` (fp32 [sequences, drafted + 1],
+    the target's log probabilities of the tokens, 0 behind them).  Calls on one
+    object must not overlap in time."""
+
+    def __init__(self, sequences: int, drafted: int, vocab: int, dtype: torch.dtype,
+                 scale: float = 1.0, draft_scale: float = 1.0, device: int = 0):
+        if dtype not in _DTYPES:
+            raise TypeError("dtype must be float16, bfloat16 or float32")
+        self.sequences, self.drafted, self.vocab, self.dtype = sequences, drafted, vocab, dtype
+        self.scale, self.draft_scale, self.device = scale, draft_scale, device
+        self._dt = _DTYPES[dtype]
+        need = B.symtile_verify_workspace_bytes(device, sequences, drafted, vocab, self._dt)
+        at = f"cuda:{device}"
+        self.ws = torch.zeros(need, dtype=torch.uint8, device=at) if need else None
+        if need and not torch.cuda.is_current_stream_capturing():
+            # the calls may come on any stream, and find the workspace zero on each
+            torch.cuda.current_stream(device).synchronize()
+        self.tokens = torch.empty((sequences, drafted + 1), dtype=torch.int64, device=at)
+        self.accepted = torch.empty((sequences,), dtype=torch.int64, device=at)
+        self.logprob = torch.empty((sequences, drafted + 1), dtype=torch.float32, device=at)
+        self._out = (self.tokens.data_ptr(), self.accepted.data_ptr(), self.logprob.data_ptr(),
+                     None if self.ws is None else self.ws.data_ptr(), need)
+
+    def run(self, logits: torch.Tensor, ids: torch.Tensor, uniforms: torch.Tensor | None = None,
+            noise: torch.Tensor | None = None, draft_logits: torch.Tensor | None = None,
+            stream: int | None = None) -> None:
+        """One call (enqueued on the stream, asynchronous).  ``logits``:
+        [sequences * (drafted + 1), vocab], the rows of a sequence's positions next
+        to each other, contiguous rows any distance apart; ``ids``: int64
+        [sequences, drafted], a draft ending at its first negative one.
+        ``uniforms`` [sequences, drafted] in [0, 1) and ``noise`` [sequences,
+        vocab] of independent exponential numbers, fp32 (rows of noise any
+        distance apart); neither of them: greedy.  ``draft_logits``: [sequences *
+        drafted, vocab], from which softmax(draft_scale * draft_logits) the drafted
+        tokens were drawn; None: they were not drawn."""
+        S, k, V, dev = self.sequences, self.drafted, self.vocab, self.device
+        ld = _matrix(logits, "logits", S * (k + 1), V, self.dtype, dev)
+        ld_draft = 0 if draft_logits is None else _matrix(draft_logits, "draft_logits", S * k, V,
+                                                          self.dtype, dev)
+        ld_noise = 0 if noise is None else _matrix(noise, "noise", S, V, torch.float32, dev)
+        st = B.lib.symtile_verify_draft(
+            dev, logits.data_ptr(), S, k, V, ld, self._dt, self.scale,
+            _vector(ids, "ids", (S, k), torch.int64, dev),
+            None if draft_logits is None else draft_logits.data_ptr(), ld_draft, self.draft_scale,
+            _vector(uniforms, "uniforms", (S, k), torch.float32, dev),
+            None if noise is None else noise.data_ptr(), ld_noise, *self._out,
+            current_stream(dev) if stream is None else stream)
+        if st:
+            B._check(st, "symtile_verify_draft")
+
+
+class EmbeddingGrad:
+    """The gradient of a vocabulary-parallel table's shard from ``T`` rows of ``D``
+    columns; holds the workspace.  Calls on one object must not overlap in time."""
+
+    def __init__(self, T: int, D: int, dtype: torch.dtype, device: int = 0):
+        if dtype not in _DTYPES:
+            raise TypeError("dtype must be float16, bfloat16 or float32")
+        self.T, self.D, self.dtype, self.device = T, D, dtype, device
+        need = B.symtile_embed_workspace_bytes(device, T, D)
+        self.ws = torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}") if need else None
+        if need and not torch.cuda.is_current_stream_capturing():
+            # the calls may come on any stream, and what had this memory before is done with it
+            torch.cuda.current_stream(device).synchronize()
+        self._ws = (None if self.ws is None else self.ws.data_ptr(), need)
+
+    def run(self, tokens: torch.Tensor, drows: torch.Tensor, dtable: torch.Tensor, first: int = 0,
+            scale: float = 1.0, accumulate: bool = False, stream: int | None = None) -> None:
+        """dtable[v] = ``scale`` * the sum of drows[t] over the tokens t of id
+        ``first`` + v, rows without one zero; with ``accumulate`` added to what
+        dtable holds.  ``tokens``: int64 [T]; ``drows``: [T, D]; ``dtable``: [rows,
+        D] of any of the three types; both with contiguous rows.  Enqueued on the
+        stream, asynchronous."""
+        if dtable.dtype not in _DTYPES:
+            raise TypeError("dtable must be float16, bfloat16 or float32")
+        if dtable.dim() != 2:
+            raise ValueError("dtable must be a matrix")
+        ld = _matrix(drows, "drows", self.T, self.D, self.dtype, self.device)
+        rows = dtable.shape[0]
+        ld_table = _matrix(dtable, "dtable", rows, self.D, dtable.dtype, self.device)
+        st = B.lib.symtile_embed_backward(
+            self.device, _vector(tokens, "tokens", (self.T,), torch.int64, self.device), self.T,
+            drows.data_ptr(), self.D, ld, _DTYPES[self.dtype], first, rows, scale,
+            dtable.data_ptr(), ld_table, _DTYPES[dtable.dtype], int(accumulate), *self._ws,
+            current_stream(self.device) if stream is None else stream)
+        if st:
+            B._check(st, "symtile_embed_backward")

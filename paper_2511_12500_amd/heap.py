@@ -149,6 +149,7 @@ class GatheredOutput:
         self.ws = None           # split-K workspace (uint8 device tensor), grown on demand
         self.ws_seen = heap.failed_barriers   # failed barriers already answered by a reset
         self.ws_w4 = {}          # run_w4's workspace (uint8 device tensor or None) per (K, group)
+        self.ws_mx4 = {}         # run_mx4's, per K
         # per-call constants, computed once (run() is on the host's launch path):
         # the output's and counters' addresses per rank, the workspace size per
         # slice count, and one config struct filled in by every call
@@ -306,3 +307,103 @@ class GatheredOutput:
             current_stream(self.heap.device) if stream is None else stream)
         if st:
             B._check(st, "symtile_w4_all_scatter")
+
+    def _workspace_mx4(self, K: int, stream: int | None) -> torch.Tensor | None:
+        """run_mx4's workspace for this K, as run_w4's."""
+        if K not in self.ws_mx4:
+            need = B.symtile_mx4_workspace_bytes(self.heap.device, self.M, self.N_local, K)
+            with launching(stream, self.heap.device):
+                self.ws_mx4[K] = (torch.zeros(need, dtype=torch.uint8, device=self.heap.mem.device)
+                                  if need else None)
+        return self.ws_mx4[K]
+
+    def run_mx4(self, X, weight, rank: int, stream: int | None = None) -> None:
+        """The call of rank ``rank`` for tokens X and its shard of weights, both
+        ``MX4Matrix`` ([M, K] and [N_local, K]): the product lands in the same
+        places and counts the same arrivals as ``run``'s, in tiles of MX4_TILE_M x
+        MX4_TILE_N, which this object must have been made with.  Enqueued on the
+        stream, asynchronous; calls on one object must not overlap in time.  It can
+        be captured in a graph; make one eager call first so that its workspace
+        exists."""
+        device = self.heap.device
+        if X.device != device or weight.device != device:
+            raise ValueError(f"X and the weight must be on cuda:{device}")
+        M, K = X.rows, X.K
+        if M != self.M or weight.rows != self.N_local or weight.K != K:
+            raise ValueError("shape mismatch")
+        if (self.tile_m, self.tile_n) != (B.MX4_TILE_M, B.MX4_TILE_N):
+            raise ValueError("the output must be made with MX4_TILE_M x MX4_TILE_N tiles")
+        ptrs = self._ptrs.get(rank)
+        if ptrs is None:
+            ptrs = self._ptrs[rank] = (self.heap.ptr(rank, self.c_off),
+                                       self.heap.ptr(rank, self.flag_off))
+        ws = self._workspace_mx4(K, stream)
+        st = B.lib.symtile_mx4_all_scatter(
+            self.heap.handle, *X.pointers, *weight.pointers, ptrs[0], ptrs[1], M, self.N_local, K,
+            self._dt, rank, self.heap.world, None if ws is None else ws.data_ptr(),
+            0 if ws is None else ws.numel(), current_stream(device) if stream is None else stream)
+        if st:
+            B._check(st, "symtile_mx4_all_scatter")
+
+
+class GatheredRows:
+    """The symmetric objects of the lookup of ``T`` tokens in a vocabulary-parallel
+    table of ``D`` columns in ``heap``: the rows [T, D], which every rank's call
+    fills with those of its own tokens, and the arrival counters [w, tiles_m,
+    tiles_n] of EMBED_TILE_M tokens by EMBED_TILE_BYTES each."""
+
+    def __init__(self, heap: Heap, T: int, D: int, dtype: torch.dtype):
+        dt = {torch.float16: B.F16, torch.bfloat16: B.BF16, torch.float32: B.F32}.get(dtype)
+        if dt is None:
+            raise TypeError("dtype must be float16, bfloat16 or float32")
+        self.heap, self.T, self.D, self.dtype, self._dt = heap, T, D, dtype, dt
+        self.tiles_m = _tiles(T, B.EMBED_TILE_M)
+        self.tiles_n = _tiles(D * dtype.itemsize, B.EMBED_TILE_BYTES)
+        self.out_off = heap.alloc(max(T * D * dtype.itemsize, 16), 256)
+        self.flag_off = heap.alloc(max(heap.world * self.tiles_m * self.tiles_n * 4, 4), 256)
+        self._ptrs = {}
+
+    def rows(self, rank: int) -> torch.Tensor:
+        return self.heap.view(rank, self.out_off, (self.T, self.D), self.dtype)
+
+    def rows_all(self) -> torch.Tensor:
+        return self.heap.slots_view(self.out_off, (self.T, self.D), self.dtype)
+
+    def arrived(self, rank: int) -> torch.Tensor:
+        return self.heap.view(rank, self.flag_off, (self.heap.world, self.tiles_m, self.tiles_n),
+                              torch.int32)
+
+    def arrived_all(self) -> torch.Tensor:
+        return self.heap.slots_view(self.flag_off, (self.heap.world, self.tiles_m, self.tiles_n),
+                                    torch.int32)
+
+    def run(self, tokens: torch.Tensor, table: torch.Tensor, rank: int, first: int | None = None,
+            scale: float = 1.0, stream: int | None = None) -> None:
+        """The call of rank ``rank`` for its shard ``table`` [rows, D] (contiguous
+        rows), which holds the tokens from ``first`` on (default: rank * rows):
+        ``scale`` times the rows of its tokens into every slot; rank 0 also stores
+        zeros for negative ``tokens`` (int64 [T]).  Enqueued on the stream,
+        asynchronous; it can be captured in a graph."""
+        device = self.heap.device
+        if tokens.dtype != torch.int64 or table.dtype != self.dtype:
+            raise TypeError(f"tokens must be int64, table {self.dtype}")
+        if tokens.get_device() != device or tokens.shape != (self.T,) or not tokens.is_contiguous():
+            raise ValueError(f"tokens must be a contiguous tensor [{self.T}] on cuda:{device}")
+        if table.get_device() != device or table.dim() != 2 or table.shape[1] != self.D:
+            raise ValueError(f"table must be a [rows, {self.D}] tensor on cuda:{device}")
+        rows = table.shape[0]
+        if self.D > 1 and table.stride(1) != 1:
+            raise ValueError("table must have contiguous rows")
+        ld = table.stride(0) if rows > 1 else self.D
+        if ld < self.D:
+            raise ValueError("rows of the table must not overlap")
+        ptrs = self._ptrs.get(rank)
+        if ptrs is None:
+            ptrs = self._ptrs[rank] = (self.heap.ptr(rank, self.out_off),
+                                       self.heap.ptr(rank, self.flag_off))
+        st = B.lib.symtile_embed_all_scatter(
+            self.heap.handle, tokens.data_ptr(), self.T, table.data_ptr(), rows, self.D, ld,
+            self._dt, rank * rows if first is None else first, scale, *ptrs, rank,
+            self.heap.world, current_stream(device) if stream is None else stream)
+        if st:
+            B._check(st, "symtile_embed_all_scatter")
