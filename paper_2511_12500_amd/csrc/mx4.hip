@@ -113,8 +113,26 @@ struct ProductParams {
     uint64_t c_off, flag_off;   // of the rank's column block and its counters in a slot
     int M, N, groups, world;    // groups: blocks of a row
     size_t ldc;                 // elements
-    int tiles_n;
+    int tiles_n;                // of the counters
+    // of the kernel for many rows: its tiles, and how they are numbered
+    int gm, gn, per_xcd, xcd_rest;
+    int band;                   // tiles of a band
+    symtile_host::Div by_band;
 };
+
+// Tile b of the grid.  Workgroups go to the 8 XCDs in turn; each takes tiles next to each
+// other, in bands of kBandRows tile rows, so that those that run together share rows of
+// both matrices in its L2.
+constexpr int kXcds = 8, kBandRows = 8;
+__device__ __forceinline__ void place_tile(const ProductParams& p, int b, int* tm, int* tn) {
+    const int xcd = b % kXcds, i = b / kXcds;
+    const int id = xcd * p.per_xcd + min(xcd, p.xcd_rest) + i;
+    const int band = p.by_band(id), first = band * kBandRows, in = id - band * p.band;
+    const int height = min(kBandRows, p.gm - first);
+    const int n = height == kBandRows ? in / kBandRows : in / height;
+    *tm = first + in - n * height;
+    *tn = n;
+}
 
 struct __attribute__((packed, aligned(1))) Unaligned16 {
     u32x4 v;
@@ -227,6 +245,275 @@ __global__ void __launch_bounds__(64 * kWaves) mx4_kernel(ProductParams p) {
         if (lane == 0)
             symtile::flag_signal(reinterpret_cast<uint32_t*>(base + p.flag_off) +
                                  (size_t)tm * p.tiles_n + tn);
+    }
+}
+
+// ---- many rows ----------------------------------------------------------------------------
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// 32 rows of `a` by 32 rows of `b`, 64 values each: lane (r = lane % 32, g = lane / 32)
+// holds a block of row r of both.  Byte S of sa and sb are its scales.
+template <int S>
+__device__ __forceinline__ f32x16 mfma32(const u32x4& a, const u32x4& b, f32x16 c, uint32_t sa,
+                                         uint32_t sb) {
+    const i32x8 va = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+    const i32x8 vb = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(va, vb, c, 4, 4, S, (int)sa, S, (int)sb);
+}
+
+// s_waitcnt immediate: at most n vector-memory operations outstanding, no LDS ones
+// (gfx9 encoding: vmcnt 3:0 and 15:14, expcnt 6:4, lgkmcnt 11:8).
+constexpr int wait_loads(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4); }
+
+// A workgroup of 4 waves takes TM rows of X by TN of W.  K goes by stages of 256 values,
+// 128 bytes a row, loaded straight into one of two buffers in LDS while the other is
+// multiplied; row r's 16-byte vector v lies at place v ^ (r % 8), so that 8 rows' same
+// vector touch every bank once.  In instruction s of a stage lane half g takes block
+// 4 g + s of its rows, so a lane's four scales of a stage are one word; the scales of two
+// stages come by 16 bytes a row, through registers.
+constexpr int kStageBytes = 128;
+template <int TM, int TN>
+struct GemmLds {
+    struct Stage {
+        uint8_t w[TN * kStageBytes], x[TM * kStageBytes];
+    };
+    union {
+        Stage stage[2];
+        uint16_t out[TM * TN];
+    };
+    u32x4 scales[2][TN + TM];
+};
+
+// The wave's loads are there and its LDS accesses done, and so are all other waves'.
+__device__ __forceinline__ void meet() {
+    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+template <bool BF, int TM, int TN>
+__global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_kernel(ProductParams p) {
+    typedef GemmLds<TM, TN> Lds;
+    __shared__ __attribute__((aligned(16))) Lds lds;
+    constexpr int kMT = TM / 64, kNT = TN / 64;           // 32 x 32 tiles of a wave
+    constexpr int kRows = TN + TM;
+    constexpr int kScaleLoads = (kRows + 255) / 256;
+    const int t = threadIdx.x, lane = t % 64, r = lane % 32, g = lane / 32;
+    const int wave = __builtin_amdgcn_readfirstlane(t / 64), wn = wave % 2, wm = wave / 2;
+    int tm, tn;
+    place_tile(p, blockIdx.x, &tm, &tn);
+    const int m0 = tm * TM, n0 = tn * TN;
+    const int rows = min(TM, p.M - m0), cols = min(TN, p.N - n0);
+    const int row_bytes = p.groups * (kBlock / 2);
+    const int stages = (p.groups + 7) / 8;
+    const symtile::i32x4_t ws = symtile::make_rsrc_words(p.w + (size_t)n0 * row_bytes,
+                                                         (uint32_t)(cols * row_bytes));
+    const symtile::i32x4_t xs = symtile::make_rsrc_words(p.x + (size_t)m0 * row_bytes,
+                                                         (uint32_t)(rows * row_bytes));
+    const int vec = (lane % 8) ^ (lane / 8);
+    const uint32_t at = (uint32_t)(lane / 8 * row_bytes + vec * 16);
+    const uint32_t lds0 = symtile::lds_addr(&lds);
+    // Part `q` of 4 of stage st's loads (behind a row's end: outside of the resources, zeros).
+    auto load = [&](int st, int q) {
+        const uint32_t from = st * kStageBytes + vec * 16 < row_bytes ? at : symtile::kOOB;
+        const uint32_t to = lds0 + (st & 1) * (uint32_t)sizeof(typename Lds::Stage);
+#pragma unroll
+        for (int u = q * (TN / 128); u < (q + 1) * (TN / 128); ++u) {
+            const int row = (wave * (TN / 32) + u) * 8;
+            symtile::buf_ld16_lds_async(ws, to + row * kStageBytes, from,
+                                        (uint32_t)(row * row_bytes + st * kStageBytes));
+        }
+#pragma unroll
+        for (int u = q * (TM / 128); u < (q + 1) * (TM / 128); ++u) {
+            const int row = (wave * (TM / 32) + u) * 8;
+            symtile::buf_ld16_lds_async(xs, to + (TN + row) * kStageBytes, from,
+                                        (uint32_t)(row * row_bytes + st * kStageBytes));
+        }
+    };
+    // Scales of two stages for the rows t + 256 i of W and X, those of the last ones again for
+    // the rows that are not there.  fetch_scales() asks for 16 bytes, the last ones of the array
+    // where it ends before; place_scales() moves them into place, zeros behind a row's end.
+    u32x4 sc[kScaleLoads];
+    int shift[kScaleLoads];
+    const uint8_t *scales_of[kScaleLoads], *scales_end[kScaleLoads];
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i) {
+        const int row = t + i * 256;
+        const bool of_w = row < TN;
+        scales_of[i] = of_w ? p.w_scales + (size_t)(n0 + min(row, cols - 1)) * p.groups
+                            : p.x_scales + (size_t)(m0 + min(row - TN, rows - 1)) * p.groups;
+        scales_end[i] = (of_w ? p.w_scales + (size_t)p.N * p.groups
+                              : p.x_scales + (size_t)p.M * p.groups) - 16;
+    }
+    auto fetch_scales = [&](int pair) {
+#pragma unroll
+        for (int i = 0; i < kScaleLoads; ++i) {
+            const uint8_t* from = scales_of[i] + min(pair * 16, p.groups - 1);
+            const uint8_t* first = from < scales_end[i] ? from : scales_end[i];
+            shift[i] = (int)(from - first) * 8;
+            sc[i] = reinterpret_cast<const Unaligned16*>(first)->v;
+        }
+    };
+    auto place_scales = [&](int pair) {
+        const int valid = p.groups - pair * 16;
+        if (valid < 16) {
+#pragma unroll
+            for (int i = 0; i < kScaleLoads; ++i) {
+                const uint64_t lo = (uint64_t)sc[i][1] << 32 | sc[i][0];
+                const uint64_t hi = (uint64_t)sc[i][3] << 32 | sc[i][2];
+                const int n = shift[i];
+                const uint64_t l = n == 0 ? lo : n < 64 ? lo >> n | hi << (64 - n) : hi >> (n - 64);
+                const uint64_t h = n < 64 ? hi >> n : 0;
+                sc[i] = u32x4{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int keep = valid - 4 * j;
+                    if (keep < 4) sc[i][j] = keep <= 0 ? 0u : sc[i][j] & ((1u << (8 * keep)) - 1u);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kScaleLoads; ++i)
+            if (t + i * 256 < kRows) lds.scales[pair & 1][t + i * 256] = sc[i];
+    };
+    f32x16 acc[kNT][kMT] = {};
+    // A lane's operands of instruction S in a stage: its row's base ^ S * 16.
+    struct Operands {
+        u32x4 w[kNT], x[kMT];
+    };
+    const int base_w = (wn * (TN / 2) + r) * kStageBytes + (((4 * g) ^ (r % 8)) * 16);
+    const int base_x = (wm * (TM / 2) + r) * kStageBytes + (((4 * g) ^ (r % 8)) * 16);
+    auto read = [&](Operands& o, int st, int S) {
+        const typename Lds::Stage& now = lds.stage[st & 1];
+#pragma unroll
+        for (int i = 0; i < kNT; ++i)
+            o.w[i] = symtile::ld16(&now.w[(base_w ^ (S * 16)) + i * 32 * kStageBytes]);
+#pragma unroll
+        for (int j = 0; j < kMT; ++j)
+            o.x[j] = symtile::ld16(&now.x[(base_x ^ (S * 16)) + j * 32 * kStageBytes]);
+    };
+    struct Bytes {
+        uint32_t w[kNT], x[kMT];
+    };
+    auto read_scales = [&](Bytes& o, int st) {
+        const uint32_t* of = reinterpret_cast<const uint32_t*>(lds.scales[st >> 1 & 1]) +
+                             (st & 1) * 2 + g;
+#pragma unroll
+        for (int i = 0; i < kNT; ++i) o.w[i] = of[(wn * (TN / 2) + i * 32 + r) * 4];
+#pragma unroll
+        for (int j = 0; j < kMT; ++j) o.x[j] = of[(TN + wm * (TM / 2) + j * 32 + r) * 4];
+    };
+    auto row_of_tiles = [&](auto s_, int i, const Operands& o, const Bytes& e) {
+        constexpr int S = decltype(s_)::value;
+#pragma unroll
+        for (int j = 0; j < kMT; ++j)
+            acc[i][j] = mfma32<S>(o.w[i], o.x[j], acc[i][j], e.w[i], e.x[j]);
+    };
+    // The matrix instructions before stay before what follows.
+    auto pin = [&](int i) {
+#pragma unroll
+        for (int j = 0; j < kMT; ++j) asm volatile("" : "+a"(acc[i][j]));
+    };
+    // Multiplies `o` while the operands of instruction S + 1 are read into `next`, the reads
+    // between the matrix instructions.
+    auto multiply = [&](auto s_, const Operands& o, const Bytes& e, Operands& next, int st) {
+        read(next, st, decltype(s_)::value + 1);
+#pragma unroll
+        for (int i = 0; i < kNT; ++i) row_of_tiles(s_, i, o, e);
+#pragma unroll
+        for (int i = 0; i < kNT + kMT; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // an LDS read
+            __builtin_amdgcn_sched_group_barrier(0x8, kNT * kMT / (kNT + kMT), 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // A stage's first three multiplications go on while its other operands are read; then all
+    // waves have read it, the next one is there, and its place is the stage's after the next,
+    // whose loads go between the matrix instructions of the fourth.
+    Operands a, b;
+    Bytes even, odd;
+    auto stage = [&](int st, const Bytes& e, Bytes& e_next, bool is_odd) {
+        multiply(std::integral_constant<int, 0>{}, a, e, b, st);
+        multiply(std::integral_constant<int, 1>{}, b, e, a, st);
+        multiply(std::integral_constant<int, 2>{}, a, e, b, st);
+#pragma unroll
+        for (int i = 0; i < kNT; ++i) pin(i);
+        __builtin_amdgcn_s_waitcnt(wait_loads(0));
+        if (is_odd) place_scales((st + 1) >> 1);
+        meet();
+        if (!is_odd) fetch_scales((st + 2) >> 1);
+        read(a, st + 1, 0);
+        read_scales(e_next, st + 1);
+#pragma unroll
+        for (int i = 0; i < kNT; ++i) {
+            row_of_tiles(std::integral_constant<int, 3>{}, i, b, e);
+            pin(i);
+#pragma unroll
+            for (int q = i * 4 / kNT; q < (i + 1) * 4 / kNT; ++q) load(st + 2, q);
+        }
+    };
+    if (p.groups) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) load(0, q);
+        fetch_scales(0);
+        place_scales(0);
+        meet();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) load(1, q);
+        read(a, 0, 0);
+        read_scales(even, 0);
+        // (in pairs; stages behind K are zeros)
+        for (int st = 0; st < stages; st += 2) {
+            stage(st, even, odd, false);
+            stage(st + 1, odd, even, true);
+        }
+        __builtin_amdgcn_s_waitcnt(wait_loads(0));
+    }
+    // The stages' place is the results' from here on, rows of TN: vector v of 8 values of row
+    // m at v ^ (m % 32).  A lane has four values in a row of each group of accumulators.
+    __syncthreads();
+    constexpr int kVecs = TN / 8, kMask = (kVecs < 32 ? kVecs : 32) - 1;
+#pragma unroll
+    for (int i = 0; i < kNT; ++i)
+#pragma unroll
+        for (int j = 0; j < kMT; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int n = wn * (TN / 2) + i * 32 + 8 * q + 4 * g, m = wm * (TM / 2) + j * 32 + r;
+                uint2 v;
+                const f32x16& a = acc[i][j];
+                v.x = rounded<BF>(a[4 * q]) | (uint32_t)rounded<BF>(a[4 * q + 1]) << 16;
+                v.y = rounded<BF>(a[4 * q + 2]) | (uint32_t)rounded<BF>(a[4 * q + 3]) << 16;
+                *reinterpret_cast<uint2*>(
+                    &lds.out[m * TN + (((n / 8) ^ (m & kMask)) * 8) + n % 8]) = v;
+            }
+    __syncthreads();
+    // a wave stores 64 rows by kCols columns into every slot and counts their tiles
+    constexpr int kCols = TM * TN / 256, kAcross = TN / kCols;
+    constexpr int kLanes = kCols / 8, kPer = 64 / kLanes, kSteps = 64 / kPer;
+    const int sr = wave / kAcross * 64, sn = wave % kAcross * kCols;
+    const int own_rows = min(64, rows - sr), own_cols = min(kCols, cols - sn);
+    if (own_rows <= 0 || own_cols <= 0) return;
+    const int row0 = lane / kLanes, v0 = lane % kLanes;
+    const bool in = v0 * 8 < own_cols;
+    for (int s = 0; s < p.world; ++s) {
+        char* base = reinterpret_cast<char*>(p.bases[s]);
+        const symtile::rsrc_t dst = symtile::make_rsrc(
+            base + p.c_off + ((size_t)(m0 + sr) * p.ldc + n0 + sn) * 2,
+            (uint32_t)(((size_t)(own_rows - 1) * p.ldc + own_cols) * 2));
+#pragma unroll 8
+        for (int i = 0; i < kSteps; ++i) {
+            const int m = i * kPer + row0;
+            symtile::buf_st16p<symtile::kStoreWriteThrough>(
+                symtile::ld16(&lds.out[(sr + m) * TN + (((sn / 8 + v0) ^ ((sr + m) & kMask)) * 8)]),
+                dst, in ? (uint32_t)((row0 * p.ldc + v0 * 8) * 2) : symtile::kOOB,
+                (uint32_t)(i * kPer * p.ldc * 2));
+        }
+        symtile::release_written_through();
+        if (lane < (own_cols + kTileN - 1) / kTileN)
+            symtile::flag_signal(reinterpret_cast<uint32_t*>(base + p.flag_off) +
+                                 (size_t)((m0 + sr) / kTileM) * p.tiles_n + (n0 + sn) / kTileN + lane);
     }
 }
 
@@ -366,6 +653,28 @@ extern "C" symtile_status symtile_mx4_all_scatter(
     p.world = world_size;
     p.ldc = ldc;
     p.tiles_n = tiles_n;
+    if (M > kTileM && (size_t)N_local * p.groups >= 16) {   // (scales come by 16)
+        constexpr int TM = 256, TN = 256;
+        p.gm = ceil_div(M, TM);
+        p.gn = ceil_div(N_local, TN);
+        const size_t tiles = (size_t)p.gm * p.gn;
+        if (tiles > (1u << 24)) return fail(SYMTILE_EINVAL, "more than 16777216 tiles");
+        p.per_xcd = (int)(tiles / kXcds);
+        p.xcd_rest = (int)(tiles % kXcds);
+        p.band = kBandRows * p.gn;
+        p.by_band = symtile_host::make_div(p.band);
+        int prev = -1;
+        if (symtile_status st = symtile_host::set_device(h, &prev)) return st;
+        void* args[] = {&p};
+        const void* kernel = dtype == SYMTILE_BF16
+                                 ? reinterpret_cast<const void*>(&mx4_gemm_kernel<true, TM, TN>)
+                                 : reinterpret_cast<const void*>(&mx4_gemm_kernel<false, TM, TN>);
+        hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)tiles), dim3(256), args, 0,
+                                       static_cast<hipStream_t>(s));
+        if (e == hipSuccess) e = hipGetLastError();
+        if (prev >= 0) (void)hipSetDevice(prev);
+        return e == hipSuccess ? SYMTILE_OK : symtile_host::hip_fail(e, "mx4_gemm_kernel launch");
+    }
     const int mt = M > 48 ? 4 : M > 32 ? 3 : M > 16 ? 2 : 1;
     const void* const kernels[2][4] = {
         {reinterpret_cast<const void*>(&mx4_kernel<false, 1>),
