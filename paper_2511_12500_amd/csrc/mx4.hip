@@ -265,39 +265,41 @@ __device__ __forceinline__ f32x16 mfma32(const u32x4& a, const u32x4& b, f32x16 
 // (gfx9 encoding: vmcnt 3:0 and 15:14, expcnt 6:4, lgkmcnt 11:8).
 constexpr int wait_loads(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4); }
 
-// A workgroup of 4 waves takes TM rows of X by TN of W.  K goes by stages of 256 values,
-// 128 bytes a row, loaded straight into one of two buffers in LDS while the other is
-// multiplied; row r's 16-byte vector v lies at place v ^ (r % 8), so that 8 rows' same
-// vector touch every bank once.  In instruction s of a stage lane half g takes block
-// 4 g + s of its rows, so a lane's four scales of a stage are one word; the scales of two
-// stages come by 16 bytes a row, through registers.
-constexpr int kStageBytes = 128;
+// At most N of the wave's loads are out, its LDS accesses done, and so for all waves.
+template <int N>
+__device__ __forceinline__ void meet() {
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (0 << 8));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// A workgroup of 4 waves takes TM rows of X by TN of W.  K goes by stages of 128 values,
+// 64 bytes a row, loaded straight into a ring of four buffers in LDS; row r's 16-byte
+// vector v lies at place v ^ (r / 4 % 4), so that 16 rows' same vector touch every bank
+// once.  In instruction S of a stage's two lane half g takes block 2 g + S of its rows, so
+// a lane's scales of a stage are two bytes next to each other; scales come for four
+// stages, 16 bytes a row, straight into LDS too where rows of scales are whole numbers of
+// 16 aligned bytes (ALIGNED), else through registers.
+constexpr int kStageBytes = 64, kRing = 4;
 template <int TM, int TN>
 struct GemmLds {
     struct Stage {
         uint8_t w[TN * kStageBytes], x[TM * kStageBytes];
     };
     union {
-        Stage stage[2];
+        Stage stage[kRing];
         uint16_t out[TM * TN];
     };
     u32x4 scales[2][TN + TM];
 };
 
-// The wave's loads are there and its LDS accesses done, and so are all other waves'.
-__device__ __forceinline__ void meet() {
-    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
-template <bool BF, int TM, int TN>
+template <bool BF, int TM, int TN, bool ALIGNED>
 __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_kernel(ProductParams p) {
     typedef GemmLds<TM, TN> Lds;
     __shared__ __attribute__((aligned(16))) Lds lds;
     constexpr int kMT = TM / 64, kNT = TN / 64;           // 32 x 32 tiles of a wave
-    constexpr int kRows = TN + TM;
+    constexpr int kRows = TN + TM, kLoads = kRows / 64;   // loads of 16 rows a wave and stage
     constexpr int kScaleLoads = (kRows + 255) / 256;
     const int t = threadIdx.x, lane = t % 64, r = lane % 32, g = lane / 32;
     const int wave = __builtin_amdgcn_readfirstlane(t / 64), wn = wave % 2, wm = wave / 2;
@@ -306,167 +308,184 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
     const int m0 = tm * TM, n0 = tn * TN;
     const int rows = min(TM, p.M - m0), cols = min(TN, p.N - n0);
     const int row_bytes = p.groups * (kBlock / 2);
-    const int stages = (p.groups + 7) / 8;
+    const int stages = (p.groups + 3) / 4;
     const symtile::i32x4_t ws = symtile::make_rsrc_words(p.w + (size_t)n0 * row_bytes,
                                                          (uint32_t)(cols * row_bytes));
     const symtile::i32x4_t xs = symtile::make_rsrc_words(p.x + (size_t)m0 * row_bytes,
                                                          (uint32_t)(rows * row_bytes));
-    const int vec = (lane % 8) ^ (lane / 8);
-    const uint32_t at = (uint32_t)(lane / 8 * row_bytes + vec * 16);
     const uint32_t lds0 = symtile::lds_addr(&lds);
-    // Part `q` of 4 of stage st's loads (behind a row's end: outside of the resources, zeros).
-    auto load = [&](int st, int q) {
-        const uint32_t from = st * kStageBytes + vec * 16 < row_bytes ? at : symtile::kOOB;
-        const uint32_t to = lds0 + (st & 1) * (uint32_t)sizeof(typename Lds::Stage);
-#pragma unroll
-        for (int u = q * (TN / 128); u < (q + 1) * (TN / 128); ++u) {
-            const int row = (wave * (TN / 32) + u) * 8;
+    // A load fills 16 rows: lane l place l % 4 of row l / 4.
+    const int vec = (lane % 4) ^ (lane / 16);
+    const uint32_t row_at = (uint32_t)(lane / 4 * row_bytes + vec * 16);
+    // Load u of the wave's for stage st into the ring's place `to_slot` = st % 4 (behind a row's
+    // end: outside of the resources, zeros).
+    auto load = [&](int st, int to_slot, int u) {
+        const uint32_t from = st * kStageBytes + vec * 16 < row_bytes ? row_at : symtile::kOOB;
+        const uint32_t to = lds0 + to_slot * (uint32_t)sizeof(typename Lds::Stage);
+        if (u < TN / 64) {
+            const int row = (wave * (TN / 64) + u) * 16;
             symtile::buf_ld16_lds_async(ws, to + row * kStageBytes, from,
                                         (uint32_t)(row * row_bytes + st * kStageBytes));
-        }
-#pragma unroll
-        for (int u = q * (TM / 128); u < (q + 1) * (TM / 128); ++u) {
-            const int row = (wave * (TM / 32) + u) * 8;
+        } else {
+            const int row = (wave * (TM / 64) + u - TN / 64) * 16;
             symtile::buf_ld16_lds_async(xs, to + (TN + row) * kStageBytes, from,
                                         (uint32_t)(row * row_bytes + st * kStageBytes));
         }
     };
-    // Scales of two stages for the rows t + 256 i of W and X, those of the last ones again for
-    // the rows that are not there.  fetch_scales() asks for 16 bytes, the last ones of the array
-    // where it ends before; place_scales() moves them into place, zeros behind a row's end.
+    // Scales of four stages (a quad) for the rows of W and X, those of the last ones again for
+    // the rows that are not there.
+    symtile::i32x4_t scale_rsrc[kScaleLoads];
+    uint32_t scale_at[kScaleLoads];
     u32x4 sc[kScaleLoads];
     int shift[kScaleLoads];
     const uint8_t *scales_of[kScaleLoads], *scales_end[kScaleLoads];
 #pragma unroll
     for (int i = 0; i < kScaleLoads; ++i) {
-        const int row = t + i * 256;
-        const bool of_w = row < TN;
-        scales_of[i] = of_w ? p.w_scales + (size_t)(n0 + min(row, cols - 1)) * p.groups
-                            : p.x_scales + (size_t)(m0 + min(row - TN, rows - 1)) * p.groups;
-        scales_end[i] = (of_w ? p.w_scales + (size_t)p.N * p.groups
-                              : p.x_scales + (size_t)p.M * p.groups) - 16;
+        if constexpr (ALIGNED) {
+            const int first = wave * (kRows / 4) + i * 64, row = first + lane;   // 64 of one matrix
+            const bool of_w = first < TN;
+            scale_rsrc[i] = of_w ? symtile::make_rsrc_words(p.w_scales + (size_t)n0 * p.groups,
+                                                            (uint32_t)(cols * p.groups))
+                                 : symtile::make_rsrc_words(p.x_scales + (size_t)m0 * p.groups,
+                                                            (uint32_t)(rows * p.groups));
+            scale_at[i] = (uint32_t)((of_w ? row : row - TN) * p.groups);
+        } else {
+            const int row = t + i * 256;
+            const bool of_w = row < TN;
+            scales_of[i] = of_w ? p.w_scales + (size_t)(n0 + min(row, cols - 1)) * p.groups
+                                : p.x_scales + (size_t)(m0 + min(row - TN, rows - 1)) * p.groups;
+            scales_end[i] = (of_w ? p.w_scales + (size_t)p.N * p.groups
+                                  : p.x_scales + (size_t)p.M * p.groups) - 16;
+        }
     }
-    auto fetch_scales = [&](int pair) {
+    // Asks for a quad's scales: into LDS, or 16 bytes a row into registers, the last ones of the
+    // array where it ends before; place_scales() moves those into place, zeros behind a row's
+    // end (which meet zeros of both matrices; a neighbour row's byte may be a NaN's).
+    auto fetch_scales = [&](int quad) {
 #pragma unroll
         for (int i = 0; i < kScaleLoads; ++i) {
-            const uint8_t* from = scales_of[i] + min(pair * 16, p.groups - 1);
-            const uint8_t* first = from < scales_end[i] ? from : scales_end[i];
-            shift[i] = (int)(from - first) * 8;
-            sc[i] = reinterpret_cast<const Unaligned16*>(first)->v;
-        }
-    };
-    auto place_scales = [&](int pair) {
-        const int valid = p.groups - pair * 16;
-        if (valid < 16) {
-#pragma unroll
-            for (int i = 0; i < kScaleLoads; ++i) {
-                const uint64_t lo = (uint64_t)sc[i][1] << 32 | sc[i][0];
-                const uint64_t hi = (uint64_t)sc[i][3] << 32 | sc[i][2];
-                const int n = shift[i];
-                const uint64_t l = n == 0 ? lo : n < 64 ? lo >> n | hi << (64 - n) : hi >> (n - 64);
-                const uint64_t h = n < 64 ? hi >> n : 0;
-                sc[i] = u32x4{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int keep = valid - 4 * j;
-                    if (keep < 4) sc[i][j] = keep <= 0 ? 0u : sc[i][j] & ((1u << (8 * keep)) - 1u);
-                }
+            if constexpr (ALIGNED) {
+                symtile::buf_ld16_lds_async(
+                    scale_rsrc[i],
+                    lds0 + (uint32_t)(offsetof(Lds, scales) +
+                                      ((quad & 1) * kRows + wave * (kRows / 4) + i * 64) * 16),
+                    quad * 16 < p.groups ? scale_at[i] : symtile::kOOB, (uint32_t)(quad * 16));
+            } else {
+                const uint8_t* from = scales_of[i] + min(quad * 16, p.groups - 1);
+                const uint8_t* first = from < scales_end[i] ? from : scales_end[i];
+                shift[i] = (int)(from - first) * 8;
+                sc[i] = reinterpret_cast<const Unaligned16*>(first)->v;
             }
         }
+    };
+    auto place_scales = [&](int quad) {
+        if constexpr (!ALIGNED) {
+            const int valid = p.groups - quad * 16;
+            if (valid < 16) {
 #pragma unroll
-        for (int i = 0; i < kScaleLoads; ++i)
-            if (t + i * 256 < kRows) lds.scales[pair & 1][t + i * 256] = sc[i];
+                for (int i = 0; i < kScaleLoads; ++i) {
+                    const uint64_t lo = (uint64_t)sc[i][1] << 32 | sc[i][0];
+                    const uint64_t hi = (uint64_t)sc[i][3] << 32 | sc[i][2];
+                    const int n = shift[i];
+                    const uint64_t l = n == 0 ? lo : n < 64 ? lo >> n | hi << (64 - n) : hi >> (n - 64);
+                    const uint64_t h = n < 64 ? hi >> n : 0;
+                    sc[i] = u32x4{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int keep = valid - 4 * j;
+                        if (keep < 4) sc[i][j] = keep <= 0 ? 0u : sc[i][j] & ((1u << (8 * keep)) - 1u);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kScaleLoads; ++i)
+                if (t + i * 256 < kRows) lds.scales[quad & 1][t + i * 256] = sc[i];
+        }
     };
     f32x16 acc[kNT][kMT] = {};
-    // A lane's operands of instruction S in a stage: its row's base ^ S * 16.
+    // A lane's operands of an instruction, and its scales' bytes of a stage.
     struct Operands {
-        u32x4 w[kNT], x[kMT];
-    };
-    const int base_w = (wn * (TN / 2) + r) * kStageBytes + (((4 * g) ^ (r % 8)) * 16);
-    const int base_x = (wm * (TM / 2) + r) * kStageBytes + (((4 * g) ^ (r % 8)) * 16);
-    auto read = [&](Operands& o, int st, int S) {
-        const typename Lds::Stage& now = lds.stage[st & 1];
-#pragma unroll
-        for (int i = 0; i < kNT; ++i)
-            o.w[i] = symtile::ld16(&now.w[(base_w ^ (S * 16)) + i * 32 * kStageBytes]);
-#pragma unroll
-        for (int j = 0; j < kMT; ++j)
-            o.x[j] = symtile::ld16(&now.x[(base_x ^ (S * 16)) + j * 32 * kStageBytes]);
+        u32x4 x[kMT], w[kNT];
     };
     struct Bytes {
         uint32_t w[kNT], x[kMT];
     };
-    auto read_scales = [&](Bytes& o, int st) {
-        const uint32_t* of = reinterpret_cast<const uint32_t*>(lds.scales[st >> 1 & 1]) +
-                             (st & 1) * 2 + g;
-#pragma unroll
-        for (int i = 0; i < kNT; ++i) o.w[i] = of[(wn * (TN / 2) + i * 32 + r) * 4];
-#pragma unroll
-        for (int j = 0; j < kMT; ++j) o.x[j] = of[(TN + wm * (TM / 2) + j * 32 + r) * 4];
+    const int base_w = (wn * (TN / 2) + r) * kStageBytes + (((2 * g) ^ (r / 4 % 4)) * 16);
+    const int base_x = (wm * (TM / 2) + r) * kStageBytes + (((2 * g) ^ (r / 4 % 4)) * 16);
+    // Read k of the kMT + kNT of instruction S of the stage at `slot`.
+    auto read = [&](Operands& o, int slot, int S, int k) {
+        const typename Lds::Stage& now = lds.stage[slot];
+        if (k < kMT) o.x[k] = symtile::ld16(&now.x[(base_x ^ (S * 16)) + k * 32 * kStageBytes]);
+        else o.w[k - kMT] = symtile::ld16(&now.w[(base_w ^ (S * 16)) + (k - kMT) * 32 * kStageBytes]);
     };
-    auto row_of_tiles = [&](auto s_, int i, const Operands& o, const Bytes& e) {
-        constexpr int S = decltype(s_)::value;
-#pragma unroll
-        for (int j = 0; j < kMT; ++j)
-            acc[i][j] = mfma32<S>(o.w[i], o.x[j], acc[i][j], e.w[i], e.x[j]);
+    auto read_scale = [&](Bytes& o, int quad, int slot, int k) {
+        const uint16_t* of = reinterpret_cast<const uint16_t*>(lds.scales[quad & 1]) + slot * 2 + g;
+        if (k < kMT) o.x[k] = of[(TN + wm * (TM / 2) + k * 32 + r) * 8];
+        else o.w[k - kMT] = of[(wn * (TN / 2) + (k - kMT) * 32 + r) * 8];
     };
-    // The matrix instructions before stay before what follows.
-    auto pin = [&](int i) {
-#pragma unroll
-        for (int j = 0; j < kMT; ++j) asm volatile("" : "+a"(acc[i][j]));
-    };
-    // Multiplies `o` while the operands of instruction S + 1 are read into `next`, the reads
-    // between the matrix instructions.
-    auto multiply = [&](auto s_, const Operands& o, const Bytes& e, Operands& next, int st) {
-        read(next, st, decltype(s_)::value + 1);
-#pragma unroll
-        for (int i = 0; i < kNT; ++i) row_of_tiles(s_, i, o, e);
-#pragma unroll
-        for (int i = 0; i < kNT + kMT; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // an LDS read
-            __builtin_amdgcn_sched_group_barrier(0x8, kNT * kMT / (kNT + kMT), 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    // A stage's first three multiplications go on while its other operands are read; then all
-    // waves have read it, the next one is there, and its place is the stage's after the next,
-    // whose loads go between the matrix instructions of the fourth.
-    Operands a, b;
-    Bytes even, odd;
-    auto stage = [&](int st, const Bytes& e, Bytes& e_next, bool is_odd) {
-        multiply(std::integral_constant<int, 0>{}, a, e, b, st);
-        multiply(std::integral_constant<int, 1>{}, b, e, a, st);
-        multiply(std::integral_constant<int, 2>{}, a, e, b, st);
-#pragma unroll
-        for (int i = 0; i < kNT; ++i) pin(i);
-        __builtin_amdgcn_s_waitcnt(wait_loads(0));
-        if (is_odd) place_scales((st + 1) >> 1);
-        meet();
-        if (!is_odd) fetch_scales((st + 2) >> 1);
-        read(a, st + 1, 0);
-        read_scales(e_next, st + 1);
-#pragma unroll
-        for (int i = 0; i < kNT; ++i) {
-            row_of_tiles(std::integral_constant<int, 3>{}, i, b, e);
-            pin(i);
-#pragma unroll
-            for (int q = i * 4 / kNT; q < (i + 1) * 4 / kNT; ++q) load(st + 2, q);
-        }
-    };
+    // After a stage's first instructions all waves have read it, and the next one is there: its
+    // place is the stage's four further on, whose loads are asked for from there on to the next
+    // such point.
     if (p.groups) {
+        Operands a, b;
+        Bytes even, odd;
+        // The instructions S of stage st on `o`; between them, one or two each, the reads of the
+        // next operands (and scales) and half of a stage's loads.  A wave issues in order and is
+        // the only one of its SIMD: what stands between two matrix instructions for longer than
+        // the 32 cycles of the first leaves the unit idle (with reads and loads between rows of
+        // four of them 520 us in place of ).
+        auto multiply = [&](auto s_, auto slot_, int st, const Operands& o, const Bytes& e,
+                            Operands& next, Bytes& e_next) {
+            constexpr int S = decltype(s_)::value, kSlot = decltype(slot_)::value;
+            constexpr int kReads = kMT + kNT, kBytes = S == 1 ? kReads : 0, kHalf = kLoads / 2;
+            constexpr int kOthers = kBytes + kReads + kHalf, kTiles = kNT * kMT;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) load(0, q);
+            for (int q = 0; q < kTiles; ++q) {
+                const int i = q / kMT, j = q % kMT;
+                acc[i][j] = mfma32<S>(o.w[i], o.x[j], acc[i][j], e.w[i], e.x[j]);
+                asm volatile("" : "+a"(acc[i][j]));
+#pragma unroll
+                for (int k = q * kOthers / kTiles; k < (q + 1) * kOthers / kTiles; ++k) {
+                    if (k < kBytes)
+                        read_scale(e_next, (st + 1) >> 2, (kSlot + 1) % kRing, k);
+                    else if (k < kBytes + kReads)
+                        read(next, (kSlot + S) % kRing, 1 - S, k - kBytes);
+                    else if (S == 0)
+                        load(st + 3, (kSlot + 3) % kRing, kHalf + k - kBytes - kReads);
+                    else
+                        load(st + 4, kSlot, k - kBytes - kReads);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        auto stage = [&](auto slot_, int st, const Bytes& e, Bytes& e_next) {
+            constexpr int kSlot = decltype(slot_)::value;
+            if (kSlot == 0) fetch_scales((st >> 2) + 1);
+            multiply(std::integral_constant<int, 0>{}, slot_, st, a, e, b, e_next);
+            if (kSlot == 3) place_scales((st >> 2) + 1);
+            meet<2 * kLoads>();
+            multiply(std::integral_constant<int, 1>{}, slot_, st, b, e, a, e_next);
+        };
         fetch_scales(0);
-        place_scales(0);
-        meet();
 #pragma unroll
-        for (int q = 0; q < 4; ++q) load(1, q);
-        read(a, 0, 0);
-        read_scales(even, 0);
-        // (in pairs; stages behind K are zeros)
-        for (int st = 0; st < stages; st += 2) {
-            stage(st, even, odd, false);
-            stage(st + 1, odd, even, true);
+        for (int i = 0; i < 3; ++i)
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) load(i, i, u);
+#pragma unroll
+        for (int u = 0; u < kLoads / 2; ++u) load(3, 3, u);
+        place_scales(0);
+        meet<2 * kLoads + kLoads / 2>();
+#pragma unroll
+        for (int k = 0; k < kMT + kNT; ++k) {
+            read(a, 0, 0, k);
+            read_scale(even, 0, 0, k);
+        }
+        // (in fours; stages behind K are zeros)
+        for (int st = 0; st < stages; st += 4) {
+            stage(std::integral_constant<int, 0>{}, st, even, odd);
+            stage(std::integral_constant<int, 1>{}, st + 1, odd, even);
+            stage(std::integral_constant<int, 2>{}, st + 2, even, odd);
+            stage(std::integral_constant<int, 3>{}, st + 3, odd, even);
         }
         __builtin_amdgcn_s_waitcnt(wait_loads(0));
     }
@@ -666,9 +685,13 @@ extern "C" symtile_status symtile_mx4_all_scatter(
         int prev = -1;
         if (symtile_status st = symtile_host::set_device(h, &prev)) return st;
         void* args[] = {&p};
-        const void* kernel = dtype == SYMTILE_BF16
-                                 ? reinterpret_cast<const void*>(&mx4_gemm_kernel<true, TM, TN>)
-                                 : reinterpret_cast<const void*>(&mx4_gemm_kernel<false, TM, TN>);
+        const bool aligned = p.groups % 16 == 0 && !misaligned(x_scales, 16) && !misaligned(scales, 16);
+        const void* kernel =
+            dtype == SYMTILE_BF16
+                ? aligned ? reinterpret_cast<const void*>(&mx4_gemm_kernel<true, TM, TN, true>)
+                          : reinterpret_cast<const void*>(&mx4_gemm_kernel<true, TM, TN, false>)
+            : aligned ? reinterpret_cast<const void*>(&mx4_gemm_kernel<false, TM, TN, true>)
+                      : reinterpret_cast<const void*>(&mx4_gemm_kernel<false, TM, TN, false>);
         hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)tiles), dim3(256), args, 0,
                                        static_cast<hipStream_t>(s));
         if (e == hipSuccess) e = hipGetLastError();
