@@ -265,6 +265,11 @@ __device__ __forceinline__ f32x16 mfma32(const u32x4& a, const u32x4& b, f32x16 
 // (gfx9 encoding: vmcnt 3:0 and 15:14, expcnt 6:4, lgkmcnt 11:8).
 constexpr int wait_loads(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4); }
 
+// Written through (sc0 sc1) with the streaming hint (nt): the acknowledgement is the same,
+// and lines that nobody on this GPU reads soon leave the caches first (4096 x 8192 x 3584
+// into 8 slots 105.5 us, without the hint 112.9; 28672 columns into one 481, 491).
+constexpr int kStoreThroughStream = symtile::kStoreWriteThrough | symtile::kStoreNonTemporal;
+
 // At most N of the wave's loads are out, its LDS accesses done, and so for all waves.
 template <int N>
 __device__ __forceinline__ void meet() {
@@ -274,21 +279,23 @@ __device__ __forceinline__ void meet() {
     asm volatile("" ::: "memory");
 }
 
-// A workgroup of 4 waves takes TM rows of X by TN of W.  K goes by stages of 128 values,
-// 64 bytes a row, loaded straight into a ring of four buffers in LDS; row r's 16-byte
-// vector v lies at place v ^ (r / 4 % 4), so that 16 rows' same vector touch every bank
-// once.  In instruction S of a stage's two lane half g takes block 2 g + S of its rows, so
-// a lane's scales of a stage are two bytes next to each other; scales come for four
-// stages, 16 bytes a row, straight into LDS too where rows of scales are whole numbers of
-// 16 aligned bytes (ALIGNED), else through registers.
-constexpr int kStageBytes = 64, kRing = 4;
+// A workgroup of 4 waves takes TM rows of X by TN of W.  K goes by stages of 256 values,
+// 128 bytes a row, loaded straight into one of two buffers in LDS while the other is
+// multiplied; row r's 16-byte vector v lies at place v ^ (r / 2 % 8), so that 16 rows' same
+// vector touch every bank once.  (Stages of 64 bytes a row and four buffers: 513 us for
+// 4096 x 8192 x 28672, since a CU has only so many requests out, of 64 bytes each then.)
+// In instruction S of a stage's four lane half g takes block 4 g + S of its rows, so a
+// lane's scales of a stage are one word; scales come for two stages (a pair), 16 bytes a
+// row, straight into LDS too where rows of scales are whole numbers of 16 aligned bytes
+// (ALIGNED), else through registers.
+constexpr int kStageBytes = 128;
 template <int TM, int TN>
 struct GemmLds {
     struct Stage {
         uint8_t w[TN * kStageBytes], x[TM * kStageBytes];
     };
     union {
-        Stage stage[kRing];
+        Stage stage[2];
         uint16_t out[TM * TN];
     };
     u32x4 scales[2][TN + TM];
@@ -299,7 +306,7 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
     typedef GemmLds<TM, TN> Lds;
     __shared__ __attribute__((aligned(16))) Lds lds;
     constexpr int kMT = TM / 64, kNT = TN / 64;           // 32 x 32 tiles of a wave
-    constexpr int kRows = TN + TM, kLoads = kRows / 64;   // loads of 16 rows a wave and stage
+    constexpr int kRows = TN + TM, kLoads = kRows / 32;   // loads of 8 rows a wave and stage
     constexpr int kScaleLoads = (kRows + 255) / 256;
     const int t = threadIdx.x, lane = t % 64, r = lane % 32, g = lane / 32;
     const int wave = __builtin_amdgcn_readfirstlane(t / 64), wn = wave % 2, wm = wave / 2;
@@ -308,31 +315,32 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
     const int m0 = tm * TM, n0 = tn * TN;
     const int rows = min(TM, p.M - m0), cols = min(TN, p.N - n0);
     const int row_bytes = p.groups * (kBlock / 2);
-    const int stages = (p.groups + 3) / 4;
+    const int stages = (p.groups + 7) / 8;
     const symtile::i32x4_t ws = symtile::make_rsrc_words(p.w + (size_t)n0 * row_bytes,
                                                          (uint32_t)(cols * row_bytes));
     const symtile::i32x4_t xs = symtile::make_rsrc_words(p.x + (size_t)m0 * row_bytes,
                                                          (uint32_t)(rows * row_bytes));
     const uint32_t lds0 = symtile::lds_addr(&lds);
-    // A load fills 16 rows: lane l place l % 4 of row l / 4.
-    const int vec = (lane % 4) ^ (lane / 16);
-    const uint32_t row_at = (uint32_t)(lane / 4 * row_bytes + vec * 16);
-    // Load u of the wave's for stage st into the ring's place `to_slot` = st % 4 (behind a row's
-    // end: outside of the resources, zeros).
-    auto load = [&](int st, int to_slot, int u) {
-        const uint32_t from = st * kStageBytes + vec * 16 < row_bytes ? row_at : symtile::kOOB;
-        const uint32_t to = lds0 + to_slot * (uint32_t)sizeof(typename Lds::Stage);
-        if (u < TN / 64) {
-            const int row = (wave * (TN / 64) + u) * 16;
+    // A load fills 8 rows, lane l place l % 8 of row l / 8, of the first or second 8 of 16.
+    const int vec[2] = {(lane % 8) ^ (lane / 16), (lane % 8) ^ (4 + lane / 16)};
+    const uint32_t row_at = (uint32_t)(lane / 8 * row_bytes);
+    // Load u of the wave's for stage st into buffer `slot` (behind a row's end: outside of the
+    // resources, zeros).
+    auto load = [&](int st, int slot, int u) {
+        const int v = vec[u % 2] * 16;
+        const uint32_t from = st * kStageBytes + v < row_bytes ? row_at + v : symtile::kOOB;
+        const uint32_t to = lds0 + slot * (uint32_t)sizeof(typename Lds::Stage);
+        if (u < TN / 32) {
+            const int row = (wave * (TN / 32) + u) * 8;
             symtile::buf_ld16_lds_async(ws, to + row * kStageBytes, from,
                                         (uint32_t)(row * row_bytes + st * kStageBytes));
         } else {
-            const int row = (wave * (TM / 64) + u - TN / 64) * 16;
+            const int row = (wave * (TM / 32) + u - TN / 32) * 8;
             symtile::buf_ld16_lds_async(xs, to + (TN + row) * kStageBytes, from,
                                         (uint32_t)(row * row_bytes + st * kStageBytes));
         }
     };
-    // Scales of four stages (a quad) for the rows of W and X, those of the last ones again for
+    // Scales of two stages (a pair) for the rows of W and X, those of the last ones again for
     // the rows that are not there.
     symtile::i32x4_t scale_rsrc[kScaleLoads];
     uint32_t scale_at[kScaleLoads];
@@ -358,29 +366,29 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
                                   : p.x_scales + (size_t)p.M * p.groups) - 16;
         }
     }
-    // Asks for a quad's scales: into LDS, or 16 bytes a row into registers, the last ones of the
+    // Asks for a pair's scales: into LDS, or 16 bytes a row into registers, the last ones of the
     // array where it ends before; place_scales() moves those into place, zeros behind a row's
     // end (which meet zeros of both matrices; a neighbour row's byte may be a NaN's).
-    auto fetch_scales = [&](int quad) {
+    auto fetch_scales = [&](int pair) {
 #pragma unroll
         for (int i = 0; i < kScaleLoads; ++i) {
             if constexpr (ALIGNED) {
                 symtile::buf_ld16_lds_async(
                     scale_rsrc[i],
                     lds0 + (uint32_t)(offsetof(Lds, scales) +
-                                      ((quad & 1) * kRows + wave * (kRows / 4) + i * 64) * 16),
-                    quad * 16 < p.groups ? scale_at[i] : symtile::kOOB, (uint32_t)(quad * 16));
+                                      ((pair & 1) * kRows + wave * (kRows / 4) + i * 64) * 16),
+                    pair * 16 < p.groups ? scale_at[i] : symtile::kOOB, (uint32_t)(pair * 16));
             } else {
-                const uint8_t* from = scales_of[i] + min(quad * 16, p.groups - 1);
+                const uint8_t* from = scales_of[i] + min(pair * 16, p.groups - 1);
                 const uint8_t* first = from < scales_end[i] ? from : scales_end[i];
                 shift[i] = (int)(from - first) * 8;
                 sc[i] = reinterpret_cast<const Unaligned16*>(first)->v;
             }
         }
     };
-    auto place_scales = [&](int quad) {
+    auto place_scales = [&](int pair) {
         if constexpr (!ALIGNED) {
-            const int valid = p.groups - quad * 16;
+            const int valid = p.groups - pair * 16;
             if (valid < 16) {
 #pragma unroll
                 for (int i = 0; i < kScaleLoads; ++i) {
@@ -399,7 +407,7 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
             }
 #pragma unroll
             for (int i = 0; i < kScaleLoads; ++i)
-                if (t + i * 256 < kRows) lds.scales[quad & 1][t + i * 256] = sc[i];
+                if (t + i * 256 < kRows) lds.scales[pair & 1][t + i * 256] = sc[i];
         }
     };
     f32x16 acc[kNT][kMT] = {};
@@ -410,34 +418,34 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
     struct Bytes {
         uint32_t w[kNT], x[kMT];
     };
-    const int base_w = (wn * (TN / 2) + r) * kStageBytes + (((2 * g) ^ (r / 4 % 4)) * 16);
-    const int base_x = (wm * (TM / 2) + r) * kStageBytes + (((2 * g) ^ (r / 4 % 4)) * 16);
+    const int base_w = (wn * (TN / 2) + r) * kStageBytes + (((4 * g) ^ (r / 2 % 8)) * 16);
+    const int base_x = (wm * (TM / 2) + r) * kStageBytes + (((4 * g) ^ (r / 2 % 8)) * 16);
     // Read k of the kMT + kNT of instruction S of the stage at `slot`.
     auto read = [&](Operands& o, int slot, int S, int k) {
         const typename Lds::Stage& now = lds.stage[slot];
         if (k < kMT) o.x[k] = symtile::ld16(&now.x[(base_x ^ (S * 16)) + k * 32 * kStageBytes]);
         else o.w[k - kMT] = symtile::ld16(&now.w[(base_w ^ (S * 16)) + (k - kMT) * 32 * kStageBytes]);
     };
-    auto read_scale = [&](Bytes& o, int quad, int slot, int k) {
-        const uint16_t* of = reinterpret_cast<const uint16_t*>(lds.scales[quad & 1]) + slot * 2 + g;
-        if (k < kMT) o.x[k] = of[(TN + wm * (TM / 2) + k * 32 + r) * 8];
-        else o.w[k - kMT] = of[(wn * (TN / 2) + (k - kMT) * 32 + r) * 8];
+    auto read_scale = [&](Bytes& o, int pair, int slot, int k) {
+        const uint32_t* of = reinterpret_cast<const uint32_t*>(lds.scales[pair & 1]) + slot * 2 + g;
+        if (k < kMT) o.x[k] = of[(TN + wm * (TM / 2) + k * 32 + r) * 4];
+        else o.w[k - kMT] = of[(wn * (TN / 2) + (k - kMT) * 32 + r) * 4];
     };
-    // After a stage's first instructions all waves have read it, and the next one is there: its
-    // place is the stage's four further on, whose loads are asked for from there on to the next
-    // such point.
+    // After a stage's third instructions all waves have read it, and the next one is there: its
+    // place is the stage's after the next, whose loads are asked for during the fourth and the
+    // next stage's first.
     if (p.groups) {
         Operands a, b;
         Bytes even, odd;
         // The instructions S of stage st on `o`; between them, one or two each, the reads of the
         // next operands (and scales) and half of a stage's loads.  A wave issues in order and is
         // the only one of its SIMD: what stands between two matrix instructions for longer than
-        // the 32 cycles of the first leaves the unit idle (with reads and loads between rows of
-        // four of them 520 us in place of ).
+        // the 32 cycles of the first leaves the unit idle.
         auto multiply = [&](auto s_, auto slot_, int st, const Operands& o, const Bytes& e,
                             Operands& next, Bytes& e_next) {
             constexpr int S = decltype(s_)::value, kSlot = decltype(slot_)::value;
-            constexpr int kReads = kMT + kNT, kBytes = S == 1 ? kReads : 0, kHalf = kLoads / 2;
+            constexpr int kReads = kMT + kNT, kBytes = S == 3 ? kReads : 0;
+            constexpr int kHalf = S == 0 || S == 3 ? kLoads / 2 : 0;
             constexpr int kOthers = kBytes + kReads + kHalf, kTiles = kNT * kMT;
 #pragma unroll
             for (int q = 0; q < kTiles; ++q) {
@@ -447,45 +455,43 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
 #pragma unroll
                 for (int k = q * kOthers / kTiles; k < (q + 1) * kOthers / kTiles; ++k) {
                     if (k < kBytes)
-                        read_scale(e_next, (st + 1) >> 2, (kSlot + 1) % kRing, k);
+                        read_scale(e_next, (st + 1) >> 1, 1 - kSlot, k);
                     else if (k < kBytes + kReads)
-                        read(next, (kSlot + S) % kRing, 1 - S, k - kBytes);
+                        read(next, S == 3 ? 1 - kSlot : kSlot, (S + 1) % 4, k - kBytes);
                     else if (S == 0)
-                        load(st + 3, (kSlot + 3) % kRing, kHalf + k - kBytes - kReads);
+                        load(st + 1, 1 - kSlot, kHalf + k - kBytes - kReads);
                     else
-                        load(st + 4, kSlot, k - kBytes - kReads);
+                        load(st + 2, kSlot, k - kBytes - kReads);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
         auto stage = [&](auto slot_, int st, const Bytes& e, Bytes& e_next) {
             constexpr int kSlot = decltype(slot_)::value;
-            if (kSlot == 0) fetch_scales((st >> 2) + 1);
+            if (kSlot == 0) fetch_scales((st >> 1) + 1);
             multiply(std::integral_constant<int, 0>{}, slot_, st, a, e, b, e_next);
-            if (kSlot == 3) place_scales((st >> 2) + 1);
-            meet<2 * kLoads>();
             multiply(std::integral_constant<int, 1>{}, slot_, st, b, e, a, e_next);
+            multiply(std::integral_constant<int, 2>{}, slot_, st, a, e, b, e_next);
+            if (kSlot == 1) place_scales((st >> 1) + 1);
+            meet<0>();
+            multiply(std::integral_constant<int, 3>{}, slot_, st, b, e, a, e_next);
         };
         fetch_scales(0);
 #pragma unroll
-        for (int i = 0; i < 3; ++i)
+        for (int u = 0; u < kLoads; ++u) load(0, 0, u);
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u) load(i, i, u);
-#pragma unroll
-        for (int u = 0; u < kLoads / 2; ++u) load(3, 3, u);
+        for (int u = 0; u < kLoads / 2; ++u) load(1, 1, u);
         place_scales(0);
-        meet<2 * kLoads + kLoads / 2>();
+        meet<kLoads / 2>();
 #pragma unroll
         for (int k = 0; k < kMT + kNT; ++k) {
             read(a, 0, 0, k);
             read_scale(even, 0, 0, k);
         }
-        // (in fours; stages behind K are zeros)
-        for (int st = 0; st < stages; st += 4) {
+        // (in pairs; stages behind K are zeros)
+        for (int st = 0; st < stages; st += 2) {
             stage(std::integral_constant<int, 0>{}, st, even, odd);
             stage(std::integral_constant<int, 1>{}, st + 1, odd, even);
-            stage(std::integral_constant<int, 2>{}, st + 2, even, odd);
-            stage(std::integral_constant<int, 3>{}, st + 3, odd, even);
         }
         __builtin_amdgcn_s_waitcnt(wait_loads(0));
     }
@@ -515,25 +521,31 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
     const int own_rows = min(64, rows - sr), own_cols = min(kCols, cols - sn);
     if (own_rows <= 0 || own_cols <= 0) return;
     const int row0 = lane / kLanes, v0 = lane % kLanes;
-    const bool in = v0 * 8 < own_cols;
-    for (int s = 0; s < p.world; ++s) {
-        char* base = reinterpret_cast<char*>(p.bases[s]);
-        const symtile::rsrc_t dst = symtile::make_rsrc(
-            base + p.c_off + ((size_t)(m0 + sr) * p.ldc + n0 + sn) * 2,
-            (uint32_t)(((size_t)(own_rows - 1) * p.ldc + own_cols) * 2));
-#pragma unroll 8
-        for (int i = 0; i < kSteps; ++i) {
-            const int m = i * kPer + row0;
-            symtile::buf_st16p<symtile::kStoreWriteThrough>(
-                symtile::ld16(&lds.out[(sr + m) * TN + (((sn / 8 + v0) ^ ((sr + m) & kMask)) * 8)]),
-                dst, in ? (uint32_t)((row0 * p.ldc + v0 * 8) * 2) : symtile::kOOB,
-                (uint32_t)(i * kPer * p.ldc * 2));
+    const uint32_t at = v0 * 8 < own_cols ? (uint32_t)((row0 * p.ldc + v0 * 8) * 2) : symtile::kOOB;
+    constexpr int kBatch = kSteps < 8 ? kSteps : 8;
+    for (int i0 = 0; i0 < kSteps; i0 += kBatch) {
+        u32x4 v[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int m = sr + (i0 + i) * kPer + row0;
+            v[i] = symtile::ld16(&lds.out[m * TN + (((sn / 8 + v0) ^ (m & kMask)) * 8)]);
         }
-        symtile::release_written_through();
-        if (lane < (own_cols + kTileN - 1) / kTileN)
-            symtile::flag_signal(reinterpret_cast<uint32_t*>(base + p.flag_off) +
-                                 (size_t)((m0 + sr) / kTileM) * p.tiles_n + (n0 + sn) / kTileN + lane);
+        for (int s = 0; s < p.world; ++s) {
+            const symtile::rsrc_t dst = symtile::make_rsrc(
+                reinterpret_cast<char*>(p.bases[s]) + p.c_off + ((size_t)(m0 + sr) * p.ldc + n0 + sn) * 2,
+                (uint32_t)(((size_t)(own_rows - 1) * p.ldc + own_cols) * 2));
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                symtile::buf_st16p<kStoreThroughStream>(
+                    v[i], dst, at, (uint32_t)((i0 + i) * kPer * p.ldc * 2));
+        }
     }
+    symtile::release_written_through();
+    const int tiles = (own_cols + kTileN - 1) / kTileN;
+    for (int s = 0; s < p.world; ++s)
+        if (lane < tiles)
+            symtile::flag_signal(reinterpret_cast<uint32_t*>(p.bases[s] + p.flag_off) +
+                                 (size_t)((m0 + sr) / kTileM) * p.tiles_n + (n0 + sn) / kTileN + lane);
 }
 
 // ---- host ------------------------------------------------------------------------------
