@@ -114,24 +114,33 @@ struct ProductParams {
     int M, N, groups, world;    // groups: blocks of a row
     size_t ldc;                 // elements
     int tiles_n;                // of the counters
-    // of the kernel for many rows: its tiles, and how they are numbered
-    int gm, gn, per_xcd, xcd_rest;
+    // of the kernel for many rows: its tiles, and how they and their parts are numbered
+    int gm, per_xcd, xcd_rest;
     int band;                   // tiles of a band
     symtile_host::Div by_band;
+    // K in `splits` parts of `part_stages` stages each (the last may have fewer), whose sums
+    // meet in `partials`
+    int splits, part_stages;
+    symtile_host::Div by_splits;
+    uint32_t* counters;
+    float* partials;
 };
 
-// Tile b of the grid.  Workgroups go to the 8 XCDs in turn; each takes tiles next to each
-// other, in bands of kBandRows tile rows, so that those that run together share rows of
-// both matrices in its L2.
+// Tile and part b of the grid.  Workgroups go to the 8 XCDs in turn; each takes tiles next
+// to each other, in bands of kBandRows tile rows, so that those that run together share
+// rows of both matrices in its L2.  A tile's parts are next to each other too.
 constexpr int kXcds = 8, kBandRows = 8;
-__device__ __forceinline__ void place_tile(const ProductParams& p, int b, int* tm, int* tn) {
+__device__ __forceinline__ int place_tile(const ProductParams& p, int b, int* tm, int* tn,
+                                          int* split) {
     const int xcd = b % kXcds, i = b / kXcds;
-    const int id = xcd * p.per_xcd + min(xcd, p.xcd_rest) + i;
+    const int unit = xcd * p.per_xcd + min(xcd, p.xcd_rest) + i, id = p.by_splits(unit);
+    *split = unit - id * p.splits;
     const int band = p.by_band(id), first = band * kBandRows, in = id - band * p.band;
     const int height = min(kBandRows, p.gm - first);
     const int n = height == kBandRows ? in / kBandRows : in / height;
     *tm = first + in - n * height;
     *tn = n;
+    return id;
 }
 
 struct __attribute__((packed, aligned(1))) Unaligned16 {
@@ -289,33 +298,40 @@ __device__ __forceinline__ void meet() {
 // row, straight into LDS too where rows of scales are whole numbers of 16 aligned bytes
 // (ALIGNED), else through registers.
 constexpr int kStageBytes = 128;
-template <int TM, int TN>
+template <int TM, int TN, int RING>
 struct GemmLds {
+    static constexpr int kPairs = RING / 2 + 1;
     struct Stage {
         uint8_t w[TN * kStageBytes], x[TM * kStageBytes];
     };
     union {
-        Stage stage[2];
+        Stage stage[RING];
         uint16_t out[TM * TN];
     };
-    u32x4 scales[2][TN + TM];
+    u32x4 scales[kPairs][TN + TM];
+    int last;
 };
 
-template <bool BF, int TM, int TN, bool ALIGNED>
-__global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_kernel(ProductParams p) {
-    typedef GemmLds<TM, TN> Lds;
+template <bool BF, int TM, int TN, int RING, bool ALIGNED>
+__global__ void __launch_bounds__(256, sizeof(GemmLds<TM, TN, RING>) > 80 * 1024 ? 1 : 2)
+mx4_gemm_kernel(ProductParams p) {
+    constexpr bool kSplits = TM < 256;      // builds whose calls may split K
+    typedef GemmLds<TM, TN, RING> Lds;
     __shared__ __attribute__((aligned(16))) Lds lds;
     constexpr int kMT = TM / 64, kNT = TN / 64;           // 32 x 32 tiles of a wave
     constexpr int kRows = TN + TM, kLoads = kRows / 32;   // loads of 8 rows a wave and stage
     constexpr int kScaleLoads = (kRows + 255) / 256;
     const int t = threadIdx.x, lane = t % 64, r = lane % 32, g = lane / 32;
     const int wave = __builtin_amdgcn_readfirstlane(t / 64), wn = wave % 2, wm = wave / 2;
-    int tm, tn;
-    place_tile(p, blockIdx.x, &tm, &tn);
+    int tm, tn, split;
+    const int tile = place_tile(p, blockIdx.x, &tm, &tn, &split);
     const int m0 = tm * TM, n0 = tn * TN;
     const int rows = min(TM, p.M - m0), cols = min(TN, p.N - n0);
     const int row_bytes = p.groups * (kBlock / 2);
-    const int stages = (p.groups + 7) / 8;
+    // the part's stages from `first` on, and the blocks before its end
+    const int first = split * p.part_stages;
+    const int stages = min((p.groups + 7) / 8 - first, p.part_stages);
+    const int end = min(p.groups, (first + stages) * 8);
     const symtile::i32x4_t ws = symtile::make_rsrc_words(p.w + (size_t)n0 * row_bytes,
                                                          (uint32_t)(cols * row_bytes));
     const symtile::i32x4_t xs = symtile::make_rsrc_words(p.x + (size_t)m0 * row_bytes,
@@ -324,11 +340,11 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
     // A load fills 8 rows, lane l place l % 8 of row l / 8, of the first or second 8 of 16.
     const int vec[2] = {(lane % 8) ^ (lane / 16), (lane % 8) ^ (4 + lane / 16)};
     const uint32_t row_at = (uint32_t)(lane / 8 * row_bytes);
-    // Load u of the wave's for stage st into buffer `slot` (behind a row's end: outside of the
-    // resources, zeros).
-    auto load = [&](int st, int slot, int u) {
-        const int v = vec[u % 2] * 16;
-        const uint32_t from = st * kStageBytes + v < row_bytes ? row_at + v : symtile::kOOB;
+    // Load u of the wave's for stage st of the part into buffer `slot` (behind the part's end:
+    // outside of the resources, zeros).
+    auto load = [&](int st_, int slot, int u) {
+        const int st = first + st_, v = vec[u % 2] * 16;
+        const uint32_t from = st * kStageBytes + v < end * 16 ? row_at + v : symtile::kOOB;
         const uint32_t to = lds0 + slot * (uint32_t)sizeof(typename Lds::Stage);
         if (u < TN / 32) {
             const int row = (wave * (TN / 32) + u) * 8;
@@ -350,13 +366,13 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
 #pragma unroll
     for (int i = 0; i < kScaleLoads; ++i) {
         if constexpr (ALIGNED) {
-            const int first = wave * (kRows / 4) + i * 64, row = first + lane;   // 64 of one matrix
-            const bool of_w = first < TN;
+            const int row = (i * 4 + wave) * 64;      // 64 of one matrix
+            const bool of_w = row < TN;
             scale_rsrc[i] = of_w ? symtile::make_rsrc_words(p.w_scales + (size_t)n0 * p.groups,
                                                             (uint32_t)(cols * p.groups))
                                  : symtile::make_rsrc_words(p.x_scales + (size_t)m0 * p.groups,
                                                             (uint32_t)(rows * p.groups));
-            scale_at[i] = (uint32_t)((of_w ? row : row - TN) * p.groups);
+            scale_at[i] = (uint32_t)(((of_w ? row : row - TN) + lane) * p.groups);
         } else {
             const int row = t + i * 256;
             const bool of_w = row < TN;
@@ -366,29 +382,31 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
                                   : p.x_scales + (size_t)p.M * p.groups) - 16;
         }
     }
-    // Asks for a pair's scales: into LDS, or 16 bytes a row into registers, the last ones of the
-    // array where it ends before; place_scales() moves those into place, zeros behind a row's
-    // end (which meet zeros of both matrices; a neighbour row's byte may be a NaN's).
-    auto fetch_scales = [&](int pair) {
+    // Asks for a pair's scales, into place `to`: into LDS, or 16 bytes a row into registers, the
+    // last ones of the array where it ends before; place_scales() moves those into place, zeros
+    // behind the part's end (which meet zeros of both matrices; a neighbour row's byte may be a
+    // NaN's).
+    auto fetch_scales = [&](int pair_, int to) {
+        const int pair = first / 2 + pair_;
 #pragma unroll
         for (int i = 0; i < kScaleLoads; ++i) {
             if constexpr (ALIGNED) {
-                symtile::buf_ld16_lds_async(
-                    scale_rsrc[i],
-                    lds0 + (uint32_t)(offsetof(Lds, scales) +
-                                      ((pair & 1) * kRows + wave * (kRows / 4) + i * 64) * 16),
-                    pair * 16 < p.groups ? scale_at[i] : symtile::kOOB, (uint32_t)(pair * 16));
+                const int row = (i * 4 + wave) * 64;
+                if (row < kRows)
+                    symtile::buf_ld16_lds_async(
+                        scale_rsrc[i], lds0 + (uint32_t)(offsetof(Lds, scales) + (to * kRows + row) * 16),
+                        pair * 16 < end ? scale_at[i] : symtile::kOOB, (uint32_t)(pair * 16));
             } else {
                 const uint8_t* from = scales_of[i] + min(pair * 16, p.groups - 1);
-                const uint8_t* first = from < scales_end[i] ? from : scales_end[i];
-                shift[i] = (int)(from - first) * 8;
-                sc[i] = reinterpret_cast<const Unaligned16*>(first)->v;
+                const uint8_t* at = from < scales_end[i] ? from : scales_end[i];
+                shift[i] = (int)(from - at) * 8;
+                sc[i] = reinterpret_cast<const Unaligned16*>(at)->v;
             }
         }
     };
-    auto place_scales = [&](int pair) {
+    auto place_scales = [&](int pair_, int to) {
         if constexpr (!ALIGNED) {
-            const int valid = p.groups - pair * 16;
+            const int valid = end - (first / 2 + pair_) * 16;
             if (valid < 16) {
 #pragma unroll
                 for (int i = 0; i < kScaleLoads; ++i) {
@@ -407,7 +425,7 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
             }
 #pragma unroll
             for (int i = 0; i < kScaleLoads; ++i)
-                if (t + i * 256 < kRows) lds.scales[pair & 1][t + i * 256] = sc[i];
+                if (t + i * 256 < kRows) lds.scales[to][t + i * 256] = sc[i];
         }
     };
     f32x16 acc[kNT][kMT] = {};
@@ -426,21 +444,22 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
         if (k < kMT) o.x[k] = symtile::ld16(&now.x[(base_x ^ (S * 16)) + k * 32 * kStageBytes]);
         else o.w[k - kMT] = symtile::ld16(&now.w[(base_w ^ (S * 16)) + (k - kMT) * 32 * kStageBytes]);
     };
-    auto read_scale = [&](Bytes& o, int pair, int slot, int k) {
-        const uint32_t* of = reinterpret_cast<const uint32_t*>(lds.scales[pair & 1]) + slot * 2 + g;
+    auto read_scale = [&](Bytes& o, int place, int odd, int k) {
+        const uint32_t* of = reinterpret_cast<const uint32_t*>(lds.scales[place]) + odd * 2 + g;
         if (k < kMT) o.x[k] = of[(TN + wm * (TM / 2) + k * 32 + r) * 4];
         else o.w[k - kMT] = of[(wn * (TN / 2) + (k - kMT) * 32 + r) * 4];
     };
     // After a stage's third instructions all waves have read it, and the next one is there: its
-    // place is the stage's after the next, whose loads are asked for during the fourth and the
+    // place is the stage's RING further on, whose loads are asked for during the fourth and the
     // next stage's first.
-    if (p.groups) {
+    if (stages > 0) {
         Operands a, b;
         Bytes even, odd;
+        int place = 0;               // of the pair's scales
         // The instructions S of stage st on `o`; between them, one or two each, the reads of the
         // next operands (and scales) and half of a stage's loads.  A wave issues in order and is
-        // the only one of its SIMD: what stands between two matrix instructions for longer than
-        // the 32 cycles of the first leaves the unit idle.
+        // the only one of its SIMD in the largest build: what stands between two matrix
+        // instructions for longer than the 32 cycles of the first leaves the unit idle.
         auto multiply = [&](auto s_, auto slot_, int st, const Operands& o, const Bytes& e,
                             Operands& next, Bytes& e_next) {
             constexpr int S = decltype(s_)::value, kSlot = decltype(slot_)::value;
@@ -455,45 +474,112 @@ __global__ void __launch_bounds__(256, TM * TN >= 256 * 256 ? 1 : 2) mx4_gemm_ke
 #pragma unroll
                 for (int k = q * kOthers / kTiles; k < (q + 1) * kOthers / kTiles; ++k) {
                     if (k < kBytes)
-                        read_scale(e_next, (st + 1) >> 1, 1 - kSlot, k);
+                        read_scale(e_next, place, 1 - kSlot % 2, k);
                     else if (k < kBytes + kReads)
-                        read(next, S == 3 ? 1 - kSlot : kSlot, (S + 1) % 4, k - kBytes);
+                        read(next, S == 3 ? (kSlot + 1) % RING : kSlot, (S + 1) % 4, k - kBytes);
                     else if (S == 0)
-                        load(st + 1, 1 - kSlot, kHalf + k - kBytes - kReads);
+                        load(st + RING - 1, (kSlot + RING - 1) % RING, kHalf + k - kBytes - kReads);
                     else
-                        load(st + 2, kSlot, k - kBytes - kReads);
+                        load(st + RING, kSlot, k - kBytes - kReads);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
+        // The place of the scales of the pair `ahead` pairs further on.
+        auto place_of = [&](int ahead) {
+            const int at = place + ahead;
+            return at >= Lds::kPairs ? at - Lds::kPairs : at;
+        };
+        constexpr int kAhead = ALIGNED ? RING / 2 : 1;      // pairs
         auto stage = [&](auto slot_, int st, const Bytes& e, Bytes& e_next) {
             constexpr int kSlot = decltype(slot_)::value;
-            if (kSlot == 0) fetch_scales((st >> 1) + 1);
+            if (kSlot % 2 == 0) fetch_scales((st >> 1) + kAhead, place_of(kAhead));
             multiply(std::integral_constant<int, 0>{}, slot_, st, a, e, b, e_next);
             multiply(std::integral_constant<int, 1>{}, slot_, st, b, e, a, e_next);
             multiply(std::integral_constant<int, 2>{}, slot_, st, a, e, b, e_next);
-            if (kSlot == 1) place_scales((st >> 1) + 1);
-            meet<0>();
+            if (kSlot % 2 == 1) {
+                place_scales((st >> 1) + 1, place_of(1));
+                place = place_of(1);
+            }
+            meet<(RING - 2) * kLoads>();
             multiply(std::integral_constant<int, 3>{}, slot_, st, b, e, a, e_next);
         };
-        fetch_scales(0);
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) load(0, 0, u);
+        for (int i = 0; i < kAhead; ++i) fetch_scales(i, i);
 #pragma unroll
-        for (int u = 0; u < kLoads / 2; ++u) load(1, 1, u);
-        place_scales(0);
-        meet<kLoads / 2>();
+        for (int i = 0; i < RING - 1; ++i)
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) load(i, i, u);
+#pragma unroll
+        for (int u = 0; u < kLoads / 2; ++u) load(RING - 1, RING - 1, u);
+        place_scales(0, 0);
+        meet<(RING - 2) * kLoads + kLoads / 2>();
 #pragma unroll
         for (int k = 0; k < kMT + kNT; ++k) {
             read(a, 0, 0, k);
             read_scale(even, 0, 0, k);
         }
-        // (in pairs; stages behind K are zeros)
-        for (int st = 0; st < stages; st += 2) {
+        // (in pairs, or fours; stages behind the part's end are zeros)
+        for (int st = 0; st < stages; st += RING) {
             stage(std::integral_constant<int, 0>{}, st, even, odd);
             stage(std::integral_constant<int, 1>{}, st + 1, odd, even);
+            if constexpr (RING == 4) {
+                stage(std::integral_constant<int, 2>{}, st + 2, even, odd);
+                stage(std::integral_constant<int, 3>{}, st + 3, odd, even);
+            }
         }
         __builtin_amdgcn_s_waitcnt(wait_loads(0));
+    }
+    if (kSplits && p.splits > 1) {
+        // [tile][split][wave][tile of the wave][quarter][lane]
+        constexpr int kPart = TM * TN;
+        const uint32_t at = (uint32_t)((wave * kNT * kMT * 4 * 64 + lane) * 16);
+        const symtile::rsrc_t to =
+            symtile::make_rsrc(p.partials + ((size_t)tile * p.splits + split) * kPart, kPart * 4);
+#pragma unroll
+        for (int i = 0; i < kNT; ++i)
+#pragma unroll
+            for (int j = 0; j < kMT; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x16& v = acc[i][j];
+                    const f32x4 u = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                    symtile::buf_st16p<symtile::kStoreWriteThrough>(
+                        __builtin_bit_cast(u32x4, u), to, at, ((i * kMT + j) * 4 + q) * 1024);
+                }
+        symtile::wg_stores_done();
+        if (t == 0) {
+            symtile::release_written_through();
+            const uint32_t before = symtile::atomic_add<__ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT>(
+                p.counters + tile, 1u);
+            lds.last = before == (uint32_t)p.splits - 1;
+            if (lds.last)
+                __hip_atomic_store(symtile::global_ptr(p.counters + tile), 0u, __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (!lds.last) return;
+        symtile::acquire_coherent_reads();
+        const symtile::rsrc_t from = symtile::make_rsrc(p.partials + (size_t)tile * p.splits * kPart,
+                                                        (uint32_t)(p.splits * kPart * 4));
+#pragma unroll
+        for (int i = 0; i < kNT; ++i)
+#pragma unroll
+            for (int j = 0; j < kMT; ++j) acc[i][j] = f32x16{};
+        // the parts in the order of K
+        for (int s = 0; s < p.splits; ++s)
+#pragma unroll
+            for (int i = 0; i < kNT; ++i)
+#pragma unroll
+                for (int j = 0; j < kMT; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x4 u = __builtin_bit_cast(
+                            f32x4, symtile::buf_ld16p<symtile::kLoadCoherent>(
+                                       from, at, (uint32_t)(s * kPart * 4 + ((i * kMT + j) * 4 + q) * 1024)));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += u[e];
+                    }
     }
     // The stages' place is the results' from here on, rows of TN: vector v of 8 values of row
     // m at v ^ (m % 32).  A lane has four values in a row of each group of accumulators.
@@ -559,6 +645,44 @@ symtile_status check_sizes(int M, int N, int K) {
     if (K > (1 << 22)) return fail(SYMTILE_EINVAL, "K exceeds 4194304");
     if (M > (1 << 21)) return fail(SYMTILE_EINVAL, "M exceeds 2097152");
     return SYMTILE_OK;
+}
+
+// A build of the kernel for many rows, and the parts that K is split into; tm = 0: the other
+// kernel.
+struct GemmBuild {
+    int tm, tn, splits;
+    const void* kernels[2][2];     // [bfloat16][scales aligned]
+};
+template <int TM, int TN, int RING>
+GemmBuild gemm_of() {
+    return {TM, TN, 1,
+            {{reinterpret_cast<const void*>(&mx4_gemm_kernel<false, TM, TN, RING, false>),
+              reinterpret_cast<const void*>(&mx4_gemm_kernel<false, TM, TN, RING, true>)},
+             {reinterpret_cast<const void*>(&mx4_gemm_kernel<true, TM, TN, RING, false>),
+              reinterpret_cast<const void*>(&mx4_gemm_kernel<true, TM, TN, RING, true>)}}};
+}
+
+GemmBuild gemm_build(int cus, int M, int N, int groups) {
+    GemmBuild b{};
+    b.splits = 1;
+    if (M <= 16 || (size_t)N * groups < 16 || (size_t)M * groups < 16) return b;   // (scales come by 16)
+    auto tiles = [&](int tm, int tn) { return (size_t)ceil_div(M, tm) * ceil_div(N, tn); };
+    b = M <= 64 ? gemm_of<64, 128, 4>()
+        : M <= 128 || 2 * tiles(256, 256) < (size_t)cus ? gemm_of<128, 128, 2>()
+                                                       : gemm_of<256, 256, 2>();
+    const size_t n = tiles(b.tm, b.tn);
+    // as many parts as give every CU one workgroup, of two pairs of stages at least
+    if (b.tm < 256 && n <= (size_t)symtile_host::kWorkspaceCounters)
+        b.splits = (int)std::max<size_t>(1, std::min<size_t>((size_t)cus / n, ceil_div(groups, 8) / 4));
+    return b;
+}
+
+// Counters, one per tile, then the partial sums.
+constexpr size_t kCounterBytes = (size_t)symtile_host::kWorkspaceCounters * 4;
+
+size_t workspace_bytes_of(const GemmBuild& b, int splits, int M, int N) {
+    if (splits <= 1) return 0;
+    return kCounterBytes + (size_t)ceil_div(M, b.tm) * ceil_div(N, b.tn) * splits * b.tm * b.tn * 4;
 }
 
 bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
@@ -631,8 +755,12 @@ extern "C" symtile_status symtile_mx4_workspace_bytes(int device, int M, int N_l
     if (!bytes) return fail(SYMTILE_EINVAL, "bytes is NULL");
     *bytes = 0;
     if (symtile_status st = check_sizes(M, N_local, K)) return st;
-    if (symtile_host::cu_count(device) <= 0)
+    const int cus = symtile_host::cu_count(device);
+    if (cus <= 0)
         return fail(SYMTILE_EINVAL, "device " + std::to_string(device) + " out of range");
+    if (M == 0 || N_local == 0) return SYMTILE_OK;
+    const GemmBuild build = gemm_build(cus, M, N_local, K / kBlock);
+    *bytes = workspace_bytes_of(build, build.splits, M, N_local);
     return SYMTILE_OK;
 }
 
@@ -666,7 +794,7 @@ extern "C" symtile_status symtile_mx4_all_scatter(
         return fail(SYMTILE_EINVAL, "arrived_local not inside slot of rank");
     if (overlap(C_gathered_local, c_bytes, arrived_local, flag_bytes))
         return fail(SYMTILE_EINVAL, "arrived_local overlaps C_gathered_local");
-    (void)workspace_bytes;
+    const int cus = std::max(1, symtile_host::cu_count(h->device));
 
     ProductParams p{};
     p.x = x;
@@ -684,27 +812,35 @@ extern "C" symtile_status symtile_mx4_all_scatter(
     p.world = world_size;
     p.ldc = ldc;
     p.tiles_n = tiles_n;
-    if (M > kTileM && (size_t)N_local * p.groups >= 16) {   // (scales come by 16)
-        constexpr int TM = 256, TN = 256;
-        p.gm = ceil_div(M, TM);
-        p.gn = ceil_div(N_local, TN);
-        const size_t tiles = (size_t)p.gm * p.gn;
-        if (tiles > (1u << 24)) return fail(SYMTILE_EINVAL, "more than 16777216 tiles");
-        p.per_xcd = (int)(tiles / kXcds);
-        p.xcd_rest = (int)(tiles % kXcds);
-        p.band = kBandRows * p.gn;
+    const GemmBuild build = gemm_build(cus, M, N_local, p.groups);
+    if (build.tm) {
+        p.gm = ceil_div(M, build.tm);
+        const int gn = ceil_div(N_local, build.tn);
+        const int stages = ceil_div(p.groups, 8);
+        int splits = workspace ? build.splits : 1;
+        const size_t need = workspace_bytes_of(build, splits, M, N_local);
+        if (workspace && workspace_bytes < need)
+            return fail(SYMTILE_EINVAL, "workspace of " + std::to_string(need) + " bytes needed");
+        p.part_stages = std::max(2, ceil_div(ceil_div(stages, splits), 2) * 2);   // whole pairs
+        splits = std::max(1, ceil_div(stages, p.part_stages));                    // none empty
+        p.splits = splits;
+        p.by_splits = symtile_host::make_div(splits);
+        if (splits > 1) {
+            p.counters = static_cast<uint32_t*>(workspace);
+            p.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes);
+        }
+        const size_t units = (size_t)p.gm * gn * splits;
+        if (units > (1u << 23)) return fail(SYMTILE_EINVAL, "more than 8388608 tiles");
+        p.per_xcd = (int)(units / kXcds);
+        p.xcd_rest = (int)(units % kXcds);
+        p.band = kBandRows * gn;
         p.by_band = symtile_host::make_div(p.band);
+        const bool aligned = p.groups % 16 == 0 && !misaligned(x_scales, 16) && !misaligned(scales, 16);
         int prev = -1;
         if (symtile_status st = symtile_host::set_device(h, &prev)) return st;
         void* args[] = {&p};
-        const bool aligned = p.groups % 16 == 0 && !misaligned(x_scales, 16) && !misaligned(scales, 16);
-        const void* kernel =
-            dtype == SYMTILE_BF16
-                ? aligned ? reinterpret_cast<const void*>(&mx4_gemm_kernel<true, TM, TN, true>)
-                          : reinterpret_cast<const void*>(&mx4_gemm_kernel<true, TM, TN, false>)
-            : aligned ? reinterpret_cast<const void*>(&mx4_gemm_kernel<false, TM, TN, true>)
-                      : reinterpret_cast<const void*>(&mx4_gemm_kernel<false, TM, TN, false>);
-        hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)tiles), dim3(256), args, 0,
+        hipError_t e = hipLaunchKernel(build.kernels[dtype == SYMTILE_BF16][aligned],
+                                       dim3((unsigned)units), dim3(256), args, 0,
                                        static_cast<hipStream_t>(s));
         if (e == hipSuccess) e = hipGetLastError();
         if (prev >= 0) (void)hipSetDevice(prev);
