@@ -566,21 +566,40 @@ mx4_gemm_kernel(ProductParams p) {
         for (int i = 0; i < kNT; ++i)
 #pragma unroll
             for (int j = 0; j < kMT; ++j) acc[i][j] = f32x16{};
-        // the parts in the order of K
-        for (int s = 0; s < p.splits; ++s)
+        // the parts in the order of K, several parts' loads in flight together (parts that are
+        // not there are zeros)
+        constexpr int kTogether = kNT * kMT <= 2 ? 4 : 2;
+        for (int s0 = 0; s0 < p.splits; s0 += kTogether) {
+            f32x4 u[kTogether][kNT * kMT * 4];
 #pragma unroll
-            for (int i = 0; i < kNT; ++i)
+            for (int s = 0; s < kTogether; ++s)
 #pragma unroll
-                for (int j = 0; j < kMT; ++j)
+                for (int q = 0; q < kNT * kMT * 4; ++q)
+                    u[s][q] = __builtin_bit_cast(
+                        f32x4, symtile::buf_ld16p<symtile::kLoadCoherent>(
+                                   from, s0 + s < p.splits ? at : symtile::kOOB,
+                                   (uint32_t)((s0 + s) * kPart * 4 + q * 1024)));
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const f32x4 u = __builtin_bit_cast(
-                            f32x4, symtile::buf_ld16p<symtile::kLoadCoherent>(
-                                       from, at, (uint32_t)(s * kPart * 4 + ((i * kMT + j) * 4 + q) * 1024)));
+            for (int s = 0; s < kTogether; ++s)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += u[e];
-                    }
+                for (int q = 0; q < kNT * kMT * 4; ++q)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        acc[q / 4 / kMT][q / 4 % kMT][q % 4 * 4 + e] += u[s][q][e];
+        }
     }
+    // The slots' bases, all asked for before the first is needed: for the stores, and for the
+    // lane's counter (64x8192x3584 into 8 slots: one after the other in the loops over the slots
+    // they took 6 us).
+    uint64_t bases[SYMTILE_MAX_WORLD];
+#pragma unroll
+    for (int s = 0; s < SYMTILE_MAX_WORLD; ++s) bases[s] = p.bases[min(s, p.world - 1)];
+    constexpr int kCols = TM * TN / 256, kTiles16 = kCols / kTileN;      // columns that a wave stores
+    constexpr int kSlots = 64 / kTiles16;                                // slots that 64 lanes count
+    uint64_t counter_base[(SYMTILE_MAX_WORLD + kSlots - 1) / kSlots];
+#pragma unroll
+    for (int i = 0; i < (SYMTILE_MAX_WORLD + kSlots - 1) / kSlots; ++i)
+        counter_base[i] = p.bases[min(i * kSlots + lane / kTiles16, p.world - 1)];
     // The stages' place is the results' from here on, rows of TN: vector v of 8 values of row
     // m at v ^ (m % 32).  A lane has four values in a row of each group of accumulators.
     __syncthreads();
@@ -601,7 +620,7 @@ mx4_gemm_kernel(ProductParams p) {
             }
     __syncthreads();
     // a wave stores 64 rows by kCols columns into every slot and counts their tiles
-    constexpr int kCols = TM * TN / 256, kAcross = TN / kCols;
+    constexpr int kAcross = TN / kCols;
     constexpr int kLanes = kCols / 8, kPer = 64 / kLanes, kSteps = 64 / kPer;
     const int sr = wave / kAcross * 64, sn = wave % kAcross * kCols;
     const int own_rows = min(64, rows - sr), own_cols = min(kCols, cols - sn);
@@ -616,9 +635,11 @@ mx4_gemm_kernel(ProductParams p) {
             const int m = sr + (i0 + i) * kPer + row0;
             v[i] = symtile::ld16(&lds.out[m * TN + (((sn / 8 + v0) ^ (m & kMask)) * 8)]);
         }
-        for (int s = 0; s < p.world; ++s) {
+#pragma unroll
+        for (int s = 0; s < SYMTILE_MAX_WORLD; ++s) {
+            if (s >= p.world) break;
             const symtile::rsrc_t dst = symtile::make_rsrc(
-                reinterpret_cast<char*>(p.bases[s]) + p.c_off + ((size_t)(m0 + sr) * p.ldc + n0 + sn) * 2,
+                reinterpret_cast<char*>(bases[s]) + p.c_off + ((size_t)(m0 + sr) * p.ldc + n0 + sn) * 2,
                 (uint32_t)(((size_t)(own_rows - 1) * p.ldc + own_cols) * 2));
 #pragma unroll
             for (int i = 0; i < kBatch; ++i)
@@ -627,11 +648,13 @@ mx4_gemm_kernel(ProductParams p) {
         }
     }
     symtile::release_written_through();
-    const int tiles = (own_cols + kTileN - 1) / kTileN;
-    for (int s = 0; s < p.world; ++s)
-        if (lane < tiles)
-            symtile::flag_signal(reinterpret_cast<uint32_t*>(p.bases[s] + p.flag_off) +
-                                 (size_t)((m0 + sr) / kTileM) * p.tiles_n + (n0 + sn) / kTileN + lane);
+    const int counted = lane % kTiles16;
+#pragma unroll
+    for (int i = 0; i < (SYMTILE_MAX_WORLD + kSlots - 1) / kSlots; ++i)
+        if (i * kSlots + lane / kTiles16 < p.world && counted * kTileN < own_cols)
+            symtile::flag_signal(reinterpret_cast<uint32_t*>(counter_base[i] + p.flag_off) +
+                                 (size_t)((m0 + sr) / kTileM) * p.tiles_n + (n0 + sn) / kTileN +
+                                 counted);
 }
 
 // ---- host ------------------------------------------------------------------------------
