@@ -201,6 +201,7 @@ __global__ void __launch_bounds__(64 * kWaves) mx4_kernel(ProductParams p) {
     const symtile::rsrc_t xs =
         symtile::make_rsrc(p.x + (size_t)m0 * row_bytes, (uint32_t)(rows * row_bytes));
     const int wc = min(c, cols - 1);
+    const uint64_t slot_base = p.bases[min(wave, p.world - 1)];
     f32x4 total[MT] = {};
     for (int first = wave * 16; first < p.groups; first += kWaves * 16) {
         const u32x4 sw = scales16(p.w_scales, p.N, n0 + wc, p.groups, first);
@@ -238,9 +239,9 @@ __global__ void __launch_bounds__(64 * kWaves) mx4_kernel(ProductParams p) {
         out[e / 256 * 16 + e % 256 / 64 * 4 + e % 4][e / 4 % 16] = rounded<BF>(v);
     }
     __syncthreads();
-    // wave s: slot s
-    for (int s = wave; s < p.world; s += kWaves) {
-        char* base = reinterpret_cast<char*>(p.bases[s]);
+    static_assert(kWaves >= SYMTILE_MAX_WORLD, "a slot a wave");
+    if (wave < p.world) {
+        char* base = reinterpret_cast<char*>(slot_base);
         const int vecs = cols / 8;
         const symtile::rsrc_t dst = symtile::make_rsrc(
             base + p.c_off + ((size_t)m0 * p.ldc + n0) * 2,
@@ -688,11 +689,16 @@ GemmBuild gemm_of() {
 GemmBuild gemm_build(int cus, int M, int N, int groups) {
     GemmBuild b{};
     b.splits = 1;
-    if (M <= 16 || (size_t)N * groups < 16 || (size_t)M * groups < 16) return b;   // (scales come by 16)
+    // Up to 64 rows the other kernel while there is little to do: its tiles read X once each, but
+    // K needs no second way through memory.  (M x K x N, us, other kernel / this one:
+    // 1x8192x3584 6.6 / 12.3, 1x8192x8192 12.6 / 12.5, 1x8192x28672 30.7 / 20.3, 48x8192x3584 13.3 /
+    // 14.5, 64x8192x3584 16.2 / 15.7, 64x2048x4096 6.0 / 8.3, 32x8192x8192 18.5 / 12.6.)
+    const bool little = M <= kTileM && (double)ceil_div(M, 16) * N * groups * kBlock <= 1e8;
+    if (little || (size_t)N * groups < 16 || (size_t)M * groups < 16) return b;   // (scales come by 16)
     auto tiles = [&](int tm, int tn) { return (size_t)ceil_div(M, tm) * ceil_div(N, tn); };
-    b = M <= 64 ? gemm_of<64, 128, 4>()
+    b = M <= 64 || tiles(64, 128) <= (size_t)cus ? gemm_of<64, 128, 4>()
         : M <= 128 || 2 * tiles(256, 256) < (size_t)cus ? gemm_of<128, 128, 2>()
-                                                       : gemm_of<256, 256, 2>();
+                                                        : gemm_of<256, 256, 2>();
     const size_t n = tiles(b.tm, b.tn);
     // as many parts as give every CU one workgroup, of two pairs of stages at least
     if (b.tm < 256 && n <= (size_t)symtile_host::kWorkspaceCounters)

@@ -192,7 +192,8 @@ SHAPES = [  # M, K, N, world, rank
     (7, 512, 64, 4, 2), (16, 544, 136, 8, 3), (17, 992, 16, 1, 0), (33, 1024, 256, 2, 1), (49, 2080, 48, 2, 0),
     (64, 4096, 1480, 4, 1), (65, 32, 8, 1, 0), (100, 480, 88, 2, 1), (128, 1056, 264, 8, 5), (129, 256, 128, 1, 0),
     (255, 800, 104, 2, 0), (256, 512, 256, 4, 3), (257, 544, 520, 2, 1), (300, 2048, 1000, 1, 0),
-    (511, 1120, 248, 2, 1), (700, 8224, 40, 1, 0), (1000, 96, 1016, 2, 0), (40, 16416, 4104, 1, 0)]
+    (511, 1120, 248, 2, 1), (700, 8224, 40, 1, 0), (1000, 96, 1016, 2, 0), (40, 16416, 4104, 1, 0),
+    (1000, 544, 2400, 1, 0), (3000, 608, 3000, 1, 0), (2900, 1024, 3200, 2, 1)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
