@@ -17,12 +17,13 @@ using symtile::u32x4;
 
 enum Mode { kGreedy, kTokens, kDraft };   // drafts without and with their logits
 
-// A segment's part of a row's numbers: the largest logit, the sum of exp(scale (x - m))
-// and, greedy, the lowest id of the largest.
+// A segment's part of a row's numbers: the largest logit, the sum of exp(scale (x - m)),
+// greedy the lowest id of the largest, and the drafted token's logit (-inf in the other
+// segments).
 struct __attribute__((aligned(16))) Part {
     float m, s;
     uint32_t best;
-    uint32_t unused;
+    float drafted;
 };
 
 struct VerifyParams {
@@ -39,6 +40,7 @@ struct VerifyParams {
     int seq0, k, rows, vocab;   // rows of a sequence: k + 1 target ones, then k draft ones
     int segs, seg_len;          // of the first kernel
     int draw_segs, draw_len;    // of the second
+    int join_lanes;             // threads that join a row's parts
     float scale, draft_scale;
 };
 
@@ -72,7 +74,14 @@ __global__ void __launch_bounds__(kMaxThreads) verify_sums_kernel(VerifyParams p
     const int begin = seg * p.seg_len, len = min(p.seg_len, p.vocab - begin);
     const float scale = r <= p.k ? p.scale : p.draft_scale;
     Segment<DT, NV> d;
-    d.load(row_of<DT>(p, seq, r) + begin, len, threads);
+    const typename Elem<DT>::type* x = row_of<DT>(p, seq, r);
+    d.load(x + begin, len, threads);
+    const int at = r <= p.k ? r : r - p.k - 1;
+    float drafted = -kInf;
+    if (at < p.k) {
+        const int64_t id = p.ids[((size_t)p.seq0 + seq) * p.k + at];
+        if (t == 0 && id >= begin && id < begin + len) drafted = (float)x[id];
+    }
     float vec[NV];
     const float mine = wave_max(d.thread_max(vec));
     if (t % 64 == 0) m_of[t / 64] = mine;
@@ -100,7 +109,7 @@ __global__ void __launch_bounds__(kMaxThreads) verify_sums_kernel(VerifyParams p
         const float s = waves_sum(s_of, waves) * exp2f(-ex.shift);
         if constexpr (GREEDY)
             for (int w = 0; w < waves; ++w) best = min(best, best_of[w]);
-        if (t == 0) p.parts[unit] = Part{m, s, best, 0u};
+        if (t == 0) p.parts[unit] = Part{m, s, best, drafted};
     }
 }
 
@@ -109,22 +118,30 @@ __global__ void __launch_bounds__(kMaxThreads) verify_sums_kernel(VerifyParams p
 // above -inf) has s not positive and finite.
 struct RowStat {
     float m;
-    double s;
     uint32_t best;
+    float inv;         // of the sum as Exponent's own shift has it
+    float drafted;
+    double s;
     __device__ __forceinline__ bool good() const { return s > 0.0 && s < (double)kInf; }
 };
 
-__device__ __forceinline__ RowStat join(const Part* parts, int segs, float scale) {
-    RowStat r{-kInf, 0.0, 0xFFFFFFFFu};
-    for (int i = 0; i < segs; ++i) r.m = fmaxf(r.m, parts[i].m);
-    for (int i = 0; i < segs; ++i) {
-        const Part q = parts[i];
-        // (a segment at -inf alone has s = 0; beside a NaN sum nothing else matters)
-        r.s += q.m == -kInf ? (double)q.s
-                            : (double)q.s * exp((double)(q.m - r.m) * (double)scale);
-        if (q.m == r.m) r.best = min(r.best, q.best);
+// By `lanes` (a power of two from segs on, at most a wave) threads a row, a part each.
+__device__ __forceinline__ RowStat join(const Part* parts, int segs, int lanes, float scale) {
+    const int i = threadIdx.x % lanes;
+    Part q{-kInf, 0.0f, 0xFFFFFFFFu, -kInf};
+    if (i < segs) q = parts[i];
+    float m = q.m;
+    for (int o = lanes / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    // (a segment at -inf alone has s = 0; beside a NaN sum nothing else matters)
+    double s = q.m == -kInf || q.m == m
+                   ? (double)q.s : (double)(q.s * exp2f((q.m - m) * scale * kLog2e));
+    uint32_t best = q.m == m ? q.best : 0xFFFFFFFFu;
+    for (int o = lanes / 2; o; o >>= 1) {
+        s += __shfl_xor(s, o);
+        best = min(best, (uint32_t)__shfl_xor(best, o));
+        q.drafted = fmaxf(q.drafted, __shfl_xor(q.drafted, o));
     }
-    return r;
+    return RowStat{m, best, exp2f(-Exponent(m, scale).shift) / (float)s, q.drafted, s};
 }
 
 // Larger is better: scores as whole numbers, among equal ones the lower id; 0 = none.
@@ -143,43 +160,34 @@ __device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
 
 struct Shared {
     RowStat stat[2 * SYMTILE_DRAFT_MAX + 1];
-    uint64_t best[kMaxWaves], any[kMaxWaves];
+    double log_s[SYMTILE_DRAFT_MAX + 1];
+    uint64_t best[kMaxWaves];
+    float logit[kMaxWaves];
     int accepted;
     bool drafted;      // position `accepted` has a drafted token, which was not accepted
+    bool none;
     int last;
 };
 
-// The target's log probability of a token at position i.
-template <int DT>
-__device__ __forceinline__ float logprob_of(const VerifyParams& p, const Shared& sh, int seq, int i,
-                                            int64_t id) {
-    const float x = (float)row_of<DT>(p, seq, i)[id];
-    return (float)((double)(x - sh.stat[i].m) * (double)p.scale - log(sh.stat[i].s));
-}
-
 // Which positions are accepted; by the workgroup's first wave.
-template <int DT, int MODE>
-__device__ __forceinline__ void decide(const VerifyParams& p, int seq, Shared& sh) {
+template <int MODE>
+__device__ __forceinline__ void decide(const VerifyParams& p, int seq, int64_t id, Shared& sh) {
     const int lane = threadIdx.x;
-    const size_t at = ((size_t)p.seq0 + seq) * p.k;
     const bool in = lane < p.k;
-    const int64_t id = in ? p.ids[at + lane] : -1;
     bool good = false;
     if (in && id >= 0 && id < p.vocab && sh.stat[lane].good()) {
+        const RowStat& a = sh.stat[lane];
         if constexpr (MODE == kGreedy) {
-            good = (uint32_t)id == sh.stat[lane].best;
+            good = (uint32_t)id == a.best;
         } else {
-            const RowStat& a = sh.stat[lane];
-            const double px = exp((double)((float)row_of<DT>(p, seq, lane)[id] - a.m) * (double)p.scale) / a.s;
+            const double px = exp((double)(a.drafted - a.m) * (double)p.scale) / a.s;
             double qx = 1.0;
             if constexpr (MODE == kDraft) {
                 const RowStat& b = sh.stat[p.k + 1 + lane];
-                qx = exp((double)((float)row_of<DT>(p, seq, p.k + 1 + lane)[id] - b.m) *
-                         (double)p.draft_scale) / b.s;
-                if (!b.good()) qx = (double)kInf;
+                qx = b.good() ? exp((double)(b.drafted - b.m) * (double)p.draft_scale) / b.s : (double)kInf;
             }
             // (u = 0 and q = inf give a NaN: not accepted)
-            good = (double)p.uniforms[at + lane] * qx < px;
+            good = (double)p.uniforms[((size_t)p.seq0 + seq) * p.k + lane] * qx < px;
         }
     }
     const uint64_t mask = __ballot(good), given = __ballot(in && id >= 0);
@@ -190,16 +198,18 @@ __device__ __forceinline__ void decide(const VerifyParams& p, int seq, Shared& s
     }
 }
 
-template <int DT, int MODE>
-__device__ __forceinline__ void finish(const VerifyParams& p, int seq, const Shared& sh,
-                                       int64_t token) {
+// The outputs, with the drawn token and its logit; `id` is the thread's drafted one.
+__device__ __forceinline__ void finish(const VerifyParams& p, int seq, const Shared& sh, int64_t id,
+                                       int64_t token, float x) {
     const int i = threadIdx.x;
     if (i > p.k) return;
     const size_t at = (size_t)p.seq0 + seq;
     const int a = sh.accepted;
-    const int64_t id = i < a ? p.ids[at * p.k + i] : i == a ? token : -1;
+    if (i < a) x = sh.stat[i].drafted;
+    else id = i == a ? token : -1;
     p.tokens[at * (p.k + 1) + i] = id;
-    p.logprob[at * (p.k + 1) + i] = id >= 0 ? logprob_of<DT>(p, sh, seq, i, id) : 0.0f;
+    p.logprob[at * (p.k + 1) + i] =
+        id >= 0 ? (float)((double)(x - sh.stat[i].m) * (double)p.scale - sh.log_s[i]) : 0.0f;
     if (i == 0) p.accepted[at] = a;
 }
 
@@ -209,33 +219,144 @@ struct Weights {
     float inv;
     __device__ __forceinline__ Weights(const RowStat& r, float scale)
         : ex(r.m, scale), inv((float)(exp2(-(double)ex.shift) / r.s)) {}
-    __device__ __forceinline__ float operator()(float x) const {
-        return exp2_fast(ex.huge ? ex.y<true>(x) : ex.y<false>(x)) * inv;
+    template <bool HUGE>
+    __device__ __forceinline__ float of(float x) const {
+        return exp2_fast(ex.y<HUGE>(x)) * inv;
     }
 };
 
-constexpr int kDrawThreads = 256;
+constexpr int kDrawVecs = 2;      // vectors of a thread in a round
+
+// A thread's best of the race so far: ids come in ascending order, so that of equal scores
+// the first stays.
+template <int DT>
+struct Race {
+    static constexpr int kVec = Elem<DT>::kVec, kNoise = kVec / 4;
+    float score = -1.0f, logit = 0.0f;
+    uint32_t id = 0;
+    u32x4 noise[kDrawVecs][kNoise];
+
+    __device__ __forceinline__ uint64_t key() const { return score >= 0.0f ? race_key(score, id) : 0; }
+
+    __device__ __forceinline__ void ask(const float* of, int len, int at0) {
+        const int threads = blockDim.x;
+#pragma unroll
+        for (int v = 0; v < kDrawVecs; ++v)
+#pragma unroll
+            for (int i = 0; i < kNoise; ++i) {
+                const int at = at0 + (v * threads + (int)threadIdx.x) * kVec + 4 * i;
+                noise[v][i] = u32x4{0u, 0u, 0u, 0u};
+                if (at < len) noise[v][i] = Segment<SYMTILE_F32, 1>::fetch(of, len, at);
+            }
+    }
+    // A round's elements; `out`: the id that is none of the candidates.
+    template <bool LESS, bool HUGE>
+    __device__ __forceinline__ void run(const u32x4 (&x)[kDrawVecs], const u32x4 (&y)[kDrawVecs],
+                                        const Weights& wp, const Weights& wq, int len, int at0,
+                                        int begin, int64_t out) {
+        const int threads = blockDim.x;
+#pragma unroll
+        for (int v = 0; v < kDrawVecs; ++v) {
+            const int at = at0 + (v * threads + (int)threadIdx.x) * kVec;
+            const int left = len - at, not_this = (int)(out - begin - at);
+            float w[kVec];
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                w[e] = wp.template of<HUGE>(element<DT>(x[v], e));
+                if constexpr (LESS) w[e] -= wq.template of<HUGE>(element<DT>(y[v], e));
+            }
+            if (left < kVec || (unsigned)not_this < (unsigned)kVec) {
+#pragma unroll
+                for (int e = 0; e < kVec; ++e)
+                    if (e >= left || e == not_this) w[e] = 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                // (where the noise is none, a NaN, which is not above the score)
+                const float s = w[e] * __builtin_amdgcn_rcpf(__uint_as_float(noise[v][e / 4][e % 4]));
+                const bool better = w[e] > 0.0f && s > score;
+                score = better ? s : score;
+                logit = better ? element<DT>(x[v], e) : logit;
+                id = better ? begin + at + e : id;
+            }
+        }
+    }
+};
+
+// All of a row's elements from `begin` on, by the workgroup.
+template <int DT, bool HUGE>
+__device__ __forceinline__ void race_over(Race<DT>& race, const typename Elem<DT>::type* x,
+                                          const typename Elem<DT>::type* y, const float* noise,
+                                          bool less, const Weights& wp, const Weights& wq, int len,
+                                          int begin, int64_t out, bool asked) {
+    constexpr int kVec = Elem<DT>::kVec;
+    const int threads = blockDim.x, t = threadIdx.x;
+    for (int at0 = 0; at0 < len; at0 += threads * kDrawVecs * kVec) {
+        u32x4 xv[kDrawVecs], yv[kDrawVecs];
+#pragma unroll
+        for (int v = 0; v < kDrawVecs; ++v) {
+            const int at = at0 + (v * threads + t) * kVec;
+            xv[v] = yv[v] = u32x4{0u, 0u, 0u, 0u};
+            if (at < len) {
+                xv[v] = Segment<DT, 1>::fetch(x, len, at);
+                if (less) yv[v] = Segment<DT, 1>::fetch(y, len, at);
+            }
+        }
+        if (at0 || !asked) race.ask(noise, len, at0);
+        if (less) race.template run<true, HUGE>(xv, yv, wp, wq, len, at0, begin, out);
+        else race.template run<false, HUGE>(xv, yv, wp, wq, len, at0, begin, out);
+    }
+}
+
+// The workgroup's best, in its first wave, and its logit.
+template <int DT>
+__device__ __forceinline__ uint64_t best_of_all(const Race<DT>& race, Shared& sh, float* logit) {
+    const int t = threadIdx.x;
+    const uint64_t own = race.key(), best = wave_max_u64(own);
+    __syncthreads();
+    if (t % 64 == 0) sh.best[t / 64] = best;
+    if (own == best) sh.logit[t / 64] = race.logit;      // (keys of a wave's lanes differ, or are 0)
+    __syncthreads();
+    if (t >= 64) return 0;
+    const uint64_t wave = t < (int)blockDim.x / 64 ? sh.best[t % kMaxWaves] : 0;
+    const uint64_t all = wave_max_u64(wave);
+    const uint64_t who = __ballot(wave == all);
+    *logit = sh.logit[__builtin_ctzll(who) % kMaxWaves];
+    return all;
+}
 
 template <int DT, int MODE>
-__global__ void __launch_bounds__(kDrawThreads) verify_draw_kernel(VerifyParams p) {
-    constexpr int kVec = Elem<DT>::kVec;
+__global__ void __launch_bounds__(kMaxThreads) verify_draw_kernel(VerifyParams p) {
+    typedef typename Elem<DT>::type T;
     __shared__ Shared sh;
-    const int t = threadIdx.x, unit = blockIdx.x;
+    const int t = threadIdx.x, threads = blockDim.x, unit = blockIdx.x;
     const int seq = p.by_draw(unit), seg = unit - seq * p.draw_segs;
-    for (int r = t; r < p.rows; r += kDrawThreads)
-        sh.stat[r] = join(p.parts + ((size_t)seq * p.rows + r) * p.segs, p.segs,
-                          r <= p.k ? p.scale : p.draft_scale);
+    const int begin = seg * p.draw_len, len = min(p.draw_len, p.vocab - begin);
+    // the drafted tokens, the rows' parts and the noise are all asked for at once
+    const int64_t id = t < p.k ? p.ids[((size_t)p.seq0 + seq) * p.k + t] : -1;
+    const float* noise = p.noise + ((size_t)p.seq0 + seq) * p.ldn + begin;
+    Race<DT> race;
+    if constexpr (MODE != kGreedy) race.ask(noise, len, 0);
+    for (int r0 = 0; r0 < p.rows; r0 += threads / p.join_lanes) {
+        const int r = r0 + t / p.join_lanes;
+        if (r < p.rows) {
+            const RowStat stat = join(p.parts + ((size_t)seq * p.rows + r) * p.segs, p.segs,
+                                      p.join_lanes, r <= p.k ? p.scale : p.draft_scale);
+            if (t % p.join_lanes == 0) sh.stat[r] = stat;
+        }
+    }
     __syncthreads();
-    if (t < 64) decide<DT, MODE>(p, seq, sh);
+    if (t < 64) decide<MODE>(p, seq, id, sh);
+    else if (t - 64 <= p.k) sh.log_s[t - 64] = log(sh.stat[t - 64].s);
     __syncthreads();
     const int a = sh.accepted;
     const bool valid = sh.stat[a].good();
     if constexpr (MODE == kGreedy) {
-        finish<DT, MODE>(p, seq, sh, valid ? (int64_t)sh.stat[a].best : -1);
+        finish(p, seq, sh, id, valid ? (int64_t)sh.stat[a].best : -1, sh.stat[a].m);
         return;
     }
     if (!valid) {          // (the same for all of the sequence's workgroups)
-        if (seg == 0) finish<DT, MODE>(p, seq, sh, -1);
+        if (seg == 0) finish(p, seq, sh, id, -1, 0.0f);
         return;
     }
     // a position with a drafted token, and the draft's own distribution
@@ -243,80 +364,44 @@ __global__ void __launch_bounds__(kDrawThreads) verify_draw_kernel(VerifyParams 
     const int64_t out = MODE == kTokens && sh.drafted ? p.ids[((size_t)p.seq0 + seq) * p.k + a] : -1;
     const Weights wp(sh.stat[a], p.scale);
     const Weights wq(less ? sh.stat[p.k + 1 + a] : sh.stat[a], less ? p.draft_scale : p.scale);
-    const int begin = seg * p.draw_len, len = min(p.draw_len, p.vocab - begin);
-    typedef typename Elem<DT>::type T;
-    const T* x = row_of<DT>(p, seq, a) + begin;
-    const T* y = less ? row_of<DT>(p, seq, p.k + 1 + a) + begin : x;
-    const float* noise = p.noise + ((size_t)p.seq0 + seq) * p.ldn + begin;
-    uint64_t best = 0, any = 0;
-    for (int at = t * kVec; at < len; at += kDrawThreads * kVec) {
-        const u32x4 xv = Segment<DT, 1>::fetch(x, len, at), yv = Segment<DT, 1>::fetch(y, len, at);
-        u32x4 nv[kVec / 4];
-#pragma unroll
-        for (int i = 0; i < kVec / 4; ++i)
-            nv[i] = Segment<SYMTILE_F32, 1>::fetch(noise, len, at + 4 * i < len ? at + 4 * i : at);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-            const uint32_t id = begin + at + e;
-            const float pv = wp(element<DT>(xv, e));
-            float wv = pv;
-            if (less) wv -= wq(element<DT>(yv, e));
-            if (MODE == kTokens && (int64_t)id == out) wv = 0.0f;
-            const float over = __builtin_amdgcn_rcpf(__uint_as_float(nv[e / 4][e % 4]));
-            const float score = wv * over, plain = pv * over;
-            // (a NaN, from noise that is none, is no candidate)
-            if (at + e < len) {
-                if (wv > 0.0f && score >= 0.0f) best = max(best, race_key(score, id));
-                if (pv > 0.0f && plain >= 0.0f) any = max(any, race_key(plain, id));
-            }
-        }
-    }
-    best = wave_max_u64(best);
-    any = wave_max_u64(any);
-    if (t % 64 == 0) {
-        sh.best[t / 64] = best;
-        sh.any[t / 64] = any;
-    }
-    __syncthreads();
-    if (t == 0) {
-        for (int w = 1; w < kDrawThreads / 64; ++w) {
-            best = max(best, sh.best[w]);
-            any = max(any, sh.any[w]);
-        }
-        sh.best[0] = best;
-        sh.any[0] = any;
-    }
+    const T* x = row_of<DT>(p, seq, a);
+    const T* y = less ? row_of<DT>(p, seq, p.k + 1 + a) : x;
+    const bool huge = wp.ex.huge || wq.ex.huge;
+    if (huge) race_over<DT, true>(race, x + begin, y + begin, noise, less, wp, wq, len, begin, out, true);
+    else race_over<DT, false>(race, x + begin, y + begin, noise, less, wp, wq, len, begin, out, true);
+    float logit = 0.0f;
+    uint64_t best = best_of_all(race, sh, &logit);
     if (p.draw_segs > 1) {
+        // (a segment's best and its logit, next to each other)
+        uint64_t* mine = p.keys + (size_t)unit * 2;
         if (t == 0) {
-            put(p.keys + (size_t)unit * 2, best);
-            put(p.keys + (size_t)unit * 2 + 1, any);
+            put(mine, best);
+            put(mine + 1, (uint64_t)__float_as_uint(logit));
         }
         if (!arrive_last(p.counters + seq, p.draw_segs, &sh.last)) return;
-        best = any = 0;
         if (t < 64) {
-            for (int i = t; i < p.draw_segs; i += 64) {
-                best = max(best, take(p.keys + ((size_t)seq * p.draw_segs + i) * 2));
-                any = max(any, take(p.keys + ((size_t)seq * p.draw_segs + i) * 2 + 1));
-            }
-            best = wave_max_u64(best);
-            any = wave_max_u64(any);
-            if (t == 0) {
-                sh.best[0] = best;
-                sh.any[0] = any;
-            }
+            const uint64_t* of = p.keys + ((size_t)seq * p.draw_segs + min(t, p.draw_segs - 1)) * 2;
+            const uint64_t key = take(of), x = take(of + 1);
+            best = wave_max_u64(key);
+            logit = __shfl(__uint_as_float((uint32_t)x), __builtin_ctzll(__ballot(key == best)));
         }
     }
+    if (t == 0) sh.none = best == 0;
     __syncthreads();
-    // where no token has p > q, one is drawn from p
-    const uint64_t key = sh.best[0] ? sh.best[0] : sh.any[0];
-    finish<DT, MODE>(p, seq, sh, key ? (int64_t)(0xFFFFFFFFu - (uint32_t)key) : -1);
+    if (sh.none) {
+        // no token has p > q: one is drawn from p, by this workgroup alone
+        race.score = -1.0f;
+        race_over<DT, true>(race, x, x, noise - begin, false, wp, wp, p.vocab, 0, -1, false);
+        best = best_of_all(race, sh, &logit);
+    }
+    if (t < 64) finish(p, seq, sh, id, best ? (int64_t)(0xFFFFFFFFu - (uint32_t)best) : -1, logit);
 }
 
 // ---- host ------------------------------------------------------------------------------------
 struct VerifyPlan {
     Plan sums;
-    int draw_segs, draw_len, launch;      // sequences of a launch
-    size_t parts, keys, bytes;            // of the workspace
+    int draw_segs, draw_len, draw_threads, launch;      // sequences of a launch
+    size_t parts, keys, bytes;                          // of the workspace
 };
 
 VerifyPlan verify_plan(int device, int sequences, int k, int vocab, int dtype) {
@@ -326,12 +411,23 @@ VerifyPlan verify_plan(int device, int sequences, int k, int vocab, int dtype) {
     v.sums = make_plan(device, v.launch * rows, vocab, dtype, false, 0);
     const int vec = dtype == SYMTILE_F32 ? 4 : 8, n = (vocab + vec - 1) / vec;
     const int cus = std::max(1, symtile_host::cu_count(device));
-    // as many as give every CU two workgroups, of two vectors a thread at least
-    const int want = std::max(1, 2 * cus / v.launch);
-    const int segs = std::min({want, (n + 2 * kDrawThreads - 1) / (2 * kDrawThreads), 64});
+    // few rows: in up to 8 segments, while each has a CU (9 rows of 28672 bf16: 3.2 us, whole 4.5)
+    const int more = std::min({cus / (v.launch * rows), (n + 511) / 512, 8});
+    if (more > v.sums.segs) {
+        const int len = (n + more - 1) / more;
+        v.sums.segs = (n + len - 1) / len;
+        v.sums.seg_len = len * vec;
+        shape(len, true, &v.sums.nv, &v.sums.threads);
+    }
+    // the row of position a by as many workgroups as leave each a CU, of two vectors a thread
+    // and 256 threads at least: an element costs a wave some 100 cycles, and the join of several
+    // workgroups 2 us
+    const int most = 256 * kDrawVecs;
+    const int segs = std::max(1, std::min({cus / v.launch, (n + most - 1) / most, 64}));
     const int per = (n + segs - 1) / segs;
     v.draw_segs = (n + per - 1) / per;
     v.draw_len = per * vec;
+    v.draw_threads = std::min(kMaxThreads, std::max(128, (per + kDrawVecs * 64 - 1) / (kDrawVecs * 64) * 64));
     v.parts = (size_t)symtile_host::kWorkspaceCounters * 4;
     v.keys = v.parts + (size_t)v.launch * rows * v.sums.segs * sizeof(Part);
     v.bytes = v.keys + (size_t)v.launch * v.draw_segs * 16;
@@ -424,6 +520,8 @@ extern "C" symtile_status symtile_verify_draft(
     p.by_segs = symtile_host::make_div(p.segs);
     p.by_rows = symtile_host::make_div(p.rows);
     p.by_draw = symtile_host::make_div(p.draw_segs);
+    p.join_lanes = 1;
+    while (p.join_lanes < p.segs) p.join_lanes *= 2;
     const void* sums = pick(dtype, plan.sums.nv, [&](auto d, auto nv) -> const void* {
         constexpr int DT = decltype(d)::value, NV = decltype(nv)::value;
         return noise ? reinterpret_cast<const void*>(&verify_sums_kernel<DT, NV, false>)
@@ -441,7 +539,8 @@ extern "C" symtile_status symtile_verify_draft(
             return st;
         void* args[] = {&p};
         hipError_t e = hipLaunchKernel(draw, dim3((unsigned)n * (unsigned)p.draw_segs),
-                                       dim3(kDrawThreads), args, 0, static_cast<hipStream_t>(s));
+                                       dim3(noise ? (unsigned)plan.draw_threads : 256u), args, 0,
+                                       static_cast<hipStream_t>(s));
         if (e == hipSuccess) e = hipGetLastError();
         if (e != hipSuccess) return symtile_host::hip_fail(e, "verify_draw_kernel launch");
     }
