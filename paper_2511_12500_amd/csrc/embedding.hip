@@ -100,246 +100,325 @@ struct GradParams {
     void* dtable;
     size_t ld, ld_table;
     int64_t first;
-    int T, D, rows, accumulate;
+    int T, D, rows;
     float scale;
-    int blocks, col_blocks;
-    int fill;                        // workgroups that zero the table
-    int* total;                      // tokens of the shard
-    uint32_t* valid;                 // [block] of the block
+    int blocks;
+    int chunk, col_blocks;           // positions and columns' parts of a workgroup of the sums
+    int fill, clear;                 // workgroups that zero the table and the counters
+    uint32_t* counters;              // [chunk][columns' part]
+    int n_counters;
+    uint32_t* valid;                 // [block] of the block's tokens in the shard
     uint32_t* sorted;                // [block][kSortBlock] id and place, ascending
     int* order;                      // [T] tokens in the order of their ids
-    uint32_t* ids;                   // [T] their ids
+    uint32_t* ids;                   // [T] their ids, kAbsent behind the shard's tokens
     float* parts;                    // [chunk][2][columns]
-    int columns;
     symtile_host::Div by_cols;
 };
 
-// Every token's rank among its block's: the number of smaller keys, each wave comparing
-// one key with 8 of its own a lane.  The other workgroups zero the table.
+// The row of the shard that a token names; kAbsent for another rank's and padding.
+__device__ __forceinline__ uint32_t local_id(const GradParams& p, int64_t token) {
+    const uint64_t local = (uint64_t)token - (uint64_t)p.first;
+    return token >= 0 && local < (uint64_t)p.rows ? (uint32_t)local : kAbsent;
+}
+
+// Every token's rank among its block's: the number of smaller keys.  A workgroup ranks 32
+// of its block's keys: each lane one of them against an eighth of the 2048, which it reads
+// from LDS four at a time.  (With a comparison of a wave and a count of its bits each, the
+// CU's scalar unit took 16 us for 32768 tokens.)  The other workgroups zero the table and
+// the sums' counters meanwhile.
 template <int ESIZE>
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(GradParams p) {
     const int t = threadIdx.x;
-    if ((int)blockIdx.x >= p.blocks * kSortParts) {
+    const int other = (int)blockIdx.x - p.blocks * kSortParts;
+    if (other >= p.clear) {
         const int vecs = p.D * ESIZE / 16;
-        for (int r = blockIdx.x - p.blocks * kSortParts; r < p.rows; r += p.fill) {
+        for (int r = other - p.clear; r < p.rows; r += p.fill) {
             u32x4* row = reinterpret_cast<u32x4*>(static_cast<char*>(p.dtable) +
                                                   (size_t)r * p.ld_table * ESIZE);
             for (int i = t; i < vecs; i += kSortThreads) row[i] = u32x4{0u, 0u, 0u, 0u};
         }
         return;
     }
-    constexpr int kOwn = kSortBlock / kSortThreads;
-    __shared__ uint32_t keys[kSortPart];
+    if (other >= 0) {
+        for (int i = other * kSortThreads + t; i < p.n_counters; i += p.clear * kSortThreads)
+            p.counters[i] = 0u;
+        return;
+    }
+    constexpr int kOwn = kSortBlock / kSortThreads, kShares = kSortThreads / kSortPart;
+    __shared__ __attribute__((aligned(16))) uint32_t keys[kSortBlock];
     __shared__ int below[kSortPart];
     __shared__ int valid;
     const int block = blockIdx.x / kSortParts, part = blockIdx.x % kSortParts;
     const int t0 = block * kSortBlock, count = min(kSortBlock, p.T - t0);
     if (part * kSortPart >= count) return;       // (the first part is never empty)
-    if (t < kSortPart) {
-        keys[t] = kAbsent;
-        below[t] = 0;
-    }
+    if (t < kSortPart) below[t] = 0;
     if (t == 0) valid = 0;
-    __syncthreads();
-    uint32_t own[kOwn];
-    int here = 0;
+    uint32_t id[kOwn];
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
         const int at = i * kSortThreads + t;
-        own[i] = kAbsent;
-        if (at < count) {
-            const uint64_t local = (uint64_t)p.tokens[t0 + at] - (uint64_t)p.first;
-            if (p.tokens[t0 + at] >= 0 && local < (uint64_t)p.rows) {
-                own[i] = (uint32_t)local << kSortBits | (uint32_t)at;
-                ++here;
-                if (at / kSortPart == part) keys[at % kSortPart] = own[i];
-            }
-        }
+        id[i] = at < count ? local_id(p, p.tokens[t0 + at]) : kAbsent;
+        keys[at] = id[i] != kAbsent ? id[i] << kSortBits | (uint32_t)at : kAbsent;
     }
-    if (part == 0 && here) atomicAdd(&valid, here);
     __syncthreads();
-    for (int j = 0; j < kSortPart; ++j) {
-        const uint32_t key = __builtin_amdgcn_readfirstlane(keys[j]);
-        int n = 0;
+    int here = 0;
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) n += __popcll(__ballot(own[i] < key));
-        if (t % 64 == 0) atomicAdd(&below[j], n);
+    for (int i = 0; i < kOwn; ++i) here += __popcll(__ballot(id[i] != kAbsent));
+    if (t % 64 == 0) atomicAdd(&valid, here);
+    const uint32_t mine = keys[part * kSortPart + t % kSortPart];
+    const u32x4* share = reinterpret_cast<const u32x4*>(keys) + t / kSortPart * (kSortBlock / kShares / 4);
+    int n = 0;
+#pragma unroll 8
+    for (int i = 0; i < kSortBlock / kShares / 4; ++i) {
+        const u32x4 k = share[i];
+        n += (k[0] < mine) + (k[1] < mine) + (k[2] < mine) + (k[3] < mine);
     }
+    atomicAdd(&below[t % kSortPart], n);
     __syncthreads();
-    // (an absent token's key may equal a present one's where ids reach 2^21: by its place)
     const int at = part * kSortPart + t;
     if (t < kSortPart && at < count) {
-        const uint64_t local = (uint64_t)p.tokens[t0 + at] - (uint64_t)p.first;
-        if (p.tokens[t0 + at] >= 0 && local < (uint64_t)p.rows) {
-            if (p.blocks == 1) {
+        // (by the token: the largest present key is as an absent one's where ids reach 2^21)
+        const uint32_t local = local_id(p, p.tokens[t0 + at]);
+        if (p.blocks == 1) {
+            if (local != kAbsent) {
                 p.order[below[t]] = at;
-                p.ids[below[t]] = (uint32_t)local;
-            } else {
-                p.sorted[(size_t)block * kSortBlock + below[t]] = keys[t];
+                p.ids[below[t]] = local;
             }
+            if (at >= valid) p.ids[at] = kAbsent;
+        } else if (local != kAbsent) {
+            p.sorted[(size_t)block * kSortBlock + below[t]] = mine;
         }
     }
-    if (part == 0 && t == 0) {
-        p.valid[block] = (uint32_t)valid;
-        if (p.blocks == 1) *p.total = valid;
-    }
+    if (part == 0 && t == 0) p.valid[block] = (uint32_t)valid;
 }
 
 // The place of every token of a block among all: its place in its own block, and in every
-// other one the number of ids below its own, or, in earlier blocks, not above it.  16
-// lanes a token, a block each.
-__global__ void __launch_bounds__(kSortThreads) embed_merge_kernel(GradParams p) {
-    const int lane = threadIdx.x % 16;
-    const int64_t unit = ((int64_t)blockIdx.x * kSortThreads + threadIdx.x) / 16;
-    const int block = (int)(unit / kSortBlock), i = (int)(unit % kSortBlock);
-    if (block == 0 && i == 0) {
-        int n = 0;
-        for (int b = lane; b < p.blocks; b += 16) n += (int)p.valid[b];
-#pragma unroll
-        for (int o = 8; o; o >>= 1) n += __shfl_xor(n, o);
-        if (lane == 0) *p.total = n;
-    }
-    if (block >= p.blocks || i >= (int)p.valid[block]) return;
-    const uint32_t key = p.sorted[(size_t)block * kSortBlock + i], id = key >> kSortBits;
-    int place = lane == 0 ? i : 0;
-    for (int b = lane; b < p.blocks; b += 16) {
-        if (b == block) continue;
+// other one the number of ids below its own, or, in earlier blocks, not above it.  A
+// workgroup takes 64 tokens next to each other in their block's order, a wave of it another
+// block: one load of every 32nd key bounds where all 64 can lie, and what is left to search
+// are a few lines.  (A search over the whole block for each of them: 10 us for 32768.)
+constexpr int kMergeThreads = 1024;
+__global__ void __launch_bounds__(kMergeThreads) embed_merge_kernel(GradParams p) {
+    __shared__ int place[64];
+    __shared__ int total;
+    const int t = threadIdx.x, lane = t % 64, wave = __builtin_amdgcn_readfirstlane(t / 64);
+    const int unit0 = blockIdx.x * 64, block = unit0 / kSortBlock, i = unit0 % kSortBlock + lane;
+    const int count = (int)p.valid[block];
+    if (t < 64) place[t] = i;
+    if (t == 0) total = 0;
+    __syncthreads();
+    const bool some = i - lane < count;
+    // lanes behind the last token search for that one
+    const uint32_t key = some ? p.sorted[(size_t)block * kSortBlock + min(i, count - 1)] : 0u;
+    const uint32_t id = key >> kSortBits, first = id << kSortBits, last = first | (kSortBlock - 1);
+    int n = 0, sum = 0;
+    for (int b = wave; b < p.blocks; b += kMergeThreads / 64) {
+        const int valid = (int)p.valid[b];
+        sum += valid;
+        if (b == block || !some) continue;
         const uint32_t* of = p.sorted + (size_t)b * kSortBlock;
-        // keys of this id lie between; those with ids below it are below the first
-        const uint32_t first = id << kSortBits, last = first | (kSortBlock - 1);
-        int lo = 0, hi = (int)p.valid[b];
+        // keys of this id lie from `first` to `last`; the smaller ids' are below the first
+        const bool earlier = b < block;
+        auto is_below = [&](uint32_t k, uint32_t lo, uint32_t hi) { return earlier ? k <= hi : k < lo; };
+        const uint32_t coarse = lane * 32 < valid ? of[lane * 32] : 0u;
+        const bool there = lane * 32 < valid;
+        const uint32_t f0 = __builtin_amdgcn_readlane(first, 0), f1 = __builtin_amdgcn_readlane(first, 63);
+        const int c0 = __popcll(__ballot(there && is_below(coarse, f0, f0 | (kSortBlock - 1))));
+        const int c1 = __popcll(__ballot(there && is_below(coarse, f1, f1 | (kSortBlock - 1))));
+        int lo = max(0, (c0 - 1) * 32), hi = min(valid, c1 * 32);
         while (lo < hi) {
             const int mid = (lo + hi) / 2;
-            const uint32_t k = of[mid];
-            if (b < block ? k <= last : k < first) lo = mid + 1;
+            if (is_below(of[mid], first, last)) lo = mid + 1;
             else hi = mid;
         }
-        place += lo;
+        n += lo;
     }
-#pragma unroll
-    for (int o = 8; o; o >>= 1) place += __shfl_xor(place, o);
-    if (lane == 0) {
-        p.order[place] = block * kSortBlock + (int)(key & (kSortBlock - 1));
-        p.ids[place] = id;
+    if (n) atomicAdd(&place[lane], n);
+    if (lane == 0) atomicAdd(&total, sum);
+    __syncthreads();
+    if (t < 64) {
+        if (i < count) {
+            p.order[place[t]] = block * kSortBlock + (int)(key & (kSortBlock - 1));
+            p.ids[place[t]] = id;
+        }
+        if (unit0 + t >= total && unit0 + t < p.T) p.ids[unit0 + t] = kAbsent;
     }
 }
 
 // ---- sums ------------------------------------------------------------------------------------
-constexpr int kChunk = 32, kSumThreads = 256;
+constexpr int kMaxChunk = 32, kSumThreads = 256;
 
-// n values at p, as the table's type.
+// N values of a row of the table, at most 16 bytes of them together: rows start at
+// multiples of that.
 template <int DT, int N>
-__device__ __forceinline__ void add_row(void* table, size_t at, const float* sum, float scale,
-                                        bool accumulate) {
+struct TableRow {
     typedef typename Elem<DT>::type T;
-    // (at most 16 bytes of alignment: rows start at multiples of that)
-    constexpr int kPart = N * sizeof(T) > 16 ? 16 / (int)sizeof(T) : N;
+    static constexpr int kPart = N * sizeof(T) > 16 ? 16 / (int)sizeof(T) : N;
     typedef T V __attribute__((ext_vector_type(kPart)));
-    V* to = reinterpret_cast<V*>(static_cast<T*>(table) + at);
+    V held[N / kPart];
+    __device__ __forceinline__ void read(const void* table, size_t at) {
+        const V* from = reinterpret_cast<const V*>(static_cast<const T*>(table) + at);
 #pragma unroll
-    for (int i = 0; i < N / kPart; ++i) {
-        const float* f = sum + i * kPart;
-        V v = {};
-        if (accumulate) v = to[i];
-#pragma unroll
-        for (int e = 0; e < kPart; ++e)
-            v[e] = (T)(accumulate ? __builtin_fmaf(f[e], scale, (float)v[e]) : f[e] * scale);
-        to[i] = v;
+        for (int i = 0; i < N / kPart; ++i) held[i] = from[i];
     }
+    // scale * sum, and what is held where that is added
+    template <bool ADD>
+    __device__ __forceinline__ void write(void* table, size_t at, const float* sum, float scale) const {
+        V* to = reinterpret_cast<V*>(static_cast<T*>(table) + at);
+#pragma unroll
+        for (int i = 0; i < N / kPart; ++i) {
+            V v;
+#pragma unroll
+            for (int e = 0; e < kPart; ++e) {
+                const float f = sum[i * kPart + e];
+                v[e] = (T)(ADD ? __builtin_fmaf(f, scale, (float)held[i][e]) : f * scale);
+            }
+            to[i] = v;
+        }
+    }
+};
+
+// The first position from `lo` on (before `hi`) whose id is not below `id`, or above it.
+template <bool ABOVE>
+__device__ __forceinline__ int bound(const uint32_t* ids, int lo, int hi, uint32_t id) {
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        const uint32_t k = ids[mid];
+        if (ABOVE ? k <= id : k < id) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
 }
 
-template <int DT, int TABLE>
+// A workgroup sums the runs of `chunk` positions in its columns.  A run inside the chunk
+// goes to the table; of one that passes an end the chunk's part goes to memory, and the
+// last of its chunks to arrive adds the parts, in their order.
+template <int DT, int TABLE, bool ADD>
 __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(GradParams p) {
     typedef typename Elem<DT>::type T;
-    constexpr int kVec = Elem<DT>::kVec, kAhead = 8;
-    __shared__ uint32_t ids[kChunk + 2];     // of positions begin - 1 .. end
-    __shared__ int order[kChunk];
+    constexpr int kVec = Elem<DT>::kVec, kAhead = 8, kPartVecs = kVec / 4;
+    typedef TableRow<TABLE, kVec> Row;
+    __shared__ uint32_t ids[kMaxChunk + 2];     // of positions begin - 1 .. end
+    __shared__ int order[kMaxChunk];
+    __shared__ int first_chunk[2], last_chunk[2], arrived[2];
     const int t = threadIdx.x, threads = blockDim.x;
     const int chunk = p.by_cols(blockIdx.x), cb = blockIdx.x - chunk * p.col_blocks;
-    const int total = *p.total, begin = chunk * kChunk, end = min(begin + kChunk, total);
-    if (begin >= total) return;
-    if (t < kChunk + 2) {
+    const int begin = chunk * p.chunk, most = min(p.chunk, p.T - begin);
+    if (t < most + 2) {
         const int at = begin - 1 + t;
-        ids[t] = at >= 0 && at < total ? p.ids[at] : kAbsent;
-        if (t < kChunk) order[t] = begin + t < end ? p.order[begin + t] : 0;
+        ids[t] = at >= 0 && at < p.T ? p.ids[at] : kAbsent;
+        if (t < most) order[t] = p.order[begin + t];
     }
     __syncthreads();
+    int n = most;
+    while (n > 0 && ids[n] == kAbsent) --n;      // (few chunks end so)
+    if (n == 0) return;
     const int col = (cb * threads + t) * kVec;
-    if (col >= p.D) return;
-    const int n = end - begin;
+    const bool in = col < p.D;
     float sum[kVec] = {};
-    bool before = ids[0] == ids[1];          // the run began before the chunk
+    // The chunk's first and last runs, where they pass its ends: they may be the same.
+    const bool before = ids[0] == ids[1], after = ids[n + 1] == ids[n];
+    const bool whole = before && after && ids[1] == ids[n];
+    const symtile::rsrc_t part =
+        symtile::make_rsrc(p.parts + (size_t)chunk * 2 * p.D, (uint32_t)p.D * 8);
+    bool open = before;                          // the run began before the chunk
     for (int i0 = 0; i0 < n; i0 += kAhead) {
         u32x4 v[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
-            v[i] = symtile::ld16(static_cast<const T*>(p.drows) +
-                                 (size_t)order[min(i0 + i, n - 1)] * p.ld + col);
+            v[i] = in ? symtile::ld16(static_cast<const T*>(p.drows) +
+                                      (size_t)__builtin_amdgcn_readfirstlane(order[min(i0 + i, n - 1)]) * p.ld + col)
+                      : u32x4{0u, 0u, 0u, 0u};
+        // what the table holds where a run ends: asked for with the rows, not after their sum
+        Row held[ADD ? kAhead : 1];
+        if constexpr (ADD) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int at = min(i0 + i, n - 1);
+                if (in && ids[at + 1] != ids[at + 2])
+                    held[i].read(p.dtable, (size_t)__builtin_amdgcn_readfirstlane(ids[at + 1]) * p.ld_table + col);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             if (i0 + i >= n) break;
             const int at = i0 + i;
 #pragma unroll
             for (int e = 0; e < kVec; ++e) sum[e] += element<DT>(v[i], e);
-            const uint32_t id = ids[at + 1];
-            if (at + 1 < n && ids[at + 2] == id) continue;
-            const bool goes_on = ids[at + 2] == id;
-            if (!before && !goes_on) {
-                add_row<TABLE, kVec>(p.dtable, (size_t)id * p.ld_table + col, sum, p.scale,
-                                     p.accumulate);
+            const uint32_t id = __builtin_amdgcn_readfirstlane(ids[at + 1]);
+            const bool same = __builtin_amdgcn_readfirstlane(ids[at + 2]) == id;
+            if (at + 1 < n && same) continue;
+            if (!open && !same) {
+                if (in)
+                    held[ADD ? i : 0].template write<ADD>(p.dtable, (size_t)id * p.ld_table + col, sum,
+                                                          p.scale);
             } else {
-                float* to = p.parts + ((size_t)chunk * 2 + (before ? 0 : 1)) * p.columns + col;
+                // part 0: of the run that began before; 1: of the one that goes on.  (The offset of
+                // part 1 is no scalar operand: behind a store of 16 bytes that has one the compiler
+                // leaves no wait state before the sums' registers are cleared, and the store then
+                // wrote the cleared value of some lanes' first word.)
+                const uint32_t to = (uint32_t)col * 4 + (open ? 0u : (uint32_t)p.D * 4);
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) to[e] = sum[e];
+                for (int q = 0; q < kPartVecs; ++q) {
+                    const u32x4 f = {__float_as_uint(sum[4 * q]), __float_as_uint(sum[4 * q + 1]),
+                                     __float_as_uint(sum[4 * q + 2]), __float_as_uint(sum[4 * q + 3])};
+                    symtile::buf_st16p<symtile::kStoreWriteThrough>(
+                        f, part, in ? to + q * 16 : symtile::kOOB, 0);
+                }
             }
-            before = false;
+            open = false;
 #pragma unroll
             for (int e = 0; e < kVec; ++e) sum[e] = 0.0f;
         }
     }
-}
-
-// Runs that begin in a chunk and pass its end.
-template <int DT, int TABLE>
-__global__ void __launch_bounds__(kSumThreads) embed_join_kernel(GradParams p) {
-    constexpr int kVec = Elem<DT>::kVec, kAhead = 4;
-    __shared__ int last_chunk;
-    const int t = threadIdx.x, threads = blockDim.x;
-    const int chunk = p.by_cols(blockIdx.x), cb = blockIdx.x - chunk * p.col_blocks;
-    const int total = *p.total, begin = chunk * kChunk, end = begin + kChunk;
-    if (end >= total) return;
-    const uint32_t id = p.ids[end - 1];
-    if (p.ids[end] != id || (begin > 0 && p.ids[begin - 1] == id)) return;
-    if (t == 0) {
-        int lo = end + 1, hi = total;      // the run's end: the first position of another id
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (p.ids[mid] == id) lo = mid + 1;
-            else hi = mid;
+    if (!before && !after) return;
+    // The runs that pass an end: k = 0 the first one (or the only one), k = 1 the last one.
+    symtile::wg_stores_done();
+    if (t < 2) {
+        const bool is = t == 0 ? before : after && !whole;
+        arrived[t] = 0;
+        if (is) {
+            const uint32_t id = t == 0 ? ids[1] : ids[n];
+            const int from = t == 0 ? bound<false>(p.ids, 0, begin, id) : begin + n - 1;
+            const int to = (t == 0 && !whole ? begin + 1 : bound<true>(p.ids, begin + n, p.T, id));
+            first_chunk[t] = from / p.chunk;
+            last_chunk[t] = (to - 1) / p.chunk;
+            symtile::release_written_through();
+            const uint32_t arrivals = (uint32_t)(last_chunk[t] - first_chunk[t]);
+            arrived[t] = symtile::atomic_add<__ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT>(
+                             p.counters + (size_t)first_chunk[t] * p.col_blocks + cb, 1u) == arrivals;
         }
-        last_chunk = (lo - 1) / kChunk;
     }
     __syncthreads();
-    const int col = (cb * threads + t) * kVec, last = last_chunk;
-    if (col >= p.D) return;
-    float sum[kVec];
-    const float* from = p.parts + (size_t)chunk * 2 * p.columns + col;
+    symtile::acquire_coherent_reads();
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) sum[e] = from[p.columns + e];
-    for (int c = chunk + 1; c <= last; c += kAhead) {
-        float v[kAhead][kVec];
+    for (int k = 0; k < 2; ++k) {
+        if (!__builtin_amdgcn_readfirstlane(arrived[k]) || !in) continue;
+        const int c0 = first_chunk[k], c1 = last_chunk[k];
+        const uint32_t id = k == 0 ? ids[1] : ids[n];
+        for (int c = c0; c <= c1; c += kAhead) {
+            u32x4 v[kAhead][kPartVecs];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
+            for (int i = 0; i < kAhead; ++i) {
+                const symtile::rsrc_t of = symtile::make_rsrc(
+                    p.parts + (size_t)min(c + i, c1) * 2 * p.D, (uint32_t)p.D * 8);
 #pragma unroll
-            for (int e = 0; e < kVec; ++e)
-                v[i][e] = p.parts[(size_t)min(c + i, last) * 2 * p.columns + col + e];
+                for (int q = 0; q < kPartVecs; ++q)
+                    v[i][q] = symtile::buf_ld16p<symtile::kLoadCoherent>(
+                        of, c + i <= c1 ? (uint32_t)(col * 4 + q * 16) : symtile::kOOB,
+                        c + i == c0 ? (uint32_t)p.D * 4 : 0u);
+            }
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-            if (c + i <= last)
+            for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) sum[e] += v[i][e];
+                for (int e = 0; e < kVec; ++e) sum[e] += __uint_as_float(v[i][e / 4][e % 4]);
+        }
+        Row row;
+        if constexpr (ADD) row.read(p.dtable, (size_t)id * p.ld_table + col);
+        row.template write<ADD>(p.dtable, (size_t)id * p.ld_table + col, sum, p.scale);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) sum[e] = 0.0f;
     }
-    add_row<TABLE, kVec>(p.dtable, (size_t)id * p.ld_table + col, sum, p.scale, p.accumulate);
 }
 
 // ---- host --------------------------------------------------------------------------------------
@@ -347,18 +426,45 @@ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
 
-struct GradWorkspace {
-    size_t valid, sorted, order, ids, parts, bytes;
+// How the sums are laid out over workgroups: columns by 16 bytes a thread, up to 256 threads,
+// and chunks of 32 positions, of 8 where that leaves the GPU with few workgroups (a chunk's
+// rows are asked for 8 at a time).
+struct GradPlan {
+    int threads, col_blocks, chunk, chunks;
 };
+GradPlan grad_plan(int T, int D, size_t esize) {
+    GradPlan g{};
+    const int vecs = (int)((size_t)D * esize / 16);
+    auto fill = [&](int chunk, int threads) {
+        g.chunk = chunk;
+        g.chunks = ceil_div(T, chunk);
+        g.threads = std::min(threads, std::max(64, ceil_div(vecs, 64) * 64));
+        g.col_blocks = ceil_div(vecs, g.threads);
+    };
+    fill(kMaxChunk, kSumThreads);
+    if ((size_t)g.chunks * g.col_blocks < 2048) fill(8, 64);
+    return g;
+}
+
+struct GradWorkspace {
+    size_t valid, counters, sorted, order, ids, parts, bytes;
+};
+// For rows of any of the types.
 GradWorkspace grad_workspace(int T, int D) {
     GradWorkspace w{};
     const size_t blocks = (size_t)ceil_div(T, kSortBlock);
-    w.valid = 256;                       // the total before it
-    w.sorted = w.valid + up(blocks * 4);
+    size_t counters = 0, chunks = 0;
+    for (size_t esize : {2, 4}) {
+        const GradPlan g = grad_plan(T, D, esize);
+        counters = std::max(counters, (size_t)g.chunks * g.col_blocks);
+        chunks = std::max(chunks, (size_t)g.chunks);
+    }
+    w.counters = up(blocks * 4);
+    w.sorted = w.counters + up(counters * 4);
     w.order = w.sorted + (blocks > 1 ? blocks * kSortBlock * 4 : 0);
     w.ids = w.order + up((size_t)T * 4);
     w.parts = w.ids + up((size_t)T * 4);
-    w.bytes = w.parts + (T > kChunk ? (size_t)ceil_div(T, kChunk) * 2 * D * 4 : 0);
+    w.bytes = w.parts + chunks * 2 * D * 4;
     return w;
 }
 
@@ -396,14 +502,17 @@ symtile_status launch_grid(const void* kernel, unsigned wgs, unsigned threads, v
     return e == hipSuccess ? SYMTILE_OK : symtile_host::hip_fail(e, what);
 }
 
-template <template <int, int> class K>
-const void* by_types(int dtype, int table) {
+const void* sum_kernel_of(int dtype, int table, bool add) {
+    auto with = [&](auto d, auto w) -> const void* {
+        constexpr int DT = decltype(d)::value, TABLE = decltype(w)::value;
+        return add ? reinterpret_cast<const void*>(&embed_sum_kernel<DT, TABLE, true>)
+                   : reinterpret_cast<const void*>(&embed_sum_kernel<DT, TABLE, false>);
+    };
     auto second = [&](auto d) -> const void* {
-        constexpr int DT = decltype(d)::value;
         switch (table) {
-            case SYMTILE_F16: return K<DT, SYMTILE_F16>::get();
-            case SYMTILE_BF16: return K<DT, SYMTILE_BF16>::get();
-            default: return K<DT, SYMTILE_F32>::get();
+            case SYMTILE_F16: return with(d, std::integral_constant<int, SYMTILE_F16>{});
+            case SYMTILE_BF16: return with(d, std::integral_constant<int, SYMTILE_BF16>{});
+            default: return with(d, std::integral_constant<int, SYMTILE_F32>{});
         }
     };
     switch (dtype) {
@@ -412,14 +521,6 @@ const void* by_types(int dtype, int table) {
         default: return second(std::integral_constant<int, SYMTILE_F32>{});
     }
 }
-template <int DT, int TABLE>
-struct SumKernel {
-    static const void* get() { return reinterpret_cast<const void*>(&embed_sum_kernel<DT, TABLE>); }
-};
-template <int DT, int TABLE>
-struct JoinKernel {
-    static const void* get() { return reinterpret_cast<const void*>(&embed_join_kernel<DT, TABLE>); }
-};
 
 }  // namespace
 
@@ -523,42 +624,36 @@ extern "C" symtile_status symtile_embed_backward(
     p.T = T;
     p.D = D;
     p.rows = rows;
-    p.accumulate = accumulate;
     p.scale = scale;
     p.blocks = ceil_div(T, kSortBlock);
     p.fill = accumulate ? 0 : std::min(rows, 1024);
     if (T) {
+        const GradPlan g = grad_plan(T, D, esize);
+        p.chunk = g.chunk;
+        p.col_blocks = g.col_blocks;
+        p.by_cols = symtile_host::make_div(g.col_blocks);
+        p.n_counters = g.chunks * g.col_blocks;
+        p.clear = std::min(64, ceil_div(p.n_counters, kSortThreads));
         char* base = static_cast<char*>(workspace);
-        p.total = reinterpret_cast<int*>(base);
-        p.valid = reinterpret_cast<uint32_t*>(base + w.valid);
+        p.valid = reinterpret_cast<uint32_t*>(base);
+        p.counters = reinterpret_cast<uint32_t*>(base + w.counters);
         p.sorted = reinterpret_cast<uint32_t*>(base + w.sorted);
         p.order = reinterpret_cast<int*>(base + w.order);
         p.ids = reinterpret_cast<uint32_t*>(base + w.ids);
         p.parts = reinterpret_cast<float*>(base + w.parts);
     }
-    p.columns = D;
     OnDevice on(device);
     if (on.status) return on.status;
     const void* sort = table_esize == 4 ? reinterpret_cast<const void*>(&embed_sort_kernel<4>)
                                         : reinterpret_cast<const void*>(&embed_sort_kernel<2>);
-    if (symtile_status st = launch_grid(sort, (unsigned)(p.blocks * kSortParts + p.fill), kSortThreads,
-                                        &p, s, "embed_sort_kernel launch"))
+    if (symtile_status st = launch_grid(sort, (unsigned)(p.blocks * kSortParts + p.clear + p.fill),
+                                        kSortThreads, &p, s, "embed_sort_kernel launch"))
         return st;
     if (T == 0) return SYMTILE_OK;
     if (p.blocks > 1)
         if (symtile_status st = launch_grid(reinterpret_cast<const void*>(&embed_merge_kernel),
-                                            (unsigned)(p.blocks * (kSortBlock * 16 / kSortThreads)),
-                                            kSortThreads, &p, s, "embed_merge_kernel launch"))
+                                            (unsigned)(p.blocks * (kSortBlock / 64)), kMergeThreads, &p, s, "embed_merge_kernel launch"))
             return st;
-    const int vecs = D * (int)esize / 16;
-    const int threads = std::min(kSumThreads, ceil_div(vecs, 64) * 64);
-    p.col_blocks = ceil_div(vecs, threads);
-    p.by_cols = symtile_host::make_div(p.col_blocks);
-    const unsigned wgs = (unsigned)ceil_div(T, kChunk) * (unsigned)p.col_blocks;
-    if (symtile_status st = launch_grid(by_types<SumKernel>(dtype, table_dtype), wgs,
-                                        (unsigned)threads, &p, s, "embed_sum_kernel launch"))
-        return st;
-    if (T <= kChunk) return SYMTILE_OK;
-    return launch_grid(by_types<JoinKernel>(dtype, table_dtype), wgs, (unsigned)threads, &p, s,
-                       "embed_join_kernel launch");
+    return launch_grid(sum_kernel_of(dtype, table_dtype, accumulate != 0), (unsigned)p.n_counters,
+                       (unsigned)grad_plan(T, D, esize).threads, &p, s, "embed_sum_kernel launch");
 }
