@@ -20,6 +20,9 @@ using symtile::u32x4;
 constexpr int kTileM = SYMTILE_EMBED_TILE_M, kTileBytes = SYMTILE_EMBED_TILE_BYTES;
 constexpr int kLookupThreads = kTileBytes / 16;
 
+// Written through (sc0 sc1) with the streaming hint (nt): the acknowledgement is the same.
+constexpr int kStoreThroughStream = symtile::kStoreWriteThrough | symtile::kStoreNonTemporal;
+
 struct LookupParams {
     const int64_t* tokens;
     const void* table;
@@ -51,6 +54,11 @@ __global__ void __launch_bounds__(kLookupThreads) embed_kernel(LookupParams p) {
         at[t] = of;
     }
     __syncthreads();
+    // the slots' bases, all asked for before the first is needed, and that of the lane's counter
+    uint64_t bases[SYMTILE_MAX_WORLD];
+#pragma unroll
+    for (int s = 0; s < SYMTILE_MAX_WORLD; ++s) bases[s] = p.bases[min(s, p.world - 1)];
+    const uint64_t counter_base = p.bases[min(t, p.world - 1)];
     if (col < p.D) {
         u32x4 v[kTileM];
         int of[kTileM];
@@ -69,27 +77,29 @@ __global__ void __launch_bounds__(kLookupThreads) embed_kernel(LookupParams p) {
             v[i] = of[i] == -2 ? u32x4{0u, 0u, 0u, 0u} : pack<DT>(f);
         }
         const uint32_t row_bytes = (uint32_t)(p.D * sizeof(T));
-        for (int s = 0; s < p.world; ++s) {
+#pragma unroll
+        for (int s = 0; s < SYMTILE_MAX_WORLD; ++s) {
+            if (s >= p.world) break;
             const symtile::rsrc_t dst = symtile::make_rsrc(
-                reinterpret_cast<char*>(p.bases[s]) + p.out_off + (size_t)t0 * row_bytes,
+                reinterpret_cast<char*>(bases[s]) + p.out_off + (size_t)t0 * row_bytes,
                 (uint32_t)count * row_bytes);
 #pragma unroll
             for (int i = 0; i < kTileM; ++i)
                 if (of[i] != -1)
-                    symtile::buf_st16p<symtile::kStoreWriteThrough>(
-                        v[i], dst, (uint32_t)(col * sizeof(T)), i * row_bytes);
+                    symtile::buf_st16p<kStoreThroughStream>(v[i], dst, (uint32_t)(col * sizeof(T)),
+                                                            i * row_bytes);
         }
     }
     symtile::wg_stores_done();
     if (t < p.world) {
         symtile::release_written_through();
-        symtile::flag_signal(reinterpret_cast<uint32_t*>(p.bases[t] + p.flag_off) + tile);
+        symtile::flag_signal(reinterpret_cast<uint32_t*>(counter_base + p.flag_off) + tile);
     }
 }
 
 // ---- tokens in the order of their ids -------------------------------------------------------
 constexpr int kSortBlock = 2048, kSortBits = 11, kSortThreads = 256;
-constexpr int kSortPart = 32;        // tokens that a workgroup places
+constexpr int kSortPart = 16;        // tokens that a workgroup places (32: 1 us more)
 constexpr int kSortParts = kSortBlock / kSortPart;
 constexpr uint32_t kAbsent = 0xFFFFFFFFu;
 static_assert(SYMTILE_VOCAB_MAX <= 1 << (32 - kSortBits), "an id and a place in 32 bits");
@@ -104,7 +114,7 @@ struct GradParams {
     float scale;
     int blocks;
     int chunk, col_blocks;           // positions and columns' parts of a workgroup of the sums
-    int fill, clear;                 // workgroups that zero the table and the counters
+    int clear;                       // workgroups that zero the counters
     uint32_t* counters;              // [chunk][columns' part]
     int n_counters;
     uint32_t* valid;                 // [block] of the block's tokens in the shard
@@ -121,24 +131,14 @@ __device__ __forceinline__ uint32_t local_id(const GradParams& p, int64_t token)
     return token >= 0 && local < (uint64_t)p.rows ? (uint32_t)local : kAbsent;
 }
 
-// Every token's rank among its block's: the number of smaller keys.  A workgroup ranks 32
-// of its block's keys: each lane one of them against an eighth of the 2048, which it reads
-// from LDS four at a time.  (With a comparison of a wave and a count of its bits each, the
-// CU's scalar unit took 16 us for 32768 tokens.)  The other workgroups zero the table and
-// the sums' counters meanwhile.
-template <int ESIZE>
+// Every token's rank among its block's: the number of smaller keys.  A workgroup ranks 16
+// of its block's keys: each lane one of them against a sixteenth of the 2048, which it
+// reads from LDS four at a time.  (With a comparison of a wave and a count of its bits each, the
+// CU's scalar unit took 16 us for 32768 tokens.)  The other workgroups zero the sums'
+// counters meanwhile.
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(GradParams p) {
     const int t = threadIdx.x;
     const int other = (int)blockIdx.x - p.blocks * kSortParts;
-    if (other >= p.clear) {
-        const int vecs = p.D * ESIZE / 16;
-        for (int r = other - p.clear; r < p.rows; r += p.fill) {
-            u32x4* row = reinterpret_cast<u32x4*>(static_cast<char*>(p.dtable) +
-                                                  (size_t)r * p.ld_table * ESIZE);
-            for (int i = t; i < vecs; i += kSortThreads) row[i] = u32x4{0u, 0u, 0u, 0u};
-        }
-        return;
-    }
     if (other >= 0) {
         for (int i = other * kSortThreads + t; i < p.n_counters; i += p.clear * kSortThreads)
             p.counters[i] = 0u;
@@ -148,17 +148,20 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(GradParams p) 
     __shared__ __attribute__((aligned(16))) uint32_t keys[kSortBlock];
     __shared__ int below[kSortPart];
     __shared__ int valid;
+    __shared__ bool last_there;
     const int block = blockIdx.x / kSortParts, part = blockIdx.x % kSortParts;
     const int t0 = block * kSortBlock, count = min(kSortBlock, p.T - t0);
     if (part * kSortPart >= count) return;       // (the first part is never empty)
     if (t < kSortPart) below[t] = 0;
     if (t == 0) valid = 0;
+    if (t == kSortThreads - 1) last_there = false;
     uint32_t id[kOwn];
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
         const int at = i * kSortThreads + t;
         id[i] = at < count ? local_id(p, p.tokens[t0 + at]) : kAbsent;
         keys[at] = id[i] != kAbsent ? id[i] << kSortBits | (uint32_t)at : kAbsent;
+        if (at == kSortBlock - 1 && id[i] != kAbsent) last_there = true;
     }
     __syncthreads();
     int here = 0;
@@ -177,8 +180,9 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(GradParams p) 
     __syncthreads();
     const int at = part * kSortPart + t;
     if (t < kSortPart && at < count) {
-        // (by the token: the largest present key is as an absent one's where ids reach 2^21)
-        const uint32_t local = local_id(p, p.tokens[t0 + at]);
+        // (the block's last token may have a key like an absent one's, where ids reach 2^21)
+        const uint32_t local = mine != kAbsent || (at % kSortBlock == kSortBlock - 1 && last_there)
+                                   ? mine >> kSortBits : kAbsent;
         if (p.blocks == 1) {
             if (local != kAbsent) {
                 p.order[below[t]] = at;
@@ -246,7 +250,7 @@ __global__ void __launch_bounds__(kMergeThreads) embed_merge_kernel(GradParams p
 }
 
 // ---- sums ------------------------------------------------------------------------------------
-constexpr int kMaxChunk = 32, kSumThreads = 256;
+constexpr int kMaxChunk = 32, kSumThreads = 64;
 
 // N values of a row of the table, at most 16 bytes of them together: rows start at
 // multiples of that.
@@ -278,14 +282,18 @@ struct TableRow {
     }
 };
 
-// The first position from `lo` on (before `hi`) whose id is not below `id`, or above it.
+// The first position from `lo` on (before `hi`) whose id is not below `id`, or above it; by
+// a wave, 64 positions a step.
 template <bool ABOVE>
 __device__ __forceinline__ int bound(const uint32_t* ids, int lo, int hi, uint32_t id) {
+    const int lane = threadIdx.x % 64;
     while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        const uint32_t k = ids[mid];
-        if (ABOVE ? k <= id : k < id) lo = mid + 1;
-        else hi = mid;
+        const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const uint32_t k = at < hi ? ids[at] : kAbsent;
+        const int c = __popcll(__ballot(at < hi && (ABOVE ? k <= id : k < id)));
+        if (c == 0) break;
+        hi = min(hi, lo + c * step);
+        lo += (c - 1) * step + 1;
     }
     return lo;
 }
@@ -293,6 +301,41 @@ __device__ __forceinline__ int bound(const uint32_t* ids, int lo, int hi, uint32
 // A workgroup sums the runs of `chunk` positions in its columns.  A run inside the chunk
 // goes to the table; of one that passes an end the chunk's part goes to memory, and the
 // last of its chunks to arrive adds the parts, in their order.
+// The other workgroups zero the rows of the table that no token names, 8 each, where
+// nothing is added.
+constexpr int kFillRows = 8;
+template <int TABLE>
+__device__ __forceinline__ void fill_rows(const GradParams& p, int r0) {
+    const int t = threadIdx.x, n = min(kFillRows, p.rows - r0);
+    const int at = bound<false>(p.ids, 0, p.T, (uint32_t)r0);
+    const uint32_t id = at + t < p.T ? p.ids[at + t] : kAbsent;
+    // lane l < 8: is there a token of row r0 + l?
+    bool there = false;
+#pragma unroll
+    for (int l = 0; l < kFillRows; ++l) {
+        const bool any = __ballot(id == (uint32_t)(r0 + l)) != 0;
+        there = t == l ? any : there;
+    }
+    if (__builtin_amdgcn_readlane(id, 63) < (uint32_t)(r0 + n) && t < n && !there) {
+        // (the 64 positions end before the rows do)
+        int lo = at + 64, hi = p.T;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (p.ids[mid] < (uint32_t)(r0 + t)) lo = mid + 1;
+            else hi = mid;
+        }
+        there = lo < p.T && p.ids[lo] == (uint32_t)(r0 + t);
+    }
+    const uint64_t absent = __ballot(t < n && !there);
+    const int vecs = p.D * (int)sizeof(typename Elem<TABLE>::type) / 16;
+    for (int l = 0; l < n; ++l) {
+        if (!(absent >> l & 1)) continue;
+        u32x4* row = reinterpret_cast<u32x4*>(static_cast<typename Elem<TABLE>::type*>(p.dtable) +
+                                              (size_t)(r0 + l) * p.ld_table);
+        for (int i = t; i < vecs; i += kSumThreads) row[i] = u32x4{0u, 0u, 0u, 0u};
+    }
+}
+
 template <int DT, int TABLE, bool ADD>
 __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(GradParams p) {
     typedef typename Elem<DT>::type T;
@@ -301,7 +344,13 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(GradParams p) {
     __shared__ uint32_t ids[kMaxChunk + 2];     // of positions begin - 1 .. end
     __shared__ int order[kMaxChunk];
     __shared__ int first_chunk[2], last_chunk[2], arrived[2];
-    const int t = threadIdx.x, threads = blockDim.x;
+    const int t = threadIdx.x;
+    if constexpr (!ADD) {
+        if ((int)blockIdx.x >= p.n_counters) {
+            fill_rows<TABLE>(p, ((int)blockIdx.x - p.n_counters) * kFillRows);
+            return;
+        }
+    }
     const int chunk = p.by_cols(blockIdx.x), cb = blockIdx.x - chunk * p.col_blocks;
     const int begin = chunk * p.chunk, most = min(p.chunk, p.T - begin);
     if (t < most + 2) {
@@ -309,11 +358,14 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(GradParams p) {
         ids[t] = at >= 0 && at < p.T ? p.ids[at] : kAbsent;
         if (t < most) order[t] = p.order[begin + t];
     }
+    // the ids on both sides of the chunk, for runs that pass its ends
+    const uint32_t back = begin - 1 - t >= 0 ? p.ids[begin - 1 - t] : kAbsent;
+    const uint32_t ahead = begin + most + t < p.T ? p.ids[begin + most + t] : kAbsent;
     __syncthreads();
     int n = most;
     while (n > 0 && ids[n] == kAbsent) --n;      // (few chunks end so)
     if (n == 0) return;
-    const int col = (cb * threads + t) * kVec;
+    const int col = (cb * kSumThreads + t) * kVec;
     const bool in = col < p.D;
     float sum[kVec] = {};
     // The chunk's first and last runs, where they pass its ends: they may be the same.
@@ -374,19 +426,27 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(GradParams p) {
     if (!before && !after) return;
     // The runs that pass an end: k = 0 the first one (or the only one), k = 1 the last one.
     symtile::wg_stores_done();
+    const uint32_t id0 = __builtin_amdgcn_readfirstlane(ids[1]);
+    const uint32_t id1 = __builtin_amdgcn_readfirstlane(ids[n]);
+    int from = begin, to = begin + n;
+    if (before) {
+        const uint64_t other = __ballot(back != id0);
+        from = other ? begin - __builtin_ctzll(other) : bound<false>(p.ids, 0, begin - 64, id0);
+    }
+    if (after) {
+        const uint64_t other = __ballot(ahead != id1);
+        to = other ? begin + n + __builtin_ctzll(other)
+                   : bound<true>(p.ids, begin + n + 64, p.T, id1);
+    }
     if (t < 2) {
-        const bool is = t == 0 ? before : after && !whole;
+        const int c0 = t == 0 ? from / p.chunk : chunk, c1 = t == 1 || whole ? (to - 1) / p.chunk : chunk;
+        first_chunk[t] = c0;
+        last_chunk[t] = c1;
         arrived[t] = 0;
-        if (is) {
-            const uint32_t id = t == 0 ? ids[1] : ids[n];
-            const int from = t == 0 ? bound<false>(p.ids, 0, begin, id) : begin + n - 1;
-            const int to = (t == 0 && !whole ? begin + 1 : bound<true>(p.ids, begin + n, p.T, id));
-            first_chunk[t] = from / p.chunk;
-            last_chunk[t] = (to - 1) / p.chunk;
+        if (t == 0 ? before : after && !whole) {
             symtile::release_written_through();
-            const uint32_t arrivals = (uint32_t)(last_chunk[t] - first_chunk[t]);
             arrived[t] = symtile::atomic_add<__ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT>(
-                             p.counters + (size_t)first_chunk[t] * p.col_blocks + cb, 1u) == arrivals;
+                             p.counters + (size_t)c0 * p.col_blocks + cb, 1u) == (uint32_t)(c1 - c0);
         }
     }
     __syncthreads();
@@ -426,23 +486,18 @@ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
 
-// How the sums are laid out over workgroups: columns by 16 bytes a thread, up to 256 threads,
-// and chunks of 32 positions, of 8 where that leaves the GPU with few workgroups (a chunk's
-// rows are asked for 8 at a time).
+// How the sums are laid out over workgroups: one wave each, columns by 16 bytes a lane (32768
+// tokens of 4096 columns 149 us, four waves 156), and chunks of 32 positions (16384 tokens of
+// 4096 columns 157 us, 179 with chunks of 8), of 8 where that leaves the GPU with few
+// workgroups; a chunk's rows are asked for 8 at a time.
 struct GradPlan {
-    int threads, col_blocks, chunk, chunks;
+    int col_blocks, chunk, chunks;
 };
 GradPlan grad_plan(int T, int D, size_t esize) {
     GradPlan g{};
-    const int vecs = (int)((size_t)D * esize / 16);
-    auto fill = [&](int chunk, int threads) {
-        g.chunk = chunk;
-        g.chunks = ceil_div(T, chunk);
-        g.threads = std::min(threads, std::max(64, ceil_div(vecs, 64) * 64));
-        g.col_blocks = ceil_div(vecs, g.threads);
-    };
-    fill(kMaxChunk, kSumThreads);
-    if ((size_t)g.chunks * g.col_blocks < 2048) fill(8, 64);
+    g.col_blocks = ceil_div((int)((size_t)D * esize / 16), kSumThreads);
+    g.chunk = (size_t)ceil_div(T, kMaxChunk) * g.col_blocks < 4096 ? 8 : kMaxChunk;
+    g.chunks = ceil_div(T, g.chunk);
     return g;
 }
 
@@ -626,7 +681,6 @@ extern "C" symtile_status symtile_embed_backward(
     p.rows = rows;
     p.scale = scale;
     p.blocks = ceil_div(T, kSortBlock);
-    p.fill = accumulate ? 0 : std::min(rows, 1024);
     if (T) {
         const GradPlan g = grad_plan(T, D, esize);
         p.chunk = g.chunk;
@@ -644,16 +698,19 @@ extern "C" symtile_status symtile_embed_backward(
     }
     OnDevice on(device);
     if (on.status) return on.status;
-    const void* sort = table_esize == 4 ? reinterpret_cast<const void*>(&embed_sort_kernel<4>)
-                                        : reinterpret_cast<const void*>(&embed_sort_kernel<2>);
-    if (symtile_status st = launch_grid(sort, (unsigned)(p.blocks * kSortParts + p.clear + p.fill),
-                                        kSortThreads, &p, s, "embed_sort_kernel launch"))
-        return st;
-    if (T == 0) return SYMTILE_OK;
-    if (p.blocks > 1)
-        if (symtile_status st = launch_grid(reinterpret_cast<const void*>(&embed_merge_kernel),
-                                            (unsigned)(p.blocks * (kSortBlock / 64)), kMergeThreads, &p, s, "embed_merge_kernel launch"))
+    if (T) {
+        if (symtile_status st = launch_grid(reinterpret_cast<const void*>(&embed_sort_kernel),
+                                            (unsigned)(p.blocks * kSortParts + p.clear), kSortThreads,
+                                            &p, s, "embed_sort_kernel launch"))
             return st;
-    return launch_grid(sum_kernel_of(dtype, table_dtype, accumulate != 0), (unsigned)p.n_counters,
-                       (unsigned)grad_plan(T, D, esize).threads, &p, s, "embed_sum_kernel launch");
+    }
+    if (p.blocks > 1) {
+        if (symtile_status st = launch_grid(reinterpret_cast<const void*>(&embed_merge_kernel),
+                                            (unsigned)(p.blocks * (kSortBlock / 64)), kMergeThreads, &p,
+                                            s, "embed_merge_kernel launch"))
+            return st;
+    }
+    const unsigned fill = accumulate ? 0u : (unsigned)ceil_div(rows, kFillRows);
+    return launch_grid(sum_kernel_of(dtype, table_dtype, accumulate != 0), (unsigned)p.n_counters + fill,
+                       kSumThreads, &p, s, "embed_sum_kernel launch");
 }
