@@ -186,10 +186,9 @@ __device__ __forceinline__ uint16_t rounded(float v) {
 }
 
 // A workgroup takes 16 columns and up to 64 rows; its waves share the chunks of 512 values.
-constexpr int kWaves = 8;
-template <bool BF, int MT>
-__global__ void __launch_bounds__(64 * kWaves) mx4_kernel(ProductParams p) {
-    __shared__ float sums[kWaves][MT][256];
+template <bool BF, int MT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) mx4_kernel(ProductParams p) {
+    __shared__ float sums[WAVES][MT][256];
     __shared__ __attribute__((aligned(16))) uint16_t out[16 * MT][kTileN];
     const int t = threadIdx.x, lane = t % 64, c = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(t / 64);
@@ -203,7 +202,7 @@ __global__ void __launch_bounds__(64 * kWaves) mx4_kernel(ProductParams p) {
     const int wc = min(c, cols - 1);
     const uint64_t slot_base = p.bases[min(wave, p.world - 1)];
     f32x4 total[MT] = {};
-    for (int first = wave * 16; first < p.groups; first += kWaves * 16) {
+    for (int first = wave * 16; first < p.groups; first += WAVES * 16) {
         const u32x4 sw = scales16(p.w_scales, p.N, n0 + wc, p.groups, first);
         u32x4 sx[MT], w[4];
 #pragma unroll
@@ -232,14 +231,14 @@ __global__ void __launch_bounds__(64 * kWaves) mx4_kernel(ProductParams p) {
     for (int i = 0; i < MT; ++i) *reinterpret_cast<f32x4*>(&sums[wave][i][4 * lane]) = total[i];
     __syncthreads();
     // element 4 * lane + e: column lane % 16, row 4 * (lane / 16) + e
-    for (int e = t; e < MT * 256; e += 64 * kWaves) {
+    for (int e = t; e < MT * 256; e += 64 * WAVES) {
         float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) v += sums[w][e / 256][e % 256];
+        for (int w = 0; w < WAVES; ++w) v += sums[w][e / 256][e % 256];
         out[e / 256 * 16 + e % 256 / 64 * 4 + e % 4][e / 4 % 16] = rounded<BF>(v);
     }
     __syncthreads();
-    static_assert(kWaves >= SYMTILE_MAX_WORLD, "a slot a wave");
+    static_assert(WAVES >= SYMTILE_MAX_WORLD, "a slot a wave");
     if (wave < p.world) {
         char* base = reinterpret_cast<char*>(slot_base);
         const int vecs = cols / 8;
@@ -700,9 +699,9 @@ GemmBuild gemm_build(int cus, int M, int N, int groups) {
         : M <= 128 || 2 * tiles(256, 256) < (size_t)cus ? gemm_of<128, 128, 2>()
                                                         : gemm_of<256, 256, 2>();
     const size_t n = tiles(b.tm, b.tn);
-    // as many parts as give every CU one workgroup, of two pairs of stages at least
+    // as many parts as give every CU one workgroup, of four pairs of stages at least (64x8192x3584 into 8 slots: 14.3 us, of two pairs 15.7)
     if (b.tm < 256 && n <= (size_t)symtile_host::kWorkspaceCounters)
-        b.splits = (int)std::max<size_t>(1, std::min<size_t>((size_t)cus / n, ceil_div(groups, 8) / 4));
+        b.splits = (int)std::max<size_t>(1, std::min<size_t>((size_t)cus / n, ceil_div(groups, 8) / 8));
     return b;
 }
 
@@ -875,22 +874,27 @@ extern "C" symtile_status symtile_mx4_all_scatter(
         if (prev >= 0) (void)hipSetDevice(prev);
         return e == hipSuccess ? SYMTILE_OK : symtile_host::hip_fail(e, "mx4_gemm_kernel launch");
     }
+    // 16 waves, so that 8192 values are one round of chunks, where every workgroup has a CU and its
+    // sums' 16 parts are few
     const int mt = M > 48 ? 4 : M > 32 ? 3 : M > 16 ? 2 : 1;
-    const void* const kernels[2][4] = {
-        {reinterpret_cast<const void*>(&mx4_kernel<false, 1>),
-         reinterpret_cast<const void*>(&mx4_kernel<false, 2>),
-         reinterpret_cast<const void*>(&mx4_kernel<false, 3>),
-         reinterpret_cast<const void*>(&mx4_kernel<false, 4>)},
-        {reinterpret_cast<const void*>(&mx4_kernel<true, 1>),
-         reinterpret_cast<const void*>(&mx4_kernel<true, 2>),
-         reinterpret_cast<const void*>(&mx4_kernel<true, 3>),
-         reinterpret_cast<const void*>(&mx4_kernel<true, 4>)}};
+    const bool many = mt == 1 && p.groups > 128 && (size_t)tiles_m * tiles_n <= (size_t)cus;
+    const void* const kernels[2][5] = {
+        {reinterpret_cast<const void*>(&mx4_kernel<false, 1, 8>),
+         reinterpret_cast<const void*>(&mx4_kernel<false, 2, 8>),
+         reinterpret_cast<const void*>(&mx4_kernel<false, 3, 8>),
+         reinterpret_cast<const void*>(&mx4_kernel<false, 4, 8>),
+         reinterpret_cast<const void*>(&mx4_kernel<false, 1, 16>)},
+        {reinterpret_cast<const void*>(&mx4_kernel<true, 1, 8>),
+         reinterpret_cast<const void*>(&mx4_kernel<true, 2, 8>),
+         reinterpret_cast<const void*>(&mx4_kernel<true, 3, 8>),
+         reinterpret_cast<const void*>(&mx4_kernel<true, 4, 8>),
+         reinterpret_cast<const void*>(&mx4_kernel<true, 1, 16>)}};
     int prev = -1;
     if (symtile_status st = symtile_host::set_device(h, &prev)) return st;
     void* args[] = {&p};
-    hipError_t e = hipLaunchKernel(kernels[dtype == SYMTILE_BF16][mt - 1],
-                                   dim3((unsigned)tiles_n, (unsigned)tiles_m), dim3(64 * kWaves),
-                                   args, 0, static_cast<hipStream_t>(s));
+    hipError_t e = hipLaunchKernel(kernels[dtype == SYMTILE_BF16][many ? 4 : mt - 1],
+                                   dim3((unsigned)tiles_n, (unsigned)tiles_m),
+                                   dim3(many ? 1024 : 512), args, 0, static_cast<hipStream_t>(s));
     if (e == hipSuccess) e = hipGetLastError();
     if (prev >= 0) (void)hipSetDevice(prev);
     return e == hipSuccess ? SYMTILE_OK : symtile_host::hip_fail(e, "mx4_kernel launch");
