@@ -91,14 +91,16 @@ __global__ void __launch_bounds__(kMaxThreads) verify_sums_kernel(VerifyParams p
     const float sum = wave_sum(ex.huge ? sum_of<DT, NV, true>(d, ex) : sum_of<DT, NV, false>(d, ex));
     uint32_t best = 0xFFFFFFFFu;
     if constexpr (GREEDY) {
+        // (few vectors hold the largest)
 #pragma unroll
         for (int i = 0; i < NV; ++i)
+            if (vec[i] == m) {
 #pragma unroll
-            for (int e = Segment<DT, NV>::kVec - 1; e >= 0; --e)
-                if (element<DT>(d.v[i], e) == m) {
+                for (int e = 0; e < Segment<DT, NV>::kVec; ++e) {
                     const uint32_t at = (i * threads + t) * Segment<DT, NV>::kVec + e;
-                    if ((int)at < len) best = min(best, begin + at);
+                    if (element<DT>(d.v[i], e) == m && (int)at < len) best = min(best, begin + at);
                 }
+            }
 #pragma unroll
         for (int o = 32; o; o >>= 1) best = min(best, (uint32_t)__shfl_xor(best, o));
         if (t % 64 == 0) best_of[t / 64] = best;
