@@ -764,7 +764,8 @@ symtile_status symtile_verify_workspace_bytes(int device, int sequences, int dra
  *  accepted     device int64 [sequences]
  *  logprob      device fp32 [sequences, drafted + 1]
  *  drafted      0 .. SYMTILE_DRAFT_MAX; vocab 1 .. SYMTILE_VOCAB_MAX
- * EINVAL for anything else; sequences = 0 launches nothing. */
+ * Every address a multiple of its type's size.  EINVAL for anything else; sequences = 0
+ * launches nothing. */
 symtile_status symtile_verify_draft(int device, const void* logits, int sequences, int drafted,
                                     int vocab, size_t ld, int dtype, float scale,
                                     const int64_t* ids, const void* draft_logits, size_t ld_draft,
@@ -810,8 +811,8 @@ symtile_status symtile_embed_workspace_bytes(int device, int T, int D, size_t* b
 
 /* The gradient of a table's shard: for every row v of `rows`
  *   dtable[v] = scale * sum over t with tokens[t] = first + v of drows[t],
- * in the order of t within each 32 tokens of sorted ids and then of those, with fp32 sums,
- * so results do not depend on timing; with accumulate = 1 added to what dtable[v] holds
+ * with fp32 sums in the order of t within chunks of the sorted tokens (8 or 32 of them,
+ * by T, D and dtype) and then of the chunks, so results do not depend on timing; with accumulate = 1 added to what dtable[v] holds
  * (in fp32, rounded once to table_dtype) and rows without a token left alone, else those
  * are zero.  Other tokens (other ranks', padding) are not read.
  *

@@ -699,7 +699,8 @@ GemmBuild gemm_build(int cus, int M, int N, int groups) {
         : M <= 128 || 2 * tiles(256, 256) < (size_t)cus ? gemm_of<128, 128, 2>()
                                                         : gemm_of<256, 256, 2>();
     const size_t n = tiles(b.tm, b.tn);
-    // as many parts as give every CU one workgroup, of four pairs of stages at least (64x8192x3584 into 8 slots: 14.3 us, of two pairs 15.7)
+    // as many parts as give every CU one workgroup, of four pairs of stages at least
+    // (64x8192x3584 into 8 slots: 14.3 us, of two pairs 15.7)
     if (b.tm < 256 && n <= (size_t)symtile_host::kWorkspaceCounters)
         b.splits = (int)std::max<size_t>(1, std::min<size_t>((size_t)cus / n, ceil_div(groups, 8) / 8));
     return b;

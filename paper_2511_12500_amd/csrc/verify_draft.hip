@@ -336,9 +336,12 @@ __global__ void __launch_bounds__(kMaxThreads) verify_draw_kernel(VerifyParams p
     const int begin = seg * p.draw_len, len = min(p.draw_len, p.vocab - begin);
     // the drafted tokens, the rows' parts and the noise are all asked for at once
     const int64_t id = t < p.k ? p.ids[((size_t)p.seq0 + seq) * p.k + t] : -1;
-    const float* noise = p.noise + ((size_t)p.seq0 + seq) * p.ldn + begin;
+    const float* noise = nullptr;
     Race<DT> race;
-    if constexpr (MODE != kGreedy) race.ask(noise, len, 0);
+    if constexpr (MODE != kGreedy) {
+        noise = p.noise + ((size_t)p.seq0 + seq) * p.ldn + begin;
+        race.ask(noise, len, 0);
+    }
     for (int r0 = 0; r0 < p.rows; r0 += threads / p.join_lanes) {
         const int r = r0 + t / p.join_lanes;
         if (r < p.rows) {
@@ -491,6 +494,11 @@ extern "C" symtile_status symtile_verify_draft(
     if (noise && drafted && !uniforms) return fail(SYMTILE_EINVAL, "noise comes with uniforms");
     if ((drafted && !ids) || !tokens || !accepted || !logprob)
         return fail(SYMTILE_EINVAL, "NULL pointer");
+    auto misaligned = [](const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; };
+    if (misaligned(uniforms, 4) || misaligned(noise, 4) || misaligned(logprob, 4))
+        return fail(SYMTILE_EINVAL, "uniforms, noise or logprob not aligned to their type");
+    if (misaligned(ids, 8) || misaligned(tokens, 8) || misaligned(accepted, 8))
+        return fail(SYMTILE_EINVAL, "ids, tokens or accepted not aligned to their type");
     const VerifyPlan plan = verify_plan(device, sequences, drafted, vocab, dtype);
     if (symtile_status st = check_workspace(workspace, workspace_bytes, plan.bytes)) return st;
     const bool draft = draft_logits && drafted;

@@ -48,7 +48,8 @@ def test_verify():
     refused(pkg.symtile_verify_draft, args, [
         {1: 0}, {1: P[0] + 2}, {2: -1}, {3: 33}, {3: -1}, {4: 0}, {5: 99}, {6: 7}, {7: 0.0}, {7: float("inf")},
         {7: float("nan")}, {8: 0}, {10: 50}, {11: -1.0}, {12: 0}, {13: 0}, {13: 0, 12: 0}, {14: 99}, {15: 0}, {16: 0},
-        {17: 0}, {18: 0}, {18: P[8] + 4}, {19: 100}])
+        {17: 0}, {18: 0}, {18: P[8] + 4}, {19: 100}, {8: P[1] + 4}, {12: P[3] + 2}, {13: P[4] + 2}, {15: P[5] + 4},
+        {16: P[6] + 4}, {17: P[7] + 2}])
     pkg.symtile_verify_draft(0, 0, 0, 3, 100, 0, pkg.F32, 1.0, 0, 0, 0, 1.0, 0, 0, 0, 0, 0, 0, 0, 0)
 
 

@@ -224,8 +224,9 @@ def test_many_sequences():
     call(S, k, V, "f32", t, "draft")
 
 
-def test_shared_noise_and_another_stream():
-    """One row of noise for all sequences; a call on another stream."""
+def test_another_stream_and_shared_noise():
+    """A call on another stream; one row of noise for all sequences, which would tie their
+    draws together, is refused."""
     S, k, V = 4, 2, 1000
     x, ids, u, e, y = inputs(S, k, V, "f32", 9)
     s = torch.cuda.Stream()
@@ -237,6 +238,8 @@ def test_shared_noise_and_another_stream():
     op.run(*args, stream=s.cuda_stream)
     s.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, (op.tokens, op.accepted, op.logprob)))
+    with pytest.raises(ValueError, match="noise: rows must not overlap"):
+        op.run(*args[:3], args[3][:1].expand(S, V), args[4])
 
 
 @pytest.mark.parametrize("V", [3000, 50001])
