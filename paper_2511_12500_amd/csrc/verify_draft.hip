@@ -128,10 +128,13 @@ struct RowStat {
 };
 
 // By `lanes` (a power of two from segs on, at most a wave) threads a row, a part each.
-__device__ __forceinline__ RowStat join(const Part* parts, int segs, int lanes, float scale) {
+__device__ __forceinline__ Part part_of(const Part* parts, int segs, int lanes) {
     const int i = threadIdx.x % lanes;
     Part q{-kInf, 0.0f, 0xFFFFFFFFu, -kInf};
     if (i < segs) q = parts[i];
+    return q;
+}
+__device__ __forceinline__ RowStat join(Part q, int lanes, float scale) {
     float m = q.m;
     for (int o = lanes / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
     // (a segment at -inf alone has s = 0; beside a NaN sum nothing else matters)
@@ -146,51 +149,38 @@ __device__ __forceinline__ RowStat join(const Part* parts, int segs, int lanes, 
     return RowStat{m, best, exp2f(-Exponent(m, scale).shift) / (float)s, q.drafted, s};
 }
 
-// Larger is better: scores as whole numbers, among equal ones the lower id; 0 = none.
-__device__ __forceinline__ uint64_t race_key(float score, uint32_t id) {
-    return (uint64_t)(__float_as_uint(score) + 1u) << 32 | (0xFFFFFFFFu - id);
-}
-
-__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        const uint64_t u = __shfl_xor((unsigned long long)v, o);
-        v = u > v ? u : v;
-    }
-    return v;
-}
-
 struct Shared {
     RowStat stat[2 * SYMTILE_DRAFT_MAX + 1];
     double log_s[SYMTILE_DRAFT_MAX + 1];
-    uint64_t best[kMaxWaves];
-    float logit[kMaxWaves];
+    float score[kMaxWaves], id[kMaxWaves], logit[kMaxWaves];
     int accepted;
     bool drafted;      // position `accepted` has a drafted token, which was not accepted
     bool none;
     int last;
 };
 
-// Which positions are accepted; by the workgroup's first wave.
+// Which positions are accepted; by the workgroup's first wave, lane l with position l's id
+// and uniform number.  Lanes l and l + 32 take its p and its q.
 template <int MODE>
-__device__ __forceinline__ void decide(const VerifyParams& p, int seq, int64_t id, Shared& sh) {
+__device__ __forceinline__ void decide(const VerifyParams& p, int64_t id, float u, Shared& sh) {
     const int lane = threadIdx.x;
     const bool in = lane < p.k;
-    bool good = false;
-    if (in && id >= 0 && id < p.vocab && sh.stat[lane].good()) {
-        const RowStat& a = sh.stat[lane];
-        if constexpr (MODE == kGreedy) {
-            good = (uint32_t)id == a.best;
-        } else {
-            const double px = exp((double)(a.drafted - a.m) * (double)p.scale) / a.s;
-            double qx = 1.0;
-            if constexpr (MODE == kDraft) {
-                const RowStat& b = sh.stat[p.k + 1 + lane];
-                qx = b.good() ? exp((double)(b.drafted - b.m) * (double)p.draft_scale) / b.s : (double)kInf;
-            }
-            // (u = 0 and q = inf give a NaN: not accepted)
-            good = (double)p.uniforms[((size_t)p.seq0 + seq) * p.k + lane] * qx < px;
+    bool good = in && id >= 0 && id < p.vocab && sh.stat[lane].good();
+    if constexpr (MODE == kGreedy) {
+        good = good && (uint32_t)id == sh.stat[lane].best;
+    } else {
+        static_assert(SYMTILE_DRAFT_MAX <= 32, "two lanes a position");
+        const int at = lane % 32;
+        const bool draft = MODE == kDraft && lane >= 32;
+        double x = 1.0;
+        if (at < p.k && (MODE == kDraft || lane < 32)) {
+            const RowStat& a = sh.stat[draft ? p.k + 1 + at : at];
+            x = a.good() ? exp((double)(a.drafted - a.m) * (double)(draft ? p.draft_scale : p.scale)) / a.s
+                         : (double)kInf;
         }
+        const double q = __shfl(x, at + 32);
+        // (u = 0 and q = inf give a NaN: not accepted)
+        good = good && (double)u * q < x;
     }
     const uint64_t mask = __ballot(good), given = __ballot(in && id >= 0);
     if (lane == 0) {
@@ -220,7 +210,7 @@ struct Weights {
     Exponent ex;
     float inv;
     __device__ __forceinline__ Weights(const RowStat& r, float scale)
-        : ex(r.m, scale), inv((float)(exp2(-(double)ex.shift) / r.s)) {}
+        : ex(r.m, scale), inv(r.inv) {}
     template <bool HUGE>
     __device__ __forceinline__ float of(float x) const {
         return exp2_fast(ex.y<HUGE>(x)) * inv;
@@ -235,10 +225,8 @@ template <int DT>
 struct Race {
     static constexpr int kVec = Elem<DT>::kVec, kNoise = kVec / 4;
     float score = -1.0f, logit = 0.0f;
-    uint32_t id = 0;
+    int id = 0;
     u32x4 noise[kDrawVecs][kNoise];
-
-    __device__ __forceinline__ uint64_t key() const { return score >= 0.0f ? race_key(score, id) : 0; }
 
     __device__ __forceinline__ void ask(const float* of, int len, int at0) {
         const int threads = blockDim.x;
@@ -310,21 +298,37 @@ __device__ __forceinline__ void race_over(Race<DT>& race, const typename Elem<DT
     }
 }
 
-// The workgroup's best, in its first wave, and its logit.
-template <int DT>
-__device__ __forceinline__ uint64_t best_of_all(const Race<DT>& race, Shared& sh, float* logit) {
+// The largest score (-1: none), the lowest id of equal ones, and its logit.
+static_assert(SYMTILE_VOCAB_MAX <= 1 << 24, "ids are whole numbers in 32-bit floats");
+struct Best {
+    float score, id, logit;
+    // Of the wave's lanes.
+    __device__ __forceinline__ void reduce() {
+        const float most = wave_max(score), first = -wave_max(score == most ? -id : -kInf);
+        const uint64_t who = __ballot(score == most && id == first);
+        logit = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(logit), __builtin_ctzll(who)));
+        score = most;
+        id = first;
+    }
+};
+
+// Of the workgroup, in its first wave.
+__device__ __forceinline__ Best best_of_all(Best b, Shared& sh) {
     const int t = threadIdx.x;
-    const uint64_t own = race.key(), best = wave_max_u64(own);
+    b.reduce();
     __syncthreads();
-    if (t % 64 == 0) sh.best[t / 64] = best;
-    if (own == best) sh.logit[t / 64] = race.logit;      // (keys of a wave's lanes differ, or are 0)
+    if (t % 64 == 0) {
+        sh.score[t / 64] = b.score;
+        sh.id[t / 64] = b.id;
+        sh.logit[t / 64] = b.logit;
+    }
     __syncthreads();
-    if (t >= 64) return 0;
-    const uint64_t wave = t < (int)blockDim.x / 64 ? sh.best[t % kMaxWaves] : 0;
-    const uint64_t all = wave_max_u64(wave);
-    const uint64_t who = __ballot(wave == all);
-    *logit = sh.logit[__builtin_ctzll(who) % kMaxWaves];
-    return all;
+    if (t < 64) {
+        const int w = min(t, (int)blockDim.x / 64 - 1);
+        b = Best{sh.score[w], sh.id[w], sh.logit[w]};
+        b.reduce();
+    }
+    return b;
 }
 
 template <int DT, int MODE>
@@ -338,21 +342,29 @@ __global__ void __launch_bounds__(kMaxThreads) verify_draw_kernel(VerifyParams p
     const int64_t id = t < p.k ? p.ids[((size_t)p.seq0 + seq) * p.k + t] : -1;
     const float* noise = nullptr;
     Race<DT> race;
+    const Part* parts = p.parts + (size_t)seq * p.rows * p.segs;
+    Part part{};
+    int r = t / p.join_lanes;
+    if (r < p.rows) part = part_of(parts + (size_t)r * p.segs, p.segs, p.join_lanes);
+    float u = 0.0f;
     if constexpr (MODE != kGreedy) {
+        if (t < p.k) u = p.uniforms[((size_t)p.seq0 + seq) * p.k + t];
         noise = p.noise + ((size_t)p.seq0 + seq) * p.ldn + begin;
         race.ask(noise, len, 0);
     }
-    for (int r0 = 0; r0 < p.rows; r0 += threads / p.join_lanes) {
-        const int r = r0 + t / p.join_lanes;
-        if (r < p.rows) {
-            const RowStat stat = join(p.parts + ((size_t)seq * p.rows + r) * p.segs, p.segs,
-                                      p.join_lanes, r <= p.k ? p.scale : p.draft_scale);
-            if (t % p.join_lanes == 0) sh.stat[r] = stat;
-        }
+    while (r < p.rows) {
+        const RowStat stat = join(part, p.join_lanes, r <= p.k ? p.scale : p.draft_scale);
+        if (t % p.join_lanes == 0) sh.stat[r] = stat;
+        r += threads / p.join_lanes;
+        if (r < p.rows) part = part_of(parts + (size_t)r * p.segs, p.segs, p.join_lanes);
     }
     __syncthreads();
-    if (t < 64) decide<MODE>(p, seq, id, sh);
-    else if (t - 64 <= p.k) sh.log_s[t - 64] = log(sh.stat[t - 64].s);
+    // (needed at the end, and taken by a wave that would wait)
+    auto logs = [&] {
+        if (t >= 64 && t - 64 <= p.k) sh.log_s[t - 64] = log(sh.stat[t - 64].s);
+    };
+    if (t < 64) decide<MODE>(p, id, u, sh);
+    else if (MODE == kGreedy) logs();
     __syncthreads();
     const int a = sh.accepted;
     const bool valid = sh.stat[a].good();
@@ -361,7 +373,10 @@ __global__ void __launch_bounds__(kMaxThreads) verify_draw_kernel(VerifyParams p
         return;
     }
     if (!valid) {          // (the same for all of the sequence's workgroups)
-        if (seg == 0) finish(p, seq, sh, id, -1, 0.0f);
+        if (seg) return;
+        logs();
+        __syncthreads();
+        finish(p, seq, sh, id, -1, 0.0f);
         return;
     }
     // a position with a drafted token, and the draft's own distribution
@@ -374,32 +389,33 @@ __global__ void __launch_bounds__(kMaxThreads) verify_draw_kernel(VerifyParams p
     const bool huge = wp.ex.huge || wq.ex.huge;
     if (huge) race_over<DT, true>(race, x + begin, y + begin, noise, less, wp, wq, len, begin, out, true);
     else race_over<DT, false>(race, x + begin, y + begin, noise, less, wp, wq, len, begin, out, true);
-    float logit = 0.0f;
-    uint64_t best = best_of_all(race, sh, &logit);
+    Best best = best_of_all(Best{race.score, (float)race.id, race.logit}, sh);
+    logs();
     if (p.draw_segs > 1) {
         // (a segment's best and its logit, next to each other)
         uint64_t* mine = p.keys + (size_t)unit * 2;
         if (t == 0) {
-            put(mine, best);
-            put(mine + 1, (uint64_t)__float_as_uint(logit));
+            put(mine, (uint64_t)__float_as_uint(best.score) << 32 | __float_as_uint(best.id));
+            put(mine + 1, (uint64_t)__float_as_uint(best.logit));
         }
         if (!arrive_last(p.counters + seq, p.draw_segs, &sh.last)) return;
         if (t < 64) {
             const uint64_t* of = p.keys + ((size_t)seq * p.draw_segs + min(t, p.draw_segs - 1)) * 2;
             const uint64_t key = take(of), x = take(of + 1);
-            best = wave_max_u64(key);
-            logit = __shfl(__uint_as_float((uint32_t)x), __builtin_ctzll(__ballot(key == best)));
+            best = Best{__uint_as_float((uint32_t)(key >> 32)), __uint_as_float((uint32_t)key),
+                        __uint_as_float((uint32_t)x)};
+            best.reduce();
         }
     }
-    if (t == 0) sh.none = best == 0;
+    if (t == 0) sh.none = best.score < 0.0f;
     __syncthreads();
     if (sh.none) {
         // no token has p > q: one is drawn from p, by this workgroup alone
         race.score = -1.0f;
         race_over<DT, true>(race, x, x, noise - begin, false, wp, wp, p.vocab, 0, -1, false);
-        best = best_of_all(race, sh, &logit);
+        best = best_of_all(Best{race.score, (float)race.id, race.logit}, sh);
     }
-    if (t < 64) finish(p, seq, sh, id, best ? (int64_t)(0xFFFFFFFFu - (uint32_t)best) : -1, logit);
+    if (t < 64) finish(p, seq, sh, id, best.score >= 0.0f ? (int64_t)best.id : -1, best.logit);
 }
 
 // ---- host ------------------------------------------------------------------------------------
