@@ -185,7 +185,11 @@ __device__ __forceinline__ uint16_t rounded(float v) {
     else return __builtin_bit_cast(uint16_t, (_Float16)v);
 }
 
-// A workgroup takes 16 columns and up to 64 rows; its waves share the chunks of 512 values.
+// A workgroup takes 16 columns and up to 64 rows; its waves share the chunks of 512 values,
+// whose 16-byte blocks go from memory to the operands' registers, and add their sums through
+// LDS.  Bound by latency: one round of loads, the waves' sums, the stores' acknowledgement and
+// the counters follow each other (1 x 8192 x 3584 into 8 slots, 15.7 MB: 6.2 us of which 2.9 are
+// an empty kernel's; 16 rows 7.8).
 template <bool BF, int MT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) mx4_kernel(ProductParams p) {
     __shared__ float sums[WAVES][MT][256];
@@ -315,7 +319,7 @@ struct GemmLds {
 template <bool BF, int TM, int TN, int RING, bool ALIGNED>
 __global__ void __launch_bounds__(256, sizeof(GemmLds<TM, TN, RING>) > 80 * 1024 ? 1 : 2)
 mx4_gemm_kernel(ProductParams p) {
-    constexpr bool kSplits = TM < 256;      // builds whose calls may split K
+    constexpr bool kSplits = TM * TN == 64 * 64;     // the build whose calls may split K
     typedef GemmLds<TM, TN, RING> Lds;
     __shared__ __attribute__((aligned(16))) Lds lds;
     constexpr int kMT = TM / 64, kNT = TN / 64;           // 32 x 32 tiles of a wave
@@ -568,7 +572,7 @@ mx4_gemm_kernel(ProductParams p) {
             for (int j = 0; j < kMT; ++j) acc[i][j] = f32x16{};
         // the parts in the order of K, several parts' loads in flight together (parts that are
         // not there are zeros)
-        constexpr int kTogether = kNT * kMT <= 2 ? 4 : 2;
+        constexpr int kTogether = 4;
         for (int s0 = 0; s0 < p.splits; s0 += kTogether) {
             f32x4 u[kTogether][kNT * kMT * 4];
 #pragma unroll
@@ -594,7 +598,12 @@ mx4_gemm_kernel(ProductParams p) {
     uint64_t bases[SYMTILE_MAX_WORLD];
 #pragma unroll
     for (int s = 0; s < SYMTILE_MAX_WORLD; ++s) bases[s] = p.bases[min(s, p.world - 1)];
-    constexpr int kCols = TM * TN / 256, kTiles16 = kCols / kTileN;      // columns that a wave stores
+    // Rows and columns that a wave stores: 64 rows, whose tiles it counts; of 64 alone a quarter
+    // of the rows in their whole width (64x8192x3584 into 8 slots, tiles of 64 x 128: 12.5 us;
+    // 64 rows of 32 columns a wave, 64 bytes of a row together, 14.2).
+    constexpr bool kShared = TM == 64;
+    constexpr int kCols = kShared ? TN : TM * TN / 256, kStoreRows = TM * TN / 4 / kCols;
+    constexpr int kTiles16 = kCols / kTileN;
     constexpr int kSlots = 64 / kTiles16;                                // slots that 64 lanes count
     uint64_t counter_base[(SYMTILE_MAX_WORLD + kSlots - 1) / kSlots];
 #pragma unroll
@@ -619,16 +628,16 @@ mx4_gemm_kernel(ProductParams p) {
                     &lds.out[m * TN + (((n / 8) ^ (m & kMask)) * 8) + n % 8]) = v;
             }
     __syncthreads();
-    // a wave stores 64 rows by kCols columns into every slot and counts their tiles
     constexpr int kAcross = TN / kCols;
-    constexpr int kLanes = kCols / 8, kPer = 64 / kLanes, kSteps = 64 / kPer;
-    const int sr = wave / kAcross * 64, sn = wave % kAcross * kCols;
-    const int own_rows = min(64, rows - sr), own_cols = min(kCols, cols - sn);
-    if (own_rows <= 0 || own_cols <= 0) return;
+    constexpr int kLanes = kCols / 8, kPer = 64 / kLanes, kSteps = kStoreRows / kPer;
+    const int sr = wave / kAcross * kStoreRows, sn = wave % kAcross * kCols;
+    const int own_rows = min(kStoreRows, rows - sr), own_cols = min(kCols, cols - sn);
+    const bool none = own_rows <= 0 || own_cols <= 0;
+    if (!kShared && none) return;
     const int row0 = lane / kLanes, v0 = lane % kLanes;
     const uint32_t at = v0 * 8 < own_cols ? (uint32_t)((row0 * p.ldc + v0 * 8) * 2) : symtile::kOOB;
     constexpr int kBatch = kSteps < 8 ? kSteps : 8;
-    for (int i0 = 0; i0 < kSteps; i0 += kBatch) {
+    for (int i0 = 0; i0 < kSteps && !none; i0 += kBatch) {
         u32x4 v[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
@@ -648,6 +657,10 @@ mx4_gemm_kernel(ProductParams p) {
         }
     }
     symtile::release_written_through();
+    if constexpr (kShared) {
+        __syncthreads();
+        if (wave) return;
+    }
     const int counted = lane % kTiles16;
 #pragma unroll
     for (int i = 0; i < (SYMTILE_MAX_WORLD + kSlots - 1) / kSlots; ++i)
@@ -688,20 +701,30 @@ GemmBuild gemm_of() {
 GemmBuild gemm_build(int cus, int M, int N, int groups) {
     GemmBuild b{};
     b.splits = 1;
-    // Up to 64 rows the other kernel while there is little to do: its tiles read X once each, but
-    // K needs no second way through memory.  (M x K x N, us, other kernel / this one:
-    // 1x8192x3584 6.6 / 12.3, 1x8192x8192 12.6 / 12.5, 1x8192x28672 30.7 / 20.3, 48x8192x3584 13.3 /
-    // 14.5, 64x8192x3584 16.2 / 15.7, 64x2048x4096 6.0 / 8.3, 32x8192x8192 18.5 / 12.6.)
-    const bool little = M <= kTileM && (double)ceil_div(M, 16) * N * groups * kBlock <= 1e8;
+    // Up to 32 rows the other kernel while there is little to do: its tiles read X once each, but
+    // K needs no second way through memory.  (M x K x N, us, other kernel / 64 x 64 tiles:
+    // 1x8192x3584 6.3 / 9.0, 1x8192x8192 12.5 / 10.5, 1x8192x28672 31 / 20, 16x8192x3584 7.8 / 9.1,
+    // 32x4096x4096 6.1 / 7.7, 32x8192x2048 9.2 / 7.9, 16x2048x16384 7.0 / 6.3, 48x4096x1024 7.2 / 7.5,
+    // 48x1024x8192 5.5 / 4.9, 64x2048x4096 6.0 / 5.8, 64x8192x3584 16.2 / 10.0.)
+    const size_t rounds = std::max<size_t>(1, ceil_div(ceil_div(N, kTileN), cus));
+    const size_t values = (size_t)ceil_div(M, 16) * groups * kBlock * rounds;
+    const bool little = M <= 32 && values <= (rounds == 1 ? 12288 : M <= 16 ? 8192 : 0);
     if (little || (size_t)N * groups < 16 || (size_t)M * groups < 16) return b;   // (scales come by 16)
+    // The largest tiles that leave no CU without one, where there are as many (into 8 slots where
+    // N is 3584 or 1024; us, tiles of 64 x 64 / 64 x 128 / 128 x 128 / 256 x 256: 64x8192x3584
+    // 10.0 / 12.5, 256x8192x3584 13.5 / 15.7 / 20.3 / 60, 1024x4096x1024 10.2 / 13.7 / 17.1 / 37,
+    // 128x8192x28672 36 / 32 / 36 / 49, 512x8192x8192 38 / 32 / 30 / 49, 512x8192x28672 115 / 106 / 77 /
+    // 67, 2048x8192x3584 72 / 76 / 56 / 70, 2048x8192x8192 130 / 119 / 82 / 70).
     auto tiles = [&](int tm, int tn) { return (size_t)ceil_div(M, tm) * ceil_div(N, tn); };
-    b = M <= 64 || tiles(64, 128) <= (size_t)cus ? gemm_of<64, 128, 4>()
-        : M <= 128 || 2 * tiles(256, 256) < (size_t)cus ? gemm_of<128, 128, 2>()
+    b = tiles(64, 64) <= (size_t)cus                    ? gemm_of<64, 64, 4>()
+        : M <= 128 || tiles(64, 128) <= (size_t)cus     ? gemm_of<64, 128, 4>()
+        : 2 * tiles(256, 256) < (size_t)cus             ? gemm_of<128, 128, 2>()
                                                         : gemm_of<256, 256, 2>();
     const size_t n = tiles(b.tm, b.tn);
     // as many parts as give every CU one workgroup, of four pairs of stages at least
-    // (64x8192x3584 into 8 slots: 14.3 us, of two pairs 15.7)
-    if (b.tm < 256 && n <= (size_t)symtile_host::kWorkspaceCounters)
+    // (64x8192x2048 7.9 us, of two pairs 8.7; 64x4096x1024 7.5, 6.9)
+    // (the larger tiles come with more than half as many as there are CUs)
+    if (b.tm * b.tn == 64 * 64)
         b.splits = (int)std::max<size_t>(1, std::min<size_t>((size_t)cus / n, ceil_div(groups, 8) / 8));
     return b;
 }
@@ -877,23 +900,21 @@ extern "C" symtile_status symtile_mx4_all_scatter(
     }
     // 16 waves, so that 8192 values are one round of chunks, where every workgroup has a CU and its
     // sums' 16 parts are few
-    const int mt = M > 48 ? 4 : M > 32 ? 3 : M > 16 ? 2 : 1;
-    const bool many = mt == 1 && p.groups > 128 && (size_t)tiles_m * tiles_n <= (size_t)cus;
-    const void* const kernels[2][5] = {
+    const int mt = M > 32 ? 2 : M > 16 ? 1 : 0;
+    const bool many = mt == 0 && p.groups > 128 && (size_t)tiles_m * tiles_n <= (size_t)cus;
+    const void* const kernels[2][4] = {
         {reinterpret_cast<const void*>(&mx4_kernel<false, 1, 8>),
          reinterpret_cast<const void*>(&mx4_kernel<false, 2, 8>),
-         reinterpret_cast<const void*>(&mx4_kernel<false, 3, 8>),
          reinterpret_cast<const void*>(&mx4_kernel<false, 4, 8>),
          reinterpret_cast<const void*>(&mx4_kernel<false, 1, 16>)},
         {reinterpret_cast<const void*>(&mx4_kernel<true, 1, 8>),
          reinterpret_cast<const void*>(&mx4_kernel<true, 2, 8>),
-         reinterpret_cast<const void*>(&mx4_kernel<true, 3, 8>),
          reinterpret_cast<const void*>(&mx4_kernel<true, 4, 8>),
          reinterpret_cast<const void*>(&mx4_kernel<true, 1, 16>)}};
     int prev = -1;
     if (symtile_status st = symtile_host::set_device(h, &prev)) return st;
     void* args[] = {&p};
-    hipError_t e = hipLaunchKernel(kernels[dtype == SYMTILE_BF16][many ? 4 : mt - 1],
+    hipError_t e = hipLaunchKernel(kernels[dtype == SYMTILE_BF16][many ? 3 : mt],
                                    dim3((unsigned)tiles_n, (unsigned)tiles_m),
                                    dim3(many ? 1024 : 512), args, 0, static_cast<hipStream_t>(s));
     if (e == hipSuccess) e = hipGetLastError();

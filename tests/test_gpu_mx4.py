@@ -193,7 +193,9 @@ SHAPES = [  # M, K, N, world, rank
     (64, 4096, 1480, 4, 1), (65, 32, 8, 1, 0), (100, 480, 88, 2, 1), (128, 1056, 264, 8, 5), (129, 256, 128, 1, 0),
     (255, 800, 104, 2, 0), (256, 512, 256, 4, 3), (257, 544, 520, 2, 1), (300, 2048, 1000, 1, 0),
     (511, 1120, 248, 2, 1), (700, 8224, 40, 1, 0), (1000, 96, 1016, 2, 0), (40, 16416, 4104, 1, 0),
-    (1000, 544, 2400, 1, 0), (3000, 608, 3000, 1, 0), (2900, 1024, 3200, 2, 1)]
+    (1000, 544, 2400, 1, 0), (3000, 608, 3000, 1, 0), (2900, 1024, 3200, 2, 1), (64, 512, 16400, 1, 0),
+    (50, 544, 16424, 2, 1), (120, 1056, 8200, 1, 0), (700, 1024, 4104, 2, 0), (16, 1056, 4104, 1, 0),
+    (1, 8192, 8200, 1, 0), (20, 8192, 264, 8, 7)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
