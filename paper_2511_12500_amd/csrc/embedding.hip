@@ -99,8 +99,10 @@ __global__ void __launch_bounds__(kLookupThreads) embed_kernel(LookupParams p) {
 
 // ---- tokens in the order of their ids -------------------------------------------------------
 constexpr int kSortBlock = 2048, kSortBits = 11, kSortThreads = 256;
-constexpr int kSortPart = 16;        // tokens that a workgroup places (32: 1 us more)
-constexpr int kSortParts = kSortBlock / kSortPart;
+// Tokens that a workgroup places: few where there is a CU for all (64 tokens of 8192 columns
+// 8.4 us with 8, 9.1 with 16), more of them share the block's keys where there is not (32768
+// tokens of 4096 columns 156 us with 8, 149 with 16, 150 with 32).
+constexpr int kFewPart = 8, kSortPart = 16;
 constexpr uint32_t kAbsent = 0xFFFFFFFFu;
 static_assert(SYMTILE_VOCAB_MAX <= 1 << (32 - kSortBits), "an id and a place in 32 bits");
 
@@ -131,28 +133,30 @@ __device__ __forceinline__ uint32_t local_id(const GradParams& p, int64_t token)
     return token >= 0 && local < (uint64_t)p.rows ? (uint32_t)local : kAbsent;
 }
 
-// Every token's rank among its block's: the number of smaller keys.  A workgroup ranks 16
-// of its block's keys: each lane one of them against a sixteenth of the 2048, which it
-// reads from LDS four at a time.  (With a comparison of a wave and a count of its bits each, the
+// Every token's rank among its block's: the number of smaller keys.  A workgroup ranks PART
+// of its block's keys: each lane one of them against a share of the 2048, which it reads
+// from LDS four at a time.  (With a comparison of a wave and a count of its bits each, the
 // CU's scalar unit took 16 us for 32768 tokens.)  The other workgroups zero the sums'
 // counters meanwhile.
+template <int PART>
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(GradParams p) {
+    constexpr int kParts = kSortBlock / PART;
     const int t = threadIdx.x;
-    const int other = (int)blockIdx.x - p.blocks * kSortParts;
+    const int other = (int)blockIdx.x - p.blocks * kParts;
     if (other >= 0) {
         for (int i = other * kSortThreads + t; i < p.n_counters; i += p.clear * kSortThreads)
             p.counters[i] = 0u;
         return;
     }
-    constexpr int kOwn = kSortBlock / kSortThreads, kShares = kSortThreads / kSortPart;
+    constexpr int kOwn = kSortBlock / kSortThreads, kShares = kSortThreads / PART;
     __shared__ __attribute__((aligned(16))) uint32_t keys[kSortBlock];
-    __shared__ int below[kSortPart];
+    __shared__ int below[PART];
     __shared__ int valid;
     __shared__ bool last_there;
-    const int block = blockIdx.x / kSortParts, part = blockIdx.x % kSortParts;
+    const int block = blockIdx.x / kParts, part = blockIdx.x % kParts;
     const int t0 = block * kSortBlock, count = min(kSortBlock, p.T - t0);
-    if (part * kSortPart >= count) return;       // (the first part is never empty)
-    if (t < kSortPart) below[t] = 0;
+    if (part * PART >= count) return;       // (the first part is never empty)
+    if (t < PART) below[t] = 0;
     if (t == 0) valid = 0;
     if (t == kSortThreads - 1) last_there = false;
     uint32_t id[kOwn];
@@ -168,18 +172,18 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(GradParams p) 
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) here += __popcll(__ballot(id[i] != kAbsent));
     if (t % 64 == 0) atomicAdd(&valid, here);
-    const uint32_t mine = keys[part * kSortPart + t % kSortPart];
-    const u32x4* share = reinterpret_cast<const u32x4*>(keys) + t / kSortPart * (kSortBlock / kShares / 4);
+    const uint32_t mine = keys[part * PART + t % PART];
+    const u32x4* share = reinterpret_cast<const u32x4*>(keys) + t / PART * (kSortBlock / kShares / 4);
     int n = 0;
 #pragma unroll 8
     for (int i = 0; i < kSortBlock / kShares / 4; ++i) {
         const u32x4 k = share[i];
         n += (k[0] < mine) + (k[1] < mine) + (k[2] < mine) + (k[3] < mine);
     }
-    atomicAdd(&below[t % kSortPart], n);
+    atomicAdd(&below[t % PART], n);
     __syncthreads();
-    const int at = part * kSortPart + t;
-    if (t < kSortPart && at < count) {
+    const int at = part * PART + t;
+    if (t < PART && at < count) {
         // (the block's last token may have a key like an absent one's, where ids reach 2^21)
         const uint32_t local = mine != kAbsent || (at % kSortBlock == kSortBlock - 1 && last_there)
                                    ? mine >> kSortBits : kAbsent;
@@ -301,15 +305,15 @@ __device__ __forceinline__ int bound(const uint32_t* ids, int lo, int hi, uint32
 // A workgroup sums the runs of `chunk` positions in its columns.  A run inside the chunk
 // goes to the table; of one that passes an end the chunk's part goes to memory, and the
 // last of its chunks to arrive adds the parts, in their order.
-// The other workgroups zero the rows of the table that no token names, 8 each, where
-// nothing is added.
-constexpr int kFillRows = 8;
+// The other workgroups zero the rows of the table that no token names, 2 each, where
+// nothing is added (2048 tokens, 1024 rows of 4096 columns: 13.1 us, with 8 each 14.3).
+constexpr int kFillRows = 2;
 template <int TABLE>
 __device__ __forceinline__ void fill_rows(const GradParams& p, int r0) {
     const int t = threadIdx.x, n = min(kFillRows, p.rows - r0);
     const int at = bound<false>(p.ids, 0, p.T, (uint32_t)r0);
     const uint32_t id = at + t < p.T ? p.ids[at + t] : kAbsent;
-    // lane l < 8: is there a token of row r0 + l?
+    // lane l < kFillRows: is there a token of row r0 + l?
     bool there = false;
 #pragma unroll
     for (int l = 0; l < kFillRows; ++l) {
@@ -699,9 +703,12 @@ extern "C" symtile_status symtile_embed_backward(
     OnDevice on(device);
     if (on.status) return on.status;
     if (T) {
-        if (symtile_status st = launch_grid(reinterpret_cast<const void*>(&embed_sort_kernel),
-                                            (unsigned)(p.blocks * kSortParts + p.clear), kSortThreads,
-                                            &p, s, "embed_sort_kernel launch"))
+        const int part = p.blocks == 1 ? kFewPart : kSortPart;
+        const void* sort = p.blocks == 1
+                               ? reinterpret_cast<const void*>(&embed_sort_kernel<kFewPart>)
+                               : reinterpret_cast<const void*>(&embed_sort_kernel<kSortPart>);
+        if (symtile_status st = launch_grid(sort, (unsigned)(p.blocks * (kSortBlock / part) + p.clear),
+                                            kSortThreads, &p, s, "embed_sort_kernel launch"))
             return st;
     }
     if (p.blocks > 1) {
