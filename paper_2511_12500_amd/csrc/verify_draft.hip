@@ -128,13 +128,8 @@ struct RowStat {
 };
 
 // By `lanes` (a power of two from segs on, at most a wave) threads a row, a part each.
-__device__ __forceinline__ Part part_of(const Part* parts, int segs, int lanes) {
-    const int i = threadIdx.x % lanes;
-    Part q{-kInf, 0.0f, 0xFFFFFFFFu, -kInf};
-    if (i < segs) q = parts[i];
-    return q;
-}
-__device__ __forceinline__ RowStat join(Part q, int lanes, float scale) {
+__device__ __forceinline__ RowStat join(Part q, int segs, int lanes, float scale) {
+    if ((int)threadIdx.x % lanes >= segs) q = Part{-kInf, 0.0f, 0xFFFFFFFFu, -kInf};
     float m = q.m;
     for (int o = lanes / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
     // (a segment at -inf alone has s = 0; beside a NaN sum nothing else matters)
@@ -218,6 +213,7 @@ struct Weights {
 };
 
 constexpr int kDrawVecs = 2;      // vectors of a thread in a round
+constexpr int kDrawThreads = 512; // at most, so that a thread has 256 registers
 
 // A thread's best of the race so far: ids come in ascending order, so that of equal scores
 // the first stays.
@@ -228,22 +224,38 @@ struct Race {
     int id = 0;
     u32x4 noise[kDrawVecs][kNoise];
 
-    __device__ __forceinline__ void ask(const float* of, int len, int at0) {
-        const int threads = blockDim.x;
+    // No branch, so that what was asked for before can be waited for alone: the last 4 in place
+    // of those that pass the end, and anything of the call's where there are no 4.
+    __device__ __forceinline__ void ask(const float* of, int len, int at0, const Part* any) {
+        const float* from = len >= 4 ? of : reinterpret_cast<const float*>(any);
 #pragma unroll
         for (int v = 0; v < kDrawVecs; ++v)
 #pragma unroll
-            for (int i = 0; i < kNoise; ++i) {
-                const int at = at0 + (v * threads + (int)threadIdx.x) * kVec + 4 * i;
-                noise[v][i] = u32x4{0u, 0u, 0u, 0u};
-                if (at < len) noise[v][i] = Segment<SYMTILE_F32, 1>::fetch(of, len, at);
+            for (int i = 0; i < kNoise; ++i)
+                noise[v][i] = load16(from + max(0, min(at_of(at0, v, i), len - 4)));
+    }
+    static __device__ __forceinline__ int at_of(int at0, int v, int i) {
+        return at0 + (v * (int)blockDim.x + (int)threadIdx.x) * kVec + 4 * i;
+    }
+    // The noise of the vectors that pass the end.
+    __device__ __forceinline__ void mend(int v, const float* of, int len, int at0) {
+#pragma unroll
+        for (int i = 0; i < kNoise; ++i) {
+            u32x4& n = noise[v][i];
+            const int at = at_of(at0, v, i), by = at + 4 - len;
+            if (len < 4) {
+                if (at < len) n = Segment<SYMTILE_F32, 1>::fetch(of, len, at);
+            } else if (by > 0) {
+                if (by & 1) n = u32x4{n[1], n[2], n[3], n[3]};
+                if (by & 2) n = u32x4{n[2], n[3], n[3], n[3]};
             }
+        }
     }
     // A round's elements; `out`: the id that is none of the candidates.
     template <bool LESS, bool HUGE>
     __device__ __forceinline__ void run(const u32x4 (&x)[kDrawVecs], const u32x4 (&y)[kDrawVecs],
-                                        const Weights& wp, const Weights& wq, int len, int at0,
-                                        int begin, int64_t out) {
+                                        const Weights& wp, const Weights& wq, const float* of,
+                                        int len, int at0, int begin, int64_t out) {
         const int threads = blockDim.x;
 #pragma unroll
         for (int v = 0; v < kDrawVecs; ++v) {
@@ -256,6 +268,7 @@ struct Race {
                 if constexpr (LESS) w[e] -= wq.template of<HUGE>(element<DT>(y[v], e));
             }
             if (left < kVec || (unsigned)not_this < (unsigned)kVec) {
+                mend(v, of, len, at0);
 #pragma unroll
                 for (int e = 0; e < kVec; ++e)
                     if (e >= left || e == not_this) w[e] = 0.0f;
@@ -278,7 +291,7 @@ template <int DT, bool HUGE>
 __device__ __forceinline__ void race_over(Race<DT>& race, const typename Elem<DT>::type* x,
                                           const typename Elem<DT>::type* y, const float* noise,
                                           bool less, const Weights& wp, const Weights& wq, int len,
-                                          int begin, int64_t out, bool asked) {
+                                          int begin, int64_t out, bool asked, const Part* any) {
     constexpr int kVec = Elem<DT>::kVec;
     const int threads = blockDim.x, t = threadIdx.x;
     for (int at0 = 0; at0 < len; at0 += threads * kDrawVecs * kVec) {
@@ -292,9 +305,9 @@ __device__ __forceinline__ void race_over(Race<DT>& race, const typename Elem<DT
                 if (less) yv[v] = Segment<DT, 1>::fetch(y, len, at);
             }
         }
-        if (at0 || !asked) race.ask(noise, len, at0);
-        if (less) race.template run<true, HUGE>(xv, yv, wp, wq, len, at0, begin, out);
-        else race.template run<false, HUGE>(xv, yv, wp, wq, len, at0, begin, out);
+        if (at0 || !asked) race.ask(noise, len, at0, any);
+        if (less) race.template run<true, HUGE>(xv, yv, wp, wq, noise, len, at0, begin, out);
+        else race.template run<false, HUGE>(xv, yv, wp, wq, noise, len, at0, begin, out);
     }
 }
 
@@ -332,7 +345,7 @@ __device__ __forceinline__ Best best_of_all(Best b, Shared& sh) {
 }
 
 template <int DT, int MODE>
-__global__ void __launch_bounds__(kMaxThreads) verify_draw_kernel(VerifyParams p) {
+__global__ void __launch_bounds__(kDrawThreads) verify_draw_kernel(VerifyParams p) {
     typedef typename Elem<DT>::type T;
     __shared__ Shared sh;
     const int t = threadIdx.x, threads = blockDim.x, unit = blockIdx.x;
@@ -343,21 +356,26 @@ __global__ void __launch_bounds__(kMaxThreads) verify_draw_kernel(VerifyParams p
     const float* noise = nullptr;
     Race<DT> race;
     const Part* parts = p.parts + (size_t)seq * p.rows * p.segs;
-    Part part{};
-    int r = t / p.join_lanes;
-    if (r < p.rows) part = part_of(parts + (size_t)r * p.segs, p.segs, p.join_lanes);
+    auto part_of = [&](int r) {
+        return parts[min(r, p.rows - 1) * p.segs + min(t % p.join_lanes, p.segs - 1)];
+    };
+    auto join_row = [&](const Part& part, int r) {
+        const RowStat stat = join(part, p.segs, p.join_lanes, r <= p.k ? p.scale : p.draft_scale);
+        if (r < p.rows && t % p.join_lanes == 0) sh.stat[r] = stat;
+    };
+    const int at_once = threads / p.join_lanes;
+    const Part part = part_of(t / p.join_lanes);
     float u = 0.0f;
     if constexpr (MODE != kGreedy) {
-        if (t < p.k) u = p.uniforms[((size_t)p.seq0 + seq) * p.k + t];
+        const float* uniforms = p.k ? p.uniforms + ((size_t)p.seq0 + seq) * p.k
+                                    : reinterpret_cast<const float*>(parts);
+        u = uniforms[min(t, max(p.k - 1, 0))];
         noise = p.noise + ((size_t)p.seq0 + seq) * p.ldn + begin;
-        race.ask(noise, len, 0);
+        race.ask(noise, len, 0, parts);
     }
-    while (r < p.rows) {
-        const RowStat stat = join(part, p.join_lanes, r <= p.k ? p.scale : p.draft_scale);
-        if (t % p.join_lanes == 0) sh.stat[r] = stat;
-        r += threads / p.join_lanes;
-        if (r < p.rows) part = part_of(parts + (size_t)r * p.segs, p.segs, p.join_lanes);
-    }
+    join_row(part, t / p.join_lanes);
+    for (int r0 = at_once; r0 < p.rows; r0 += at_once)
+        join_row(part_of(r0 + t / p.join_lanes), r0 + t / p.join_lanes);
     __syncthreads();
     // (needed at the end, and taken by a wave that would wait)
     auto logs = [&] {
@@ -387,8 +405,8 @@ __global__ void __launch_bounds__(kMaxThreads) verify_draw_kernel(VerifyParams p
     const T* x = row_of<DT>(p, seq, a);
     const T* y = less ? row_of<DT>(p, seq, p.k + 1 + a) : x;
     const bool huge = wp.ex.huge || wq.ex.huge;
-    if (huge) race_over<DT, true>(race, x + begin, y + begin, noise, less, wp, wq, len, begin, out, true);
-    else race_over<DT, false>(race, x + begin, y + begin, noise, less, wp, wq, len, begin, out, true);
+    if (huge) race_over<DT, true>(race, x + begin, y + begin, noise, less, wp, wq, len, begin, out, true, parts);
+    else race_over<DT, false>(race, x + begin, y + begin, noise, less, wp, wq, len, begin, out, true, parts);
     Best best = best_of_all(Best{race.score, (float)race.id, race.logit}, sh);
     logs();
     if (p.draw_segs > 1) {
@@ -412,7 +430,7 @@ __global__ void __launch_bounds__(kMaxThreads) verify_draw_kernel(VerifyParams p
     if (sh.none) {
         // no token has p > q: one is drawn from p, by this workgroup alone
         race.score = -1.0f;
-        race_over<DT, true>(race, x, x, noise - begin, false, wp, wp, p.vocab, 0, -1, false);
+        race_over<DT, true>(race, x, x, noise - begin, false, wp, wp, p.vocab, 0, -1, false, parts);
         best = best_of_all(Best{race.score, (float)race.id, race.logit}, sh);
     }
     if (t < 64) finish(p, seq, sh, id, best.score >= 0.0f ? (int64_t)best.id : -1, best.logit);
@@ -448,7 +466,7 @@ VerifyPlan verify_plan(int device, int sequences, int k, int vocab, int dtype) {
     const int per = (n + segs - 1) / segs;
     v.draw_segs = (n + per - 1) / per;
     v.draw_len = per * vec;
-    v.draw_threads = std::min(kMaxThreads, std::max(128, (per + kDrawVecs * 64 - 1) / (kDrawVecs * 64) * 64));
+    v.draw_threads = std::min(kDrawThreads, std::max(128, (per + kDrawVecs * 64 - 1) / (kDrawVecs * 64) * 64));
     v.parts = (size_t)symtile_host::kWorkspaceCounters * 4;
     v.keys = v.parts + (size_t)v.launch * rows * v.sums.segs * sizeof(Part);
     v.bytes = v.keys + (size_t)v.launch * v.draw_segs * 16;
