@@ -100,7 +100,8 @@ SHAPES = [  # sequences, drafted, vocab, scale, draft scale, pad, masked
     (1, 0, 1, 1.0, 1.0, 0, 0), (1, 1, 1, 1.0, 1.0, 0, 0), (3, 2, 7, 1.0, 1.0, 0, 0), (40, 4, 100, 0.7, 0.9, 1, 20),
     (17, 3, 1000, 1.25, 1.0, 3, 0), (5, 8, 4097, 1.0, 1.0, 0, 100), (64, 1, 2051, 1.0, 0.5, 5, 0),
     (2, 32, 777, 1.0, 1.0, 0, 0), (1, 4, 28672, 1.0, 1.0, 0, 0), (6, 5, 50001, 0.8, 0.8, 3, 2000),
-    (2, 1, 140001, 1.0, 1.0, 0, 0), (300, 1, 64, 1.0, 1.0, 0, 0), (3, 0, 32000, 1.0, 1.0, 8, 0)]
+    (2, 1, 140001, 1.0, 1.0, 0, 0), (300, 1, 64, 1.0, 1.0, 0, 0), (3, 0, 32000, 1.0, 1.0, 8, 0),
+    (9, 2, 2, 1.0, 1.0, 2, 0), (9, 3, 3, 1.0, 1.0, 0, 0), (9, 1, 5, 1.0, 1.0, 1, 1), (260, 1, 9001, 1.0, 1.0, 0, 0)]
 
 
 @pytest.mark.parametrize("mode", ["draft", "tokens", "greedy"])
@@ -192,6 +193,20 @@ def test_rows_without_a_distribution(mode, V):
     assert op.tokens[[0, 1, 2, 3], [0, 1, 2, 0]].tolist() == [-1] * 4
     if mode == "draft":
         assert op.accepted[4:].tolist() == [1, 0]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [4, 6, 1001, 1002, 1003, 8195, 50001])
+def test_tokens_at_the_end(V, dtype):
+    """All but the last four tokens masked: each of them is drawn with its own noise."""
+    S, k = 64, 1
+    x, ids, u, e, y = inputs(S, k, V, dtype, V, "tokens", short=False)
+    x[:, :V - 4] = -math.inf
+    y[:, :V - 4] = -math.inf
+    ids = V - 1 - torch.randint(0, 4, (S, k), generator=torch.Generator().manual_seed(V))
+    op = call(S, k, V, dtype, (x, ids, u, e, y), "draft", pad=V % 3)
+    drawn = op.tokens.cpu()[torch.arange(S), op.accepted.cpu()]
+    assert sorted(set(drawn.tolist())) == list(range(V - 4, V))
 
 
 @pytest.mark.parametrize("low", [-1e4, -1e10, -3e38])
