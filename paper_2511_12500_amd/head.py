@@ -278,7 +278,8 @@ class DraftVerification:
     the accepted tokens, the one that follows them, then -1), ``accepted`` (int64
     [sequences], how many were) and ``logprob`` (fp32 [sequences, drafted + 1],
     the target's log probabilities of the tokens, 0 behind them).  Calls on one
-    object must not overlap in time."""
+    object must not overlap in time; an object that is made during a capture is
+    for that graph's replays alone."""
 
     def __init__(self, sequences: int, drafted: int, vocab: int, dtype: torch.dtype,
                  scale: float = 1.0, draft_scale: float = 1.0, device: int = 0):

@@ -309,10 +309,13 @@ class GatheredOutput:
             B._check(st, "symtile_w4_all_scatter")
 
     def _workspace_mx4(self, K: int, stream: int | None) -> torch.Tensor | None:
-        """run_mx4's workspace for this K, as run_w4's."""
+        """run_mx4's workspace for this K, as run_w4's; none for a call that is captured
+        before it exists, since what a capture allocates is zero in its replays alone."""
         if K not in self.ws_mx4:
             need = B.symtile_mx4_workspace_bytes(self.heap.device, self.M, self.N_local, K)
             with launching(stream, self.heap.device):
+                if need and torch.cuda.is_current_stream_capturing():
+                    return None
                 self.ws_mx4[K] = (torch.zeros(need, dtype=torch.uint8, device=self.heap.mem.device)
                                   if need else None)
         return self.ws_mx4[K]
@@ -323,8 +326,8 @@ class GatheredOutput:
         places and counts the same arrivals as ``run``'s, in tiles of MX4_TILE_M x
         MX4_TILE_N, which this object must have been made with.  Enqueued on the
         stream, asynchronous; calls on one object must not overlap in time.  It can
-        be captured in a graph; make one eager call first so that its workspace
-        exists."""
+        be captured in a graph; without an eager call before, a captured one has no
+        workspace, and its K is not split over workgroups."""
         device = self.heap.device
         if X.device != device or weight.device != device:
             raise ValueError(f"X and the weight must be on cuda:{device}")

@@ -332,3 +332,24 @@ def test_captured_and_on_another_stream(M, K, N):
             s.synchronize()
             calls += 1
             c.check(rank, calls=calls)
+
+
+def test_captured_before_any_eager_call():
+    """A workspace that a capture allocates would be zero in its replays alone: the captured
+    call has none, and an eager one before the first replay makes its own."""
+    pkg = sym()
+    M, K, N = 64, 8192, 264
+    assert pkg.symtile_mx4_workspace_bytes(0, M, N, K) > 0
+    c = Call(M, K, N, 2, "bf16", operands(M, K, N, 5, whole=True))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.out.run_mx4(c.x, c.w, 1)
+    assert not c.out.ws_mx4
+    for calls in range(1, 5):
+        if calls % 2:
+            c.out.run_mx4(c.x, c.w, 1)
+        else:
+            graph.replay()
+        c.check(1, whole=True, calls=calls)
+    assert int(c.out.ws_mx4[K][:65536].sum()) == 0
