@@ -128,6 +128,15 @@ struct GradParams {
     uint32_t* ids;                   // [T] their ids, kAbsent behind the shard's tokens
     float* parts;                    // [chunk][2][columns]
     symtile_host::Div by_cols;
+    // of the order by digits
+    int tiles, digit_bits;
+    uint32_t *hist, *totals;         // [digit][tile] and [digit]
+    // a digit's keys and where they go; `keys` NULL: from the tokens
+    const uint32_t* keys;
+    const int* from;
+    uint32_t* keys_to;
+    int* to;
+    int shift, last;
 };
 
 // The row of the shard that a token names; kAbsent for another rank's and padding.
@@ -256,6 +265,144 @@ __global__ void __launch_bounds__(kMergeThreads) embed_merge_kernel(GradParams p
             p.ids[place[t]] = id;
         }
         if (unit0 + t >= total && unit0 + t < p.T) p.ids[unit0 + t] = kAbsent;
+    }
+}
+
+// ---- many tokens: their order digit by digit ----------------------------------------------
+// From the lowest digit of the ids to the highest, each time in the order so far: the tiles'
+// counts of every digit, their sums over the tiles before, and every key to its place.  Other
+// ranks' tokens and padding leave with the first digit.
+constexpr int kTile = 2048, kDigitThreads = 256, kDigits = 256, kDigitWaves = kDigitThreads / 64;
+constexpr int kPerLane = kTile / kDigitThreads;
+
+// Key i of the tile's wave and lane, kAbsent behind the last; positions go up with i.
+__device__ __forceinline__ int tile_place(int i) {
+    return (threadIdx.x / 64 * kPerLane + i) * 64 + threadIdx.x % 64;
+}
+__device__ __forceinline__ uint32_t tile_key(const GradParams& p, int at, int n) {
+    if (at >= n) return kAbsent;
+    return p.keys ? p.keys[at] : local_id(p, p.tokens[at]);
+}
+__device__ __forceinline__ int digit_of(const GradParams& p, uint32_t key) {
+    return (int)(key >> p.shift & ((1u << p.digit_bits) - 1u));
+}
+
+// The other workgroups zero the sums' counters, with the first digit.
+__global__ void __launch_bounds__(kDigitThreads) embed_count_kernel(GradParams p) {
+    const int t = threadIdx.x, other = (int)blockIdx.x - p.tiles;
+    if (other >= 0) {
+        for (int i = other * kDigitThreads + t; i < p.n_counters; i += p.clear * kDigitThreads)
+            p.counters[i] = 0u;
+        return;
+    }
+    __shared__ uint32_t count[kDigits];
+    const int n = p.keys ? (int)p.valid[0] : p.T, tile = blockIdx.x;
+    count[t] = 0;
+    uint32_t key[kPerLane];
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) key[i] = tile_key(p, tile * kTile + tile_place(i), n);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i)
+        if (key[i] != kAbsent) atomicAdd(&count[digit_of(p, key[i])], 1u);
+    __syncthreads();
+    p.hist[(size_t)t * p.tiles + tile] = count[t];
+}
+
+__device__ __forceinline__ uint32_t sum_below(uint32_t v, uint32_t* lds, uint32_t* total) {
+    const int t = threadIdx.x, lane = t % 64;
+    uint32_t up = v;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const uint32_t u = __shfl_up(up, o);
+        up += lane >= o ? u : 0u;
+    }
+    __syncthreads();
+    if (lane == 63) lds[t / 64] = up;
+    __syncthreads();
+    uint32_t before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kDigitWaves; ++w) {
+        before += w < t / 64 ? lds[w] : 0u;
+        all += lds[w];
+    }
+    *total = all;
+    return before + up - v;
+}
+
+// A workgroup a digit: its tiles' counts become the sums of those before.
+__global__ void __launch_bounds__(kDigitThreads) embed_scan_kernel(GradParams p) {
+    __shared__ uint32_t lds[kDigitWaves];
+    uint32_t* row = p.hist + (size_t)blockIdx.x * p.tiles;
+    uint32_t before = 0;
+    for (int i0 = 0; i0 < p.tiles; i0 += kDigitThreads) {
+        const int i = i0 + threadIdx.x;
+        uint32_t total;
+        const uint32_t v = i < p.tiles ? row[i] : 0u, sum = sum_below(v, lds, &total);
+        if (i < p.tiles) row[i] = before + sum;
+        before += total;
+    }
+    if (threadIdx.x == 0) p.totals[blockIdx.x] = before;
+}
+
+// Places: the digits below, the tiles before, the waves before, and in a wave the keys of the
+// same digit before, 64 at a time by a comparison of all lanes' bits.
+__global__ void __launch_bounds__(kDigitThreads) embed_place_kernel(GradParams p) {
+    __shared__ uint32_t lds[kDigitWaves];
+    __shared__ volatile uint32_t seen[kDigitWaves][kDigits];
+    __shared__ uint32_t first[kDigitWaves][kDigits];
+    const int t = threadIdx.x, lane = t % 64, wave = t / 64, tile = blockIdx.x;
+    const int n = p.keys ? (int)p.valid[0] : p.T;
+    uint32_t key[kPerLane], rank[kPerLane];
+    int order[kPerLane];
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+        const int at = tile * kTile + tile_place(i);
+        key[i] = tile_key(p, at, n);
+        order[i] = p.keys && at < n ? p.from[at] : at;
+    }
+    const uint32_t here = p.hist[(size_t)t * p.tiles + tile];
+    uint32_t total;
+    const uint32_t below = sum_below(p.totals[t], lds, &total);
+#pragma unroll
+    for (int w = 0; w < kDigitWaves; ++w) seen[w][t] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+        const bool there = key[i] != kAbsent;
+        const int d = digit_of(p, key[i]);
+        uint64_t same = __ballot(there);
+        for (int b = 0; b < p.digit_bits; ++b) {
+            const uint64_t set = __ballot(d >> b & 1);
+            same &= d >> b & 1 ? set : ~set;
+        }
+        // (a wave's LDS accesses happen in their order)
+        const uint32_t so_far = seen[wave][d];
+        rank[i] = so_far + __popcll(same & ((1ull << lane) - 1));
+        if (there && lane == __builtin_ctzll(same)) seen[wave][d] = so_far + __popcll(same);
+    }
+    __syncthreads();
+    uint32_t at = below + here;
+#pragma unroll
+    for (int w = 0; w < kDigitWaves; ++w) {
+        first[w][t] = at;
+        at += seen[w][t];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+        if (key[i] == kAbsent) continue;
+        const uint32_t to = first[wave][digit_of(p, key[i])] + rank[i];
+        p.keys_to[to] = key[i];
+        p.to[to] = order[i];
+    }
+    if (!p.keys && tile == 0 && t == 0) p.valid[0] = total;
+    if (p.last) {
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) {
+            const int behind = tile * kTile + tile_place(i);
+            if (behind >= (int)total && behind < p.T) p.ids[behind] = kAbsent;
+        }
     }
 }
 
@@ -513,8 +660,13 @@ GradPlan grad_plan(int T, int D, size_t esize) {
     return g;
 }
 
+// By digits from here on: counting and merging take 18 us for 32768 tokens and grow with the
+// square of their number.
+constexpr int kByDigits = 32768;
+
 struct GradWorkspace {
     size_t valid, counters, sorted, order, ids, parts, bytes;
+    size_t keys, hist;               // of the order by digits, in place of `sorted`
 };
 // For rows of any of the types.
 GradWorkspace grad_workspace(int T, int D) {
@@ -528,7 +680,10 @@ GradWorkspace grad_workspace(int T, int D) {
     }
     w.counters = up(blocks * 4);
     w.sorted = w.counters + up(counters * 4);
-    w.order = w.sorted + (blocks > 1 ? blocks * kSortBlock * 4 : 0);
+    w.keys = w.sorted + up((size_t)T * 4);
+    w.hist = w.keys + up((size_t)T * 4);
+    w.order = T > kByDigits ? w.hist + up((size_t)kDigits * (ceil_div(T, kTile) + 1) * 4)
+                            : w.sorted + (blocks > 1 ? blocks * kSortBlock * 4 : 0);
     w.ids = w.order + up((size_t)T * 4);
     w.parts = w.ids + up((size_t)T * 4);
     w.bytes = w.parts + chunks * 2 * D * 4;
@@ -567,6 +722,39 @@ symtile_status launch_grid(const void* kernel, unsigned wgs, unsigned threads, v
                                    static_cast<hipStream_t>(s));
     if (e == hipSuccess) e = hipGetLastError();
     return e == hipSuccess ? SYMTILE_OK : symtile_host::hip_fail(e, what);
+}
+
+symtile_status order_by_digits(GradParams p, const GradWorkspace& w, char* base, symtile_stream s) {
+    int bits = 1;
+    while (bits < 32 && (p.rows - 1) >> bits) ++bits;
+    const int digits = ceil_div(bits, 8);
+    p.digit_bits = ceil_div(bits, digits);
+    p.tiles = ceil_div(p.T, kTile);
+    p.hist = reinterpret_cast<uint32_t*>(base + w.hist);
+    p.totals = p.hist + (size_t)kDigits * p.tiles;
+    uint32_t* const keys[2] = {p.ids, reinterpret_cast<uint32_t*>(base + w.keys)};
+    int* const order[2] = {p.order, reinterpret_cast<int*>(base + w.sorted)};
+    for (int d = 0; d < digits; ++d) {
+        const int to = (digits - 1 - d) % 2;         // the last one into ids and order
+        p.keys = d ? keys[1 - to] : nullptr;
+        p.from = d ? order[1 - to] : nullptr;
+        p.keys_to = keys[to];
+        p.to = order[to];
+        p.shift = d * p.digit_bits;
+        p.last = d == digits - 1;
+        const unsigned clear = d ? 0u : (unsigned)p.clear;
+        symtile_status st = launch_grid(reinterpret_cast<const void*>(&embed_count_kernel),
+                                        (unsigned)p.tiles + clear, kDigitThreads, &p, s,
+                                        "embed_count_kernel launch");
+        if (!st)
+            st = launch_grid(reinterpret_cast<const void*>(&embed_scan_kernel), kDigits, kDigitThreads,
+                             &p, s, "embed_scan_kernel launch");
+        if (!st)
+            st = launch_grid(reinterpret_cast<const void*>(&embed_place_kernel), (unsigned)p.tiles,
+                             kDigitThreads, &p, s, "embed_place_kernel launch");
+        if (st) return st;
+    }
+    return SYMTILE_OK;
 }
 
 const void* sum_kernel_of(int dtype, int table, bool add) {
@@ -710,7 +898,9 @@ extern "C" symtile_status symtile_embed_backward(
     }
     OnDevice on(device);
     if (on.status) return on.status;
-    if (T) {
+    if (T > kByDigits) {
+        if (symtile_status st = order_by_digits(p, w, static_cast<char*>(workspace), s)) return st;
+    } else if (T) {
         const int part = p.blocks == 1 ? kFewPart : kSortPart;
         const void* sort = p.blocks == 1
                                ? reinterpret_cast<const void*>(&embed_sort_kernel<kFewPart>)
@@ -719,7 +909,7 @@ extern "C" symtile_status symtile_embed_backward(
                                             kSortThreads, &p, s, "embed_sort_kernel launch"))
             return st;
     }
-    if (p.blocks > 1) {
+    if (p.blocks > 1 && T <= kByDigits) {
         if (symtile_status st = launch_grid(reinterpret_cast<const void*>(&embed_merge_kernel),
                                             (unsigned)(p.blocks * (kSortBlock / 64)), kMergeThreads, &p,
                                             s, "embed_merge_kernel launch"))
