@@ -271,7 +271,8 @@ __global__ void __launch_bounds__(kMergeThreads) embed_merge_kernel(GradParams p
 // ---- many tokens: their order digit by digit ----------------------------------------------
 // From the lowest digit of the ids to the highest, each time in the order so far: the tiles'
 // counts of every digit, their sums over the tiles before, and every key to its place.  Other
-// ranks' tokens and padding leave with the first digit.
+// ranks' tokens and padding leave with the first digit.  Six launches, or nine from 65537 rows
+// on, bound it up to some 100000 tokens (1048576 tokens of 512 columns, with their sums, 369 us).
 constexpr int kTile = 2048, kDigitThreads = 256, kDigits = 256, kDigitWaves = kDigitThreads / 64;
 constexpr int kPerLane = kTile / kDigitThreads;
 
@@ -660,9 +661,10 @@ GradPlan grad_plan(int T, int D, size_t esize) {
     return g;
 }
 
-// By digits from here on: counting and merging take 18 us for 32768 tokens and grow with the
-// square of their number.
-constexpr int kByDigits = 32768;
+// Above it by digits, six launches or more, where counting and merging grow with the square of
+// the tokens (of 64 columns, added to 28672 rows, whole calls, us, by digits / by merging: 32768
+// 42 / 26, 65536 50 / 50, 131072 52 / 96).
+constexpr int kByDigits = 65536;
 
 struct GradWorkspace {
     size_t valid, counters, sorted, order, ids, parts, bytes;

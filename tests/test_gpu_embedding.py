@@ -147,8 +147,8 @@ GRADS = [  # tokens, D, rows, first, scale, share of one token
     (33, 2048, 3, 0, 1.0, 0.5), (100, 2056, 1000, 50, 1.5, 0.0), (1000, 136, 300, 300, 45.25, 0.3),
     (2048, 520, 64, 0, 1.0, 0.0), (2049, 64, 100, 10, 1.0, 0.6), (5000, 32, 2000, 0, 1.0, 0.1),
     (9000, 16, 3, 1, 0.1, 0.97), (20000, 8, 30000, 0, 1.0, 0.0), (70000, 8, 40, 20, 1.0, 0.2),
-    (32768, 8, 500, 0, 1.0, 0.0), (32769, 16, 256, 0, 1.0, 0.3), (40000, 8, 1, 1, 1.0, 0.5), (70000, 8, 100000, 5, 0.5, 0.1),
-    (100001, 8, 30000, 0, 1.0, 0.01), (35000, 24, 2000000, 9, 1.0, 0.0)]
+    (65536, 8, 500, 0, 1.0, 0.0), (65537, 16, 256, 0, 1.0, 0.3), (66000, 8, 1, 1, 1.0, 0.5), (70000, 8, 100000, 5, 0.5, 0.1),
+    (100001, 8, 30000, 0, 1.0, 0.01), (67000, 24, 2000000, 9, 1.0, 0.0)]
 
 
 @pytest.mark.parametrize("types", [("bf16", "f32"), ("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("f32", "bf16")],
@@ -230,7 +230,7 @@ def test_the_longest_table():
 
 def test_gradient_captured_and_on_another_stream():
     """Replays on new tokens, among eager calls of the same object."""
-    for T in (500, 5000, 40000):
+    for T in (500, 5000, 66000):
         D, rows = 128, 40
         g = torch.Generator().manual_seed(T)
         op = sym().EmbeddingGrad(T, D, torch.float32)
