@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(kMergeThreads) embed_merge_kernel(GradParams p
 // From the lowest digit of the ids to the highest, each time in the order so far: the tiles'
 // counts of every digit, their sums over the tiles before, and every key to its place.  Other
 // ranks' tokens and padding leave with the first digit.  Six launches, or nine from 65537 rows
-// on, bound it up to some 100000 tokens (1048576 tokens of 512 columns, with their sums, 369 us).
+// on, bound it up to some 100000 tokens (1048576 tokens of 512 columns, with their sums, 316 us).
 constexpr int kTile = 2048, kDigitThreads = 256, kDigits = 256, kDigitWaves = kDigitThreads / 64;
 constexpr int kPerLane = kTile / kDigitThreads;
 
@@ -408,7 +408,7 @@ __global__ void __launch_bounds__(kDigitThreads) embed_place_kernel(GradParams p
 }
 
 // ---- sums ------------------------------------------------------------------------------------
-constexpr int kMaxChunk = 32, kSumThreads = 64;
+constexpr int kMaxChunk = 128, kSumThreads = 64;
 
 // N values of a row of the table, at most 16 bytes of them together: rows start at
 // multiples of that.
@@ -513,10 +513,10 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(GradParams p) {
     }
     const int chunk = p.by_cols(blockIdx.x), cb = blockIdx.x - chunk * p.col_blocks;
     const int begin = chunk * p.chunk, most = min(p.chunk, p.T - begin);
-    if (t < most + 2) {
-        const int at = begin - 1 + t;
-        ids[t] = at >= 0 && at < p.T ? p.ids[at] : kAbsent;
-        if (t < most) order[t] = p.order[begin + t];
+    for (int i = t; i < most + 2; i += kSumThreads) {
+        const int at = begin - 1 + i;
+        ids[i] = at >= 0 && at < p.T ? p.ids[at] : kAbsent;
+        if (i < most) order[i] = p.order[begin + i];
     }
     // the ids on both sides of the chunk, for runs that pass its ends
     const uint32_t back = begin - 1 - t >= 0 ? p.ids[begin - 1 - t] : kAbsent;
@@ -647,16 +647,18 @@ size_t up(size_t n) { return (n + 255) / 256 * 256; }
 bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
 
 // How the sums are laid out over workgroups: one wave each, columns by 16 bytes a lane (32768
-// tokens of 4096 columns 149 us, four waves 156), and chunks of 32 positions (16384 tokens of
-// 4096 columns 157 us, 179 with chunks of 8), of 8 where that leaves the GPU with few
-// workgroups; a chunk's rows are asked for 8 at a time.
+// tokens of 4096 columns 149 us, four waves 156), and the largest chunks of 8, 32 or 128
+// positions that leave 4096 workgroups, since the parts of runs that pass their ends go through
+// memory (16384 tokens of 4096 columns: 8 179 us, 32 157; 131072: 32 408, 64 381, 128 369); a
+// chunk's rows are asked for 8 at a time.
 struct GradPlan {
     int col_blocks, chunk, chunks;
 };
 GradPlan grad_plan(int T, int D, size_t esize) {
     GradPlan g{};
     g.col_blocks = ceil_div((int)((size_t)D * esize / 16), kSumThreads);
-    g.chunk = (size_t)ceil_div(T, kMaxChunk) * g.col_blocks < 4096 ? 8 : kMaxChunk;
+    const size_t positions = (size_t)T * g.col_blocks;
+    g.chunk = positions < 4096 * 32 ? 8 : positions < 4096 * kMaxChunk ? 32 : kMaxChunk;
     g.chunks = ceil_div(T, g.chunk);
     return g;
 }

@@ -148,7 +148,8 @@ GRADS = [  # tokens, D, rows, first, scale, share of one token
     (2048, 520, 64, 0, 1.0, 0.0), (2049, 64, 100, 10, 1.0, 0.6), (5000, 32, 2000, 0, 1.0, 0.1),
     (9000, 16, 3, 1, 0.1, 0.97), (20000, 8, 30000, 0, 1.0, 0.0), (70000, 8, 40, 20, 1.0, 0.2),
     (65536, 8, 500, 0, 1.0, 0.0), (65537, 16, 256, 0, 1.0, 0.3), (66000, 8, 1, 1, 1.0, 0.5), (70000, 8, 100000, 5, 0.5, 0.1),
-    (100001, 8, 30000, 0, 1.0, 0.01), (67000, 24, 2000000, 9, 1.0, 0.0)]
+    (100001, 8, 30000, 0, 1.0, 0.01), (67000, 24, 2000000, 9, 1.0, 0.0),
+    (600000, 8, 3000, 0, 1.0, 0.2)]
 
 
 @pytest.mark.parametrize("types", [("bf16", "f32"), ("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("f32", "bf16")],
