@@ -308,9 +308,10 @@ __device__ __forceinline__ void meet() {
 // PFLOP/s; without its loads 390, without its stores 447.  Power bounds it: matrix units that
 // are busy all the time, from registers alone, run at 1.35 to 1.4 GHz on random data (343 us for
 // as many instructions; 229 at full clock), and here they are busy for half of the cycles at 1.8
-// to 1.9 GHz.  So hiding more did not help: one workgroup a CU that goes through tiles with the
-// next one's loads ahead of the stores took 484 us where this took 484, and tiles of 256 x 128,
-// which move more, 644.  Into 8 slots, 4096 x 8192 x 3584, 102 us: 59 to the end of K, 235 MB of
+// to 1.9 GHz.  So hiding more did not help: lines asked for into L2 three stages ahead, by the CUs
+// that share them, took 474 us where this took 475 (on zeros 361 and 417), one workgroup a CU
+// that goes through tiles with the next one's loads ahead of the stores 484 where this took 484,
+// and tiles of 256 x 128, which move more, 644.  Into 8 slots, 4096 x 8192 x 3584, 102 us: 59 to the end of K, 235 MB of
 // stores behind it, since all tiles run at once.
 //   64 x 64, 4 stages, K in parts: 64 x 8192 x 3584 into 8 slots 10.0 us, 16 MB of weights and X
 // read and 7.4 MB written; latency: loads, parts to memory and back, stores.
