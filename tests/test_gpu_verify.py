@@ -101,7 +101,8 @@ SHAPES = [  # sequences, drafted, vocab, scale, draft scale, pad, masked
     (17, 3, 1000, 1.25, 1.0, 3, 0), (5, 8, 4097, 1.0, 1.0, 0, 100), (64, 1, 2051, 1.0, 0.5, 5, 0),
     (2, 32, 777, 1.0, 1.0, 0, 0), (1, 4, 28672, 1.0, 1.0, 0, 0), (6, 5, 50001, 0.8, 0.8, 3, 2000),
     (2, 1, 140001, 1.0, 1.0, 0, 0), (300, 1, 64, 1.0, 1.0, 0, 0), (3, 0, 32000, 1.0, 1.0, 8, 0),
-    (9, 2, 2, 1.0, 1.0, 2, 0), (9, 3, 3, 1.0, 1.0, 0, 0), (9, 1, 5, 1.0, 1.0, 1, 1), (260, 1, 9001, 1.0, 1.0, 0, 0)]
+    (9, 2, 2, 1.0, 1.0, 2, 0), (9, 3, 3, 1.0, 1.0, 0, 0), (9, 1, 5, 1.0, 1.0, 1, 1), (260, 1, 9001, 1.0, 1.0, 0, 0),
+    (2, 2, 2097152, 1.0, 1.0, 0, 0), (3, 1, 2097147, 0.9, 1.0, 1, 1000)]
 
 
 @pytest.mark.parametrize("mode", ["draft", "tokens", "greedy"])
