@@ -254,16 +254,16 @@ struct Race {
             }
         }
     }
-    // A round's elements; `out`: the id that is none of the candidates.
+    // A round's elements; `out`: the id that is none of the candidates (-1: all are).
     template <bool LESS, bool HUGE>
     __device__ __forceinline__ void run(const u32x4 (&x)[kDrawVecs], const u32x4 (&y)[kDrawVecs],
                                         const Weights& wp, const Weights& wq, const float* of,
-                                        int len, int at0, int begin, int64_t out) {
+                                        int len, int at0, int begin, int out) {
         const int threads = blockDim.x;
 #pragma unroll
         for (int v = 0; v < kDrawVecs; ++v) {
             const int at = at0 + (v * threads + (int)threadIdx.x) * kVec;
-            const int left = len - at, not_this = (int)(out - begin - at);
+            const int left = len - at, not_this = out - begin - at;
             float w[kVec];
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
@@ -294,7 +294,7 @@ template <int DT, bool HUGE>
 __device__ __forceinline__ void race_over(Race<DT>& race, const typename Elem<DT>::type* x,
                                           const typename Elem<DT>::type* y, const float* noise,
                                           bool less, const Weights& wp, const Weights& wq, int len,
-                                          int begin, int64_t out, bool asked, const Part* any) {
+                                          int begin, int out, bool asked, const Part* any) {
     constexpr int kVec = Elem<DT>::kVec;
     const int threads = blockDim.x, t = threadIdx.x;
     for (int at0 = 0; at0 < len; at0 += threads * kDrawVecs * kVec) {
@@ -407,7 +407,9 @@ __global__ void __launch_bounds__(kDrawThreads) verify_draw_kernel(VerifyParams 
     }
     // a position with a drafted token, and the draft's own distribution
     const bool less = MODE == kDraft && sh.drafted && sh.stat[p.k + 1 + a].good();
-    const int64_t out = MODE == kTokens && sh.drafted ? p.ids[((size_t)p.seq0 + seq) * p.k + a] : -1;
+    // the drafted token is none of the candidates, where it is one of the vocabulary
+    const int64_t drafted = MODE == kTokens && sh.drafted ? p.ids[((size_t)p.seq0 + seq) * p.k + a] : -1;
+    const int out = drafted < p.vocab ? (int)drafted : -1;
     const Weights wp(sh.stat[a], p.scale);
     const Weights wq(less ? sh.stat[p.k + 1 + a] : sh.stat[a], less ? p.draft_scale : p.scale);
     const T* x = row_of<DT>(p, seq, a);
