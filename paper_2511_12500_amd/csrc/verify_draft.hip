@@ -203,12 +203,15 @@ __device__ __forceinline__ void finish(const VerifyParams& p, int seq, const Sha
     if (i == 0) p.accepted[at] = a;
 }
 
-// The exponentials of a row's elements, over their sum.
+// The exponentials of a row's elements, over their sum: with the exponent's shift in `inv`, or,
+// where they are taken of differences, whose shift is 0, without (`huge`: of this row or of the
+// other one, since both are taken alike).
 struct Weights {
     Exponent ex;
     float inv;
     __device__ __forceinline__ Weights(const RowStat& r, float scale)
         : ex(r.m, scale), inv(r.inv) {}
+    __device__ __forceinline__ void of_differences(const RowStat& r) { inv = 1.0f / (float)r.s; }
     template <bool HUGE>
     __device__ __forceinline__ float of(float x) const {
         return exp2_fast(ex.y<HUGE>(x)) * inv;
@@ -410,13 +413,18 @@ __global__ void __launch_bounds__(kDrawThreads) verify_draw_kernel(VerifyParams 
     // the drafted token is none of the candidates, where it is one of the vocabulary
     const int64_t drafted = MODE == kTokens && sh.drafted ? p.ids[((size_t)p.seq0 + seq) * p.k + a] : -1;
     const int out = drafted < p.vocab ? (int)drafted : -1;
-    const Weights wp(sh.stat[a], p.scale);
-    const Weights wq(less ? sh.stat[p.k + 1 + a] : sh.stat[a], less ? p.draft_scale : p.scale);
+    const RowStat &of_p = sh.stat[a], &of_q = less ? sh.stat[p.k + 1 + a] : of_p;
+    Weights wp(of_p, p.scale), wq(of_q, less ? p.draft_scale : p.scale);
     const T* x = row_of<DT>(p, seq, a);
     const T* y = less ? row_of<DT>(p, seq, p.k + 1 + a) : x;
     const bool huge = wp.ex.huge || wq.ex.huge;
-    if (huge) race_over<DT, true>(race, x + begin, y + begin, noise, less, wp, wq, len, begin, out, true, parts);
-    else race_over<DT, false>(race, x + begin, y + begin, noise, less, wp, wq, len, begin, out, true, parts);
+    if (huge) {
+        wp.of_differences(of_p);
+        wq.of_differences(of_q);
+        race_over<DT, true>(race, x + begin, y + begin, noise, less, wp, wq, len, begin, out, true, parts);
+    } else {
+        race_over<DT, false>(race, x + begin, y + begin, noise, less, wp, wq, len, begin, out, true, parts);
+    }
     Best best = best_of_all(Best{race.score, (float)race.id, race.logit}, sh);
     logs();
     if (p.draw_segs > 1) {

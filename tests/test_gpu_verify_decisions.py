@@ -1,6 +1,8 @@
 """GPU tests of the verification of drafted tokens where a decision or a draw hangs on one
 number: drafted ids outside the vocabulary, rows whose largest logits are far apart, logits
 whose difference is no fp32 number, residuals that leave nothing."""
+import math
+
 import pytest
 import torch
 
@@ -33,3 +35,24 @@ def test_drafted_ids_far_outside_the_vocabulary(V, dtype):
     op = call(S, k, V, dtype, (x.view(-1, V).to(TD[dtype]), ids, u, e, None), "tokens", least=S)
     assert op.accepted.tolist() == [0] * S
     assert op.tokens[:, 0].cpu().tolist() == v.tolist()
+
+
+@pytest.mark.parametrize("V", [3, 28672])
+@pytest.mark.parametrize("at", [(2476475.5, 3000000.0), (3000000.0, 1913162.75)], ids=["target_below", "draft_below"])
+def test_rows_on_both_sides_of_the_exponents_forms(at, V):
+    """Exponentials are taken of rounded products up to a size of the largest logit and of
+    differences beyond it.  With one row on each side p - q has the same scale for both: token
+    1, with p = 0.404 and q = 0.419, has no residual, though its noise is the smallest."""
+    S, k = 2, 1
+    tokens = [0, V // 2, V - 1]
+    x = torch.full((S, k + 1, V), -math.inf)
+    y = torch.full((S, k, V), -math.inf)
+    x[:, :, tokens] = at[0] + torch.tensor([0.0, 0.0, -0.75])
+    y[:, :, tokens] = at[1] + torch.tensor([-0.25, 0.0, -0.5])
+    ids = torch.full((S, k), tokens[1])
+    u = torch.full((S, k), 0.9999)
+    e = torch.ones((S, V))
+    e[:, tokens[1]] = 0.01
+    op = call(S, k, V, "f32", (x.view(-1, V), ids, u, e, y.view(-1, V)), "draft", least=S)
+    assert op.accepted.tolist() == [0] * S
+    assert op.tokens[:, 0].tolist() == [0] * S
