@@ -173,7 +173,7 @@ __device__ __forceinline__ void decide(const VerifyParams& p, int64_t id, float 
         double x = 1.0;
         if (at < p.k && (MODE == kDraft || lane < 32)) {
             const RowStat& a = sh.stat[draft ? p.k + 1 + at : at];
-            x = a.good() ? exp((double)(a.drafted - a.m) * (double)(draft ? p.draft_scale : p.scale)) / a.s
+            x = a.good() ? exp(((double)a.drafted - a.m) * (double)(draft ? p.draft_scale : p.scale)) / a.s
                          : (double)kInf;
         }
         const double q = __shfl(x, at + 32);
@@ -199,7 +199,7 @@ __device__ __forceinline__ void finish(const VerifyParams& p, int seq, const Sha
     else id = i == a ? token : -1;
     p.tokens[at * (p.k + 1) + i] = id;
     p.logprob[at * (p.k + 1) + i] =
-        id >= 0 ? (float)((double)(x - sh.stat[i].m) * (double)p.scale - sh.log_s[i]) : 0.0f;
+        id >= 0 ? (float)(((double)x - sh.stat[i].m) * (double)p.scale - sh.log_s[i]) : 0.0f;
     if (i == 0) p.accepted[at] = a;
 }
 

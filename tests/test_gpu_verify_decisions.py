@@ -3,10 +3,11 @@ number: drafted ids outside the vocabulary, rows whose largest logits are far ap
 whose difference is no fp32 number, residuals that leave nothing."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
-from tests.gpu_util import require_gpu
+from tests.gpu_util import require_gpu, sym
 from tests.test_gpu_verify import TD, call
 
 pytestmark = pytest.mark.gpu
@@ -56,3 +57,42 @@ def test_rows_on_both_sides_of_the_exponents_forms(at, V):
     op = call(S, k, V, "f32", (x.view(-1, V), ids, u, e, y.view(-1, V)), "draft", least=S)
     assert op.accepted.tolist() == [0] * S
     assert op.tokens[:, 0].tolist() == [0] * S
+
+
+@pytest.mark.parametrize("mode", ["draft", "tokens"])
+def test_decisions_are_made_in_64_bits(mode):
+    """Two logits whose difference is no fp32 number, and a u between p (or p / q) as it is and
+    as the rounded difference would have it.  The largest logit's probability is 1 in fp32, the
+    sum that the decision takes."""
+    S, V, scale = 256, 2, np.float32(0.05)
+    g = np.random.default_rng(5)
+    m = g.uniform(500.0, 1000.0, S).astype(np.float32)
+    d = (-g.uniform(1e-3, 500.0, S)).astype(np.float32)
+    exact = np.exp((d.astype(np.float64) - m.astype(np.float64)) * np.float64(scale))
+    rounded = np.exp((d - m).astype(np.float64) * np.float64(scale))
+    x = torch.zeros((S, 2, V))
+    y = torch.zeros((S, 1, V))
+    if mode == "tokens":
+        x[:, 0, 0], x[:, 0, 1] = torch.from_numpy(m), torch.from_numpy(d)
+        border, other = exact, rounded
+    else:
+        # p of an exact difference, a little below q
+        t = np.floor((d.astype(np.float64) - m) * 16) / 16 - 2
+        p = np.exp(t * np.float64(scale))
+        x[:, 0, 1] = torch.from_numpy(t.astype(np.float32))
+        y[:, 0, 0], y[:, 0, 1] = torch.from_numpy(m), torch.from_numpy(d)
+        border, other = p / exact, p / rounded
+    u = ((border + other) / 2).astype(np.float32)
+    want = u.astype(np.float64) < border
+    tells = (u.astype(np.float64) < other) != want
+    # (half of a difference's last place, some 0.00003, times the scale is 25 times u's; where u
+    # comes next to the border itself the device's exponential and numpy's may differ)
+    tells &= np.abs(u.astype(np.float64) / border - 1) > 1e-9
+    assert tells.sum() > S // 2 and 0 < want[tells].sum() < tells.sum()
+    ids = torch.ones((S, 1), dtype=torch.int64)
+    op = sym().DraftVerification(S, 1, V, torch.float32, float(scale), float(scale))
+    op.run(x.view(-1, V).cuda(), ids.cuda(), torch.from_numpy(u)[:, None].cuda(),
+           torch.ones((S, V), device="cuda"), y.view(-1, V).cuda() if mode == "draft" else None)
+    torch.cuda.synchronize()
+    got = op.accepted.cpu().numpy() == 1
+    assert (got == want)[tells].all(), int((got != want)[tells].sum())
