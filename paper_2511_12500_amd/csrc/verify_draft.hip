@@ -218,6 +218,12 @@ struct Weights {
     }
 };
 
+// p - q of two rounded products.
+__device__ __forceinline__ float difference(float p, float q) {
+#pragma clang fp contract(off)
+    return p - q;
+}
+
 constexpr int kDrawVecs = 2;      // vectors of a thread in a round
 constexpr int kDrawThreads = 512; // at most, so that a thread has 256 registers
 
@@ -271,7 +277,9 @@ struct Race {
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
                 w[e] = wp.template of<HUGE>(element<DT>(x[v], e));
-                if constexpr (LESS) w[e] -= wq.template of<HUGE>(element<DT>(y[v], e));
+                // (q rounded as p was, not one operation with the difference: of equal
+                // distributions nothing may be left)
+                if constexpr (LESS) w[e] = difference(w[e], wq.template of<HUGE>(element<DT>(y[v], e)));
             }
             if (left < kVec || (unsigned)not_this < (unsigned)kVec) {
                 mend(v, of, len, at0);

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from tests.gpu_util import require_gpu, sym
-from tests.test_gpu_verify import TD, call
+from tests.test_gpu_verify import TD, call, inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -96,3 +96,35 @@ def test_decisions_are_made_in_64_bits(mode):
     torch.cuda.synchronize()
     got = op.accepted.cpu().numpy() == 1
     assert (got == want)[tells].all(), int((got != want)[tells].sum())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("S,V", [(1, 28672), (4, 50001), (2, 2097147)])
+def test_nothing_of_the_residual_is_left(S, V, dtype):
+    """Where the draft is the target the token is drawn from p, over the whole of a row that
+    several workgroups take; without the draft's logits where the drafted token is the only one."""
+    k = 2
+    x, _, _, e, _ = inputs(S, k, V, dtype, V, short=False)
+    y = x.view(S, k + 1, V)[:, :k].reshape(-1, V)
+    ids = torch.randint(0, V, (S, k), generator=torch.Generator().manual_seed(V))
+    u = torch.full((S, k), 2.0)
+    op = call(S, k, V, dtype, (x, ids, u, e, y), "draft", least=0)
+    assert op.accepted.tolist() == [0] * S
+    lp = torch.log_softmax(x.view(S, k + 1, V)[:, 0].double(), 1)
+    score, order = (lp - e.double().log()).sort(1, descending=True)
+    assert bool((score[:, 0] - score[:, 1] > 1e-4).all())
+    assert op.tokens[:, 0].cpu().tolist() == order[:, 0].tolist()
+    alone = torch.full((S * (k + 1), V), -math.inf)
+    alone.view(S, k + 1, V)[torch.arange(S), :, ids[:, 0]] = 3.0
+    op = call(S, k, V, dtype, (alone.to(TD[dtype]), ids, u, e, None), "tokens", least=0)
+    assert op.accepted.tolist() == [0] * S
+    assert op.tokens[:, 0].cpu().tolist() == ids[:, 0].tolist()
+
+
+@pytest.mark.parametrize("mode", ["draft", "tokens", "greedy"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_drafts_over_rows_in_many_segments(dtype, mode):
+    S, k, V = 3, 2, 140001
+    t = inputs(S, k, V, dtype, 8, mode, short=False)
+    assert bool((t[1] >= 0).all())
+    call(S, k, V, dtype, t, mode)
