@@ -725,8 +725,10 @@ symtile_status symtile_mx4_all_scatter(symtile_heap* h, const uint8_t* x, const 
 /* Bytes of the workspace of a symtile_verify_draft call on `device` with these sizes:
  * 16-byte aligned device memory that must be zero before the first call that uses it;
  * every call leaves its counters, its first 64 KiB, zero again, so calls of other sizes
- * and of the other operators may follow.  Calls that share a workspace must not overlap
- * in time.  EINVAL for what the call refuses. */
+ * and of symtile_token_logprobs, symtile_distill_topk, symtile_w4_all_scatter,
+ * symtile_mx4_all_scatter and symtile_embed_backward may follow (not
+ * symtile_gemm_all_scatter's with split_k > 1, whose counters are of another size).  Calls
+ * that share a workspace must not overlap in time.  EINVAL for what the call refuses. */
 symtile_status symtile_verify_workspace_bytes(int device, int sequences, int drafted, int vocab,
                                               int dtype, size_t* bytes);
 
@@ -805,8 +807,10 @@ symtile_status symtile_embed_all_scatter(symtile_heap* h, const int64_t* tokens,
                                          symtile_stream s);
 
 /* Bytes of the workspace of a symtile_embed_backward call on `device` for T tokens of D
- * columns: 16-byte aligned device memory of any contents.  Calls that share a workspace
- * must not overlap in time.  EINVAL for what the call refuses. */
+ * columns: 16-byte aligned device memory of any contents.  Its first 64 KiB, where other
+ * operators' calls keep their counters, are left as they are, so a workspace may be shared
+ * with them (see symtile_verify_workspace_bytes).  Calls that share one must not overlap in
+ * time.  EINVAL for what the call refuses. */
 symtile_status symtile_embed_workspace_bytes(int device, int T, int D, size_t* bytes);
 
 /* The gradient of a table's shard: for every row v of `rows`

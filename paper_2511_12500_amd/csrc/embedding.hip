@@ -672,7 +672,8 @@ struct GradWorkspace {
     size_t valid, counters, sorted, order, ids, parts, bytes;
     size_t keys, hist;               // of the order by digits, in place of `sorted`
 };
-// For rows of any of the types.
+// For rows of any of the types.  Behind the counters that other operators leave at zero for
+// each other.
 GradWorkspace grad_workspace(int T, int D) {
     GradWorkspace w{};
     const size_t blocks = (size_t)ceil_div(T, kSortBlock);
@@ -682,7 +683,8 @@ GradWorkspace grad_workspace(int T, int D) {
         counters = std::max(counters, (size_t)g.chunks * g.col_blocks);
         chunks = std::max(chunks, (size_t)g.chunks);
     }
-    w.counters = up(blocks * 4);
+    w.valid = (size_t)symtile_host::kWorkspaceCounters * 4;
+    w.counters = w.valid + up(blocks * 4);
     w.sorted = w.counters + up(counters * 4);
     w.keys = w.sorted + up((size_t)T * 4);
     w.hist = w.keys + up((size_t)T * 4);
@@ -893,7 +895,7 @@ extern "C" symtile_status symtile_embed_backward(
         p.n_counters = g.chunks * g.col_blocks;
         p.clear = std::min(64, ceil_div(p.n_counters, kSortThreads));
         char* base = static_cast<char*>(workspace);
-        p.valid = reinterpret_cast<uint32_t*>(base);
+        p.valid = reinterpret_cast<uint32_t*>(base + w.valid);
         p.counters = reinterpret_cast<uint32_t*>(base + w.counters);
         p.sorted = reinterpret_cast<uint32_t*>(base + w.sorted);
         p.order = reinterpret_cast<int*>(base + w.order);
