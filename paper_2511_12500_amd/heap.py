@@ -134,6 +134,8 @@ class GatheredOutput:
 
     def __init__(self, heap: Heap, M: int, N_local: int, dtype: torch.dtype,
                  tile_m: int, tile_n: int):
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise TypeError("dtype must be float16 or bfloat16")
         self.heap = heap
         self.M, self.N_local, self.dtype = M, N_local, dtype
         self.tile_m, self.tile_n = tile_m, tile_n
