@@ -648,9 +648,12 @@ bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p)
 
 // How the sums are laid out over workgroups: one wave each, columns by 16 bytes a lane (32768
 // tokens of 4096 columns 149 us, four waves 156), and the largest chunks of 8, 32 or 128
-// positions that leave 4096 workgroups, since the parts of runs that pass their ends go through
-// memory (16384 tokens of 4096 columns: 8 179 us, 32 157; 131072: 32 408, 64 381, 128 369); a
-// chunk's rows are asked for 8 at a time.
+// positions that leave 4096 workgroups if all tokens are the shard's, since the parts of runs that
+// pass their ends go through memory (16384 tokens of 4096 columns: 8 179 us, 32 157; 131072: 32
+// 408, 64 381, 128 369); a chunk's rows are asked for 8 at a time.  The host does not know how many
+// tokens are the shard's; the workgroups behind those return at once.  (With chunks by that number,
+// which the device knows, a rank of 8 took: 8192 tokens of 8192 columns 26 us for 30, 65536 55 for
+// 63, but 32768 35 for 33 and 131072 77 to 81 for 70.)
 struct GradPlan {
     int col_blocks, chunk, chunks;
 };

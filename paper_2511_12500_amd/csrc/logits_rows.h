@@ -1,4 +1,5 @@
-// What the operators over rows of logits share (token_logprobs.hip, distill.hip).
+// What the operators over rows of logits share (token_logprobs.hip, distill.hip,
+// verify_draft.hip); embedding.hip and mx4.hip take the element types and checks.
 //
 // A workgroup takes one row, or one segment of a row, and holds it in
 // registers: NV vectors of 16 bytes a thread.  A row of z = scale * x is used

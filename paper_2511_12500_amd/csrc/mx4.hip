@@ -187,7 +187,8 @@ __device__ __forceinline__ uint16_t rounded(float v) {
     else return __builtin_bit_cast(uint16_t, (_Float16)v);
 }
 
-// A workgroup takes 16 columns and up to 64 rows; its waves share the chunks of 512 values,
+// A workgroup takes 16 columns and up to 64 rows (over 32 only where there is next to nothing to
+// sum: K = 0, or a matrix of fewer than 16 scales); its waves share the chunks of 512 values,
 // whose 16-byte blocks go from memory to the operands' registers, and add their sums through
 // LDS.  Bound by latency: one round of loads, the waves' sums, the stores' acknowledgement and
 // the counters follow each other (1 x 8192 x 3584 into 8 slots, 15.7 MB: 6.2 us of which 2.9 are
@@ -302,19 +303,22 @@ __device__ __forceinline__ void meet() {
 // In instruction S of a stage's four lane half g takes block 4 g + S of its rows, so a
 // lane's scales of a stage are one word; scales come for two stages (a pair), 16 bytes a
 // row, straight into LDS too where rows of scales are whole numbers of 16 aligned bytes
-// (ALIGNED), else through registers.
+// (ALIGNED: K a multiple of 512), else through registers, one pair ahead (K = 8160 where 8192 takes
+// the first time: 64 x K x 3584 into 8 slots 13.2 us and 10.9, 128 x K x 28672 73 and 49, 4096 x K x
+// 28672 617 and 495, x 3584 into 8 slots 115 and 104).
 //   256 x 256, 2 stages: each 32 x 32 x 64 operand read feeds 4 instructions, and the 256
-// accumulators fill the AGPRs of one wave a SIMD.  4096 x 8192 x 28672 in 473 to 497 us, 4.0
-// PFLOP/s; without its loads 390, without its stores 447.  Power bounds it: matrix units that
-// are busy all the time, from registers alone, run at 1.35 to 1.4 GHz on random data (343 us for
-// as many instructions; 229 at full clock), and here they are busy for half of the cycles at 1.8
-// to 1.9 GHz.  So hiding more did not help: lines asked for into L2 three stages ahead, by the CUs
-// that share them, took 474 us where this took 475 (on zeros 361 and 417), one workgroup a CU
-// that goes through tiles with the next one's loads ahead of the stores 484 where this took 484,
-// and tiles of 256 x 128, which move more, 644.  Into 8 slots, 4096 x 8192 x 3584, 102 us: 59 to the end of K, 235 MB of
-// stores behind it, since all tiles run at once.
-//   64 x 64, 4 stages, K in parts: 64 x 8192 x 3584 into 8 slots 10.0 us, 16 MB of weights and X
-// read and 7.4 MB written; latency: loads, parts to memory and back, stores.
+// accumulators fill the AGPRs of one wave a SIMD.  4096 x 8192 x 28672 in 485 to 495 us, 3.9
+// PFLOP/s, with inputs in turn (the first calls after a pause 517; on the same inputs 459); without
+// its loads 376 where this took 475.  Power bounds it: matrix units that are busy all the time, from
+// registers alone, run at 1.35 to 1.4 GHz on random data (as many instructions at that rate, 5.6
+// PFLOP/s, 343 us; 229 at full clock), and here they are busy for half of the cycles.  So hiding
+// more did not help: lines asked for into L2 three stages ahead, by the CUs that share them, took
+// 474 us where this took 475 (on zeros 361 and 417), one workgroup a CU that goes through tiles with
+// the next one's loads ahead of the stores 484 where this took 484, and tiles of 256 x 128, which
+// move more, 644.  Into 8 slots, 4096 x 8192 x 3584, 104 us: 59 to the end of K, 235 MB of stores
+// behind it, since all tiles run at once.
+//   64 x 64, 4 stages, K in parts: 64 x 8192 x 3584 into 8 slots 10.1 to 11 us, 16 MB of weights and
+// X read and 7.4 MB written; latency: loads, parts to memory and back, stores.
 constexpr int kStageBytes = 128;
 template <int TM, int TN, int RING>
 struct GemmLds {
@@ -718,8 +722,9 @@ GemmBuild gemm_build(int cus, int M, int N, int groups) {
     // Up to 32 rows the other kernel while there is little to do: its tiles read X once each, but
     // K needs no second way through memory.  (M x K x N, us, other kernel / 64 x 64 tiles:
     // 1x8192x3584 6.3 / 9.0, 1x8192x8192 12.5 / 10.5, 1x8192x28672 31 / 20, 16x8192x3584 7.8 / 9.1,
-    // 32x4096x4096 6.1 / 7.7, 32x8192x2048 9.2 / 7.9, 16x2048x16384 7.0 / 6.3, 48x4096x1024 7.2 / 7.5,
-    // 48x1024x8192 5.5 / 4.9, 64x2048x4096 6.0 / 5.8, 64x8192x3584 16.2 / 10.0.)
+    // 32x4096x4096 6.1 / 7.7, 32x8192x2048 9.2 / 7.9, 16x2048x16384 7.0 / 6.3; over 32 rows, where it
+    // gains little at best, never: 48x4096x1024 7.2 / 7.5, 48x1024x8192 5.5 / 4.9, 64x2048x4096 6.0 /
+    // 5.8, 64x8192x3584 16.2 / 10.0.)
     const size_t rounds = std::max<size_t>(1, ceil_div(ceil_div(N, kTileN), cus));
     const size_t values = (size_t)ceil_div(M, 16) * groups * kBlock * rounds;
     const bool little = M <= 32 && values <= (rounds == 1 ? 12288 : M <= 16 ? 8192 : 0);
@@ -728,7 +733,8 @@ GemmBuild gemm_build(int cus, int M, int N, int groups) {
     // N is 3584 or 1024; us, tiles of 64 x 64 / 64 x 128 / 128 x 128 / 256 x 256: 64x8192x3584
     // 10.0 / 12.5, 256x8192x3584 13.5 / 15.7 / 20.3 / 60, 1024x4096x1024 10.2 / 13.7 / 17.1 / 37,
     // 128x8192x28672 36 / 32 / 36 / 49, 512x8192x8192 38 / 32 / 30 / 49, 512x8192x28672 115 / 106 / 77 /
-    // 67, 2048x8192x3584 72 / 76 / 56 / 70, 2048x8192x8192 130 / 119 / 82 / 70).
+    // 67, 2048x8192x3584 72 / 76 / 56 / 70, 2048x8192x8192 130 / 119 / 82 / 70; all on the same
+    // weights, which the memory-side cache keeps: from memory 128x8192x28672 takes 48, 512 rows 75).
     auto tiles = [&](int tm, int tn) { return (size_t)ceil_div(M, tm) * ceil_div(N, tn); };
     b = tiles(64, 64) <= (size_t)cus                    ? gemm_of<64, 64, 4>()
         : M <= 128 || tiles(64, 128) <= (size_t)cus     ? gemm_of<64, 128, 4>()

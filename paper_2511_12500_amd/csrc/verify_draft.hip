@@ -55,8 +55,9 @@ __device__ __forceinline__ const typename Elem<DT>::type* row_of(const VerifyPar
 
 // ---- largest logits and sums ---------------------------------------------------------------
 // A workgroup holds a row's segment in registers, so logits are read once: the largest first,
-// then the sum relative to it.  Bound by memory: 704 rows of 50001 fp16 15 us, 4.6 TB/s; few
-// rows by latency (9 rows of 28672 bf16 in segments 3.2 us).
+// then the sum relative to it.  Bound by the vector units, which are busy for three quarters of
+// the cycles (7 instructions an element, the exponential for two), beside the loads: 704 rows of
+// 50001 fp16 16 us, 4.4 TB/s; few rows by latency (9 rows of 28672 bf16 in segments 3.3 us).
 template <int DT, int NV, bool HUGE>
 __device__ __forceinline__ float sum_of(Segment<DT, NV>& d, const Exponent& ex) {
     d.again();
@@ -360,9 +361,9 @@ __device__ __forceinline__ Best best_of_all(Best b, Shared& sh) {
 
 // Every workgroup of a sequence joins its rows' parts and decides; each then takes a segment
 // of position a's rows, and the last of them to arrive joins the race and writes the outputs.
-// Bound by latency: one sequence of 4 drafts over 28672 takes 6.8 us, about a third each for the
-// decision, the rows' way from memory and the race, and the segments' join (64 sequences of 5
-// over 50001 9.8 us for 24 MB).
+// Bound by latency: one sequence of 4 drafts over 28672 takes 7.0 to 7.8 us, about a third each for
+// the decision, the rows' way from memory and the race, and the segments' join (64 sequences of 5
+// over 50001 10.1 us for 24 MB, vector units busy for two fifths of the cycles).
 template <int DT, int MODE>
 __global__ void __launch_bounds__(kDrawThreads) verify_draw_kernel(VerifyParams p) {
     typedef typename Elem<DT>::type T;

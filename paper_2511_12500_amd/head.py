@@ -347,9 +347,11 @@ class EmbeddingGrad:
             scale: float = 1.0, accumulate: bool = False, stream: int | None = None) -> None:
         """dtable[v] = ``scale`` * the sum of drows[t] over the tokens t of id
         ``first`` + v, rows without one zero; with ``accumulate`` added to what
-        dtable holds.  ``tokens``: int64 [T]; ``drows``: [T, D]; ``dtable``: [rows,
-        D] of any of the three types; both with contiguous rows.  Enqueued on the
-        stream, asynchronous."""
+        dtable holds.  ``first`` is the shard's first token, 0 unless given: this
+        object knows no rank, from which ``GatheredRows.run`` takes its default.
+        ``tokens``: int64 [T]; ``drows``: [T, D]; ``dtable``: [rows, D] of any of the
+        three types; both with contiguous rows.  Enqueued on the stream,
+        asynchronous."""
         if dtable.dtype not in _DTYPES:
             raise TypeError("dtable must be float16, bfloat16 or float32")
         if dtable.dim() != 2:

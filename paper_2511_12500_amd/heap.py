@@ -385,9 +385,11 @@ class GatheredRows:
     def run(self, tokens: torch.Tensor, table: torch.Tensor, rank: int, first: int | None = None,
             scale: float = 1.0, stream: int | None = None) -> None:
         """The call of rank ``rank`` for its shard ``table`` [rows, D] (contiguous
-        rows), which holds the tokens from ``first`` on (default: rank * rows):
-        ``scale`` times the rows of its tokens into every slot; rank 0 also stores
-        zeros for negative ``tokens`` (int64 [T]).  Enqueued on the stream,
+        rows), which holds the tokens from ``first`` on: ``scale`` times the rows of
+        its tokens into every slot; rank 0 also stores zeros for negative ``tokens``
+        (int64 [T]).  Without ``first`` it is rank * rows, which is right only where
+        all ranks' shards have as many rows: with a shorter last shard give it, or
+        that rank writes over rows of other ranks' tokens.  Enqueued on the stream,
         asynchronous; it can be captured in a graph."""
         device = self.heap.device
         if tokens.dtype != torch.int64 or table.dtype != self.dtype:
