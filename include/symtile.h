@@ -818,7 +818,8 @@ symtile_status symtile_embed_workspace_bytes(int device, int T, int D, size_t* b
  * with fp32 sums in the order of t within chunks of the sorted tokens (8, 32 or 128 of
  * them, by T, D and dtype) and then of the chunks, so results do not depend on timing;
  * with accumulate = 1 added to what dtable[v] holds (in fp32, rounded once to
- * table_dtype) and rows without a token left alone, else those are zero.  Other tokens (other ranks', padding) are not read.
+ * table_dtype) and rows without a token left alone, else those are zero.  Other tokens
+ * (other ranks', padding) are not read.
  *
  *  tokens       device int64 [T]
  *  drows        device [T, D] of dtype, row stride ld (0 = D); rows 16-byte aligned
